@@ -190,7 +190,7 @@ def _compress(w, case):
 def _stack(gate, up, ffn, cols):
     import paper_2502_00922_b200 as hl
     stacked = torch.empty((hl.stacked_rows(ffn), cols), dtype=gate.dtype, device="cuda")
-    hl.stack_gate_up(gate, up, ffn, cols, stacked)
+    hl.stack_gate_up_device(gate, up, ffn, cols, stacked)
     return stacked
 
 
