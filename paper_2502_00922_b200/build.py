@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
@@ -23,12 +24,16 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not needs_build():
         return SO
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-I" + INCLUDE, "-shared", "-Xcompiler", "-fPIC", "-o", SO] + [os.path.join(CSRC, s) for s in SOURCES]
-    cmd += ["-lpthread"]
+    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-I" + INCLUDE, "-Xcompiler", "-fPIC"]
     if verbose:
         cmd.insert(1, "-Xptxas=-v")
-    subprocess.check_call(cmd)
+    with tempfile.TemporaryDirectory() as tmp:       # one compiler per source, side by side
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        running = [subprocess.Popen(cmd + ["-c", "-o", o, os.path.join(CSRC, s)]) for s, o in zip(SOURCES, objects)]
+        failed = [s for s, p in zip(SOURCES, running) if p.wait() != 0]
+        if failed:
+            raise RuntimeError("nvcc failed on " + ", ".join(failed))
+        subprocess.check_call(cmd + ["-shared", "-o", SO] + objects + ["-lpthread"])
     return SO
 
 
