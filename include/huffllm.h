@@ -370,6 +370,119 @@ huffllm_status huffllm_decode_gemm_multi_host_async(uint32_t n, const huffllm_de
 huffllm_status huffllm_decode_gemm_static(const huffllm_desc *desc, const void *blob_dev, const uint16_t *x_dev,
                                           uint32_t batch, float *y_dev, int32_t *err_flag_dev, huffllm_stream stream);
 
+/* ------------------------------------------------ device: what a decoder layer does around its products */
+
+/*
+ * Products that hand on what the next step reads instead of fp32 sums (no counterpart in the paper, whose engine ends at the sums:
+ * a decode step's bias, activation, gate, residual and rounding, which otherwise take launches of their own between the products).
+ *
+ *   plain   out[b][r] = act(sum_c W[r][c] x[b][c] + bias[r]) + residual[b][r]
+ *   gated   out[b][i] = act((Wg x)[b][i] + bias_g[i]) * ((Wu x)[b][i] + bias_u[i])        (gated_rows != 0)
+ *
+ * Everything is computed in fp32 from the sums of huffllm_decode_gemm and rounded once (to nearest, ties to even) where out is 16 bits
+ * wide; FP16 results beyond 65504 become infinite.  act: SiLU v / (1 + e^-v), GELU v/2 (1 + erf(v / sqrt 2)), GELU_TANH
+ * v/2 (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))); a NaN stays one, and where a formula has no value (SiLU and the GELUs of minus
+ * infinity) the result is NaN.
+ *
+ * A gated product runs over ONE blob, compressed from gate and up stacked by huffllm_stack_gate_up; desc->rows must be
+ * huffllm_stacked_rows(gated_rows), and out has gated_rows columns.  Both projections, the activation and the product are then one
+ * kernel in which no CTA waits for another.  A gated product takes no residual (UNSUPPORTED).
+ *
+ * residual has the type of out.  It may be out itself (same pointer, same stride: the residual stream is updated in place); other
+ * overlaps of out with x, bias or residual are not allowed.  Strides count values between vectors; 0 = packed; a stride below the
+ * number of columns is INVALID_ARG.  What lies between the columns of two vectors is left as it is.
+ */
+typedef enum {
+    HUFFLLM_ACT_NONE = 0,
+    HUFFLLM_ACT_RELU = 1,
+    HUFFLLM_ACT_SILU = 2,
+    HUFFLLM_ACT_GELU = 3,
+    HUFFLLM_ACT_GELU_TANH = 4
+} huffllm_activation;
+
+/* Type of activations that are no product's x: fp32, or the 16-bit type of the blob (of the call's dtype, where there is no blob). */
+typedef enum { HUFFLLM_ELEM_F32 = 0, HUFFLLM_ELEM_16 = 1 } huffllm_elem;
+
+typedef struct huffllm_epilogue {
+    uint32_t activation;       /* huffllm_activation                                                            */
+    uint32_t out_type;         /* huffllm_elem, of out and residual                                             */
+    uint64_t gated_rows;       /* 0: plain; else the outputs of a gated product                                 */
+    const uint16_t *bias;      /* device, desc->rows words of the blob's dtype (gated: stacked like W), or null */
+    const void *residual;      /* device, or null                                                               */
+    uint64_t residual_stride, out_stride;
+} huffllm_epilogue;
+
+/*
+ * huffllm_decode_gemm with an epilogue: the same kernels, workspace, limits and error flag.  out: device memory (or pinned host memory
+ * the device can address), aligned to its type.
+ */
+huffllm_status huffllm_decode_gemm_epilogue(const huffllm_desc *desc, const void *blob_dev, const uint16_t *x_dev, uint32_t batch,
+                                            const huffllm_epilogue *epilogue, void *out_dev, void *workspace_dev,
+                                            size_t workspace_bytes, int32_t *err_flag_dev, huffllm_stream stream);
+
+/* huffllm_decode_gemm_multi with an epilogue per matrix (q, k and v with their biases, say): epilogues is a host array of n. */
+huffllm_status huffllm_decode_gemm_multi_epilogue(uint32_t n, const huffllm_desc *const *descs, const void *const *blobs_dev,
+                                                  const uint16_t *const *xs_dev, uint32_t batch, const huffllm_epilogue *epilogues,
+                                                  void *const *outs_dev, void *const *workspaces_dev, size_t workspace_bytes_each,
+                                                  int32_t *err_flag_dev, huffllm_stream stream);
+
+/*
+ * Stack gate and up ([n][cols] 16-bit words each, row-major) for a gated product, once, before compressing: in every group of 16 rows
+ * of the result gate rows 8 g .. 8 g + 7 and then up rows 8 g .. 8 g + 7, the last group filled up with copies of each one's last row
+ * (its outputs are never written, and the codebook sees no new symbols).  With cols = 1 it stacks the two biases.
+ * huffllm_stacked_rows: 16 * ceil(n / 8).  `stacked` must not overlap the inputs.
+ * huffllm_stack_gate_up works on host memory, huffllm_stack_gate_up_device on device memory (asynchronous on `stream`, fewer than 2^26
+ * columns).
+ */
+huffllm_status huffllm_stacked_rows(uint64_t n, uint64_t *rows);
+huffllm_status huffllm_stack_gate_up(const uint16_t *gate_host, const uint16_t *up_host, uint64_t n, uint64_t cols, uint16_t *stacked_host);
+huffllm_status huffllm_stack_gate_up_device(const uint16_t *gate_dev, const uint16_t *up_dev, uint64_t n, uint64_t cols,
+                                            uint16_t *stacked_dev, huffllm_stream stream);
+
+/*
+ * Residual addition and root-mean-square norm between two products, one launch:
+ *     h = x + delta;   sum = h;   out = h / sqrt(mean(h^2) + eps) * gain
+ * for `vectors` vectors of `cols` values.  h is kept in fp32 (out is computed from it, not from the rounded sum); the squares are
+ * added up in fp32 in a fixed order (they overflow for |h| above 1e19).  x, sum: x_type; delta: delta_type; gain, out: 16-bit words
+ * of `dtype`, what the products take as x.  delta, sum and gain may be null (no addition, not wanted, ones).  sum may be x or delta
+ * itself (same pointer, stride and type); out must not overlap the inputs.  Any alignment of the types is taken; 16-byte
+ * aligned pointers, cols % 8 == 0 and strides of whole 16 bytes are faster.  Strides count values; 0 = packed.
+ */
+typedef struct huffllm_norm {
+    uint32_t dtype;                  /* huffllm_dtype of all 16-bit values */
+    uint32_t x_type, delta_type;     /* huffllm_elem                       */
+    float eps;                       /* >= 0                               */
+    uint64_t vectors, cols;
+    const void *x, *delta;           /* device                             */
+    const uint16_t *gain;            /* device, cols words                 */
+    void *sum;                       /* device                             */
+    uint16_t *out;                   /* device                             */
+    uint64_t x_stride, delta_stride, sum_stride, out_stride;
+} huffllm_norm;
+huffllm_status huffllm_add_rms_norm(const huffllm_norm *args, huffllm_stream stream);
+
+/*
+ * The feed-forward sub-layer of a decoder layer, three launches whose set-ups overlap:
+ *     n = rms_norm(h) * gain;   m = act(Wg n + b_g) * (Wu n + b_u);   out = h + Wd m + b_d
+ * gate_up: a stacked blob (huffllm_stack_gate_up) of ffn_rows gates over `hidden` columns; down: a blob of [hidden][ffn_rows] of the
+ * same dtype; ffn_rows and hidden are multiples of 32.  h and out: `batch` vectors (1..64) of type h_type (huffllm_elem); out may be h
+ * itself.  n and m are rounded to the blobs' dtype, as the products take them.  gain and the biases may be null; gate_up_bias is stacked.
+ * The workspace (256-byte aligned, at least huffllm_ffn_workspace_bytes) must be zero-filled once after allocation, and again after a
+ * call that set the error flag (a chunk number there is one of gate_up or of down); calls that share it must not overlap on the GPU.
+ */
+typedef struct huffllm_ffn {
+    const huffllm_desc *gate_up, *down;            /* host   */
+    const void *gate_up_blob, *down_blob;          /* device */
+    uint64_t ffn_rows;
+    uint32_t activation;                           /* huffllm_activation */
+    float eps;
+    const uint16_t *gain, *gate_up_bias, *down_bias;   /* device, words of the blobs' dtype */
+} huffllm_ffn;
+huffllm_status huffllm_ffn_workspace_bytes(const huffllm_ffn *ffn, uint32_t batch, size_t *bytes);
+huffllm_status huffllm_decode_ffn(const huffllm_ffn *ffn, const void *h_dev, uint64_t h_stride, uint32_t batch, void *out_dev,
+                                  uint64_t out_stride, uint32_t h_type, void *workspace_dev, size_t workspace_bytes,
+                                  int32_t *err_flag_dev, huffllm_stream stream);
+
 /*
  * Reference point for the compressed path: y = W x for an UNCOMPRESSED bf16 matrix (device,
  * row-major, 16-byte aligned rows, cols a multiple of 8), same fp32 accumulation, written as a

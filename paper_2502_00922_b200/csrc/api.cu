@@ -520,6 +520,52 @@ huffllm_status finish_args(KernelArgs *k, bool product, const DeviceInfo &dev, u
     return HUFFLLM_OK;
 }
 
+// ---- epilogues
+uint32_t elem_bytes(uint32_t type) { return type == HUFFLLM_ELEM_16 ? 2 : 4; }
+
+// The kernels' form of one matrix's epilogue; checks everything that the product's own checks do not.
+huffllm_status make_epilogue(const huffllm_epilogue &ep, const huffllm_desc *desc, void *out, EpiMat *m) {
+    if (ep.activation > HUFFLLM_ACT_GELU_TANH) return fail(HUFFLLM_ERR_INVALID_ARG, "unknown activation %u", ep.activation);
+    if (ep.out_type > HUFFLLM_ELEM_16) return fail(HUFFLLM_ERR_INVALID_ARG, "unknown type %u of out", ep.out_type);
+    const uint64_t width = ep.gated_rows ? ep.gated_rows : desc->rows;
+    if (ep.gated_rows) {
+        if (ep.gated_rows > desc->rows || desc->rows != (ep.gated_rows + 7) / 8 * 16)
+            return fail(HUFFLLM_ERR_INVALID_ARG, "a gated product of %llu outputs takes a stacked blob of 16 * ceil(outputs / 8) rows, not %llu",
+                        (unsigned long long)ep.gated_rows, (unsigned long long)desc->rows);
+        if (ep.residual) return fail(HUFFLLM_ERR_UNSUPPORTED, "a gated product takes no residual");
+    }
+    if ((ep.out_stride && ep.out_stride < width) || (ep.residual && ep.residual_stride && ep.residual_stride < width))
+        return fail(HUFFLLM_ERR_INVALID_ARG, "stride below the number of columns");
+    const uintptr_t mask = elem_bytes(ep.out_type) - 1;
+    if (((uintptr_t)out & mask) || ((uintptr_t)ep.residual & mask) || ((uintptr_t)ep.bias & 1))
+        return fail(HUFFLLM_ERR_INVALID_ARG, "out, residual and bias must be aligned to their types");
+    m->bias = ep.bias;
+    m->residual = ep.residual;
+    m->out = out;
+    m->out_stride = ep.out_stride ? ep.out_stride : width;
+    m->residual_stride = ep.residual_stride ? ep.residual_stride : width;
+    m->gated_rows = ep.gated_rows;
+    m->act = ep.activation;
+    m->out16 = ep.out_type == HUFFLLM_ELEM_16;
+    return HUFFLLM_OK;
+}
+
+// Launch a described product: with the epilogues of its matrices, or (epi null) with fp32 sums to y.
+cudaError_t launch_product(const KernelArgs &k, const EpiMat *epi, uint32_t grid, cudaStream_t stream) {
+    if (!epi) return launch_gemm(k, grid, stream);
+    EpiKernelArgs a;
+    static_cast<KernelArgs &>(a) = k;
+    memcpy(a.e, epi, k.n_mats * sizeof(EpiMat));
+    return launch_gemm(a, grid, stream);
+}
+cudaError_t launch_product_tc(const TcArgs &t, const EpiMat *epi, uint32_t grid, cudaStream_t stream) {
+    if (!epi) return launch_gemm_tc(t, grid, stream);
+    EpiTcArgs a;
+    static_cast<TcArgs &>(a) = t;
+    memcpy(a.e, epi, t.k.n_mats * sizeof(EpiMat));
+    return launch_gemm_tc(a, grid, stream);
+}
+
 }  // namespace
 
 extern "C" {
@@ -654,10 +700,11 @@ huffllm_status huffllm_decode(const huffllm_desc *desc, const void *blob, uint16
 }
 
 // Checks shared by the product entry points for one matrix of a call.
-static huffllm_status check_product_args(const huffllm_desc *desc, const uint16_t *x, const float *y, const void *workspace,
-                                         size_t workspace_bytes, uint32_t batch) {
+// (y: the fp32 sums, or an epilogue's out, whose alignment make_epilogue looks at)
+static huffllm_status check_product_args(const huffllm_desc *desc, const uint16_t *x, const void *y, const void *workspace,
+                                         size_t workspace_bytes, uint32_t batch, bool epilogue = false) {
     if (!x || !y || !workspace) return fail(HUFFLLM_ERR_INVALID_ARG, "null pointer");
-    if (((uintptr_t)x & 15) || ((uintptr_t)y & 3) || ((uintptr_t)workspace & 255))
+    if (((uintptr_t)x & 15) || (!epilogue && ((uintptr_t)y & 3)) || ((uintptr_t)workspace & 255))
         return fail(HUFFLLM_ERR_INVALID_ARG, "x must be 16-byte, y 4-byte, workspace 256-byte aligned");
     huffllm_status st = check_desc(desc);
     if (st != HUFFLLM_OK) return st;
@@ -666,16 +713,23 @@ static huffllm_status check_product_args(const huffllm_desc *desc, const uint16_
     return HUFFLLM_OK;
 }
 
-huffllm_status huffllm_decode_gemm_multi(uint32_t n, const huffllm_desc *const *descs, const void *const *blobs,
-                                         const uint16_t *const *xs, uint32_t batch, float *const *ys, void *const *workspaces,
-                                         size_t workspace_bytes_each, int32_t *err_flag, huffllm_stream stream) {
+// Several products in one launch: fp32 sums to ys (eps null), or with an epilogue each to outs.
+static huffllm_status product_multi(uint32_t n, const huffllm_desc *const *descs, const void *const *blobs, const uint16_t *const *xs,
+                                    uint32_t batch, float *const *ys, const huffllm_epilogue *eps, void *const *outs, void *const *workspaces,
+                                    size_t workspace_bytes_each, int32_t *err_flag, huffllm_stream stream) {
     clear_error();
-    DeviceInfo dev;
-    huffllm_status st = device_info(&dev);
-    if (st != HUFFLLM_OK) return st;
-    if (!descs || !blobs || !xs || !ys || !workspaces) return fail(HUFFLLM_ERR_INVALID_ARG, "null pointer");
+    huffllm_status st;
+    if (!descs || !blobs || !xs || !(eps ? (const void *)outs : (const void *)ys) || !workspaces) return fail(HUFFLLM_ERR_INVALID_ARG, "null pointer");
     if (n == 0 || n > kMaxMats) return fail(HUFFLLM_ERR_INVALID_ARG, "between 1 and %u matrices per call", kMaxMats);
     if (batch == 0 || batch > 64) return fail(HUFFLLM_ERR_INVALID_ARG, "batch must be in [1, 64]");
+    EpiMat epi[kMaxMats];
+    for (uint32_t i = 0; i < n; ++i) {
+        const void *y = eps ? outs[i] : (const void *)ys[i];
+        if ((st = check_product_args(descs[i], xs[i], y, workspaces[i], workspace_bytes_each, batch, eps != nullptr)) != HUFFLLM_OK) return st;
+        if (eps && (st = make_epilogue(eps[i], descs[i], outs[i], &epi[i])) != HUFFLLM_OK) return st;
+    }
+    DeviceInfo dev;
+    if ((st = device_info(&dev)) != HUFFLLM_OK) return st;
     if (batch > kTwoTileBatch) {
         // 17..64 vectors: the tensor-core kernel, its CTAs dealt to the matrices like the other kernels'
         TcArgs t;
@@ -684,14 +738,13 @@ huffllm_status huffllm_decode_gemm_multi(uint32_t n, const huffllm_desc *const *
         uint32_t grid;
         begin_args(&k, batch, dev);
         for (uint32_t i = 0; i < n; ++i) {
-            if ((st = check_product_args(descs[i], xs[i], ys[i], workspaces[i], workspace_bytes_each, batch)) != HUFFLLM_OK) return st;
             if (!tc_blob(descs[i]))
                 return fail(HUFFLLM_ERR_UNSUPPORTED, "more than %u vectors per call over several matrices take tables of up to 9 bits (FP16: 8)", kTwoTileBatch);
             for (uint32_t j = 0; j < i; ++j)
                 if (workspaces[j] == workspaces[i]) return fail(HUFFLLM_ERR_INVALID_ARG, "matrices %u and %u share a workspace", j, i);
             if ((st = add_matrix(&k, descs[i], blobs[i])) != HUFFLLM_OK) return st;
             k.m[i].x = xs[i];
-            k.m[i].y = ys[i];
+            k.m[i].y = eps ? nullptr : ys[i];
         }
         uint32_t flat = k.fp16_flat;
         if ((st = finish_args(&k, true, dev, &grid)) != HUFFLLM_OK) return st;      // (deals the CTAs to the matrices by their chunks)
@@ -716,7 +769,7 @@ huffllm_status huffllm_decode_gemm_multi(uint32_t n, const huffllm_desc *const *
             first += k.m[i].cta_count;
         }
         k.err = err_flag;
-        cudaError_t e = launch_gemm_tc(t, first, (cudaStream_t)stream);
+        cudaError_t e = launch_product_tc(t, eps ? epi : nullptr, first, (cudaStream_t)stream);
         if (e != cudaSuccess) return fail(HUFFLLM_ERR_CUDA, "tensor-core product launch: %s", cudaGetErrorString(e));
         return HUFFLLM_OK;
     }
@@ -724,7 +777,6 @@ huffllm_status huffllm_decode_gemm_multi(uint32_t n, const huffllm_desc *const *
     uint32_t grid;
     begin_args(&k, batch, dev);
     for (uint32_t i = 0; i < n; ++i) {
-        if ((st = check_product_args(descs[i], xs[i], ys[i], workspaces[i], workspace_bytes_each, batch)) != HUFFLLM_OK) return st;
         if (batch > kKernelBatch && !two_tile_blob(descs[i]))
             return fail(HUFFLLM_ERR_UNSUPPORTED, "more than %u vectors per call take BF16 blobs of max_code_len 8", kKernelBatch);
         for (uint32_t j = 0; j < i; ++j)
@@ -732,26 +784,49 @@ huffllm_status huffllm_decode_gemm_multi(uint32_t n, const huffllm_desc *const *
         if ((st = add_matrix(&k, descs[i], blobs[i])) != HUFFLLM_OK) return st;
         MatArgs &m = k.m[i];
         m.x = xs[i];
-        m.y = ys[i];
+        m.y = eps ? nullptr : ys[i];
         m.ws_ticket = (unsigned int *)workspaces[i];
         m.ws_partial = (float *)((uint8_t *)workspaces[i] + ws_partial_offset(descs[i]));
         m.ws_warp_pieces = (float *)((uint8_t *)workspaces[i] + ws_partial_offset(descs[i]) + ws_cta_pieces_bytes(batch));   // (used above 8 vectors)
     }
     if ((st = finish_args(&k, true, dev, &grid)) != HUFFLLM_OK) return st;
     k.err = err_flag;
-    cudaError_t e = launch_gemm(k, grid, (cudaStream_t)stream);
+    cudaError_t e = launch_product(k, eps ? epi : nullptr, grid, (cudaStream_t)stream);
     if (e != cudaSuccess) return fail(HUFFLLM_ERR_CUDA, "product launch: %s", cudaGetErrorString(e));
     return HUFFLLM_OK;
 }
 
-huffllm_status huffllm_decode_gemm(const huffllm_desc *desc, const void *blob, const uint16_t *x, uint32_t batch, float *y,
-                                   void *workspace, size_t workspace_bytes, int32_t *err_flag, huffllm_stream stream) {
+huffllm_status huffllm_decode_gemm_multi(uint32_t n, const huffllm_desc *const *descs, const void *const *blobs,
+                                         const uint16_t *const *xs, uint32_t batch, float *const *ys, void *const *workspaces,
+                                         size_t workspace_bytes_each, int32_t *err_flag, huffllm_stream stream) {
+    return product_multi(n, descs, blobs, xs, batch, ys, nullptr, nullptr, workspaces, workspace_bytes_each, err_flag, stream);
+}
+
+huffllm_status huffllm_decode_gemm_multi_epilogue(uint32_t n, const huffllm_desc *const *descs, const void *const *blobs,
+                                                  const uint16_t *const *xs, uint32_t batch, const huffllm_epilogue *epilogues,
+                                                  void *const *outs, void *const *workspaces, size_t workspace_bytes_each,
+                                                  int32_t *err_flag, huffllm_stream stream) {
     clear_error();
-    DeviceInfo dev;
-    huffllm_status st = device_info(&dev);
-    if (st != HUFFLLM_OK) return st;
+    if (!epilogues) return fail(HUFFLLM_ERR_INVALID_ARG, "null pointer");
+    return product_multi(n, descs, blobs, xs, batch, nullptr, epilogues, outs, workspaces, workspace_bytes_each, err_flag, stream);
+}
+
+// One product: fp32 sums to y (ep null), or with an epilogue to out.  `shift`: bytes that the partial sums lie further on in the workspace
+// than this matrix's counters ask for (another matrix's, larger, use the same workspace).  `dry`: all checks and plans, no launch.
+static huffllm_status product_one(const huffllm_desc *desc, const void *blob, const uint16_t *x, uint32_t batch, float *y,
+                                  const huffllm_epilogue *ep, void *out, void *workspace, size_t workspace_bytes, size_t shift,
+                                  int32_t *err_flag, huffllm_stream stream, bool dry = false) {
+    clear_error();
+    huffllm_status st;
     if (batch == 0 || batch > 64) return fail(HUFFLLM_ERR_INVALID_ARG, "batch must be in [1, 64]");
-    if ((st = check_product_args(desc, x, y, workspace, workspace_bytes, batch)) != HUFFLLM_OK) return st;
+    workspace_bytes = workspace_bytes > shift ? workspace_bytes - shift : 0;
+    if ((st = check_product_args(desc, x, ep ? out : (const void *)y, workspace, workspace_bytes, batch, ep != nullptr)) != HUFFLLM_OK) return st;
+    EpiMat epi_m;
+    if (ep && (st = make_epilogue(*ep, desc, out, &epi_m)) != HUFFLLM_OK) return st;
+    const EpiMat *const epi = ep ? &epi_m : nullptr;
+    DeviceInfo dev;
+    if ((st = device_info(&dev)) != HUFFLLM_OK) return st;
+    uint8_t *const partials = (uint8_t *)workspace + ws_partial_offset(desc) + shift;
     // Paths for more than 8 vectors.  Each returns HUFFLLM_OK with `done` set if it launched, HUFFLLM_OK without if it does
     // not apply here (the next path decides), or an error.
     bool done = false;
@@ -770,10 +845,10 @@ huffllm_status huffllm_decode_gemm(const huffllm_desc *desc, const void *blob, c
         k.m[0].x = x;
         k.m[0].y = y;
         k.m[0].ws_ticket = (unsigned int *)workspace;
-        k.m[0].ws_partial = (float *)((uint8_t *)workspace + ws_partial_offset(desc));
-        k.m[0].ws_warp_pieces = (float *)((uint8_t *)workspace + ws_partial_offset(desc) + ws_cta_pieces_bytes(batch));
+        k.m[0].ws_partial = (float *)partials;
+        k.m[0].ws_warp_pieces = (float *)(partials + ws_cta_pieces_bytes(batch));
         k.err = err_flag;
-        cudaError_t e = launch_gemm(k, grid, (cudaStream_t)stream);
+        cudaError_t e = dry ? cudaSuccess : launch_product(k, epi, grid, (cudaStream_t)stream);
         if (e != cudaSuccess) return fail(HUFFLLM_ERR_CUDA, "product launch: %s", cudaGetErrorString(e));
         done = true;
         return HUFFLLM_OK;
@@ -805,12 +880,12 @@ huffllm_status huffllm_decode_gemm(const huffllm_desc *desc, const void *blob, c
         t.m_tiles[0] = tp.m_tiles;
         t.ksplit[0] = tp.ksplit;
         t.ticket[0] = (unsigned int *)((uint8_t *)workspace + tp.ticket_off);
-        t.partial[0] = (float *)((uint8_t *)workspace + tp.partial_off);
+        t.partial[0] = (float *)((uint8_t *)workspace + tp.partial_off + shift);
         k.err = err_flag;
         const uint32_t grid = tp.items < (uint32_t)dev.sms ? tp.items : (uint32_t)dev.sms;
         k.m[0].cta_first = 0;
         k.m[0].cta_count = grid;
-        cudaError_t e = launch_gemm_tc(t, grid, (cudaStream_t)stream);
+        cudaError_t e = dry ? cudaSuccess : launch_product_tc(t, epi, grid, (cudaStream_t)stream);
         if (e != cudaSuccess) return fail(HUFFLLM_ERR_CUDA, "tensor-core product launch: %s", cudaGetErrorString(e));
         done = true;
         return HUFFLLM_OK;
@@ -836,14 +911,31 @@ huffllm_status huffllm_decode_gemm(const huffllm_desc *desc, const void *blob, c
         if ((st = add_matrix(&k, desc, blob)) != HUFFLLM_OK) return st;
         if ((st = finish_args(&k, true, dev, &grid)) != HUFFLLM_OK) return st;
         k.m[0].x = x + (uint64_t)b0 * desc->cols;
-        k.m[0].y = y + (uint64_t)b0 * desc->rows;
+        k.m[0].y = ep ? nullptr : y + (uint64_t)b0 * desc->rows;
         k.m[0].ws_ticket = (unsigned int *)workspace;
-        k.m[0].ws_partial = (float *)((uint8_t *)workspace + ws_partial_offset(desc));
+        k.m[0].ws_partial = (float *)partials;
         k.err = err_flag;
-        cudaError_t e = launch_gemm(k, grid, (cudaStream_t)stream);
+        if (ep && b0) {
+            epi_m.out = (uint8_t *)epi_m.out + kKernelBatch * epi_m.out_stride * elem_bytes(ep->out_type);
+            if (epi_m.residual) epi_m.residual = (const uint8_t *)epi_m.residual + kKernelBatch * epi_m.residual_stride * elem_bytes(ep->out_type);
+        }
+        cudaError_t e = dry ? cudaSuccess : launch_product(k, epi, grid, (cudaStream_t)stream);
         if (e != cudaSuccess) return fail(HUFFLLM_ERR_CUDA, "product launch: %s", cudaGetErrorString(e));
     }
     return HUFFLLM_OK;
+}
+
+huffllm_status huffllm_decode_gemm(const huffllm_desc *desc, const void *blob, const uint16_t *x, uint32_t batch, float *y,
+                                   void *workspace, size_t workspace_bytes, int32_t *err_flag, huffllm_stream stream) {
+    return product_one(desc, blob, x, batch, y, nullptr, nullptr, workspace, workspace_bytes, 0, err_flag, stream);
+}
+
+huffllm_status huffllm_decode_gemm_epilogue(const huffllm_desc *desc, const void *blob, const uint16_t *x, uint32_t batch,
+                                            const huffllm_epilogue *epilogue, void *out, void *workspace, size_t workspace_bytes,
+                                            int32_t *err_flag, huffllm_stream stream) {
+    clear_error();
+    if (!epilogue) return fail(HUFFLLM_ERR_INVALID_ARG, "null pointer");
+    return product_one(desc, blob, x, batch, nullptr, epilogue, out, workspace, workspace_bytes, 0, err_flag, stream);
 }
 
 huffllm_status huffllm_decode_gemv(const huffllm_desc *desc, const void *blob, const uint16_t *x, float *y, void *workspace,
@@ -1008,6 +1100,172 @@ huffllm_status huffllm_plain_gemv_multi(uint32_t n, const uint16_t *const *ws, c
 
 huffllm_status huffllm_plain_gemv(const uint16_t *w, uint64_t rows, uint64_t cols, const uint16_t *x, float *y, huffllm_stream stream) {
     return huffllm_plain_gemv_multi(1, &w, &rows, &cols, &x, &y, stream);
+}
+
+// ------------------------------------------------------------------------------ around the products
+
+huffllm_status huffllm_stacked_rows(uint64_t n, uint64_t *rows) {
+    clear_error();
+    if (!rows) return fail(HUFFLLM_ERR_INVALID_ARG, "rows is null");
+    if (n == 0 || n > (1ull << 30)) return fail(HUFFLLM_ERR_INVALID_ARG, "gates must number 1 to 2^30");
+    *rows = (n + 7) / 8 * 16;
+    return HUFFLLM_OK;
+}
+
+static huffllm_status check_stack(const uint16_t *gate, const uint16_t *up, uint64_t n, uint64_t cols, const uint16_t *stacked) {
+    uint64_t rows;
+    if (!gate || !up || !stacked) return fail(HUFFLLM_ERR_INVALID_ARG, "null pointer");
+    huffllm_status st = huffllm_stacked_rows(n, &rows);
+    if (st != HUFFLLM_OK) return st;
+    if (cols == 0 || cols > (1ull << 31)) return fail(HUFFLLM_ERR_INVALID_ARG, "cols must be in [1, 2^31]");
+    const uintptr_t s0 = (uintptr_t)stacked, s1 = s0 + rows * cols * 2, bytes = n * cols * 2;
+    for (const uint16_t *in : {gate, up})
+        if ((uintptr_t)in < s1 && s0 < (uintptr_t)in + bytes) return fail(HUFFLLM_ERR_INVALID_ARG, "stacked overlaps an input");
+    return HUFFLLM_OK;
+}
+
+huffllm_status huffllm_stack_gate_up(const uint16_t *gate, const uint16_t *up, uint64_t n, uint64_t cols, uint16_t *stacked) {
+    clear_error();
+    huffllm_status st = check_stack(gate, up, n, cols, stacked);
+    if (st != HUFFLLM_OK) return st;
+    for (uint64_t r = 0; r < (n + 7) / 8 * 8; ++r) {
+        const uint64_t from = (r < n ? r : n - 1) * cols, to = (r / 8 * 16 + r % 8) * cols;
+        memcpy(stacked + to, gate + from, cols * 2);
+        memcpy(stacked + to + 8 * cols, up + from, cols * 2);
+    }
+    return HUFFLLM_OK;
+}
+
+huffllm_status huffllm_stack_gate_up_device(const uint16_t *gate, const uint16_t *up, uint64_t n, uint64_t cols, uint16_t *stacked,
+                                            huffllm_stream stream) {
+    clear_error();
+    huffllm_status st = check_stack(gate, up, n, cols, stacked);
+    if (st != HUFFLLM_OK) return st;
+    // (the copies' pitch, sixteen rows, has to stay below 2^31 bytes)
+    if (cols >= (1ull << 26)) return fail(HUFFLLM_ERR_UNSUPPORTED, "fewer than 2^26 columns");
+    const size_t row = (size_t)cols * 2;
+    cudaError_t e = cudaSuccess;
+    for (uint32_t side = 0; side < 2 && e == cudaSuccess; ++side) {
+        const uint8_t *in = (const uint8_t *)(side ? up : gate);
+        uint8_t *to = (uint8_t *)stacked + side * 8 * row;
+        if (n >= 8) e = cudaMemcpy2DAsync(to, 16 * row, in, 8 * row, 8 * row, n / 8, cudaMemcpyDeviceToDevice, (cudaStream_t)stream);
+        for (uint64_t r = n / 8 * 8; r < (n + 7) / 8 * 8 && e == cudaSuccess; ++r)
+            e = cudaMemcpyAsync(to + (r / 8 * 16 + r % 8) * row, in + (r < n ? r : n - 1) * row, row, cudaMemcpyDeviceToDevice, (cudaStream_t)stream);
+    }
+    if (e != cudaSuccess) return fail(HUFFLLM_ERR_CUDA, "stacking gate and up: %s", cudaGetErrorString(e));
+    return HUFFLLM_OK;
+}
+
+huffllm_status huffllm_add_rms_norm(const huffllm_norm *args, huffllm_stream stream) {
+    clear_error();
+    if (!args) return fail(HUFFLLM_ERR_INVALID_ARG, "null pointer");
+    const huffllm_norm &a = *args;
+    if (!a.x || !a.out) return fail(HUFFLLM_ERR_INVALID_ARG, "null pointer");
+    if (a.dtype > HUFFLLM_FP16 || a.x_type > HUFFLLM_ELEM_16 || a.delta_type > HUFFLLM_ELEM_16) return fail(HUFFLLM_ERR_INVALID_ARG, "unknown type");
+    if (a.vectors == 0 || a.cols == 0) return fail(HUFFLLM_ERR_INVALID_ARG, "vectors and cols must be at least 1");
+    if (a.vectors > 0x7FFFFFFFull || a.cols > (1ull << 31)) return fail(HUFFLLM_ERR_UNSUPPORTED, "at most 2^31 - 1 vectors and 2^31 columns per launch");
+    if (!(a.eps >= 0.0f)) return fail(HUFFLLM_ERR_INVALID_ARG, "eps must not be negative");
+    const uintptr_t xm = elem_bytes(a.x_type) - 1, dm = elem_bytes(a.delta_type) - 1;
+    if (((uintptr_t)a.x & xm) || ((uintptr_t)a.sum & xm) || ((uintptr_t)a.delta & dm) || ((uintptr_t)a.gain & 1) || ((uintptr_t)a.out & 1))
+        return fail(HUFFLLM_ERR_INVALID_ARG, "pointers must be aligned to their types");
+    auto stride = [&](uint64_t s) -> uint64_t { return s ? s : a.cols; };
+    for (uint64_t s : {a.x_stride, a.delta_stride, a.sum_stride, a.out_stride})
+        if (stride(s) < a.cols) return fail(HUFFLLM_ERR_INVALID_ARG, "stride below the number of columns");
+    if (a.sum && a.sum == a.x && stride(a.sum_stride) != stride(a.x_stride))
+        return fail(HUFFLLM_ERR_INVALID_ARG, "sum in place of x takes x's stride");
+    if (a.sum && a.sum == a.delta && (stride(a.sum_stride) != stride(a.delta_stride) || a.x_type != a.delta_type))
+        return fail(HUFFLLM_ERR_INVALID_ARG, "sum in place of delta takes delta's stride and type");
+    NormArgs k;
+    memset(&k, 0, sizeof(k));
+    k.x = a.x;
+    k.delta = a.delta;
+    k.gain = a.gain;
+    k.sum = a.sum;
+    k.out = a.out;
+    k.x_stride = stride(a.x_stride);
+    k.delta_stride = stride(a.delta_stride);
+    k.sum_stride = stride(a.sum_stride);
+    k.out_stride = stride(a.out_stride);
+    k.cols = a.cols;
+    k.eps = a.eps;
+    k.x16 = a.x_type == HUFFLLM_ELEM_16;
+    k.delta16 = a.delta_type == HUFFLLM_ELEM_16;
+    cudaError_t e = launch_add_rms_norm(k, (uint32_t)a.vectors, a.dtype == HUFFLLM_FP16, (cudaStream_t)stream);
+    if (e != cudaSuccess) return fail(HUFFLLM_ERR_CUDA, "norm launch: %s", cudaGetErrorString(e));
+    return HUFFLLM_OK;
+}
+
+// Workspace of the feed-forward sub-layer: what its two products need, one after the other (their counters in front, with room for the
+// larger number of them), then the norm's and the gated product's outputs.
+static huffllm_status check_ffn(const huffllm_ffn *f, uint32_t batch, size_t *shift_gate_up, size_t *shift_down, size_t *n_bytes, size_t *m_bytes) {
+    if (!f) return fail(HUFFLLM_ERR_INVALID_ARG, "null pointer");
+    huffllm_status st;
+    if ((st = check_desc(f->gate_up)) != HUFFLLM_OK || (st = check_desc(f->down)) != HUFFLLM_OK) return st;
+    if (batch == 0 || batch > 64) return fail(HUFFLLM_ERR_INVALID_ARG, "batch must be in [1, 64]");
+    if (f->gate_up->dtype != f->down->dtype) return fail(HUFFLLM_ERR_UNSUPPORTED, "gate_up and down must share the dtype");
+    if (f->ffn_rows == 0 || f->ffn_rows != f->down->cols || f->gate_up->rows != (f->ffn_rows + 7) / 8 * 16 || f->gate_up->cols != f->down->rows)
+        return fail(HUFFLLM_ERR_INVALID_ARG, "gate_up must be 16 * ceil(ffn_rows / 8) x hidden and down hidden x ffn_rows");
+    const size_t a = ws_partial_offset(f->gate_up), b = ws_partial_offset(f->down), most = a > b ? a : b;
+    *shift_gate_up = most - a;
+    *shift_down = most - b;
+    *n_bytes = ((size_t)batch * f->gate_up->cols * 2 + 255) / 256 * 256;
+    *m_bytes = ((size_t)batch * f->ffn_rows * 2 + 255) / 256 * 256;
+    return HUFFLLM_OK;
+}
+
+huffllm_status huffllm_ffn_workspace_bytes(const huffllm_ffn *f, uint32_t batch, size_t *bytes) {
+    clear_error();
+    if (!bytes) return fail(HUFFLLM_ERR_INVALID_ARG, "bytes is null");
+    size_t s0, s1, n, m, w0, w1;
+    huffllm_status st = check_ffn(f, batch, &s0, &s1, &n, &m);
+    if (st != HUFFLLM_OK) return st;
+    if ((st = huffllm_workspace_bytes(f->gate_up, batch, &w0)) != HUFFLLM_OK || (st = huffllm_workspace_bytes(f->down, batch, &w1)) != HUFFLLM_OK) return st;
+    w0 += s0;
+    w1 += s1;
+    *bytes = ((w0 > w1 ? w0 : w1) + 255) / 256 * 256 + n + m;
+    return HUFFLLM_OK;
+}
+
+huffllm_status huffllm_decode_ffn(const huffllm_ffn *f, const void *h, uint64_t h_stride, uint32_t batch, void *out, uint64_t out_stride,
+                                  uint32_t h_type, void *workspace, size_t workspace_bytes, int32_t *err_flag, huffllm_stream stream) {
+    clear_error();
+    size_t s0, s1, n_bytes, m_bytes;
+    huffllm_status st = check_ffn(f, batch, &s0, &s1, &n_bytes, &m_bytes);
+    if (st != HUFFLLM_OK) return st;
+    if (!h || !out || !workspace) return fail(HUFFLLM_ERR_INVALID_ARG, "null pointer");
+    if ((uintptr_t)workspace & 255) return fail(HUFFLLM_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    if (workspace_bytes < n_bytes + m_bytes) return fail(HUFFLLM_ERR_BUFFER_TOO_SMALL, "workspace too small");
+    const size_t w = (workspace_bytes - n_bytes - m_bytes) & ~(size_t)255;
+    uint16_t *const n = (uint16_t *)((uint8_t *)workspace + w), *const m = (uint16_t *)((uint8_t *)workspace + w + n_bytes);
+    huffllm_epilogue gated = {}, down = {};
+    gated.activation = f->activation;
+    gated.out_type = HUFFLLM_ELEM_16;
+    gated.gated_rows = f->ffn_rows;
+    gated.bias = f->gate_up_bias;
+    down.out_type = h_type;
+    down.bias = f->down_bias;
+    down.residual = h;
+    down.residual_stride = h_stride;
+    down.out_stride = out_stride;
+    // (nothing is launched for a call that one of its steps refuses)
+    EpiMat unused;
+    if ((st = make_epilogue(gated, f->gate_up, m, &unused)) != HUFFLLM_OK || (st = make_epilogue(down, f->down, out, &unused)) != HUFFLLM_OK ||
+        (st = product_one(f->gate_up, f->gate_up_blob, n, batch, nullptr, &gated, m, workspace, w, s0, err_flag, stream, true)) != HUFFLLM_OK ||
+        (st = product_one(f->down, f->down_blob, m, batch, nullptr, &down, out, workspace, w, s1, err_flag, stream, true)) != HUFFLLM_OK)
+        return st;
+    huffllm_norm norm = {};
+    norm.dtype = f->gate_up->dtype;
+    norm.x_type = h_type;
+    norm.eps = f->eps;
+    norm.vectors = batch;
+    norm.cols = f->gate_up->cols;
+    norm.x = h;
+    norm.x_stride = h_stride;
+    norm.gain = f->gain;
+    norm.out = n;
+    if ((st = huffllm_add_rms_norm(&norm, stream)) != HUFFLLM_OK) return st;
+    if ((st = product_one(f->gate_up, f->gate_up_blob, n, batch, nullptr, &gated, m, workspace, w, s0, err_flag, stream)) != HUFFLLM_OK) return st;
+    return product_one(f->down, f->down_blob, m, batch, nullptr, &down, out, workspace, w, s1, err_flag, stream);
 }
 
 }  // extern "C"

@@ -30,6 +30,7 @@
 #include <cstdint>
 
 #include "decode_common.cuh"
+#include "epilogue.cuh"
 #include "row_pieces.h"
 
 namespace huffllm {
@@ -116,8 +117,9 @@ __device__ __forceinline__ void store_piece(uint16_t *dst, const uint4 &p, int32
 // weights and one vector: those run on the FMA pipe, which the decoder leaves idle.
 // SLOTS = shared-memory slots per decoder warp: 2 (a warp's next record lands while it decodes this one), or 1 for records
 // so large that pairs would leave too few warps a place (the feeder then waits for the slot before every copy).
-template <int MODE, int LB, int THREADS, int FMT, int NT = 1, int SLOTS = 2>
-__global__ void __launch_bounds__(THREADS, 1) huff_kernel(const __grid_constant__ KernelArgs A) {
+// EPI = 1 (MODE 1): a row group's sums go through the call's epilogue (epilogue.cuh) instead of to y.
+template <int MODE, int LB, int THREADS, int FMT, int NT = 1, int SLOTS = 2, int EPI = 0>
+__global__ void __launch_bounds__(THREADS, 1) huff_kernel(const __grid_constant__ ProductArgs<EPI> A) {
     constexpr int kV = NT == 2 ? 8 : 4;                       // values a lane holds of a row group's 16 x batch outputs
     constexpr int kOut = NT == 0 ? 1 : kV;                    // outputs a lane adds up and stores
     constexpr uint32_t kRawBlock = FMT ? 64u : 512u;          // raw bytes of one block of a record
@@ -380,6 +382,16 @@ __global__ void __launch_bounds__(THREADS, 1) huff_kernel(const __grid_constant_
                 for (int i = 0; i < kOut; ++i)
                     if (lane + 32 * i < vals) v[i] += __ldcg(piece + 32 * i);
             }
+        }
+        if constexpr (EPI != 0) {
+            // through this warp's entry once more (whoever had to read its piece has): the epilogue takes a tile's outputs in an order of its own
+            float *const tile = part_val + mine * vals;
+#pragma unroll
+            for (int i = 0; i < kOut; ++i)
+                if (lane + 32 * i < vals) tile[lane + 32 * i] = v[i];
+            __syncwarp();
+            finish_tile<FMT != 0, NT == 0 ? 1 : 4>(A.e[mi], tile, A.batch, rg, k.rows, lane);
+            return;
         }
         const uint64_t r = (uint64_t)rg * 16 + (lane & 15);
         float *const y = k.y + (uint64_t)(lane >> 4) * k.rows + r;
@@ -654,9 +666,9 @@ __global__ void __launch_bounds__(THREADS, 1) huff_kernel(const __grid_constant_
 
 // ------------------------------------------------------------------------------ launchers
 
-template <int MODE, int LB, int THREADS, int FMT, int NT = 1, int SLOTS = 2>
-static cudaError_t launch_one(const KernelArgs &k, uint32_t grid, cudaStream_t stream) {
-    auto fn = huff_kernel<MODE, LB, THREADS, FMT, NT, SLOTS>;
+template <int MODE, int LB, int THREADS, int FMT, int NT = 1, int SLOTS = 2, int EPI = 0>
+static cudaError_t launch_one(const ProductArgs<EPI> &k, uint32_t grid, cudaStream_t stream) {
+    auto fn = huff_kernel<MODE, LB, THREADS, FMT, NT, SLOTS, EPI>;
     static std::atomic<bool> attr_set[64];   // set twice by racing threads at worst: the call is idempotent
     int dev = 0;
     cudaGetDevice(&dev);
@@ -679,24 +691,24 @@ static cudaError_t launch_one(const KernelArgs &k, uint32_t grid, cudaStream_t s
 }
 
 // One or two slots per decoder warp (the host decides; kernels.h says for which kernels single slots exist).
-template <int MODE, int LB, int FMT, int NT = 1>
-static cudaError_t launch_slots(const KernelArgs &k, uint32_t grid, cudaStream_t stream) {
-    if (k.slots == 1) return launch_one<MODE, LB, kThreads, FMT, NT, 1>(k, grid, stream);
-    return launch_one<MODE, LB, kThreads, FMT, NT, 2>(k, grid, stream);
+template <int MODE, int LB, int FMT, int NT = 1, int EPI = 0>
+static cudaError_t launch_slots(const ProductArgs<EPI> &k, uint32_t grid, cudaStream_t stream) {
+    if (k.slots == 1) return launch_one<MODE, LB, kThreads, FMT, NT, 1, EPI>(k, grid, stream);
+    return launch_one<MODE, LB, kThreads, FMT, NT, 2, EPI>(k, grid, stream);
 }
 
 // The kernel of a launch's blobs: format, code lengths, flat codes (kernels.h).
-template <int MODE, int NT>
-static cudaError_t launch_format(const KernelArgs &k, uint32_t grid, cudaStream_t stream) {
+template <int MODE, int NT, int EPI = 0>
+static cudaError_t launch_format(const ProductArgs<EPI> &k, uint32_t grid, cudaStream_t stream) {
     if (k.fmt) {
-        if (k.lut_bits > 8) return launch_slots<MODE, 12, 1, NT>(k, grid, stream);
-        if (k.fp16_flat == kFlatBoth) return launch_slots<MODE, 8, 2, NT>(k, grid, stream);
-        if (k.fp16_flat == kFlatBothLanes) return launch_slots<MODE, 8, 4, NT>(k, grid, stream);
-        if (k.fp16_flat == kFlatUpper) return launch_slots<MODE, 8, 3, NT>(k, grid, stream);
-        return k.lut_bits == 7 ? launch_slots<MODE, 7, 1, NT>(k, grid, stream) : launch_slots<MODE, 8, 1, NT>(k, grid, stream);
+        if (k.lut_bits > 8) return launch_slots<MODE, 12, 1, NT, EPI>(k, grid, stream);
+        if (k.fp16_flat == kFlatBoth) return launch_slots<MODE, 8, 2, NT, EPI>(k, grid, stream);
+        if (k.fp16_flat == kFlatBothLanes) return launch_slots<MODE, 8, 4, NT, EPI>(k, grid, stream);
+        if (k.fp16_flat == kFlatUpper) return launch_slots<MODE, 8, 3, NT, EPI>(k, grid, stream);
+        return k.lut_bits == 7 ? launch_slots<MODE, 7, 1, NT, EPI>(k, grid, stream) : launch_slots<MODE, 8, 1, NT, EPI>(k, grid, stream);
     }
-    if (k.lut_bits > 9) return launch_one<MODE, 12, kThreads, 0, NT>(k, grid, stream);
-    return k.lut_bits == 8 ? launch_slots<MODE, 8, 0, NT>(k, grid, stream) : launch_one<MODE, 9, kThreads, 0, NT>(k, grid, stream);
+    if (k.lut_bits > 9) return launch_one<MODE, 12, kThreads, 0, NT, 2, EPI>(k, grid, stream);
+    return k.lut_bits == 8 ? launch_slots<MODE, 8, 0, NT, EPI>(k, grid, stream) : launch_one<MODE, 9, kThreads, 0, NT, 2, EPI>(k, grid, stream);
 }
 
 }  // namespace huffllm

@@ -2,6 +2,7 @@
 #pragma once
 #include <cuda_runtime.h>
 #include <cstdint>
+#include <type_traits>
 
 namespace huffllm {
 
@@ -58,6 +59,22 @@ struct KernelArgs {
 // (kFlatBoth: the exponent's table with sixteen copies of an entry, kFlatBothLanes: with one per lane; the lower half alone is not made use of)
 constexpr uint32_t kFlatNone = 0, kFlatBoth = 1, kFlatUpper = 2, kFlatBothLanes = 3;
 
+// What becomes of one matrix's sums in a product with an epilogue (the terms are huffllm_epilogue's).
+struct EpiMat {
+    const uint16_t *bias;      // [rows], may be null
+    const void *residual;      // may be null; type and form of `out`
+    void *out;                 // vectors out_stride values apart
+    uint64_t residual_stride, out_stride;
+    uint64_t gated_rows;       // 0, or the outputs of a matrix of stacked gate and up rows
+    uint32_t act;              // huffllm_activation
+    uint32_t out16;            // out and residual in the blob's 16-bit type (else fp32)
+};
+struct EpiKernelArgs : KernelArgs {
+    EpiMat e[kMaxMats];
+};
+template <int EPI>
+using ProductArgs = std::conditional_t<EPI != 0, EpiKernelArgs, KernelArgs>;
+
 // Arguments of the tensor-core kernel: the launch description plus, per matrix, its work items and where their pieces meet.
 // (The CTAs of a launch are dealt to the matrices as in the other kernels: m[i].cta_first / cta_count.)
 struct TcArgs {
@@ -68,9 +85,28 @@ struct TcArgs {
     unsigned int *ticket[kMaxMats];    // [m_tiles][32] (several slices: [m_tiles]), zero between calls
 };
 
+struct EpiTcArgs : TcArgs {
+    EpiMat e[kMaxMats];
+};
+template <int EPI>
+using TcProductArgs = std::conditional_t<EPI != 0, EpiTcArgs, TcArgs>;
+
 cudaError_t launch_decode(const KernelArgs &k, uint32_t grid, cudaStream_t stream);
 cudaError_t launch_gemm(const KernelArgs &k, uint32_t grid, cudaStream_t stream);
 cudaError_t launch_gemm_tc(const TcArgs &t, uint32_t grid, cudaStream_t stream);
+cudaError_t launch_gemm(const EpiKernelArgs &k, uint32_t grid, cudaStream_t stream);
+cudaError_t launch_gemm_tc(const EpiTcArgs &t, uint32_t grid, cudaStream_t stream);
+// Residual addition and norm: strides in values; x16, delta16: 16-bit values (else fp32), sum has x's type.
+struct NormArgs {
+    const void *x, *delta;     // delta: may be null
+    const uint16_t *gain;      // may be null (ones)
+    void *sum;                 // may be null
+    uint16_t *out;
+    uint64_t x_stride, delta_stride, sum_stride, out_stride, cols;
+    float eps;
+    uint32_t x16, delta16;
+};
+cudaError_t launch_add_rms_norm(const NormArgs &a, uint32_t vectors, bool fp16, cudaStream_t stream);
 cudaError_t launch_stage_copy(void *dst, const void *src, uint64_t bytes, uint32_t sms, cudaStream_t stream);
 // The dense bf16 comparison product: up to kMaxMats matrices per launch, rows dealt to the warps round-robin.
 struct PlainMat {

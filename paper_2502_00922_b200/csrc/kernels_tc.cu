@@ -3,6 +3,6 @@
 
 namespace huffllm {
 
-cudaError_t launch_gemm_tc(const TcArgs &t, uint32_t grid, cudaStream_t stream) { return launch_tc_format(t, grid, stream); }
+cudaError_t launch_gemm_tc(const TcArgs &t, uint32_t grid, cudaStream_t stream) { return launch_tc_format<0>(t, grid, stream); }
 
 }  // namespace huffllm

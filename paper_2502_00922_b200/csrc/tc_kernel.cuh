@@ -39,6 +39,7 @@
 #include <type_traits>
 
 #include "decode_common.cuh"
+#include "epilogue.cuh"
 
 namespace huffllm {
 
@@ -135,8 +136,9 @@ __device__ __forceinline__ bool elect_one() {
 // LB = table index bits; NPAD = batch rounded up to 16, 32 or 64 (the MMA's N); FMT = 0: BF16 blobs, 1: FP16 {1,5,5,5} blobs, 2 to 4: those with flat mantissa codes, see huff_kernel
 // (three tables, sign words as the raw part, f16 operands).
 // MULTI: the launch works through several matrices (a launch over one matrix reads its arguments without an index).
-template <int LB, int NPAD, int FMT, bool MULTI>
-__global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_constant__ TcArgs T) {
+// EPI = 1: a work item's sums go through the call's epilogue (epilogue.cuh) instead of to y.
+template <int LB, int NPAD, int FMT, bool MULTI, int EPI = 0>
+__global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_constant__ TcProductArgs<EPI> T) {
     const KernelArgs &A = T.k;
     constexpr uint32_t kRawBlock = FMT ? 64u : 512u;          // raw bytes of one block of a record
     constexpr uint32_t kRawLane = FMT ? 2u : 16u;             // of which one lane's share
@@ -479,6 +481,10 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
         const uint64_t row = (uint64_t)(mt * n_rg + acc_tile * 8) * 16 + 32u * q + lane;
         const bool row_ok = row < k.rows && acc_tile * 8 + 2 * q + (lane >> 4) < n_rg;   // (row groups behind the CTA's belong to the next item)
         auto write = [&](const float (&out)[CW]) {
+            if constexpr (EPI != 0) {
+                finish_columns<FMT != 0, CW>(T.e[MULTI ? mi : 0], out, n0, A.batch, row, row_ok, lane);
+                return;
+            }
 #pragma unroll
             for (int i = 0; i < CW; ++i)
                 if (n0 + i < A.batch && row_ok) k.y[(uint64_t)(n0 + i) * k.rows + row] = out[i];
@@ -724,10 +730,10 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
     if (warp == issuer) tmem_dealloc(tmem, 512);
 }
 
-template <int LB, int NPAD, int FMT, bool MULTI>
-static cudaError_t launch_tc_m(const TcArgs &t, uint32_t grid, cudaStream_t stream) {
+template <int LB, int NPAD, int FMT, bool MULTI, int EPI>
+static cudaError_t launch_tc_m(const TcProductArgs<EPI> &t, uint32_t grid, cudaStream_t stream) {
     const KernelArgs &k = t.k;
-    auto fn = huff_gemm_tc_kernel<LB, NPAD, FMT, MULTI>;
+    auto fn = huff_gemm_tc_kernel<LB, NPAD, FMT, MULTI, EPI>;
     static std::atomic<bool> attr_set[64];   // set twice by racing threads at worst: the call is idempotent
     int dev = 0;
     cudaGetDevice(&dev);
@@ -749,43 +755,44 @@ static cudaError_t launch_tc_m(const TcArgs &t, uint32_t grid, cudaStream_t stre
     return cudaLaunchKernelEx(&cfg, fn, t);
 }
 
-template <int LB, int NPAD, int FMT>
-static cudaError_t launch_tc_one(const TcArgs &t, uint32_t grid, cudaStream_t stream) {
-    if (t.k.n_mats > 1) return launch_tc_m<LB, NPAD, FMT, true>(t, grid, stream);
-    return launch_tc_m<LB, NPAD, FMT, false>(t, grid, stream);
+template <int LB, int NPAD, int FMT, int EPI>
+static cudaError_t launch_tc_one(const TcProductArgs<EPI> &t, uint32_t grid, cudaStream_t stream) {
+    if (t.k.n_mats > 1) return launch_tc_m<LB, NPAD, FMT, true, EPI>(t, grid, stream);
+    return launch_tc_m<LB, NPAD, FMT, false, EPI>(t, grid, stream);
 }
 
 // The kernel of a launch's blobs and padding.
-static cudaError_t launch_tc_format(const TcArgs &t, uint32_t grid, cudaStream_t stream) {
+template <int EPI>
+static cudaError_t launch_tc_format(const TcProductArgs<EPI> &t, uint32_t grid, cudaStream_t stream) {
     const KernelArgs &k = t.k;
     if (k.fmt && k.fp16_flat == kFlatUpper) {
-        if (k.tc_npad == 16) return launch_tc_one<8, 16, 3>(t, grid, stream);
-        if (k.tc_npad == 32) return launch_tc_one<8, 32, 3>(t, grid, stream);
-        return launch_tc_one<8, 64, 3>(t, grid, stream);
+        if (k.tc_npad == 16) return launch_tc_one<8, 16, 3, EPI>(t, grid, stream);
+        if (k.tc_npad == 32) return launch_tc_one<8, 32, 3, EPI>(t, grid, stream);
+        return launch_tc_one<8, 64, 3, EPI>(t, grid, stream);
     }
     if (k.fmt && k.fp16_flat == kFlatBoth) {
-        if (k.tc_npad == 16) return launch_tc_one<8, 16, 2>(t, grid, stream);
-        if (k.tc_npad == 32) return launch_tc_one<8, 32, 2>(t, grid, stream);
-        return launch_tc_one<8, 64, 2>(t, grid, stream);
+        if (k.tc_npad == 16) return launch_tc_one<8, 16, 2, EPI>(t, grid, stream);
+        if (k.tc_npad == 32) return launch_tc_one<8, 32, 2, EPI>(t, grid, stream);
+        return launch_tc_one<8, 64, 2, EPI>(t, grid, stream);
     }
     if (k.fmt && k.fp16_flat == kFlatBothLanes) {
-        if (k.tc_npad == 16) return launch_tc_one<8, 16, 4>(t, grid, stream);
-        if (k.tc_npad == 32) return launch_tc_one<8, 32, 4>(t, grid, stream);
-        return launch_tc_one<8, 64, 4>(t, grid, stream);
+        if (k.tc_npad == 16) return launch_tc_one<8, 16, 4, EPI>(t, grid, stream);
+        if (k.tc_npad == 32) return launch_tc_one<8, 32, 4, EPI>(t, grid, stream);
+        return launch_tc_one<8, 64, 4, EPI>(t, grid, stream);
     }
     if (k.fmt) {
-        if (k.tc_npad == 16) return launch_tc_one<8, 16, 1>(t, grid, stream);
-        if (k.tc_npad == 32) return launch_tc_one<8, 32, 1>(t, grid, stream);
-        return launch_tc_one<8, 64, 1>(t, grid, stream);
+        if (k.tc_npad == 16) return launch_tc_one<8, 16, 1, EPI>(t, grid, stream);
+        if (k.tc_npad == 32) return launch_tc_one<8, 32, 1, EPI>(t, grid, stream);
+        return launch_tc_one<8, 64, 1, EPI>(t, grid, stream);
     }
     if (k.lut_bits == 8) {
-        if (k.tc_npad == 16) return launch_tc_one<8, 16, 0>(t, grid, stream);
-        if (k.tc_npad == 32) return launch_tc_one<8, 32, 0>(t, grid, stream);
-        return launch_tc_one<8, 64, 0>(t, grid, stream);
+        if (k.tc_npad == 16) return launch_tc_one<8, 16, 0, EPI>(t, grid, stream);
+        if (k.tc_npad == 32) return launch_tc_one<8, 32, 0, EPI>(t, grid, stream);
+        return launch_tc_one<8, 64, 0, EPI>(t, grid, stream);
     }
-    if (k.tc_npad == 16) return launch_tc_one<9, 16, 0>(t, grid, stream);
-    if (k.tc_npad == 32) return launch_tc_one<9, 32, 0>(t, grid, stream);
-    return launch_tc_one<9, 64, 0>(t, grid, stream);
+    if (k.tc_npad == 16) return launch_tc_one<9, 16, 0, EPI>(t, grid, stream);
+    if (k.tc_npad == 32) return launch_tc_one<9, 32, 0, EPI>(t, grid, stream);
+    return launch_tc_one<9, 64, 0, EPI>(t, grid, stream);
 }
 
 }  // namespace huffllm
