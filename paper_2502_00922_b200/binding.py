@@ -8,6 +8,8 @@ import numpy as np
 
 BF16, FP16 = 0, 1
 SPLIT_PAPER, SPLIT_WHOLE_EXPONENT = 0, 1
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = range(5)
+ELEM_F32, ELEM_16 = 0, 1
 _SO = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libhuffllm.so")
 _lib = None
 
@@ -36,6 +38,44 @@ class Desc(C.Structure):
 
 assert C.sizeof(Desc) == 256
 
+
+class Epilogue(C.Structure):
+    """huffllm_epilogue: what becomes of a product's sums.  The tensors must stay alive and in place for as long as it is used."""
+    _fields_ = [("activation", C.c_uint32), ("out_type", C.c_uint32), ("gated_rows", C.c_uint64), ("bias", C.c_void_p),
+                ("residual", C.c_void_p), ("residual_stride", C.c_uint64), ("out_stride", C.c_uint64)]
+
+    def __init__(self, activation: int = ACT_NONE, out_type: int = ELEM_F32, bias=None, residual=None, residual_stride: int = 0,
+                 out_stride: int = 0, gated_rows: int = 0):
+        super().__init__(activation, out_type, gated_rows, _ptr(bias), _ptr(residual), residual_stride, out_stride)
+        self._keep = (bias, residual)
+
+
+class Norm(C.Structure):
+    """huffllm_norm: the arguments of a residual addition and norm (the tensors must stay alive and in place)."""
+    _fields_ = [("dtype", C.c_uint32), ("x_type", C.c_uint32), ("delta_type", C.c_uint32), ("eps", C.c_float),
+                ("vectors", C.c_uint64), ("cols", C.c_uint64), ("x", C.c_void_p), ("delta", C.c_void_p), ("gain", C.c_void_p),
+                ("sum", C.c_void_p), ("out", C.c_void_p), ("x_stride", C.c_uint64), ("delta_stride", C.c_uint64),
+                ("sum_stride", C.c_uint64), ("out_stride", C.c_uint64)]
+
+    def __init__(self, dtype: int, vectors: int, cols: int, x, x_type: int, gain, eps: float, out, delta=None, delta_type: int = ELEM_F32,
+                 sum=None, x_stride: int = 0, delta_stride: int = 0, sum_stride: int = 0, out_stride: int = 0):
+        super().__init__(dtype, x_type, delta_type, eps, vectors, cols, _ptr(x), _ptr(delta), _ptr(gain), _ptr(sum), _ptr(out),
+                         x_stride, delta_stride, sum_stride, out_stride)
+        self._keep = (x, delta, gain, sum, out)
+
+
+class Ffn(C.Structure):
+    """huffllm_ffn: the weights of a feed-forward sub-layer (the tensors must stay alive and in place)."""
+    _fields_ = [("gate_up", C.POINTER(Desc)), ("down", C.POINTER(Desc)), ("gate_up_blob", C.c_void_p), ("down_blob", C.c_void_p),
+                ("ffn_rows", C.c_uint64), ("activation", C.c_uint32), ("eps", C.c_float), ("gain", C.c_void_p),
+                ("gate_up_bias", C.c_void_p), ("down_bias", C.c_void_p)]
+
+    def __init__(self, gate_up: Desc, gate_up_blob, down: Desc, down_blob, ffn_rows: int, gain=None, eps: float = 1e-5,
+                 activation: int = ACT_SILU, gate_up_bias=None, down_bias=None):
+        super().__init__(C.pointer(gate_up), C.pointer(down), _ptr(gate_up_blob), _ptr(down_blob), ffn_rows, activation, eps, _ptr(gain),
+                         _ptr(gate_up_bias), _ptr(down_bias))
+        self._keep = (gate_up, gate_up_blob, down, down_blob, gain, gate_up_bias, down_bias)
+
 _SIGNATURES = {
     "huffllm_build_codebook": [C.c_void_p, C.c_uint64, C.c_uint64, C.c_int, C.c_uint32, C.POINTER(C.c_void_p)],
     "huffllm_build_codebook_split": [C.c_void_p, C.c_uint64, C.c_uint64, C.c_int, C.c_int, C.c_uint32, C.POINTER(C.c_void_p)],
@@ -62,6 +102,17 @@ _SIGNATURES = {
     "huffllm_decode_gemm_host": [C.POINTER(Desc), C.c_void_p, C.c_void_p, C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p,
                                  C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p],
     "huffllm_decode_gemm_static": [C.POINTER(Desc), C.c_void_p, C.c_void_p, C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p],
+    "huffllm_decode_gemm_epilogue": [C.POINTER(Desc), C.c_void_p, C.c_void_p, C.c_uint32, C.POINTER(Epilogue), C.c_void_p, C.c_void_p,
+                                     C.c_size_t, C.c_void_p, C.c_void_p],
+    "huffllm_decode_gemm_multi_epilogue": [C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                           C.c_size_t, C.c_void_p, C.c_void_p],
+    "huffllm_stacked_rows": [C.c_uint64, C.POINTER(C.c_uint64)],
+    "huffllm_stack_gate_up": [C.c_void_p, C.c_void_p, C.c_uint64, C.c_uint64, C.c_void_p],
+    "huffllm_stack_gate_up_device": [C.c_void_p, C.c_void_p, C.c_uint64, C.c_uint64, C.c_void_p, C.c_void_p],
+    "huffllm_add_rms_norm": [C.POINTER(Norm), C.c_void_p],
+    "huffllm_ffn_workspace_bytes": [C.POINTER(Ffn), C.c_uint32, C.POINTER(C.c_size_t)],
+    "huffllm_decode_ffn": [C.POINTER(Ffn), C.c_void_p, C.c_uint64, C.c_uint32, C.c_void_p, C.c_uint64, C.c_uint32, C.c_void_p, C.c_size_t,
+                           C.c_void_p, C.c_void_p],
     "huffllm_stage_copy": [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p],
     "huffllm_plain_gemv": [C.c_void_p, C.c_uint64, C.c_uint64, C.c_void_p, C.c_void_p, C.c_void_p],
     "huffllm_plain_gemv_multi": [C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p],
@@ -407,3 +458,114 @@ def encode_device(cb: Codebook, w_dev, rows: int, cols: int, chunk_elems, blob_d
 def stage_copy(dst, src, nbytes: int, stream=None):
     """huffllm_stage_copy: a small copy by a kernel between device-accessible buffers (device or pinned host memory)."""
     _check(lib().huffllm_stage_copy(_ptr(dst), _ptr(src), nbytes, _stream(stream)))
+
+
+def decode_gemm_epilogue(desc: Desc, blob_dev, x_dev, batch: int, epilogue: Epilogue, out_dev, workspace_dev, workspace_bytes_: int,
+                         err_flag_dev=None, stream=None):
+    """huffllm_decode_gemm_epilogue: a product with bias, activation, residual and rounding, or a gated product."""
+    _check(lib().huffllm_decode_gemm_epilogue(C.byref(desc), _ptr(blob_dev), _ptr(x_dev), batch, C.byref(epilogue), _ptr(out_dev),
+                                              _ptr(workspace_dev), workspace_bytes_, _ptr(err_flag_dev), _stream(stream)))
+
+
+class PreparedEpilogue:
+    """The arguments of a huffllm_decode_gemm_epilogue call, or of a _multi_epilogue call over several matrices (lists of equal
+    length), marshalled once.  The tensors must stay alive and in place for as long as the object is used."""
+
+    def __init__(self, descs, blobs_dev, xs_dev, batch: int, epilogues, outs_dev, workspaces_dev, workspace_bytes_each: int,
+                 err_flag_dev=None):
+        n = len(descs)
+        self._keep = (descs, blobs_dev, xs_dev, epilogues, outs_dev, workspaces_dev, err_flag_dev)
+        ptrs = lambda seq: (C.c_void_p * n)(*[_ptr(t) for t in seq])
+        eps, err = (Epilogue * n)(*epilogues), _ptr(err_flag_dev)
+        if n == 1:
+            self._fn = lib().huffllm_decode_gemm_epilogue
+            self._args = (C.pointer(descs[0]), _ptr(blobs_dev[0]), _ptr(xs_dev[0]), batch, eps, _ptr(outs_dev[0]), _ptr(workspaces_dev[0]),
+                          workspace_bytes_each, err)
+        else:
+            self._fn = lib().huffllm_decode_gemm_multi_epilogue
+            self._args = (n, (C.POINTER(Desc) * n)(*[C.pointer(d) for d in descs]), ptrs(blobs_dev), ptrs(xs_dev), batch, eps,
+                          ptrs(outs_dev), ptrs(workspaces_dev), workspace_bytes_each, err)
+
+    def run(self, stream: int):
+        """`stream` is the raw cudaStream_t value."""
+        st = self._fn(*self._args, stream)
+        if st:
+            _check(st)
+
+
+def decode_gemm_multi_epilogue(descs, blobs_dev, xs_dev, batch: int, epilogues, outs_dev, workspaces_dev, workspace_bytes_each: int,
+                               err_flag_dev=None, stream=None):
+    """huffllm_decode_gemm_multi_epilogue: lists of equal length, one entry per matrix."""
+    n = len(descs)
+    desc_arr = (C.POINTER(Desc) * n)(*[C.pointer(d) for d in descs])
+    ptrs = lambda seq: (C.c_void_p * n)(*[_ptr(t) for t in seq])
+    _check(lib().huffllm_decode_gemm_multi_epilogue(n, desc_arr, ptrs(blobs_dev), ptrs(xs_dev), batch, (Epilogue * n)(*epilogues), ptrs(outs_dev),
+                                                    ptrs(workspaces_dev), workspace_bytes_each, _ptr(err_flag_dev), _stream(stream)))
+
+
+def stacked_rows(n: int) -> int:
+    """huffllm_stacked_rows: rows of a stacked gate and up of n rows each."""
+    rows = C.c_uint64()
+    _check(lib().huffllm_stacked_rows(n, C.byref(rows)))
+    return rows.value
+
+
+def stack_gate_up(gate: np.ndarray, up: np.ndarray) -> np.ndarray:
+    """huffllm_stack_gate_up: gate and up ([n][cols] 16-bit words, host), or two biases ([n]), in the row order of a gated product."""
+    gate, up = np.ascontiguousarray(gate, dtype=np.uint16), np.ascontiguousarray(up, dtype=np.uint16)
+    if gate.shape != up.shape:
+        raise ValueError("gate and up differ in shape")
+    n, cols = gate.shape if gate.ndim == 2 else (gate.size, 1)
+    out = np.empty((stacked_rows(n), cols) if gate.ndim == 2 else stacked_rows(n), dtype=np.uint16)
+    _check(lib().huffllm_stack_gate_up(gate.ctypes.data, up.ctypes.data, n, cols, out.ctypes.data))
+    return out
+
+
+def stack_gate_up_device(gate_dev, up_dev, n: int, cols: int, stacked_dev, stream=None):
+    """huffllm_stack_gate_up_device: the same in device memory; stacked_dev has stacked_rows(n) rows."""
+    _check(lib().huffllm_stack_gate_up_device(_ptr(gate_dev), _ptr(up_dev), n, cols, _ptr(stacked_dev), _stream(stream)))
+
+
+def add_rms_norm(norm: Norm, stream=None):
+    """huffllm_add_rms_norm: h = x + delta; sum = h; out = h / sqrt(mean(h^2) + eps) * gain."""
+    _check(lib().huffllm_add_rms_norm(C.byref(norm), _stream(stream)))
+
+
+class PreparedNorm:
+    """A huffllm_add_rms_norm call, marshalled once."""
+
+    def __init__(self, norm: Norm):
+        self.norm, self._fn, self._arg = norm, lib().huffllm_add_rms_norm, C.pointer(norm)
+
+    def run(self, stream: int):
+        st = self._fn(self._arg, stream)
+        if st:
+            _check(st)
+
+
+def ffn_workspace_bytes(ffn: Ffn, batch: int = 1) -> int:
+    n = C.c_size_t()
+    _check(lib().huffllm_ffn_workspace_bytes(C.byref(ffn), batch, C.byref(n)))
+    return n.value
+
+
+class PreparedFfn:
+    """A huffllm_decode_ffn call, marshalled once (the tensors must stay alive and in place)."""
+
+    def __init__(self, ffn: Ffn, h_dev, batch: int, out_dev, h_type: int, workspace_dev, workspace_bytes_: int, err_flag_dev=None,
+                 h_stride: int = 0, out_stride: int = 0):
+        self._keep = (ffn, h_dev, out_dev, workspace_dev, err_flag_dev)
+        self._fn = lib().huffllm_decode_ffn
+        self._args = (C.pointer(ffn), _ptr(h_dev), h_stride, batch, _ptr(out_dev), out_stride, h_type, _ptr(workspace_dev), workspace_bytes_,
+                      _ptr(err_flag_dev))
+
+    def run(self, stream: int):
+        st = self._fn(*self._args, stream)
+        if st:
+            _check(st)
+
+
+def decode_ffn(ffn: Ffn, h_dev, batch: int, out_dev, h_type: int, workspace_dev, workspace_bytes_: int, err_flag_dev=None,
+               h_stride: int = 0, out_stride: int = 0, stream=None):
+    """huffllm_decode_ffn: out = h + down(act(gate(norm(h))) * up(norm(h))), from compressed weights."""
+    PreparedFfn(ffn, h_dev, batch, out_dev, h_type, workspace_dev, workspace_bytes_, err_flag_dev, h_stride, out_stride).run(_stream(stream))
