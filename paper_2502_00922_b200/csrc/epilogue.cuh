@@ -19,7 +19,26 @@ namespace huffllm {
 // v / (1 + exp(-u)).  (exp(-u) above 2^126: the quotient is 0 instead of a number below 1e-36.)
 __device__ __forceinline__ float times_sigmoid(float v, float u) { return __fdividef(v, 1.0f + expf(-u)); }
 
-// `act` on N values.  1 + tanh(t) = 2 / (1 + exp(-2 t)) and 1 + erf(t) = erfc(-t): no cancellation where v is far below zero.
+// v / 2 (1 + erf(v / sqrt 2)), from the tail q = erfc(z), z = |v| / sqrt 2:  v q / 2 below zero, v - v q / 2 above.
+// erfc(z) = exp(-z^2) t P(t) with t = 1 / (1 + z / 2): P is the polynomial of degree 8 of least relative error on 0 <= z <= 12
+// (Lawson's reweighted least squares), 1.5e-7 in fp32.  No cancellation where v is far below zero, where 1 + erf(v / sqrt 2) has it.
+// (Through erfcf, too long to be unrolled and so through local memory, 57344 x 8192 at 64 vectors took 348 us, with SiLU 289.)
+__device__ __forceinline__ float gelu(float v) {
+    const float a = fabsf(v), t = __fdividef(1.0f, fmaf(0.353553390593274f, a, 1.0f));
+    float p = -0.05936381220817566f;
+    p = fmaf(p, t, 0.2860138416290283f);
+    p = fmaf(p, t, -0.4901793599128723f);
+    p = fmaf(p, t, 0.2814750075340271f);
+    p = fmaf(p, t, -0.02897183783352375f);
+    p = fmaf(p, t, 0.2036784291267395f);
+    p = fmaf(p, t, 0.24285362660884857f);
+    p = fmaf(p, t, 0.28240957856178284f);
+    p = fmaf(p, t, 0.28208446502685547f);
+    const float q = 0.5f * t * p * expf(-0.5f * v * v);
+    return v < 0.0f ? v * q : v - fminf(v, 64.0f) * q;          // (infinity: q is 0)
+}
+
+// `act` on N values.  1 + tanh(t) = 2 / (1 + exp(-2 t)).
 template <int N>
 __device__ __forceinline__ void activate(float (&v)[N], uint32_t act) {
     if (act == HUFFLLM_ACT_SILU) {
@@ -32,14 +51,8 @@ __device__ __forceinline__ void activate(float (&v)[N], uint32_t act) {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = times_sigmoid(v[i], 1.59576912160573f * v[i] * fmaf(0.044715f * v[i], v[i], 1.0f));   // 2 sqrt(2 / pi)
     } else if (act == HUFFLLM_ACT_GELU) {
-        // (one copy of a long function in code that runs cold: the values take their turns from local memory)
-        float t[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) t[i] = v[i];
-#pragma unroll 1
-        for (int i = 0; i < N; ++i) t[i] = 0.5f * t[i] * erfcf(-0.707106781186548f * t[i]);
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = t[i];
+        for (int i = 0; i < N; ++i) v[i] = gelu(v[i]);
     }
 }
 
@@ -62,86 +75,82 @@ __device__ __forceinline__ void store_value(void *p, uint64_t at, bool is16, flo
     else ((float *)p)[at] = v;
 }
 
-// The outputs of row group rg: tile[16 b + r] is the sum of vector b and the group's row r.  U outputs of a lane at a time, so that
-// their residuals are under way together.
-template <bool F16, int U>
-__device__ __forceinline__ void finish_tile(const EpiMat &e, const float *tile, uint32_t batch, uint32_t rg, uint64_t rows, uint32_t lane) {
-    const bool gated = e.gated_rows != 0, is16 = e.out16 != 0;
-    const uint32_t shift = gated ? 3 : 4, per = 1u << shift, n = per * batch;
-    const uint64_t first = (uint64_t)rg * per, end = gated ? e.gated_rows : rows;
-#pragma unroll 1
-    for (uint32_t o0 = lane; o0 < n; o0 += 32 * U) {
-        float v[U], w[U];                                    // w: the second factor, or the residual
-        bool ok[U];
+// A lane's N sums of one row r = `row`: those of vectors n0, n0 + step, ...  The lanes of a warp hold rows that follow each other, from a
+// multiple of 16 on (lane % 16 = row % 16), so that the other factor of a gated output is what lane ^ 8 holds.  ok: the row exists.
+
+// Their residuals (zero where there are none), all loads under way together: asked about the type once per load, each waited for the one
+// before (8192 x 28672 at 64 vectors 140 us, with neither residual nor activation 128).
+template <bool F16, int N>
+__device__ __forceinline__ void load_residuals(const EpiMat &e, float (&r)[N], uint32_t n0, uint32_t step, uint32_t batch, uint64_t row, bool ok) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t o = o0 + 32 * u, i = o & (per - 1), b = o >> shift;
-            ok[u] = o < n && first + i < end;
-            v[u] = w[u] = 0.0f;
-            if (!ok[u]) continue;
-            v[u] = tile[16 * b + i];
-            if (e.bias) v[u] += widen16<F16>(__ldg(e.bias + (uint64_t)rg * 16 + i));
-            if (gated) {
-                w[u] = tile[16 * b + 8 + i];
-                if (e.bias) w[u] += widen16<F16>(__ldg(e.bias + (uint64_t)rg * 16 + 8 + i));
-            } else if (e.residual) {
-                w[u] = load_value<F16>(e.residual, (uint64_t)b * e.residual_stride + first + i, is16);
-            }
-        }
-        activate<U>(v, e.act);
+    for (int i = 0; i < N; ++i) r[i] = 0.0f;
+    if (!e.residual || !ok) return;
+    const uint64_t at = (uint64_t)n0 * e.residual_stride + row, more = (uint64_t)step * e.residual_stride;
+    if (e.out16) {
+        const unsigned short *p = (const unsigned short *)e.residual + at;
+        unsigned short raw[N];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t o = o0 + 32 * u;
-            if (ok[u]) store_value<F16>(e.out, (uint64_t)(o >> shift) * e.out_stride + first + (o & (per - 1)), is16, gated ? v[u] * w[u] : v[u] + w[u]);
-        }
+        for (int i = 0; i < N; ++i, p += more) raw[i] = n0 + step * i < batch ? __ldcg(p) : 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) r[i] = widen16<F16>(raw[i]);
+    } else {
+        const float *p = (const float *)e.residual + at;
+#pragma unroll
+        for (int i = 0; i < N; ++i, p += more)
+            if (n0 + step * i < batch) r[i] = __ldcg(p);
     }
 }
-
-// The outputs of an accumulator's row `row` (of lane `lane`; the warp's 32 lanes hold rows that follow each other, from a multiple
-// of 16 on) for vectors n0 .. n0 + CW - 1.  Called by the whole warp.
-template <bool F16, int CW>
-__device__ __forceinline__ void finish_columns(const EpiMat &e, const float (&sum)[CW], uint32_t n0, uint32_t batch, uint64_t row, bool row_ok,
-                                               uint32_t lane) {
-    const bool is16 = e.out16 != 0;
-    const float bias = e.bias && row_ok ? widen16<F16>(__ldg(e.bias + row)) : 0.0f;
-    if (e.gated_rows) {
-        // lanes with gate rows finish the even vectors, lanes with up rows the odd ones: one exchange for two outputs
-        const bool up = lane & 8;
-        float v[CW / 2], w[CW / 2];
+template <bool F16>
+__device__ __forceinline__ float load_bias(const EpiMat &e, uint64_t row, bool ok) {
+    return e.bias && ok ? widen16<F16>(__ldg(e.bias + row)) : 0.0f;
+}
+template <bool F16, int N>
+__device__ __forceinline__ void store_outputs(const EpiMat &e, const float (&v)[N], uint32_t n0, uint32_t step, uint32_t batch, uint64_t col, bool ok) {
+    if (!ok) return;
+    const uint64_t at = (uint64_t)n0 * e.out_stride + col, more = (uint64_t)step * e.out_stride;
+    if (e.out16) {
+        uint16_t *p = (uint16_t *)e.out + at;
 #pragma unroll
-        for (int j = 0; j < CW / 2; ++j) {
-            const float even = sum[2 * j] + bias, odd = sum[2 * j + 1] + bias;
-            const float got = __shfl_xor_sync(0xFFFFFFFFu, up ? even : odd, 8);
-            v[j] = up ? got : even;
-            w[j] = up ? odd : got;
-        }
-        activate<CW / 2>(v, e.act);
-        const uint64_t i = (row >> 4) * 8 + (row & 7);
-        n0 += up ? 1 : 0;
+        for (int i = 0; i < N; ++i, p += more)
+            if (n0 + step * i < batch) *p = round16<F16>(v[i]);
+    } else {
+        float *p = (float *)e.out + at;
 #pragma unroll
-        for (int j = 0; j < CW / 2; ++j)
-            if (row_ok && n0 + 2 * j < batch && i < e.gated_rows) store_value<F16>(e.out, (uint64_t)(n0 + 2 * j) * e.out_stride + i, is16, v[j] * w[j]);
-        return;
+        for (int i = 0; i < N; ++i, p += more)
+            if (n0 + step * i < batch) *p = v[i];
     }
-    float v[CW];
+}
+// From sums to outputs; called by the whole warp.  Gated, two vectors at a time: lanes with gate rows finish the even ones, lanes with up rows the
+// odd ones, one exchange for two outputs.
+template <bool F16, int N>
+__device__ __forceinline__ void finish_gated(const EpiMat &e, const float (&sum)[N], float bias, uint32_t n0, uint32_t step, uint32_t batch, uint64_t row,
+                                             bool ok, uint32_t lane) {
+    constexpr int M = N > 1 ? N / 2 : 1;
+    const bool up = lane & 8;
+    float v[M], w[M];
 #pragma unroll
-    for (int i = 0; i < CW; ++i) v[i] = sum[i] + bias;
-    activate<CW>(v, e.act);
-    constexpr int U = CW < 8 ? CW : 8;
-#pragma unroll
-    for (int i0 = 0; i0 < CW; i0 += U) {
-        if (e.residual) {
-            float r[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                r[u] = row_ok && n0 + i0 + u < batch ? load_value<F16>(e.residual, (uint64_t)(n0 + i0 + u) * e.residual_stride + row, is16) : 0.0f;
-#pragma unroll
-            for (int u = 0; u < U; ++u) v[i0 + u] += r[u];
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (row_ok && n0 + i0 + u < batch) store_value<F16>(e.out, (uint64_t)(n0 + i0 + u) * e.out_stride + row, is16, v[i0 + u]);
+    for (int j = 0; j < M; ++j) {
+        const float even = sum[N > 1 ? 2 * j : 0] + bias, odd = N > 1 ? sum[N > 1 ? 2 * j + 1 : 0] + bias : 0.0f;
+        const float got = __shfl_xor_sync(0xFFFFFFFFu, up ? even : odd, 8);
+        v[j] = up ? got : even;
+        w[j] = up ? odd : got;
     }
+    activate<M>(v, e.act);
+#pragma unroll
+    for (int j = 0; j < M; ++j) v[j] *= w[j];
+    const uint64_t col = (row >> 4) * 8 + (row & 7);
+    store_outputs<F16, M>(e, v, n0 + (up ? step : 0), 2 * step, batch, col, ok && col < e.gated_rows && (N > 1 || !up));
+}
+template <bool F16, int N>
+__device__ __forceinline__ void finish_plain(const EpiMat &e, const float (&sum)[N], float bias, const float (&residual)[N], uint32_t n0, uint32_t step,
+                                             uint32_t batch, uint64_t row, bool ok) {
+    float v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = sum[i] + bias;
+    activate<N>(v, e.act);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += residual[i];
+    store_outputs<F16, N>(e, v, n0, step, batch, row, ok);
 }
 
 }  // namespace huffllm

@@ -309,6 +309,13 @@ __global__ void __launch_bounds__(THREADS, 1) huff_kernel(const __grid_constant_
     auto flush = [&](uint32_t rg, uint32_t first_c, uint32_t last_c_excl) {
         const uint32_t g_lo = rg * KC, g_hi = g_lo + KC, my_lo = max(g_lo, cta_beg), my_hi = min(g_hi, cta_end);  // its chunks, and this CTA's part
         const bool alone = first_c <= my_lo && last_c_excl >= my_hi;   // no other warp of this CTA holds a piece
+        // what the epilogue adds is asked for now, whether or not this warp will be the one that closes the row group
+        const uint64_t e_row = (uint64_t)rg * 16 + (lane & 15);
+        float e_bias = 0.f, e_res[kOut];
+        if constexpr (EPI != 0) {
+            e_bias = load_bias<FMT != 0>(A.e[mi], e_row, e_row < k.rows);
+            load_residuals<FMT != 0, kOut>(A.e[mi], e_res, lane >> 4, 2, A.batch, e_row, e_row < k.rows);
+        }
         // D fragment -> output order (o = column * 16 + row) through this warp's shared-memory entry: the first one for the
         // row group that the warp's range starts in, the second for those behind it
         const uint32_t mine = warp * 2 + (c_beg >= g_lo ? 0u : 1u);
@@ -384,13 +391,9 @@ __global__ void __launch_bounds__(THREADS, 1) huff_kernel(const __grid_constant_
             }
         }
         if constexpr (EPI != 0) {
-            // through this warp's entry once more (whoever had to read its piece has): the epilogue takes a tile's outputs in an order of its own
-            float *const tile = part_val + mine * vals;
-#pragma unroll
-            for (int i = 0; i < kOut; ++i)
-                if (lane + 32 * i < vals) tile[lane + 32 * i] = v[i];
-            __syncwarp();
-            finish_tile<FMT != 0, NT == 0 ? 1 : 4>(A.e[mi], tile, A.batch, rg, k.rows, lane);
+            // (v[i]: row lane % 16 of the tile, vector lane / 16 + 2 i; with one vector the upper half of the warp has none)
+            if (A.e[mi].gated_rows) finish_gated<FMT != 0, kOut>(A.e[mi], v, e_bias, lane >> 4, 2, A.batch, e_row, e_row < k.rows, lane);
+            else finish_plain<FMT != 0, kOut>(A.e[mi], v, e_bias, e_res, lane >> 4, 2, A.batch, e_row, e_row < k.rows);
             return;
         }
         const uint64_t r = (uint64_t)rg * 16 + (lane & 15);

@@ -482,7 +482,18 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
         const bool row_ok = row < k.rows && acc_tile * 8 + 2 * q + (lane >> 4) < n_rg;   // (row groups behind the CTA's belong to the next item)
         auto write = [&](const float (&out)[CW]) {
             if constexpr (EPI != 0) {
-                finish_columns<FMT != 0, CW>(T.e[MULTI ? mi : 0], out, n0, A.batch, row, row_ok, lane);
+                const EpiMat &e = T.e[MULTI ? mi : 0];
+                const float bias = load_bias<FMT != 0>(e, row, row_ok);
+                constexpr int U = CW < 8 ? CW : 8;           // (vectors at a time: with 16 the registers of 32 columns did not suffice)
+#pragma unroll
+                for (int i0 = 0; i0 < CW; i0 += U) {
+                    float part[U], res[U];
+                    load_residuals<FMT != 0, U>(e, res, n0 + i0, 1, A.batch, row, row_ok);
+#pragma unroll
+                    for (int i = 0; i < U; ++i) part[i] = out[i0 + i];
+                    if (e.gated_rows) finish_gated<FMT != 0, U>(e, part, bias, n0 + i0, 1, A.batch, row, row_ok, lane);
+                    else finish_plain<FMT != 0, U>(e, part, bias, res, n0 + i0, 1, A.batch, row, row_ok);
+                }
                 return;
             }
 #pragma unroll
