@@ -135,6 +135,7 @@ __global__ void __launch_bounds__(THREADS, 1) huff_kernel(const __grid_constant_
     constexpr uint32_t kBarWarp = 48u, kNote = 32u;            // bytes per warp, and where its notes start
     __shared__ uint32_t s_arrive[kMaxWarps];   // arrival counters of row groups shared by several warps
     __shared__ uint32_t s_stop;                // a decoder gave up waiting: the feeder stops too
+    __shared__ __align__(16) uint32_t s_epi[EPI ? sizeof(EpiMat) / 4 : 4];     // the matrix's epilogue: read once a row group, too seldom to stay in the constant cache
     constexpr uint32_t kBadRecord = 0xFFFFFFFFu;
 
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nwarps_launched = blockDim.x >> 5;
@@ -275,6 +276,9 @@ __global__ void __launch_bounds__(THREADS, 1) huff_kernel(const __grid_constant_
             if (v < kLutVecs) lut_s[v] = make_uint4(e, e, e, e);
         }
         if (tid < kMaxWarps) s_arrive[tid] = 0;
+        if constexpr (EPI != 0) {
+            if (tid < sizeof(EpiMat) / 4) s_epi[tid] = ((const uint32_t *)&A.e[mi])[tid];
+        }
         if (LONG) {
             uint32_t *full_s = (uint32_t *)(dyn_smem + (full_base - smem_base));
             for (uint32_t i = tid; i < (FMT ? 3u : 1u) << A.lut_bits; i += kLutThreads) full_s[i] = lut_entry<D>(__ldg(lut_g + i), 0u, false);
@@ -313,8 +317,9 @@ __global__ void __launch_bounds__(THREADS, 1) huff_kernel(const __grid_constant_
         const uint64_t e_row = (uint64_t)rg * 16 + (lane & 15);
         float e_bias = 0.f, e_res[kOut];
         if constexpr (EPI != 0) {
-            e_bias = load_bias<FMT != 0>(A.e[mi], e_row, e_row < k.rows);
-            load_residuals<FMT != 0, kOut>(A.e[mi], e_res, lane >> 4, 2, A.batch, e_row, e_row < k.rows);
+            const EpiMat &e = *(const EpiMat *)s_epi;
+            e_bias = load_bias<FMT != 0>(e, e_row, e_row < k.rows);
+            if (kOut <= 4) load_residuals<FMT != 0, kOut>(e, e_res, lane >> 4, 2, A.batch, e_row, e_row < k.rows);
         }
         // D fragment -> output order (o = column * 16 + row) through this warp's shared-memory entry: the first one for the
         // row group that the warp's range starts in, the second for those behind it
@@ -392,8 +397,10 @@ __global__ void __launch_bounds__(THREADS, 1) huff_kernel(const __grid_constant_
         }
         if constexpr (EPI != 0) {
             // (v[i]: row lane % 16 of the tile, vector lane / 16 + 2 i; with one vector the upper half of the warp has none)
-            if (A.e[mi].gated_rows) finish_gated<FMT != 0, kOut>(A.e[mi], v, e_bias, lane >> 4, 2, A.batch, e_row, e_row < k.rows, lane);
-            else finish_plain<FMT != 0, kOut>(A.e[mi], v, e_bias, e_res, lane >> 4, 2, A.batch, e_row, e_row < k.rows);
+            const EpiMat &e = *(const EpiMat *)s_epi;
+            if (kOut > 4) load_residuals<FMT != 0, kOut>(e, e_res, lane >> 4, 2, A.batch, e_row, e_row < k.rows);
+            if (e.gated_rows) finish_gated<FMT != 0, kOut>(e, v, e_bias, lane >> 4, 2, A.batch, e_row, e_row < k.rows, lane);
+            else finish_plain<FMT != 0, kOut>(e, v, e_bias, e_res, lane >> 4, 2, A.batch, e_row, e_row < k.rows);
             return;
         }
         const uint64_t r = (uint64_t)rg * 16 + (lane & 15);

@@ -158,6 +158,7 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
     __shared__ __align__(8) uint64_t bars[kMaxWarps * 2];   // per warp: its two coded-copy barriers
     __shared__ __align__(8) uint64_t ring_bars[2 * kTcStages];   // stage may be refilled (arrived on by tcgen05.commit); every decoder warp's share is in place
     __shared__ uint32_t s_tmem_base, s_last;
+    __shared__ __align__(16) uint32_t s_epi[EPI ? sizeof(EpiMat) / 4 : 1];     // the matrix's epilogue
 
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     pdl_launch_dependents();   // the next kernel in the stream may be scheduled early; it waits for this one before it reads results
@@ -284,6 +285,9 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
             const uint32_t kc_b = cb % KC;
             issue_record(kc_b, 0, o0, o1);
             if (cb + 1 < ce) issue_record(kc_b + 1, 1, o1, o2);
+        }
+        if constexpr (EPI != 0) {
+            if (tid < sizeof(EpiMat) / 4) s_epi[tid] = ((const uint32_t *)&T.e[MULTI ? mi : 0])[tid];
         }
         uint4 *lut_s = (uint4 *)(dyn_smem + (plan.lut - smem_base));
 #pragma unroll
@@ -482,7 +486,7 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
         const bool row_ok = row < k.rows && acc_tile * 8 + 2 * q + (lane >> 4) < n_rg;   // (row groups behind the CTA's belong to the next item)
         auto write = [&](const float (&out)[CW]) {
             if constexpr (EPI != 0) {
-                const EpiMat &e = T.e[MULTI ? mi : 0];
+                const EpiMat &e = *(const EpiMat *)s_epi;
                 const float bias = load_bias<FMT != 0>(e, row, row_ok);
                 constexpr int U = CW < 8 ? CW : 8;           // (vectors at a time: with 16 the registers of 32 columns did not suffice)
 #pragma unroll
@@ -500,58 +504,66 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
             for (int i = 0; i < CW; ++i)
                 if (n0 + i < A.batch && row_ok) k.y[(uint64_t)(n0 + i) * k.rows + row] = out[i];
         };
-        if (ksplit == 1) {
+        auto add_ranges = [&]() -> bool {                    // this range's piece, and for the last one their sum; false: others will close the tile
+            // piece of (item, warp): [CW][32] floats, 32 piece slots per item
+            float *piece = tc_partial + ((size_t)item * 32 + warp) * CW * 32;
+#pragma unroll
+            for (int i = 0; i < CW; ++i) piece[i * 32 + lane] = v[i];
+            __syncwarp();
+            uint32_t last = 0;
+            if (SL == 1) {                                       // every warp finds its own pieces: a counter per row tile and warp
+                if (lane == 0) {
+                    unsigned int *ctr = tc_ticket + mt * 32 + warp;
+                    last = arrive_acq_rel(ctr) == ksplit - 1 ? 1u : 0u;
+                    if (last) *ctr = 0;
+                }
+                last = __shfl_sync(0xFFFFFFFFu, last, 0);
+            } else {                                             // small pieces: one counter per row tile (all 32 warps are here)
+                __syncthreads();
+                if (tid == 0) {
+                    unsigned int *ctr = tc_ticket + mt;
+                    s_last = arrive_acq_rel(ctr) == ksplit - 1 ? 1u : 0u;
+                    if (s_last) *ctr = 0;
+                }
+                __syncthreads();
+                last = s_last;
+            }
+            if (!last) return false;
+            // 32 independent loads in flight: every column of as many ranges as make 32; every output adds its pieces in range order
+            constexpr int U = CW >= 32 ? 1 : 32 / CW;
+            constexpr size_t kRange = (size_t)32 * CW * 32;
+            const float *pc = tc_partial + ((size_t)mt * ksplit * 32 + warp) * CW * 32 + lane;
+#pragma unroll
+            for (int i = 0; i < CW; ++i) v[i] = 0.f;
+            uint32_t r = 0;
+#pragma unroll 1
+            for (; r + U <= ksplit; r += U, pc += U * kRange) {
+                float p[U][CW];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int i = 0; i < CW; ++i) p[u][i] = __ldcg(pc + u * kRange + i * 32);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int i = 0; i < CW; ++i) v[i] += p[u][i];
+            }
+#pragma unroll 1
+            for (; r < ksplit; ++r, pc += kRange)
+#pragma unroll
+                for (int i = 0; i < CW; ++i) v[i] += __ldcg(pc + i * 32);
+            return true;
+        };
+        if constexpr (EPI != 0) {                            // (one copy of the epilogue)
+            if (ksplit == 1 || add_ranges()) write(v);
+        } else {
+            if (ksplit == 1) {
+                write(v);
+                return;
+            }
+            if (!add_ranges()) return;
             write(v);
-            return;
         }
-        // piece of (item, warp): [CW][32] floats, 32 piece slots per item
-        float *piece = tc_partial + ((size_t)item * 32 + warp) * CW * 32;
-#pragma unroll
-        for (int i = 0; i < CW; ++i) piece[i * 32 + lane] = v[i];
-        __syncwarp();
-        uint32_t last = 0;
-        if (SL == 1) {                                       // every warp finds its own pieces: a counter per row tile and warp
-            if (lane == 0) {
-                unsigned int *ctr = tc_ticket + mt * 32 + warp;
-                last = arrive_acq_rel(ctr) == ksplit - 1 ? 1u : 0u;
-                if (last) *ctr = 0;
-            }
-            last = __shfl_sync(0xFFFFFFFFu, last, 0);
-        } else {                                             // small pieces: one counter per row tile (all 32 warps are here)
-            __syncthreads();
-            if (tid == 0) {
-                unsigned int *ctr = tc_ticket + mt;
-                s_last = arrive_acq_rel(ctr) == ksplit - 1 ? 1u : 0u;
-                if (s_last) *ctr = 0;
-            }
-            __syncthreads();
-            last = s_last;
-        }
-        if (!last) return;
-        // 32 independent loads in flight: every column of as many ranges as make 32; every output adds its pieces in range order
-        constexpr int U = CW >= 32 ? 1 : 32 / CW;
-        constexpr size_t kRange = (size_t)32 * CW * 32;
-        const float *pc = tc_partial + ((size_t)mt * ksplit * 32 + warp) * CW * 32 + lane;
-#pragma unroll
-        for (int i = 0; i < CW; ++i) v[i] = 0.f;
-        uint32_t r = 0;
-#pragma unroll 1
-        for (; r + U <= ksplit; r += U, pc += U * kRange) {
-            float p[U][CW];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < CW; ++i) p[u][i] = __ldcg(pc + u * kRange + i * 32);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < CW; ++i) v[i] += p[u][i];
-        }
-#pragma unroll 1
-        for (; r < ksplit; ++r, pc += kRange)
-#pragma unroll
-            for (int i = 0; i < CW; ++i) v[i] += __ldcg(pc + i * 32);
-        write(v);
     };
 
 #pragma unroll 1
