@@ -6,7 +6,7 @@
 // fp32 in a fixed order: eight at a time, a thread's, a warp's, the CTA's.
 // `gain` does not come from the kernel in front and is asked for before the wait for it.
 #include <cuda_runtime.h>
-#include <cstdlib>
+#include <type_traits>
 
 #include "decode_common.cuh"
 #include "epilogue.cuh"
@@ -24,32 +24,45 @@ __global__ void __launch_bounds__(kNormMaxThreads) add_rms_norm_kernel(const __g
     __shared__ float s_sum[32];
     constexpr int N = ITEMS ? ITEMS : 1;
     const uint32_t tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5;
-    const uint64_t cols = A.cols, v = blockIdx.x;
+    const uint32_t cols = (uint32_t)A.cols;                    // (at most 2^31)
+    const uint64_t v = blockIdx.x;
     pdl_launch_dependents();
-    auto column = [&](uint64_t it, int j) -> uint64_t { return VEC ? (tid + it * nt) * 8 + j : tid + (it * 8 + j) * nt; };
-    auto load8 = [&](const void *p, uint64_t at, bool is16, uint64_t it, float (&o)[8]) {
+    auto column = [&](uint32_t it, int j) -> uint32_t { return VEC ? (tid + it * nt) * 8 + j : tid + (it * 8 + j) * nt; };
+    // Eight values as they lie in memory, and widened: all of a vector's loads are under way before the first value is looked at.
+    auto load8 = [&](const void *p, uint64_t at, auto is16, uint32_t it, uint32_t (&r)[8]) {
+        constexpr bool k16 = decltype(is16)::value;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r[j] = 0u;
         if (VEC) {
-            if (column(it, 0) >= cols) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = 0.0f;
-                return;
-            }
-            if (is16) {
-                const uint4 q = __ldcg((const uint4 *)((const uint16_t *)p + at + column(it, 0)));
-                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = widen16<F16>((uint16_t)(w[j >> 1] >> (16 * (j & 1))));
-            } else {
-                const float4 *q = (const float4 *)((const float *)p + at + column(it, 0));
-                const float4 a = __ldcg(q), b = __ldcg(q + 1);
-                o[0] = a.x, o[1] = a.y, o[2] = a.z, o[3] = a.w, o[4] = b.x, o[5] = b.y, o[6] = b.z, o[7] = b.w;
+            const bool in = column(it, 0) < cols;
+            const uint4 zero = make_uint4(0, 0, 0, 0), *q = (const uint4 *)((const uint8_t *)p + at * (k16 ? 2 : 4) + (uint64_t)column(it, 0) * (k16 ? 2 : 4));
+            const uint4 a = in ? __ldcg(q) : zero;
+            r[0] = a.x, r[1] = a.y, r[2] = a.z, r[3] = a.w;
+            if (!k16) {
+                const uint4 b = in ? __ldcg(q + 1) : zero;
+                r[4] = b.x, r[5] = b.y, r[6] = b.z, r[7] = b.w;
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = column(it, j) < cols ? load_value<F16>(p, at + column(it, j), is16) : 0.0f;
+            for (int j = 0; j < 8; ++j) {
+                const bool in = column(it, j) < cols;
+                if (k16) r[j] = in ? __ldcg((const unsigned short *)p + at + column(it, j)) : 0u;
+                else r[j] = in ? __ldcg((const unsigned int *)p + at + column(it, j)) : 0u;
+            }
         }
     };
-    auto store8 = [&](void *p, uint64_t at, bool is16, uint64_t it, const float (&o)[8]) {
+    auto widen8 = [](auto is16, const uint32_t (&r)[8], float (&o)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (!decltype(is16)::value) o[j] = __uint_as_float(r[j]);
+            else if (VEC) o[j] = widen16<F16>((uint16_t)(r[j >> 1] >> (16 * (j & 1))));
+            else o[j] = widen16<F16>((uint16_t)r[j]);
+        }
+    };
+    using Is16 = std::true_type;
+    using XType = std::bool_constant<X16>;
+    using DType = std::bool_constant<DT == 2>;
+    auto store8 = [&](void *p, uint64_t at, bool is16, uint32_t it, const float (&o)[8]) {
         if (VEC) {
             if (column(it, 0) >= cols) return;
             if (is16) {
@@ -68,21 +81,28 @@ __global__ void __launch_bounds__(kNormMaxThreads) add_rms_norm_kernel(const __g
                 if (column(it, j) < cols) store_value<F16>(p, at + column(it, j), is16, o[j]);
         }
     };
-    auto load_gain = [&](uint64_t it, float (&o)[8]) {
-        if (!A.gain) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = 1.0f;
-        } else {
-            load8(A.gain, 0, true, it, o);
-        }
+    auto load_gain = [&](uint32_t it, uint32_t (&r)[8]) {
+        if (A.gain) load8(A.gain, 0, Is16{}, it, r);
     };
-    auto load_h = [&](uint64_t it, float (&h)[8]) {
-        load8(A.x, v * A.x_stride, X16, it, h);
-        if (DT) {
-            float d[8];
-            load8(A.delta, v * A.delta_stride, DT == 2, it, d);
+    auto widen_gain = [&](const uint32_t (&r)[8], float (&o)[8]) {
+        if (A.gain) {
+            widen8(Is16{}, r, o);
+            return;
+        }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) h[j] += d[j];
+        for (int j = 0; j < 8; ++j) o[j] = 1.0f;
+    };
+    auto load_h = [&](uint32_t it, uint32_t (&x)[8], uint32_t (&d)[8]) {
+        load8(A.x, v * A.x_stride, XType{}, it, x);
+        if (DT) load8(A.delta, v * A.delta_stride, DType{}, it, d);
+    };
+    auto widen_h = [&](const uint32_t (&x)[8], const uint32_t (&d)[8], float (&h)[8]) {
+        widen8(XType{}, x, h);
+        if (DT) {
+            float f[8];
+            widen8(DType{}, d, f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) h[j] += f[j];
         }
     };
     auto squares = [](const float (&h)[8]) -> float {
@@ -92,22 +112,27 @@ __global__ void __launch_bounds__(kNormMaxThreads) add_rms_norm_kernel(const __g
         return s;
     };
 
-    float h[N][8], gain[1][8], total = 0.0f;
-    if (ITEMS == 1) load_gain(0, gain[0]);
+    float h[N][8], gain[8], total = 0.0f;
+    uint32_t g_raw[8], x_raw[N][8], d_raw[N][8];
+    if (ITEMS == 1) load_gain(0, g_raw);
     pdl_wait_prior_grid();
-    const uint64_t groups = (cols + 8 * nt - 1) / (8 * nt);       // of a thread
+    const uint32_t groups = (cols + 8 * nt - 1) / (8 * nt);       // of a thread
     if (ITEMS) {
 #pragma unroll
-        for (int it = 0; it < ITEMS; ++it) load_h(it, h[it]);
+        for (int it = 0; it < ITEMS; ++it) load_h(it, x_raw[it], d_raw[it]);
 #pragma unroll
-        for (int it = 0; it < ITEMS; ++it) total += squares(h[it]);
+        for (int it = 0; it < ITEMS; ++it) {
+            widen_h(x_raw[it], d_raw[it], h[it]);
+            total += squares(h[it]);
+        }
         if (A.sum) {
 #pragma unroll
             for (int it = 0; it < ITEMS; ++it) store8(A.sum, v * A.sum_stride, X16, it, h[it]);
         }
     } else {
-        for (uint64_t it = 0; it < groups; ++it) {
-            load_h(it, h[0]);
+        for (uint32_t it = 0; it < groups; ++it) {
+            load_h(it, x_raw[0], d_raw[0]);
+            widen_h(x_raw[0], d_raw[0], h[0]);
             total += squares(h[0]);
         }
     }
@@ -119,22 +144,25 @@ __global__ void __launch_bounds__(kNormMaxThreads) add_rms_norm_kernel(const __g
 #pragma unroll
     for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
     const float scale = rsqrtf(total / (float)cols + A.eps);
+    auto finish = [&](uint32_t it, float (&y)[8]) {
+        widen_gain(g_raw, gain);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = y[j] * scale * gain[j];
+        store8(A.out, v * A.out_stride, true, it, y);
+    };
     if (ITEMS) {
 #pragma unroll
         for (int it = 0; it < ITEMS; ++it) {
-            if (ITEMS > 1) load_gain(it, gain[0]);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) h[it][j] = h[it][j] * scale * gain[0][j];
-            store8(A.out, v * A.out_stride, true, it, h[it]);
+            if (ITEMS > 1) load_gain(it, g_raw);
+            finish(it, h[it]);
         }
     } else {
-        for (uint64_t it = 0; it < groups; ++it) {
-            load_h(it, h[0]);
+        for (uint32_t it = 0; it < groups; ++it) {
+            load_h(it, x_raw[0], d_raw[0]);
+            load_gain(it, g_raw);
+            widen_h(x_raw[0], d_raw[0], h[0]);
             if (A.sum) store8(A.sum, v * A.sum_stride, X16, it, h[0]);
-            load_gain(it, gain[0]);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) h[0][j] = h[0][j] * scale * gain[0][j];
-            store8(A.out, v * A.out_stride, true, it, h[0]);
+            finish(it, h[0]);
         }
     }
 }
@@ -160,11 +188,13 @@ static cudaError_t launch_norm_items(const NormArgs &a, uint32_t vectors, cudaSt
         const uint64_t t = ((groups + items - 1) / items + 31) / 32 * 32;
         return (uint32_t)(t < (uint64_t)kNormMaxThreads ? t : (uint64_t)kNormMaxThreads);
     };
-    int n = getenv("NITEMS") ? atoi(getenv("NITEMS")) : 0;
-    if (n == 2) return launch_norm_one<F16, X16, DT, 2, VEC>(a, vectors, threads(2), stream);
-    if (n == 4) return launch_norm_one<F16, X16, DT, 4, VEC>(a, vectors, threads(4), stream);
-    if (groups <= (uint64_t)kNormMaxThreads) return launch_norm_one<F16, X16, DT, 1, VEC>(a, vectors, threads(1), stream);
-    if (groups <= 2ull * kNormMaxThreads) return launch_norm_one<F16, X16, DT, 2, VEC>(a, vectors, threads(2), stream);
+    // One group of eight a thread where that makes a CTA of at most 1024 threads; where there are vectors for many rounds of CTAs anyway, two or
+    // four from 513 threads on, so that an SM's CTAs are more and wait for their sums at different times.  (us with one / two / four groups:
+    // 296 x 8192 in 16 bits 5.3 / 6.0 / 6.3, 2048 x 8192 25.4 / 23.8 / 25.5; 2048 x 4096 in fp32 19.5 / 21.1 / 23.7; 4096 x 16384 - / 105 / 88.)
+    const bool many = vectors >= 8 * 148;
+    if (groups <= 512 || (groups <= 1024 && !many)) return launch_norm_one<F16, X16, DT, 1, VEC>(a, vectors, threads(1), stream);
+    if (groups <= 1024 || (groups <= 2048 && !many)) return launch_norm_one<F16, X16, DT, 2, VEC>(a, vectors, threads(2), stream);
+    if (groups <= 4096) return launch_norm_one<F16, X16, DT, 4, VEC>(a, vectors, threads(4), stream);
     return launch_norm_one<F16, X16, DT, 0, VEC>(a, vectors, kNormMaxThreads, stream);
 }
 
