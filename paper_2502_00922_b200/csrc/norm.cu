@@ -14,12 +14,16 @@
 namespace huffllm {
 
 constexpr int kNormMaxThreads = 1024;
+enum NormForm { kAligned, kPhased, kLoose };
 
-// ITEMS groups of 8 values per thread, 0: as many as the vector has, in two passes.  VEC: everything is 16-byte aligned and a group is
-// eight columns that follow each other; otherwise a group's values are blockDim.x columns apart.
+// ITEMS groups of 8 values per thread, 0: as many as the vector has, in two passes.
+// FORM says which columns a group is.  kAligned: eight that follow each other, every vector and group on 16-byte boundaries.  kPhased: eight that
+// follow each other in memory from a multiple of eight values on; the vectors start anywhere, but all of them at the same place within
+// eight values (packed vectors of an odd length do), `phase` values behind the first group's start, so that all but the outermost groups
+// move in 16-byte pieces.  kLoose: eight that are blockDim.x columns apart, value by value.  (2048 x 5001 in 16 bits: phased 24 us, loose 41.)
 // X16, DT: x in 16 bits; delta 0: none, 1: fp32, 2: 16 bits.  (Types that are asked about at run time make every load wait for the one
 // before: 2048 x 8192 in 16 bits 45 us.)
-template <bool F16, bool X16, int DT, int ITEMS, bool VEC>
+template <bool F16, bool X16, int DT, int ITEMS, int FORM>
 __global__ void __launch_bounds__(kNormMaxThreads) add_rms_norm_kernel(const __grid_constant__ NormArgs A) {
     __shared__ float s_sum[32];
     constexpr int N = ITEMS ? ITEMS : 1;
@@ -27,27 +31,34 @@ __global__ void __launch_bounds__(kNormMaxThreads) add_rms_norm_kernel(const __g
     const uint32_t cols = (uint32_t)A.cols;                    // (at most 2^31)
     const uint64_t v = blockIdx.x;
     pdl_launch_dependents();
-    auto column = [&](uint32_t it, int j) -> uint32_t { return VEC ? (tid + it * nt) * 8 + j : tid + (it * 8 + j) * nt; };
+    const uint32_t phase = FORM == kPhased ? (uint32_t)(v * A.x_stride) & 7u : 0u;
+    // (in front of the first column: wraps to more than `cols`)
+    auto column = [&](uint32_t it, int j) -> uint32_t { return FORM == kLoose ? tid + (it * 8 + j) * nt : (tid + it * nt) * 8 + j - phase; };
+    auto whole = [&](uint32_t it) -> bool { return column(it, 0) < cols && (FORM == kAligned || column(it, 7) < cols); };
     // Eight values as they lie in memory, and widened: all of a vector's loads are under way before the first value is looked at.
     auto load8 = [&](const void *p, uint64_t at, auto is16, uint32_t it, uint32_t (&r)[8]) {
         constexpr bool k16 = decltype(is16)::value;
 #pragma unroll
         for (int j = 0; j < 8; ++j) r[j] = 0u;
-        if (VEC) {
-            const bool in = column(it, 0) < cols;
-            const uint4 zero = make_uint4(0, 0, 0, 0), *q = (const uint4 *)((const uint8_t *)p + at * (k16 ? 2 : 4) + (uint64_t)column(it, 0) * (k16 ? 2 : 4));
+        bool rest = FORM == kLoose;
+        if (FORM != kLoose) {
+            const bool in = whole(it);
+            const uint4 zero = make_uint4(0, 0, 0, 0), *q = (const uint4 *)((const uint8_t *)p + ((int64_t)at + (int32_t)column(it, 0)) * (k16 ? 2 : 4));
             const uint4 a = in ? __ldcg(q) : zero;
             r[0] = a.x, r[1] = a.y, r[2] = a.z, r[3] = a.w;
             if (!k16) {
                 const uint4 b = in ? __ldcg(q + 1) : zero;
                 r[4] = b.x, r[5] = b.y, r[6] = b.z, r[7] = b.w;
             }
-        } else {
+            rest = FORM == kPhased && !in;
+        }
+        if (rest) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const bool in = column(it, j) < cols;
-                if (k16) r[j] = in ? __ldcg((const unsigned short *)p + at + column(it, j)) : 0u;
-                else r[j] = in ? __ldcg((const unsigned int *)p + at + column(it, j)) : 0u;
+                if (!k16) r[j] = in ? __ldcg((const unsigned int *)p + at + column(it, j)) : 0u;
+                else if (FORM == kLoose) r[j] = in ? __ldcg((const unsigned short *)p + at + column(it, j)) : 0u;
+                else if (in) r[j >> 1] |= (uint32_t)__ldcg((const unsigned short *)p + at + column(it, j)) << (16 * (j & 1));
             }
         }
     };
@@ -55,7 +66,7 @@ __global__ void __launch_bounds__(kNormMaxThreads) add_rms_norm_kernel(const __g
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             if (!decltype(is16)::value) o[j] = __uint_as_float(r[j]);
-            else if (VEC) o[j] = widen16<F16>((uint16_t)(r[j >> 1] >> (16 * (j & 1))));
+            else if (FORM != kLoose) o[j] = widen16<F16>((uint16_t)(r[j >> 1] >> (16 * (j & 1))));
             else o[j] = widen16<F16>((uint16_t)r[j]);
         }
     };
@@ -63,26 +74,36 @@ __global__ void __launch_bounds__(kNormMaxThreads) add_rms_norm_kernel(const __g
     using XType = std::bool_constant<X16>;
     using DType = std::bool_constant<DT == 2>;
     auto store8 = [&](void *p, uint64_t at, bool is16, uint32_t it, const float (&o)[8]) {
-        if (VEC) {
-            if (column(it, 0) >= cols) return;
+        if (FORM != kLoose && whole(it)) {
+            uint8_t *const q = (uint8_t *)p + ((int64_t)at + (int32_t)column(it, 0)) * (is16 ? 2 : 4);
             if (is16) {
                 uint32_t w[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) w[j] = round16<F16>(o[2 * j]) | (uint32_t)round16<F16>(o[2 * j + 1]) << 16;
-                *(uint4 *)((uint16_t *)p + at + column(it, 0)) = make_uint4(w[0], w[1], w[2], w[3]);
+                *(uint4 *)q = make_uint4(w[0], w[1], w[2], w[3]);
             } else {
-                float4 *q = (float4 *)((float *)p + at + column(it, 0));
-                q[0] = make_float4(o[0], o[1], o[2], o[3]);
-                q[1] = make_float4(o[4], o[5], o[6], o[7]);
+                ((float4 *)q)[0] = make_float4(o[0], o[1], o[2], o[3]);
+                ((float4 *)q)[1] = make_float4(o[4], o[5], o[6], o[7]);
             }
-        } else {
+        } else if (FORM != kAligned) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (column(it, j) < cols) store_value<F16>(p, at + column(it, j), is16, o[j]);
         }
     };
+    // (the same for every vector, so from L1 where it cannot come in one piece)
     auto load_gain = [&](uint32_t it, uint32_t (&r)[8]) {
-        if (A.gain) load8(A.gain, 0, Is16{}, it, r);
+        if (!A.gain) return;
+        if (FORM == kAligned || (FORM == kPhased && phase == 0 && whole(it))) {
+            load8(A.gain, 0, Is16{}, it, r);
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r[j] = column(it, j) < cols ? __ldg(A.gain + column(it, j)) : 0u;
+        if (FORM == kPhased) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r[j] = r[2 * j] | r[2 * j + 1] << 16;
+        }
     };
     auto widen_gain = [&](const uint32_t (&r)[8], float (&o)[8]) {
         if (A.gain) {
@@ -116,7 +137,7 @@ __global__ void __launch_bounds__(kNormMaxThreads) add_rms_norm_kernel(const __g
     uint32_t g_raw[8], x_raw[N][8], d_raw[N][8];
     if (ITEMS == 1) load_gain(0, g_raw);
     pdl_wait_prior_grid();
-    const uint32_t groups = (cols + 8 * nt - 1) / (8 * nt);       // of a thread
+    const uint32_t groups = (cols + phase + 8 * nt - 1) / (8 * nt);       // of a thread
     if (ITEMS) {
 #pragma unroll
         for (int it = 0; it < ITEMS; ++it) load_h(it, x_raw[it], d_raw[it]);
@@ -130,6 +151,7 @@ __global__ void __launch_bounds__(kNormMaxThreads) add_rms_norm_kernel(const __g
             for (int it = 0; it < ITEMS; ++it) store8(A.sum, v * A.sum_stride, X16, it, h[it]);
         }
     } else {
+#pragma unroll 2
         for (uint32_t it = 0; it < groups; ++it) {
             load_h(it, x_raw[0], d_raw[0]);
             widen_h(x_raw[0], d_raw[0], h[0]);
@@ -167,7 +189,7 @@ __global__ void __launch_bounds__(kNormMaxThreads) add_rms_norm_kernel(const __g
     }
 }
 
-template <bool F16, bool X16, int DT, int ITEMS, bool VEC>
+template <bool F16, bool X16, int DT, int ITEMS, int FORM>
 static cudaError_t launch_norm_one(const NormArgs &a, uint32_t grid, uint32_t threads, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
@@ -178,12 +200,12 @@ static cudaError_t launch_norm_one(const NormArgs &a, uint32_t grid, uint32_t th
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, add_rms_norm_kernel<F16, X16, DT, ITEMS, VEC>, a);
+    return cudaLaunchKernelEx(&cfg, add_rms_norm_kernel<F16, X16, DT, ITEMS, FORM>, a);
 }
 
-template <bool F16, bool X16, int DT, bool VEC>
+template <bool F16, bool X16, int DT, int FORM>
 static cudaError_t launch_norm_items(const NormArgs &a, uint32_t vectors, cudaStream_t stream) {
-    const uint64_t groups = (a.cols + 7) / 8;
+    const uint64_t groups = (a.cols + (FORM == kPhased ? 7 : 0) + 7) / 8;
     auto threads = [&](uint64_t items) -> uint32_t {
         const uint64_t t = ((groups + items - 1) / items + 31) / 32 * 32;
         return (uint32_t)(t < (uint64_t)kNormMaxThreads ? t : (uint64_t)kNormMaxThreads);
@@ -192,18 +214,27 @@ static cudaError_t launch_norm_items(const NormArgs &a, uint32_t vectors, cudaSt
     // four from 513 threads on, so that an SM's CTAs are more and wait for their sums at different times.  (us with one / two / four groups:
     // 296 x 8192 in 16 bits 5.3 / 6.0 / 6.3, 2048 x 8192 25.4 / 23.8 / 25.5; 2048 x 4096 in fp32 19.5 / 21.1 / 23.7; 4096 x 16384 - / 105 / 88.)
     const bool many = vectors >= 8 * 148;
-    if (groups <= 512 || (groups <= 1024 && !many)) return launch_norm_one<F16, X16, DT, 1, VEC>(a, vectors, threads(1), stream);
-    if (groups <= 1024 || (groups <= 2048 && !many)) return launch_norm_one<F16, X16, DT, 2, VEC>(a, vectors, threads(2), stream);
-    if (groups <= 4096) return launch_norm_one<F16, X16, DT, 4, VEC>(a, vectors, threads(4), stream);
-    return launch_norm_one<F16, X16, DT, 0, VEC>(a, vectors, kNormMaxThreads, stream);
+    if (groups <= 512 || (groups <= 1024 && !many)) return launch_norm_one<F16, X16, DT, 1, FORM>(a, vectors, threads(1), stream);
+    if (groups <= 1024 || (groups <= 2048 && !many)) return launch_norm_one<F16, X16, DT, 2, FORM>(a, vectors, threads(2), stream);
+    if (groups <= 4096) return launch_norm_one<F16, X16, DT, 4, FORM>(a, vectors, threads(4), stream);
+    return launch_norm_one<F16, X16, DT, 0, FORM>(a, vectors, kNormMaxThreads, stream);
 }
 
 template <bool F16, bool X16, int DT>
 static cudaError_t launch_norm_form(const NormArgs &a, uint32_t vectors, cudaStream_t stream) {
-    auto vec = [](const void *p, uint64_t stride, bool is16) { return !((uintptr_t)p & 15) && stride % (is16 ? 8 : 4) == 0; };
-    const bool aligned = a.cols % 8 == 0 && vec(a.x, a.x_stride, X16) && (!DT || vec(a.delta, a.delta_stride, DT == 2)) &&
-                         (!a.sum || vec(a.sum, a.sum_stride, X16)) && vec(a.gain, 0, true) && vec(a.out, a.out_stride, true);
-    return aligned ? launch_norm_items<F16, X16, DT, true>(a, vectors, stream) : launch_norm_items<F16, X16, DT, false>(a, vectors, stream);
+    const uint64_t strides[4] = {a.x_stride, DT ? a.delta_stride : a.x_stride, a.sum ? a.sum_stride : a.x_stride, a.out_stride};
+    const bool is16[4] = {X16, DT ? DT == 2 : X16, X16, true};
+    bool own = true, same = true;
+    for (int i = 0; i < 4; ++i) {
+        own = own && strides[i] % (is16[i] ? 8 : 4) == 0;
+        same = same && strides[i] % 8 == strides[0] % 8;
+    }
+    const bool based = !(((uintptr_t)a.x | (DT ? (uintptr_t)a.delta : 0) | (uintptr_t)a.sum | (uintptr_t)a.gain | (uintptr_t)a.out) & 15);
+    if (based && own && a.cols % 8 == 0) return launch_norm_items<F16, X16, DT, kAligned>(a, vectors, stream);
+    // (phased / loose, us, x in fp32 and delta in 16 bits: 64 x 1001 2.8 / 2.6, 64 x 5001 4.7 / 3.6, 148 x 5001 4.5 / 6.2, 600 x 1001 4.8 / 4.5, 1500 x 1001
+    // 7.0 / 8.2, 1500 x 251 5.3 / 3.8, 1500 x 5001 22 / 33; 1 x 11001 4.4 / 6.8)
+    if (based && same && (a.cols > 8192 || vectors * a.cols >= 640000)) return launch_norm_items<F16, X16, DT, kPhased>(a, vectors, stream);
+    return launch_norm_items<F16, X16, DT, kLoose>(a, vectors, stream);
 }
 
 template <bool F16>
