@@ -730,8 +730,24 @@ static huffllm_status product_multi(uint32_t n, const huffllm_desc *const *descs
     }
     DeviceInfo dev;
     if ((st = device_info(&dev)) != HUFFLLM_OK) return st;
-    if (batch > kTwoTileBatch) {
-        // 17..64 vectors: the tensor-core kernel, its CTAs dealt to the matrices like the other kernels'
+    // 9..16 vectors with epilogues: tensor cores too, but for long records of blobs that the register path takes.  (4096 + 1024 + 1024 rows x 4096 at 9 and
+    // at 16 vectors, register path / tensor cores, us: chunks of 1024 28.4 / 22.3, 28.1 / 22.4, of 4096 23.7 / 18.4, 24.9 / 18.6, of 8192 19.5 / 22.1,
+    // 20.9 / 22.3; 2 x 14336 rows 56.4 / 57.9, 60.6 / 58.2.)
+    bool tensor_cores = batch > kTwoTileBatch, two_tiles = false;     // (two_tiles: the register path can take over)
+    if (eps && batch > kKernelBatch && !tensor_cores) {
+        bool shorter = true;
+        two_tiles = true;
+        tensor_cores = true;
+        for (uint32_t i = 0; i < n; ++i) {
+            tensor_cores = tensor_cores && tc_blob(descs[i]);
+            two_tiles = two_tiles && two_tile_blob(descs[i]);
+            shorter = shorter && descs[i]->chunk_cols <= 256;
+        }
+        tensor_cores = tensor_cores && (shorter || !two_tiles);
+    }
+    bool done = false;
+    auto on_tensor_cores = [&]() -> huffllm_status {
+        // the tensor-core kernel, its CTAs dealt to the matrices like the other kernels'
         TcArgs t;
         memset(&t, 0, sizeof(t));
         KernelArgs &k = t.k;
@@ -754,12 +770,12 @@ static huffllm_status product_multi(uint32_t n, const huffllm_desc *const *descs
         TcShape sh;
         TcPlan plans[kMaxMats];
         if (!tc_choose(descs, n, npad, cta, &flat, k.dyn_smem_bytes, workspace_bytes_each, &sh, plans))
-            return fail(HUFFLLM_ERR_UNSUPPORTED, "chunk records too large for the tensor-core kernel's slots");
+            return two_tiles ? HUFFLLM_OK : fail(HUFFLLM_ERR_UNSUPPORTED, "chunk records too large for the tensor-core kernel's slots");
         set_tc_shape(&k, npad, sh, flat);
         uint32_t first = 0;
         for (uint32_t i = 0; i < n; ++i) {
             const TcPlan &tp = plans[i];
-            if (workspace_bytes_each < tp.bytes) return fail(HUFFLLM_ERR_BUFFER_TOO_SMALL, "workspace of matrix %u too small for batch %u", i, batch);
+            if (workspace_bytes_each < tp.bytes) return two_tiles ? HUFFLLM_OK : fail(HUFFLLM_ERR_BUFFER_TOO_SMALL, "workspace of matrix %u too small for batch %u", i, batch);
             t.m_tiles[i] = tp.m_tiles;
             t.ksplit[i] = tp.ksplit;
             t.ticket[i] = (unsigned int *)((uint8_t *)workspaces[i] + tp.ticket_off);
@@ -771,8 +787,10 @@ static huffllm_status product_multi(uint32_t n, const huffllm_desc *const *descs
         k.err = err_flag;
         cudaError_t e = launch_product_tc(t, eps ? epi : nullptr, first, (cudaStream_t)stream);
         if (e != cudaSuccess) return fail(HUFFLLM_ERR_CUDA, "tensor-core product launch: %s", cudaGetErrorString(e));
+        done = true;
         return HUFFLLM_OK;
-    }
+    };
+    if (tensor_cores && ((st = on_tensor_cores()) != HUFFLLM_OK || done)) return st;
     KernelArgs k;
     uint32_t grid;
     begin_args(&k, batch, dev);
@@ -896,7 +914,11 @@ static huffllm_status product_one(const huffllm_desc *desc, const void *blob, co
         // cross-CTA sums of 16-vector pieces expensive), unless they have so few rows that it gets few row tiles; measured
         // at 12 and 16 vectors on seven shapes from 1024 x 8192 to 28672 x 8192, before that kernel had column slices (the line has
         // not been drawn again).  Above 16 vectors it is the only one.
-        const bool wide = desc->cols >= desc->rows && desc->rows >= 2048;
+        // A product with an epilogue always tries the tensor-core kernel first: its slices and ranges, measured again, make it the faster one at
+        // every shape (register path / tensor cores at 9 and at 16 vectors, us: 1024 x 4096 11.7 / 10.3, 12.3 / 9.3; 1024 x 14336 21.0 / 13.0, 23.0 /
+        // 13.1; 11008 x 4096 28.7 / 25.2, 31.0 / 25.5; 57344 x 8192 185 / 186, 214 / 203; 2720 x 1024 8.6 / 8.8, 8.8 / 8.5).  (The sums of the plain
+        // calls stay what they were.)
+        const bool wide = ep || (desc->cols >= desc->rows && desc->rows >= 2048);
         if (!wide && (st = two_tiles()) != HUFFLLM_OK) return st;
         if (!done && (st = tensor_core(wide && batch <= kTwoTileBatch && two_tile_blob(desc))) != HUFFLLM_OK) return st;
         if (!done && wide && (st = two_tiles()) != HUFFLLM_OK) return st;
