@@ -49,7 +49,8 @@ huffllm_status device_info(DeviceInfo *out) {
 }
 
 // Scratch layout of one matrix's workspace:
-//   [0, 4096)            arrival counters of the register-path kernel (one per CTA)
+//   [0, 4096)            arrival counters of the register-path kernel (one per CTA: 2048 bytes), and behind them two counters of the
+//                        tensor-core kernel with epilogues (work items fetched, CTAs done)
 //   [4096, partial_off)  arrival counters of the tensor-core kernel, sized for its smallest tile
 //   [partial_off, ...)   partial sums: of the register path's CTAs, or of the tensor-core path's work items
 // Everything in front of partial_off is zero between calls; what lies behind it is overwritten freely by either path.
@@ -563,6 +564,7 @@ cudaError_t launch_product_tc(const TcArgs &t, const EpiMat *epi, uint32_t grid,
     EpiTcArgs a;
     static_cast<TcArgs &>(a) = t;
     memcpy(a.e, epi, t.k.n_mats * sizeof(EpiMat));
+    for (uint32_t i = 0; i < kMaxMats; ++i) a.fetched[i] = i < t.k.n_mats ? t.ticket[i] - (4096 - kMaxGrid * 4) / 4 : nullptr;
     return launch_gemm_tc(a, grid, stream);
 }
 

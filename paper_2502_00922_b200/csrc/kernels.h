@@ -87,6 +87,7 @@ struct TcArgs {
 
 struct EpiTcArgs : TcArgs {
     EpiMat e[kMaxMats];
+    unsigned int *fetched[kMaxMats];   // two counters, zero between calls: work items fetched beyond the first of every CTA, CTAs that are done
 };
 template <int EPI>
 using TcProductArgs = std::conditional_t<EPI != 0, EpiTcArgs, TcArgs>;

@@ -159,6 +159,8 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
     __shared__ __align__(8) uint64_t ring_bars[2 * kTcStages];   // stage may be refilled (arrived on by tcgen05.commit); every decoder warp's share is in place
     __shared__ uint32_t s_tmem_base, s_last;
     __shared__ __align__(16) uint32_t s_epi[EPI ? sizeof(EpiMat) / 4 : 1];     // the matrix's epilogue
+    __shared__ __align__(8) uint64_t s_next_bar;               // (EPI) the item behind the one at hand has been fetched, to
+    __shared__ uint32_t s_next[2];                             // these two places by turns
 
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     pdl_launch_dependents();   // the next kernel in the stream may be scheduled early; it waits for this one before it reads results
@@ -274,6 +276,12 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
         if (tid < S) {
             mbar_init(empty_bar(tid), 1);
             mbar_init(full_bar(tid), tiles == 4u ? 31u : tiles * 8u + 1u);      // (every warp but the issuer, decoding or not)
+        }
+        if constexpr (EPI != 0) {
+            if (tid == 0) {
+                mbar_init(smem_u32(&s_next_bar), 1);
+                s_next[0] = s_next[1] = ~0u;
+            }
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         if (warp == issuer) {
@@ -566,8 +574,13 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
         }
     };
 
+    // With epilogues, and more items than CTAs: a CTA's first item is its number, the others come from a counter in the workspace, when it starts on
+    // the last chunk of the one before.  A CTA that closes a row tile (sums of all ranges, epilogue) is late for its next item, whose tile it is then
+    // the last to arrive at: dealt out in turn, the same CTAs paid in every round.
+    const bool fetches = EPI != 0 && n_items > n_cta;
+    uint32_t turn = 0;
 #pragma unroll 1
-    for (uint32_t item = J; item < n_items; item += n_cta) {
+    for (uint32_t item = J, next = 0; item < n_items; item = EPI != 0 ? next : item + n_cta) {
         const uint32_t mt = item / ksplit;
         uint32_t k0, k1;
         item_range(item, k0, k1);
@@ -615,6 +628,13 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
                 for (uint32_t sl = 0; sl < 4; ++sl) {
                     nkb[sl] = sl < slices ? step_blocks(sl, j) : 0u;
                     if (sl < slices) least = min(least, nkb[sl]);
+                }
+                if constexpr (EPI != 0) {
+                    if (fetches && j + 1 == steps && lane == 0) {
+                        *(volatile uint32_t *)&s_next[turn & 1u] = n_cta + atomicAdd(T.fetched[MULTI ? mi : 0], 1u);
+                        mbar_arrive(smem_u32(&s_next_bar));
+                    }
+                    __syncwarp();
                 }
                 for (uint32_t p = 0; p < n_st; ++p) {
                     if (issuer_carries) {
@@ -724,9 +744,18 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
 
         // both slots are free again: the next item's first records are asked for now, so that they arrive behind the epilogue
         primed = false;
-        if (decodes && item + n_cta < n_items) {
+        if constexpr (EPI != 0) {
+            next = n_items;
+            if (fetches) {
+                bounded_wait(smem_u32(&s_next_bar), turn & 1u);
+                next = *(volatile uint32_t *)&s_next[turn & 1u];
+                ++turn;
+            }
+        }
+        const uint32_t behind = EPI != 0 ? next : item + n_cta;
+        if (decodes && behind < n_items) {
             uint32_t nb, ne;
-            if (item_chunks(item + n_cta, nb, ne)) {
+            if (item_chunks(behind, nb, ne)) {
                 if (lane == 0) {
                     issue(nb, 0);
                     if (nb + 1 < ne) issue(nb + 1, 1);
@@ -750,6 +779,12 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
     // ---- teardown
     tc_fence_before();
     __syncthreads();
+    if constexpr (EPI != 0) {
+        if (fetches && tid == 0) {                           // (nobody fetches behind its own arrival here: the last one leaves both counters as they were found)
+            unsigned int *const f = T.fetched[MULTI ? mi : 0];
+            if (arrive_acq_rel(f + 1) == n_cta - 1) f[0] = f[1] = 0;
+        }
+    }
     if (warp == issuer) tmem_dealloc(tmem, 512);
 }
 

@@ -436,6 +436,31 @@ def test_stacking_on_the_device(hl, torch, n, cols):
     assert np.array_equal(got[:rows * cols].reshape(rows, cols), hl.stack_gate_up(gate, up_)) and np.all(got[rows * cols:] == 0x5A5A)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch", [12, 20, 64])
+@pytest.mark.parametrize("rows,cols,chunk", [(90000, 128, 512), (40000, 1024, 512)])
+def test_more_work_items_than_ctas(hl, torch, rows, cols, chunk, batch):
+    """CTAs that fetch items from the counter in the workspace; three calls in a row on one workspace, whose counters must be zero behind each."""
+    w = wl.gaussian_weights(rows, cols, 0.05, rows)
+    blob = Blob(hl, torch, w, "bf16", chunk)
+    n, (ws,) = workspace(hl, torch, [blob], batch)
+    x = x_of(batch, cols, 3, "bf16")
+    bias = f_to_bits(np.random.default_rng(4).standard_normal(rows), "bf16")
+    bd, xd = up(torch, bias, "bf16"), up(torch, x, "bf16")
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    want, tol = Sums(bits_to_f64(w, "bf16"), bits_to_f64(x, "bf16")).plus(bits_to_f64(bias, "bf16")).through("silu")
+    first = None
+    for _ in range(3):
+        out = torch.empty((batch, rows), dtype=torch.float32, device="cuda")
+        hl.decode_gemm_epilogue(blob.desc, blob.dev, xd, batch, hl.Epilogue(hl.ACT_SILU, hl.ELEM_F32, bd), out, ws, n, err)
+        torch.cuda.synchronize()
+        assert_clean(hl, blob, ws, err)
+        first = out if first is None else first
+        assert torch.equal(out, first)
+    check(values(out), want, tol, "f32")
+    assert hl.gemm_launch_plan([blob.desc], batch, n)["work_items"][0] > torch.cuda.get_device_properties(0).multi_processor_count
+
+
 # ------------------------------------------------------------------------------------------------ several matrices in a launch (GPU)
 
 @pytest.mark.gpu
