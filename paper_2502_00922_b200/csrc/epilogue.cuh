@@ -16,12 +16,13 @@
 
 namespace huffllm {
 
-// v / (1 + exp(-u)).  (exp(-u) above 2^126: the quotient is 0 instead of a number below 1e-36.)
-__device__ __forceinline__ float times_sigmoid(float v, float u) { return __fdividef(v, 1.0f + expf(-u)); }
+// v / (1 + exp(-u)).  The fast exponential is off by |u| 2^-24 + 2^-22 of itself, which the quotient's slope takes below 3e-7 for u = v.
+// (exp(-u) above 2^126: the quotient is 0 instead of a number below 1e-36.)
+__device__ __forceinline__ float times_sigmoid(float v, float u) { return __fdividef(v, 1.0f + __expf(-u)); }
 
 // v / 2 (1 + erf(v / sqrt 2)), from the tail q = erfc(z), z = |v| / sqrt 2:  v q / 2 below zero, v - v q / 2 above.
 // erfc(z) = exp(-z^2) t P(t) with t = 1 / (1 + z / 2): P is the polynomial of degree 8 of least relative error on 0 <= z <= 12
-// (Lawson's reweighted least squares), 1.5e-7 in fp32.  No cancellation where v is far below zero, where 1 + erf(v / sqrt 2) has it.
+// (Lawson's reweighted least squares), 1.5e-7 in fp32; the fast exponential adds v^2 2^-25 + 2^-22.  No cancellation where v is far below zero, where 1 + erf(v / sqrt 2) has it.
 __device__ __forceinline__ float gelu(float v) {
     const float a = fabsf(v), t = __fdividef(1.0f, fmaf(0.353553390593274f, a, 1.0f));
     float p = -0.05936381220817566f;
@@ -33,7 +34,7 @@ __device__ __forceinline__ float gelu(float v) {
     p = fmaf(p, t, 0.24285362660884857f);
     p = fmaf(p, t, 0.28240957856178284f);
     p = fmaf(p, t, 0.28208446502685547f);
-    const float q = 0.5f * t * p * expf(-0.5f * v * v);
+    const float q = 0.5f * t * p * __expf(-0.5f * v * v);
     return v < 0.0f ? v * q : v - fminf(v, 64.0f) * q;          // (infinity: q is 0)
 }
 

@@ -496,7 +496,7 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
             if constexpr (EPI != 0) {
                 const EpiMat &e = *(const EpiMat *)s_epi;
                 const float bias = load_bias<FMT != 0>(e, row, row_ok);
-                constexpr int U = CW < 8 ? CW : 8;           // (vectors at a time: with 16 the registers of 32 columns did not suffice)
+                constexpr int U = CW < 8 ? CW : 8;           // (vectors at a time: 16 gained nothing, and of 32 columns they spilled)
 #pragma unroll
                 for (int i0 = 0; i0 < CW; i0 += U) {
                     float part[U], res[U];
@@ -587,6 +587,18 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
         const uint32_t kc0 = slice_beg(k0, k1, slice), kc1 = slice_beg(k0, k1, slice + 1);
         const uint32_t rg = mt * n_rg + rgi;
         const bool active = decodes && rg < RG && kc0 < kc1;
+        if constexpr (EPI != 0) {
+            // The tile's residuals are asked into L2 now, by the CTA with its first range, for whoever will close it.  (Streaming weights leave little else
+            // there.  Without / with it 22016 x 4096 at 32 vectors 50.6 / 49.9 us, 8192 x 28672 at 64 128.4 / 126.4.)
+            const EpiMat &e = *(const EpiMat *)s_epi;
+            if (e.residual && item % ksplit == 0 && warp < tiles * 8u) {
+                const uint32_t bytes = e.out16 ? 2u : 4u;
+                const uint64_t row0 = (uint64_t)mt * n_rg * 16, at = row0 + lane * (128u / bytes);      // (at most 496 rows: 16 lines)
+                if (at < k.rows && at < row0 + n_rg * 16u)
+                    for (uint32_t n = warp; n < A.batch; n += tiles * 8u)
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"((const uint8_t *)e.residual + ((uint64_t)n * e.residual_stride + at) * bytes));
+            }
+        }
         // The slices go through their chunks side by side: a chunk's stages (pairs of blocks), `steps` times.  (One slice: the
         // stages of the chunk at hand; several: those of a full chunk, some of which the row's last chunk leaves empty.)
         const uint32_t steps = slice_beg(k0, k1, 1) - k0, full_stages = (k.chunk_cols / 32u + 1u) >> 1;
