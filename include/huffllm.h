@@ -470,7 +470,8 @@ huffllm_status huffllm_add_rms_norm(const huffllm_norm *args, huffllm_stream str
  * same dtype; ffn_rows and hidden are multiples of 32.  h and out: `batch` vectors (1..64) of type h_type (huffllm_elem); out may be h
  * itself.  n and m are rounded to the blobs' dtype, as the products take them.  gain and the biases may be null; gate_up_bias is stacked.
  * The workspace (256-byte aligned, at least huffllm_ffn_workspace_bytes) must be zero-filled once after allocation, and again after a
- * call that set the error flag (a chunk number there is one of gate_up or of down); calls that share it must not overlap on the GPU.
+ * call that set the error flag (a chunk number there is one of gate_up or of down); calls that share it must not overlap on the GPU, and
+ * must be for matrices of the same shapes (any batch): where its counters end depends on the rows.
  */
 typedef struct huffllm_ffn {
     const huffllm_desc *gate_up, *down;            /* host   */

@@ -475,15 +475,16 @@ class PreparedEpilogue:
                  err_flag_dev=None):
         n = len(descs)
         self._keep = (descs, blobs_dev, xs_dev, epilogues, outs_dev, workspaces_dev, err_flag_dev)
+        ptr = lambda t: C.c_void_p(_ptr(t))                  # (already what the call takes: an int is converted every time)
         ptrs = lambda seq: (C.c_void_p * n)(*[_ptr(t) for t in seq])
-        eps, err = (Epilogue * n)(*epilogues), _ptr(err_flag_dev)
+        eps, err, batch, workspace_bytes_each = (Epilogue * n)(*epilogues), ptr(err_flag_dev), C.c_uint32(batch), C.c_size_t(workspace_bytes_each)
         if n == 1:
             self._fn = lib().huffllm_decode_gemm_epilogue
-            self._args = (C.pointer(descs[0]), _ptr(blobs_dev[0]), _ptr(xs_dev[0]), batch, eps, _ptr(outs_dev[0]), _ptr(workspaces_dev[0]),
+            self._args = (C.byref(descs[0]), ptr(blobs_dev[0]), ptr(xs_dev[0]), batch, C.byref(eps[0]), ptr(outs_dev[0]), ptr(workspaces_dev[0]),
                           workspace_bytes_each, err)
         else:
             self._fn = lib().huffllm_decode_gemm_multi_epilogue
-            self._args = (n, (C.POINTER(Desc) * n)(*[C.pointer(d) for d in descs]), ptrs(blobs_dev), ptrs(xs_dev), batch, eps,
+            self._args = (C.c_uint32(n), (C.POINTER(Desc) * n)(*[C.pointer(d) for d in descs]), ptrs(blobs_dev), ptrs(xs_dev), batch, eps,
                           ptrs(outs_dev), ptrs(workspaces_dev), workspace_bytes_each, err)
 
     def run(self, stream: int):
@@ -535,7 +536,7 @@ class PreparedNorm:
     """A huffllm_add_rms_norm call, marshalled once."""
 
     def __init__(self, norm: Norm):
-        self.norm, self._fn, self._arg = norm, lib().huffllm_add_rms_norm, C.pointer(norm)
+        self.norm, self._fn, self._arg = norm, lib().huffllm_add_rms_norm, C.byref(norm)
 
     def run(self, stream: int):
         st = self._fn(self._arg, stream)
@@ -556,8 +557,9 @@ class PreparedFfn:
                  h_stride: int = 0, out_stride: int = 0):
         self._keep = (ffn, h_dev, out_dev, workspace_dev, err_flag_dev)
         self._fn = lib().huffllm_decode_ffn
-        self._args = (C.pointer(ffn), _ptr(h_dev), h_stride, batch, _ptr(out_dev), out_stride, h_type, _ptr(workspace_dev), workspace_bytes_,
-                      _ptr(err_flag_dev))
+        ptr = lambda t: C.c_void_p(_ptr(t))
+        self._args = (C.byref(ffn), ptr(h_dev), C.c_uint64(h_stride), C.c_uint32(batch), ptr(out_dev), C.c_uint64(out_stride), C.c_uint32(h_type),
+                      ptr(workspace_dev), C.c_size_t(workspace_bytes_), ptr(err_flag_dev))
 
     def run(self, stream: int):
         st = self._fn(*self._args, stream)

@@ -4,7 +4,6 @@
 // read once and sum and out written once.  (Vectors longer than the registers of a CTA hold are read twice, the second time from L2;
 // every element is read by the thread that writes it, so sum may lie over x or delta either way.)  The sum of squares is taken in
 // fp32 in a fixed order: eight at a time, a thread's, a warp's, the CTA's.
-// `gain` does not come from the kernel in front and is asked for before the wait for it.
 #include <cuda_runtime.h>
 #include <type_traits>
 
@@ -135,8 +134,8 @@ __global__ void __launch_bounds__(kNormMaxThreads) add_rms_norm_kernel(const __g
 
     float h[N][8], gain[8], total = 0.0f;
     uint32_t g_raw[8], x_raw[N][8], d_raw[N][8];
+    pdl_wait_prior_grid();                                        // (for everything that is read: gain may be as young as x)
     if (ITEMS == 1) load_gain(0, g_raw);
-    pdl_wait_prior_grid();
     const uint32_t groups = (cols + phase + 8 * nt - 1) / (8 * nt);       // of a thread
     if (ITEMS) {
 #pragma unroll

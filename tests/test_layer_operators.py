@@ -720,3 +720,98 @@ def test_a_decoders_sub_layers_on_one_stream_and_as_a_captured_graph(hl, torch, 
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(results[seed], (mid, total, nrm)))
     assert int(err.item()) == 0
+
+
+# ------------------------------------------------------------------------------------------------ calls that nothing above makes (GPU)
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch", [1, 4, 12, 32])
+def test_bad_records_add_nothing_and_are_reported(hl, torch, batch):
+    """A record whose offsets point outside the payload: its chunk adds nothing, the epilogue runs over what is left, the flag is set; the
+    workspace, cleared, serves the next call."""
+    rows, cols = 64, 1024
+    w = wl.gaussian_weights(rows, cols, 0.05, 31)
+    blob = Blob(hl, torch, w, "bf16")
+    d = blob.desc
+    host = blob.host.copy()
+    idx = host[d.off_index:d.off_index + 4 * (d.n_chunks + 1)].view(np.uint32)
+    victim = int(d.n_chunks) - 1
+    idx[victim + 1] = 0x7FFFFFFF
+    bad = torch.from_numpy(host).cuda()
+    kept = np.ones((rows, cols), bool)
+    rg, kc = divmod(victim, d.col_chunks)
+    kept[rg * 16:(rg + 1) * 16, kc * d.chunk_cols:(kc + 1) * d.chunk_cols] = False
+    x = x_of(batch, cols, 3, "bf16")
+    xd = up(torch, x, "bf16")
+    n, (ws,) = workspace(hl, torch, [blob], batch)
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    res = torch.randn((batch, rows), device="cuda")
+    for dev, weights, code in ((bad, np.where(kept, w, np.uint16(0)), victim + 1), (blob.dev, w, 0)):
+        out = torch.full((batch, rows), float("nan"), device="cuda")
+        err.zero_()
+        hl.decode_gemm_epilogue(d, dev, xd, batch, hl.Epilogue(residual=res), out, ws, n, err)
+        torch.cuda.synchronize()
+        assert int(err.item()) == code
+        s = Sums(bits_to_f64(weights, "bf16"), bits_to_f64(x, "bf16"))
+        check(values(out), s.v + values(res), s.tol + F32 * (np.abs(s.v + values(res)) + s.tol), "f32")
+        ws[:hl.workspace_control_bytes(d)].zero_()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch", [1, 20])
+def test_two_calls_at_once_and_results_straight_to_pinned_host_memory(hl, torch, batch):
+    rows, cols = 512, 1024
+    blob = Blob(hl, torch, wl.gaussian_weights(rows, cols, 0.05, 1), "bf16")
+    n, wss = workspace(hl, torch, [blob] * 2, batch)
+    wss.append(torch.zeros_like(wss[0]))
+    xs = [up(torch, x_of(batch, cols, i, "bf16"), "bf16") for i in range(2)]
+    alone = [torch.empty((batch, rows), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    ep = hl.Epilogue(hl.ACT_GELU, hl.ELEM_16)
+    for x, out in zip(xs, alone):
+        hl.decode_gemm_epilogue(blob.desc, blob.dev, x, batch, ep, out, wss[0], n)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.empty((batch, rows), dtype=torch.bfloat16, device="cuda"), torch.empty((batch, rows), dtype=torch.bfloat16).pin_memory()]
+    for _ in range(20):
+        for s, x, out, ws in zip(streams, xs, outs, wss):
+            hl.decode_gemm_epilogue(blob.desc, blob.dev, x, batch, ep, out, ws, n, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], alone[0]) and torch.equal(outs[1], alone[1].cpu())
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits(hl, torch):
+    """Vectors 2^31 values apart: a product's out and residual, a norm's input and output; and 9 vectors (tensor cores) 2^29 values apart."""
+    rows, cols, far = 32, 64, (1 << 31) + 8
+    w = wl.gaussian_weights(rows, cols, 0.05, 1)
+    blob = Blob(hl, torch, w, "bf16")
+    big = torch.empty(2 * far + 64, dtype=torch.bfloat16, device="cuda")
+    at = lambda b: big[b * far:b * far + rows]
+    batch = 3
+    n, (ws,) = workspace(hl, torch, [blob], batch)
+    x = x_of(batch, cols, 2, "bf16")
+    r = torch.randn((batch, rows), device="cuda").to(torch.bfloat16)
+    for b in range(batch):
+        at(b).copy_(r[b])
+    xd = up(torch, x, "bf16")
+    hl.decode_gemm_epilogue(blob.desc, blob.dev, xd, batch, hl.Epilogue(0, hl.ELEM_16, None, big, far, far), big, ws, n)
+    torch.cuda.synchronize()
+    s = Sums(bits_to_f64(w, "bf16"), bits_to_f64(x, "bf16"))
+    want = s.v + values(r)
+    check(np.stack([values(at(b)) for b in range(batch)]), want, s.tol + F32 * np.abs(want), "bf16")
+    o = torch.empty((3, rows), dtype=torch.bfloat16, device="cuda")
+    h = np.stack([values(at(b)) for b in range(3)])
+    hl.add_rms_norm(hl.Norm(hl.BF16, 3, rows, big, hl.ELEM_16, None, 1e-5, o, x_stride=far))
+    hl.add_rms_norm(hl.Norm(hl.BF16, 3, rows, o, hl.ELEM_16, None, 1e-5, big, out_stride=far))
+    torch.cuda.synchronize()
+    check(values(o), norm64(h, 1.0, 1e-5), np.abs(norm64(h, 1.0, 1e-5)) * 2.0 ** -20, "bf16")
+    check(np.stack([values(at(b)) for b in range(3)]), norm64(values(o), 1.0, 1e-5), np.abs(norm64(values(o), 1.0, 1e-5)) * 2.0 ** -20, "bf16")
+    near = 1 << 29
+    n, (ws,) = workspace(hl, torch, [blob], 9)
+    x = x_of(9, cols, 4, "bf16")
+    xd = up(torch, x, "bf16")
+    big = torch.empty(8 * near + 64, dtype=torch.bfloat16, device="cuda")
+    hl.decode_gemm_epilogue(blob.desc, blob.dev, xd, 9, hl.Epilogue(hl.ACT_RELU, hl.ELEM_16, None, None, 0, near), big, ws, n)
+    torch.cuda.synchronize()
+    got = np.stack([values(big[b * near:b * near + rows]) for b in range(9)])
+    check(got, *Sums(bits_to_f64(w, "bf16"), bits_to_f64(x, "bf16")).through("relu"), "bf16")
