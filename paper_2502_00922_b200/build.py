@@ -9,8 +9,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(os.path.dirname(PKG), "include")
 SO = os.path.join(PKG, "libhuffllm.so")
-SOURCES = ["host_codec.cpp", "api.cu", "kernels.cu", "kernels_epilogue.cu", "kernels_tc.cu", "kernels_tc_epilogue.cu", "norm.cu", "split_explorer.cu",
-           "encode_device.cu"]
+SOURCES = ["host_codec.cpp", "api.cu", "kernels.cu", "kernels_epilogue.cu", "kernels_tc.cu", "kernels_tc_epilogue.cu", "kernels_tc_epilogue_fp16.cu",
+           "norm.cu", "split_explorer.cu", "encode_device.cu"]
 
 
 def needs_build() -> bool:

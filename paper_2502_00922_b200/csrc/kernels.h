@@ -97,6 +97,7 @@ cudaError_t launch_gemm(const KernelArgs &k, uint32_t grid, cudaStream_t stream)
 cudaError_t launch_gemm_tc(const TcArgs &t, uint32_t grid, cudaStream_t stream);
 cudaError_t launch_gemm(const EpiKernelArgs &k, uint32_t grid, cudaStream_t stream);
 cudaError_t launch_gemm_tc(const EpiTcArgs &t, uint32_t grid, cudaStream_t stream);
+cudaError_t launch_gemm_tc_fp16(const EpiTcArgs &t, uint32_t grid, cudaStream_t stream);
 // Residual addition and norm: strides in values; x16, delta16: 16-bit values (else fp32), sum has x's type.
 struct NormArgs {
     const void *x, *delta;     // delta: may be null

@@ -3,6 +3,8 @@
 
 namespace huffllm {
 
-cudaError_t launch_gemm_tc(const TcArgs &t, uint32_t grid, cudaStream_t stream) { return launch_tc_format<0>(t, grid, stream); }
+cudaError_t launch_gemm_tc(const TcArgs &t, uint32_t grid, cudaStream_t stream) {
+    return t.k.fmt ? launch_tc_fp16<0>(t, grid, stream) : launch_tc_bf16<0>(t, grid, stream);
+}
 
 }  // namespace huffllm

@@ -832,37 +832,22 @@ static cudaError_t launch_tc_one(const TcProductArgs<EPI> &t, uint32_t grid, cud
 }
 
 // The kernel of a launch's blobs and padding.
+template <int LB, int FMT, int EPI>
+static cudaError_t launch_tc_padded(const TcProductArgs<EPI> &t, uint32_t grid, cudaStream_t stream) {
+    if (t.k.tc_npad == 16) return launch_tc_one<LB, 16, FMT, EPI>(t, grid, stream);
+    if (t.k.tc_npad == 32) return launch_tc_one<LB, 32, FMT, EPI>(t, grid, stream);
+    return launch_tc_one<LB, 64, FMT, EPI>(t, grid, stream);
+}
 template <int EPI>
-static cudaError_t launch_tc_format(const TcProductArgs<EPI> &t, uint32_t grid, cudaStream_t stream) {
-    const KernelArgs &k = t.k;
-    if (k.fmt && k.fp16_flat == kFlatUpper) {
-        if (k.tc_npad == 16) return launch_tc_one<8, 16, 3, EPI>(t, grid, stream);
-        if (k.tc_npad == 32) return launch_tc_one<8, 32, 3, EPI>(t, grid, stream);
-        return launch_tc_one<8, 64, 3, EPI>(t, grid, stream);
-    }
-    if (k.fmt && k.fp16_flat == kFlatBoth) {
-        if (k.tc_npad == 16) return launch_tc_one<8, 16, 2, EPI>(t, grid, stream);
-        if (k.tc_npad == 32) return launch_tc_one<8, 32, 2, EPI>(t, grid, stream);
-        return launch_tc_one<8, 64, 2, EPI>(t, grid, stream);
-    }
-    if (k.fmt && k.fp16_flat == kFlatBothLanes) {
-        if (k.tc_npad == 16) return launch_tc_one<8, 16, 4, EPI>(t, grid, stream);
-        if (k.tc_npad == 32) return launch_tc_one<8, 32, 4, EPI>(t, grid, stream);
-        return launch_tc_one<8, 64, 4, EPI>(t, grid, stream);
-    }
-    if (k.fmt) {
-        if (k.tc_npad == 16) return launch_tc_one<8, 16, 1, EPI>(t, grid, stream);
-        if (k.tc_npad == 32) return launch_tc_one<8, 32, 1, EPI>(t, grid, stream);
-        return launch_tc_one<8, 64, 1, EPI>(t, grid, stream);
-    }
-    if (k.lut_bits == 8) {
-        if (k.tc_npad == 16) return launch_tc_one<8, 16, 0, EPI>(t, grid, stream);
-        if (k.tc_npad == 32) return launch_tc_one<8, 32, 0, EPI>(t, grid, stream);
-        return launch_tc_one<8, 64, 0, EPI>(t, grid, stream);
-    }
-    if (k.tc_npad == 16) return launch_tc_one<9, 16, 0, EPI>(t, grid, stream);
-    if (k.tc_npad == 32) return launch_tc_one<9, 32, 0, EPI>(t, grid, stream);
-    return launch_tc_one<9, 64, 0, EPI>(t, grid, stream);
+static cudaError_t launch_tc_bf16(const TcProductArgs<EPI> &t, uint32_t grid, cudaStream_t stream) {
+    return t.k.lut_bits == 8 ? launch_tc_padded<8, 0, EPI>(t, grid, stream) : launch_tc_padded<9, 0, EPI>(t, grid, stream);
+}
+template <int EPI>
+static cudaError_t launch_tc_fp16(const TcProductArgs<EPI> &t, uint32_t grid, cudaStream_t stream) {
+    if (t.k.fp16_flat == kFlatUpper) return launch_tc_padded<8, 3, EPI>(t, grid, stream);
+    if (t.k.fp16_flat == kFlatBoth) return launch_tc_padded<8, 2, EPI>(t, grid, stream);
+    if (t.k.fp16_flat == kFlatBothLanes) return launch_tc_padded<8, 4, EPI>(t, grid, stream);
+    return launch_tc_padded<8, 1, EPI>(t, grid, stream);
 }
 
 }  // namespace huffllm
