@@ -1,4 +1,4 @@
-// Launch interface between the C-ABI entry points (api.cu) and the kernels (kernels.cu).
+// Launch interface between the C-ABI entry points (api.cu) and the kernels (huff_kernel.cuh, tc_kernel.cuh, norm.cu).
 #pragma once
 #include <cuda_runtime.h>
 #include <cstdint>

@@ -1,4 +1,4 @@
-// Which weights of a row the 16-byte pieces of a decode's output hold where rows start anywhere (kernels.cu, store_piece).
+// Which weights of a row the 16-byte pieces of a decode's output hold where rows start anywhere (huff_kernel.cuh, store_piece).
 // Arithmetic only, so that the host can go through column counts no test could decode.
 #pragma once
 #include <cstdint>
