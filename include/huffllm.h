@@ -414,15 +414,16 @@ typedef struct huffllm_epilogue {
 
 /*
  * huffllm_decode_gemm with an epilogue: the same kernels, workspace, limits and error flag (which kernel runs at 9..16 vectors is chosen
- * anew, so the sums may differ from the plain call's in their last bits there).  out: device memory (or pinned host memory
+ * anew, and blobs of long codes take the tensor cores above 8 vectors too, so the sums may differ from the plain call's in their last bits
+ * there).  out: device memory (or pinned host memory
  * the device can address), aligned to its type.
  */
 huffllm_status huffllm_decode_gemm_epilogue(const huffllm_desc *desc, const void *blob_dev, const uint16_t *x_dev, uint32_t batch,
                                             const huffllm_epilogue *epilogue, void *out_dev, void *workspace_dev,
                                             size_t workspace_bytes, int32_t *err_flag_dev, huffllm_stream stream);
 
-/* huffllm_decode_gemm_multi with an epilogue per matrix (q, k and v with their biases, say): epilogues is a host array of n.  Batches of 9..16
- * take FP16 blobs of max_code_len 8 and BF16 blobs of max_code_len 9 too. */
+/* huffllm_decode_gemm_multi with an epilogue per matrix (q, k and v with their biases, say): epilogues is a host array of n.  Every batch
+ * takes blobs of every max_code_len (of more than 8 vectors UNSUPPORTED only where their records are too large for the tensor-core kernel). */
 huffllm_status huffllm_decode_gemm_multi_epilogue(uint32_t n, const huffllm_desc *const *descs, const void *const *blobs_dev,
                                                   const uint16_t *const *xs_dev, uint32_t batch, const huffllm_epilogue *epilogues,
                                                   void *const *outs_dev, void *const *workspaces_dev, size_t workspace_bytes_each,

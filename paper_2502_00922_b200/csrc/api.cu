@@ -410,7 +410,7 @@ huffllm_status add_matrix(KernelArgs *k, const huffllm_desc *desc, const void *b
 // The tensor-core kernel's part of a launch description.
 void set_tc_shape(KernelArgs *k, uint32_t npad, const TcShape &sh, uint32_t flat) {
     k->fp16_flat = flat;
-    if (k->fmt) k->lut_size = fp16_table_bytes(flat);
+    if (k->fmt && k->lut_bits <= 8) k->lut_size = fp16_table_bytes(flat);
     k->part_bytes = sh.part_bytes(npad);
     k->slots = 2;
     k->pair_recip = (uint32_t)(0x100000000ull / (2ull * k->slot_bytes));
@@ -741,7 +741,6 @@ static huffllm_status product_multi(uint32_t n, const huffllm_desc *const *descs
         two_tiles = true;
         tensor_cores = true;
         for (uint32_t i = 0; i < n; ++i) {
-            tensor_cores = tensor_cores && tc_blob(descs[i]);
             two_tiles = two_tiles && two_tile_blob(descs[i]);
             shorter = shorter && descs[i]->chunk_cols <= 256;
         }
@@ -756,7 +755,7 @@ static huffllm_status product_multi(uint32_t n, const huffllm_desc *const *descs
         uint32_t grid;
         begin_args(&k, batch, dev);
         for (uint32_t i = 0; i < n; ++i) {
-            if (!tc_blob(descs[i]))
+            if (!eps && !tc_blob(descs[i]))
                 return fail(HUFFLLM_ERR_UNSUPPORTED, "more than %u vectors per call over several matrices take tables of up to 9 bits (FP16: 8)", kTwoTileBatch);
             for (uint32_t j = 0; j < i; ++j)
                 if (workspaces[j] == workspaces[i]) return fail(HUFFLLM_ERR_INVALID_ARG, "matrices %u and %u share a workspace", j, i);
@@ -876,7 +875,8 @@ static huffllm_status product_one(const huffllm_desc *desc, const void *blob, co
     auto tensor_core = [&](bool other_path_left) -> huffllm_status {
         // one pass over the compressed weights for the whole batch (tables of up to 9 bits; longer codes take passes of 8
         // vectors through the register-path kernel and its two-level lookup)
-        if (!tc_blob(desc)) return HUFFLLM_OK;
+        // (with epilogues blobs of longer codes too)
+        if (!ep && !tc_blob(desc)) return HUFFLLM_OK;
         // (column ranges are planned within the workspace at hand)
         const uint32_t npad = tc_npad_of(batch), cta = (uint32_t)dev.sms;
         TcShape sh;

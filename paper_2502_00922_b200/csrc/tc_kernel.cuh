@@ -148,6 +148,7 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
         return ldg_stream16(p);
     };
     constexpr Decoder D = decoder_of(LB, FMT);
+    constexpr bool LONG = D == kBf12 || D == kHalf12;        // first level of 8 bits, then the whole table
     constexpr uint32_t kBStage = NPAD * 128;                // bytes of B per slice and stage: NPAD rows x 64 columns (two blocks) of bf16
     constexpr uint32_t kLbo = 128, kSbo = 1024;             // core matrices: 8 along K side by side, then the next 8 rows
     constexpr uint32_t kACol0 = kTcTiles * NPAD;            // first tensor-memory column of the A stages
@@ -230,6 +231,8 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
     }
     const uint32_t b_base = smem_base + A.dyn_smem_bytes - A.part_bytes;   // the stages of B behind everything else
     uint32_t lut_lane = lut_column<D>(plan.lut, lane), lut_low = lut_low_column<D>(plan.lut, lane);
+    // (two-level lookup: the whole table, one copy, behind the first level)
+    const uint32_t full_base = LONG ? plan.lut + kLutBytes<D> : 0u, full_mask = LONG ? ((1u << A.lut_bits) - 1u) << 2 : 0u;
     asm volatile("mov.u32 %0, %0;" : "+r"(lut_lane));
     if (D == kUpper) asm volatile("mov.u32 %0, %0;" : "+r"(lut_low));
     const uint32_t bar0 = smem_u32(&bars[warp * 2]);
@@ -302,6 +305,10 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
         for (int i = 0; i < kLutLoads; ++i) {
             const uint32_t v = tid + i * 1024u, e = lut_entry<D>(lut_v[i], LutPlan<D>::field(v));
             if (v < kLutVecs) lut_s[v] = make_uint4(e, e, e, e);
+        }
+        if constexpr (LONG) {
+            uint32_t *full_s = (uint32_t *)(dyn_smem + (plan.lut + kLutBytes<D> - smem_base));
+            for (uint32_t i = tid; i < (FMT ? 3u : 1u) << A.lut_bits; i += 1024u) full_s[i] = lut_entry<D>(__ldg(lut_g + i), 0u, false);
         }
     }
     tc_fence_before();
@@ -724,7 +731,7 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
                         // whole raw part at once, with its copy: 36.8 and 139.6 for the first two.)
                         if (FMT == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(raw_p + kRawBlock));
                         uint32_t a[8];
-                        decode_block<D>(pa, pb, lane << 2, lut_lane, lut_low, raw_c, a, 0u, 0u);
+                        decode_block<D>(pa, pb, lane << 2, lut_lane, lut_low, raw_c, a, full_base, full_mask);
                         stage_block(a, half, nblk);
                     };
                     uint32_t kb = 0;
@@ -840,13 +847,19 @@ static cudaError_t launch_tc_padded(const TcProductArgs<EPI> &t, uint32_t grid, 
 }
 template <int EPI>
 static cudaError_t launch_tc_bf16(const TcProductArgs<EPI> &t, uint32_t grid, cudaStream_t stream) {
+    if constexpr (EPI != 0)
+        if (t.k.lut_bits > 9) return launch_tc_padded<12, 0, EPI>(t, grid, stream);
     return t.k.lut_bits == 8 ? launch_tc_padded<8, 0, EPI>(t, grid, stream) : launch_tc_padded<9, 0, EPI>(t, grid, stream);
 }
 template <int EPI>
 static cudaError_t launch_tc_fp16(const TcProductArgs<EPI> &t, uint32_t grid, cudaStream_t stream) {
+    if constexpr (EPI != 0)
+        if (t.k.lut_bits > 8) return launch_tc_padded<12, 1, EPI>(t, grid, stream);
     if (t.k.fp16_flat == kFlatUpper) return launch_tc_padded<8, 3, EPI>(t, grid, stream);
     if (t.k.fp16_flat == kFlatBoth) return launch_tc_padded<8, 2, EPI>(t, grid, stream);
     if (t.k.fp16_flat == kFlatBothLanes) return launch_tc_padded<8, 4, EPI>(t, grid, stream);
+    if constexpr (EPI != 0)
+        if (t.k.lut_bits == 7) return launch_tc_padded<7, 1, EPI>(t, grid, stream);
     return launch_tc_padded<8, 1, EPI>(t, grid, stream);
 }
 

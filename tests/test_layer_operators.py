@@ -283,9 +283,12 @@ PRODUCTS = [
     (2049, 2048, "bf16", 4096, 0),        # row groups shared by warps and CTAs; as wide as tall but for a row
     (2048, 4096, "bf16", 4096, 0),        # tensor-core shapes
     (333, 1024, "bf16", 2048, 9),         # the other table size
-    (77, 640, "bf16", 1024, 12),          # two-level lookups: passes of 8 vectors
+    (77, 640, "bf16", 1024, 12),          # two-level lookups
+    (300, 1056, "bf16", 2048, 10),
+    (90, 672, "fp16", 1024, 12),
+    (96, 1024, "fp16", 8192, 0),          # records too large for the tensor-core kernel's slots: passes of 8 vectors
     (130, 1056, "fp16", 1024, 0),
-    (515, 512, "fp16", 1024, 7),          # no tensor-core kernel: passes of 8 vectors
+    (515, 512, "fp16", 1024, 7),          # tables of 128 entries
     (64, 8192, "bf16", 16384, 0),         # single slots
 ]
 
@@ -313,10 +316,10 @@ def test_every_activation_on_every_path(hl, torch, act, dtype, out16, batch):
 @pytest.mark.gpu
 @pytest.mark.parametrize("batch", [1, 4, 16, 64])
 @pytest.mark.parametrize("out16", [False, True])
-@pytest.mark.parametrize("limit", [0, 12])
-def test_the_residual_stream_is_updated_in_place(hl, torch, batch, out16, limit):
-    w = wl.gaussian_weights(528, 1024, 0.05, 9)
-    run_product(hl, torch, w, "bf16", batch, "none", True, True, out16, limit=limit, stride=16, in_place=True, seed=batch)
+@pytest.mark.parametrize("dtype,chunk,limit", [("bf16", 1024, 0), ("bf16", 1024, 12), ("fp16", 8192, 0)])
+def test_the_residual_stream_is_updated_in_place(hl, torch, batch, out16, dtype, chunk, limit):
+    w = wl.gaussian_weights(528, 1024, 0.05, 9, dtype)
+    run_product(hl, torch, w, dtype, batch, "none", True, True, out16, chunk, limit, stride=16, in_place=True, seed=batch)
 
 
 @pytest.mark.gpu
@@ -335,6 +338,15 @@ def test_without_an_epilogue_the_sums_are_those_of_the_plain_product(hl, torch, 
     hl.decode_gemm_epilogue(blob.desc, blob.dev, x, batch, hl.Epilogue(out_type=hl.ELEM_16), out16, ws, n)
     torch.cuda.synchronize()
     assert torch.equal(y, out32) and torch.equal(y.to(torch.bfloat16), out16)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,limit", [("bf16", 9), ("bf16", 10), ("bf16", 12), ("fp16", 7), ("fp16", 9), ("fp16", 12)])
+@pytest.mark.parametrize("batch", [3, 9, 32, 64])
+def test_codewords_of_every_length_on_every_path(hl, torch, dtype, limit, batch):
+    """Weights whose fields have codewords up to the limit: exponents that fall off by halves."""
+    w = wl.skewed_exponent_weights(200, 1056, 17, dtype=dtype)
+    run_product(hl, torch, w, dtype, batch, "relu", False, False, False, 1024, limit, seed=batch)
 
 
 @pytest.mark.gpu
@@ -408,7 +420,7 @@ def gated_case(hl, torch, n, cols, dtype, batch, act, bias, out16, chunk, limit,
 @pytest.mark.gpu
 @pytest.mark.parametrize("n,cols,dtype,chunk,limit", [(1, 32, "bf16", 512, 0), (7, 96, "bf16", 1024, 0), (8, 512, "bf16", 1024, 0), (201, 1056, "bf16", 1024, 0),
                                                       (1030, 2048, "bf16", 4096, 0), (333, 1024, "bf16", 2048, 9), (45, 640, "bf16", 1024, 12),
-                                                      (131, 1056, "fp16", 1024, 0), (60, 512, "fp16", 1024, 7), (1024, 4096, "bf16", 4096, 0)])
+                                                      (131, 1056, "fp16", 1024, 0), (60, 512, "fp16", 1024, 7), (1024, 4096, "bf16", 4096, 0), (70, 512, "fp16", 8192, 0)])
 @pytest.mark.parametrize("batch", [1, 2, 8, 9, 16, 17, 48, 64])
 def test_gated_products(hl, torch, n, cols, dtype, chunk, limit, batch):
     i = n + batch
@@ -465,13 +477,13 @@ def test_more_work_items_than_ctas(hl, torch, rows, cols, chunk, batch):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("batch", [1, 5, 12, 20, 64])
-@pytest.mark.parametrize("dtype,chunk", [("bf16", 1024), ("bf16", 8192), ("fp16", 1024), ("fp16", 2048)])
-def test_several_matrices_with_an_epilogue_each(hl, torch, batch, dtype, chunk):
+@pytest.mark.parametrize("dtype,chunk,limit", [("bf16", 1024, 0), ("bf16", 8192, 0), ("fp16", 1024, 0), ("fp16", 2048, 7), ("bf16", 2048, 11), ("fp16", 1024, 10)])
+def test_several_matrices_with_an_epilogue_each(hl, torch, batch, dtype, chunk, limit):
     """A gated product, one with bias and one with residual in one launch; one fp32 output among 16-bit ones."""
     cols, n = 512, 100
     gate, up_ = wl.gaussian_weights(n, cols, 0.05, 1, dtype), wl.gaussian_weights(n, cols, 0.05, 2, dtype)
     mats = [hl.stack_gate_up(gate, up_), wl.gaussian_weights(300, cols, 0.05, 3, dtype), wl.gaussian_weights(77, cols, 0.05, 4, dtype)]
-    blobs = [Blob(hl, torch, m, dtype, chunk) for m in mats]
+    blobs = [Blob(hl, torch, m, dtype, chunk, limit) for m in mats]
     x = x_of(batch, cols, 5, dtype)
     rng = np.random.default_rng(6)
     bias = f_to_bits(rng.standard_normal(300), dtype)
