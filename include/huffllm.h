@@ -423,7 +423,7 @@ huffllm_status huffllm_decode_gemm_epilogue(const huffllm_desc *desc, const void
                                             size_t workspace_bytes, int32_t *err_flag_dev, huffllm_stream stream);
 
 /* huffllm_decode_gemm_multi with an epilogue per matrix (q, k and v with their biases, say): epilogues is a host array of n.  Every batch
- * takes blobs of every max_code_len (of more than 8 vectors UNSUPPORTED only where their records are too large for the tensor-core kernel). */
+ * takes blobs of every max_code_len (more than 8 vectors of blobs whose records are too large for the tensor-core kernel take launches of their own). */
 huffllm_status huffllm_decode_gemm_multi_epilogue(uint32_t n, const huffllm_desc *const *descs, const void *const *blobs_dev,
                                                   const uint16_t *const *xs_dev, uint32_t batch, const huffllm_epilogue *epilogues,
                                                   void *const *outs_dev, void *const *workspaces_dev, size_t workspace_bytes_each,

@@ -715,6 +715,10 @@ static huffllm_status check_product_args(const huffllm_desc *desc, const uint16_
     return HUFFLLM_OK;
 }
 
+static huffllm_status product_one(const huffllm_desc *desc, const void *blob, const uint16_t *x, uint32_t batch, float *y, const huffllm_epilogue *ep,
+                                  void *out, void *workspace, size_t workspace_bytes, size_t shift, int32_t *err_flag, huffllm_stream stream,
+                                  bool dry = false);
+
 // Several products in one launch: fp32 sums to ys (eps null), or with an epilogue each to outs.
 static huffllm_status product_multi(uint32_t n, const huffllm_desc *const *descs, const void *const *blobs, const uint16_t *const *xs,
                                     uint32_t batch, float *const *ys, const huffllm_epilogue *eps, void *const *outs, void *const *workspaces,
@@ -771,12 +775,12 @@ static huffllm_status product_multi(uint32_t n, const huffllm_desc *const *descs
         TcShape sh;
         TcPlan plans[kMaxMats];
         if (!tc_choose(descs, n, npad, cta, &flat, k.dyn_smem_bytes, workspace_bytes_each, &sh, plans))
-            return two_tiles ? HUFFLLM_OK : fail(HUFFLLM_ERR_UNSUPPORTED, "chunk records too large for the tensor-core kernel's slots");
+            return eps ? HUFFLLM_OK : fail(HUFFLLM_ERR_UNSUPPORTED, "chunk records too large for the tensor-core kernel's slots");
         set_tc_shape(&k, npad, sh, flat);
         uint32_t first = 0;
         for (uint32_t i = 0; i < n; ++i) {
             const TcPlan &tp = plans[i];
-            if (workspace_bytes_each < tp.bytes) return two_tiles ? HUFFLLM_OK : fail(HUFFLLM_ERR_BUFFER_TOO_SMALL, "workspace of matrix %u too small for batch %u", i, batch);
+            if (workspace_bytes_each < tp.bytes) return eps ? HUFFLLM_OK : fail(HUFFLLM_ERR_BUFFER_TOO_SMALL, "workspace of matrix %u too small for batch %u", i, batch);
             t.m_tiles[i] = tp.m_tiles;
             t.ksplit[i] = tp.ksplit;
             t.ticket[i] = (unsigned int *)((uint8_t *)workspaces[i] + tp.ticket_off);
@@ -792,6 +796,15 @@ static huffllm_status product_multi(uint32_t n, const huffllm_desc *const *descs
         return HUFFLLM_OK;
     };
     if (tensor_cores && ((st = on_tensor_cores()) != HUFFLLM_OK || done)) return st;
+    if (eps && batch > kKernelBatch && !two_tiles) {
+        // records too large for the tensor-core kernel's slots: a launch per matrix (and for each what a call for it alone would do)
+        for (uint32_t dry = 2; dry--;)
+            for (uint32_t i = 0; i < n; ++i)
+                if ((st = product_one(descs[i], blobs[i], xs[i], batch, nullptr, &eps[i], outs[i], workspaces[i], workspace_bytes_each, 0, err_flag, stream,
+                                      dry != 0)) != HUFFLLM_OK)
+                    return st;
+        return HUFFLLM_OK;
+    }
     KernelArgs k;
     uint32_t grid;
     begin_args(&k, batch, dev);
@@ -834,7 +847,7 @@ huffllm_status huffllm_decode_gemm_multi_epilogue(uint32_t n, const huffllm_desc
 // than this matrix's counters ask for (another matrix's, larger, use the same workspace).  `dry`: all checks and plans, no launch.
 static huffllm_status product_one(const huffllm_desc *desc, const void *blob, const uint16_t *x, uint32_t batch, float *y,
                                   const huffllm_epilogue *ep, void *out, void *workspace, size_t workspace_bytes, size_t shift,
-                                  int32_t *err_flag, huffllm_stream stream, bool dry = false) {
+                                  int32_t *err_flag, huffllm_stream stream, bool dry) {
     clear_error();
     huffllm_status st;
     if (batch == 0 || batch > 64) return fail(HUFFLLM_ERR_INVALID_ARG, "batch must be in [1, 64]");

@@ -477,7 +477,7 @@ def test_more_work_items_than_ctas(hl, torch, rows, cols, chunk, batch):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("batch", [1, 5, 12, 20, 64])
-@pytest.mark.parametrize("dtype,chunk,limit", [("bf16", 1024, 0), ("bf16", 8192, 0), ("fp16", 1024, 0), ("fp16", 2048, 7), ("bf16", 2048, 11), ("fp16", 1024, 10)])
+@pytest.mark.parametrize("dtype,chunk,limit", [("bf16", 1024, 0), ("bf16", 8192, 0), ("fp16", 1024, 0), ("fp16", 2048, 7), ("bf16", 2048, 11), ("fp16", 1024, 10), ("fp16", 8192, 0)])
 def test_several_matrices_with_an_epilogue_each(hl, torch, batch, dtype, chunk, limit):
     """A gated product, one with bias and one with residual in one launch; one fp32 output among 16-bit ones."""
     cols, n = 512, 100
