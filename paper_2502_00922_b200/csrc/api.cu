@@ -340,8 +340,8 @@ bool tc_best(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const uint
 // more chunks for the 16 KB (the workspace at hand does not decide).  With fewer tiles a CTA because of it, 12288 x 12288 at 32
 // vectors in chunks of 2048 took 121.5 us and was 4.9e-6 from 64 bits, with sixteen copies 117.8 and 1.7e-6; in chunks of 1024, where
 // all tiles fit either way, 8192 x 8192 at 24 took 56.0 us with a copy per lane and 58.0 with sixteen.
-bool tc_choose(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const uint32_t *cta, uint32_t *flat, uint32_t dyn_smem, size_t max_bytes,
-               TcShape *shape, TcPlan *plans) {
+bool tc_choose_anew(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const uint32_t *cta, uint32_t *flat, uint32_t dyn_smem, size_t max_bytes,
+                    TcShape *shape, TcPlan *plans) {
     // (room for 32 decoders beside the larger table and the most stages that a shape has: every shape fits beside either table, and
     // so the plans are the same)
     const uint32_t slices = npad == 64 ? 2 : 4;
@@ -362,6 +362,53 @@ bool tc_choose(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const ui
     for (uint32_t i = 0; i < n; ++i)
         if (plans[i].bytes > max_bytes) return tc_best(d, n, npad, cta, *flat, dyn_smem, max_bytes, shape, plans);
     return true;
+}
+
+// The same, remembered: a plan is worked out from a few dozen numbers in 3 to 5 us, as long as a small product takes on the GPU, and a program asks for
+// the same few plans at every step.  A thread keeps the last ones by those numbers (all that the functions above read).
+struct TcQuestion {
+    uint32_t n, npad, flat, dyn_smem;
+    uint64_t max_bytes;
+    struct {
+        uint32_t cta, dtype, lut_bits, flat_fields, max_words, chunk_cols, row_groups, col_chunks;
+        uint64_t n_chunks;
+    } m[kMaxMats];
+};
+struct TcAnswer {
+    TcQuestion of;
+    uint32_t flat;
+    bool known, fits;
+    TcShape shape;
+    TcPlan plans[kMaxMats];
+};
+bool tc_choose(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const uint32_t *cta, uint32_t *flat, uint32_t dyn_smem, size_t max_bytes,
+               TcShape *shape, TcPlan *plans) {
+    constexpr uint32_t kKept = 16;
+    static thread_local TcAnswer kept[kKept];
+    TcQuestion q;
+    memset(&q, 0, sizeof(q));
+    q.n = n;
+    q.npad = npad;
+    q.flat = *flat;
+    q.dyn_smem = dyn_smem;
+    q.max_bytes = max_bytes;
+    uint64_t hash = 0;
+    for (uint32_t i = 0; i < n; ++i) {
+        q.m[i] = {cta[i], d[i]->dtype, d[i]->lut_bits, d[i]->flat_fields, d[i]->max_words, d[i]->chunk_cols, d[i]->row_groups, d[i]->col_chunks, d[i]->n_chunks};
+        hash = hash * 0x9E3779B97F4A7C15ull + d[i]->n_chunks * 31 + d[i]->row_groups;
+    }
+    TcAnswer &a = kept[((hash * 0x9E3779B97F4A7C15ull) >> 58) % kKept ^ (npad >> 5)];
+    if (!a.known || memcmp(&a.of, &q, sizeof(q)) != 0) {
+        a.known = false;
+        a.flat = *flat;
+        a.fits = tc_choose_anew(d, n, npad, cta, &a.flat, dyn_smem, max_bytes, &a.shape, a.plans);
+        a.of = q;
+        a.known = true;
+    }
+    *flat = a.flat;
+    *shape = a.shape;
+    for (uint32_t i = 0; i < n; ++i) plans[i] = a.plans[i];
+    return a.fits;
 }
 
 // Start a launch description.

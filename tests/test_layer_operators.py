@@ -151,6 +151,29 @@ def test_stacking_is_refused(hl):
         hl.stack_gate_up(g, g[:4])
 
 
+def test_remembered_plans_are_those_worked_out_anew(hl):
+    """Launch plans are kept per thread by the numbers that they follow from: more questions than are kept, in several orders, against threads
+    that have kept nothing."""
+    import threading
+    descs = []
+    for dtype, limit, chunk in (("bf16", 0, 1024), ("bf16", 9, 512), ("fp16", 0, 1024)):
+        for rows, cols in ((64, 512), (700, 512), (64, 4096)):
+            descs.append(Blob(hl, None, wl.gaussian_weights(rows, cols, 0.02, rows, dtype), dtype, chunk, limit).desc)
+    questions = [(d, b, w) for d in descs for b in (9, 17, 64) for w in (0, hl.workspace_bytes(d, b), hl.workspace_bytes(d, b) + (1 << 22))]
+    ask = lambda q: hl.gemm_launch_plan([q[0]], q[1], q[2])
+    anew = []
+    for q in questions:
+        t = threading.Thread(target=lambda: anew.append(ask(q)))
+        t.start()
+        t.join()
+    assert len(anew) == len(questions)
+    order = list(range(len(questions)))
+    for seed in range(3):
+        np.random.default_rng(seed).shuffle(order)
+        for i in order + order[::-1]:
+            assert ask(questions[i]) == anew[i]
+
+
 def status(call):
     from paper_2502_00922_b200 import HuffllmError
     try:
