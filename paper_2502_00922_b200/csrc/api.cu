@@ -592,6 +592,8 @@ huffllm_status make_epilogue(const huffllm_epilogue &ep, const huffllm_desc *des
     m->out = out;
     m->out_stride = ep.out_stride ? ep.out_stride : width;
     m->residual_stride = ep.residual_stride ? ep.residual_stride : width;
+    if (m->residual && m->residual == m->out && m->residual_stride != m->out_stride)
+        return fail(HUFFLLM_ERR_INVALID_ARG, "out in place of the residual takes its stride");
     m->gated_rows = ep.gated_rows;
     m->act = ep.activation;
     m->out16 = ep.out_type == HUFFLLM_ELEM_16;

@@ -197,6 +197,7 @@ def refusals(hl, desc, ws_bytes):
              ("bias off its type", dict(epilogue=E(bias=A + 1)), "INVALID_ARG"),
              ("short out stride", dict(epilogue=E(out_stride=desc.rows - 1)), "INVALID_ARG"),
              ("short residual stride", dict(epilogue=E(residual=A, residual_stride=1)), "INVALID_ARG"),
+             ("in place with another stride", dict(epilogue=E(residual=A, residual_stride=desc.rows, out_stride=desc.rows + 8)), "INVALID_ARG"),
              ("gates of another blob", dict(epilogue=E(gated_rows=desc.rows // 2 + 1)), "INVALID_ARG"),
              ("too few gates", dict(epilogue=E(gated_rows=desc.rows // 2 - 8)), "INVALID_ARG"),
              ("gates without end", dict(epilogue=E(gated_rows=(1 << 64) - 1)), "INVALID_ARG"),
@@ -254,7 +255,8 @@ def test_feed_forward_calls_are_refused(hl):
                          (dict(dn=fp16), "UNSUPPORTED"), (dict(act=9), "INVALID_ARG"), (dict(h=None), "INVALID_ARG"), (dict(out=None), "INVALID_ARG"),
                          (dict(h=A + 2), "INVALID_ARG"), (dict(h_type=2), "INVALID_ARG"), (dict(batch=0), "INVALID_ARG"), (dict(batch=65), "INVALID_ARG"),
                          (dict(ws=A + 16), "INVALID_ARG"), (dict(ws=None), "INVALID_ARG"), (dict(ws_bytes=0), "BUFFER_TOO_SMALL"),
-                         (dict(ws_bytes=8192), "BUFFER_TOO_SMALL"), (dict(h_stride=hidden - 1), "INVALID_ARG"), (dict(out_stride=1), "INVALID_ARG")]:
+                         (dict(ws_bytes=8192), "BUFFER_TOO_SMALL"), (dict(h_stride=hidden - 1), "INVALID_ARG"), (dict(out_stride=1), "INVALID_ARG"),
+                         (dict(h_stride=hidden + 8), "INVALID_ARG")]:
         assert status(lambda: call(**change)) == want, change
 
 
