@@ -54,18 +54,16 @@ static __device__ __noinline__ float activate1(float v, uint32_t act) { return a
 template <int N>
 __device__ __forceinline__ void activate(float (&v)[N], uint32_t act) {
     if (act == HUFFLLM_ACT_NONE) return;
-    if (N == 1) {
-        v[0] = activate1(v[0], act);
-        return;
-    }
+    if constexpr (N < 4) {
 #pragma unroll
-    for (int i = 0; i < N; i += 4) {
-        float4 a = make_float4(v[i], v[i + 1 < N ? i + 1 : 0], i + 2 < N ? v[i + 2 < N ? i + 2 : 0] : 0.0f, i + 3 < N ? v[i + 3 < N ? i + 3 : 0] : 0.0f);
-        a = activate4(a, act);
-        v[i] = a.x;
-        if (i + 1 < N) v[i + 1 < N ? i + 1 : 0] = a.y;
-        if (i + 2 < N) v[i + 2 < N ? i + 2 : 0] = a.z;
-        if (i + 3 < N) v[i + 3 < N ? i + 3 : 0] = a.w;
+        for (int i = 0; i < N; ++i) v[i] = activate1(v[i], act);
+    } else {
+        static_assert(N % 4 == 0, "fours");
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const float4 a = activate4(make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]), act);
+            v[i] = a.x, v[i + 1] = a.y, v[i + 2] = a.z, v[i + 3] = a.w;
+        }
     }
 }
 

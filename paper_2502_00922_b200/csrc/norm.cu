@@ -93,15 +93,19 @@ __global__ void __launch_bounds__(kNormMaxThreads) add_rms_norm_kernel(const __g
     // (the same for every vector, so from L1 where it cannot come in one piece)
     auto load_gain = [&](uint32_t it, uint32_t (&r)[8]) {
         if (!A.gain) return;
-        if (FORM == kAligned || (FORM == kPhased && phase == 0 && whole(it))) {
+        if constexpr (FORM == kAligned) {
             load8(A.gain, 0, Is16{}, it, r);
-            return;
-        }
+        } else {
+            if (FORM == kPhased && phase == 0 && whole(it)) {
+                load8(A.gain, 0, Is16{}, it, r);
+                return;
+            }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) r[j] = column(it, j) < cols ? __ldg(A.gain + column(it, j)) : 0u;
-        if (FORM == kPhased) {
+            for (int j = 0; j < 8; ++j) r[j] = column(it, j) < cols ? __ldg(A.gain + column(it, j)) : 0u;
+            if (FORM == kPhased) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) r[j] = r[2 * j] | r[2 * j + 1] << 16;
+                for (int j = 0; j < 4; ++j) r[j] = r[2 * j] | r[2 * j + 1] << 16;
+            }
         }
     };
     auto widen_gain = [&](const uint32_t (&r)[8], float (&o)[8]) {
