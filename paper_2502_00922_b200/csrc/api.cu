@@ -140,7 +140,7 @@ uint32_t planned_warps(uint32_t lut_align, uint32_t lut_size, uint64_t pair_byte
 // What a CTA of a launch decodes side by side: `na` tiles of 128 rows in each of `slices` column slices, at most four tiles in
 // all (eight warps each), and the stages through which they hand it to the tensor core.
 struct TcShape {
-    uint32_t na, slices, stages, row_groups;
+    uint32_t na, slices, stages, row_groups, slots = 2;
     uint32_t decoders() const { return row_groups * slices; }
     bool part_filled() const { return slices == 1 && na == 2 && row_groups < 16; }     // (shape 4: the second tile has rows left over)
     uint32_t part_bytes(uint32_t npad) const { return stages * slices * npad * 128; }  // the stages of activations
@@ -157,7 +157,7 @@ uint32_t tc_room(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const 
         if (o.slot_bytes > need.slot_bytes) need.slot_bytes = o.slot_bytes;
         if (o.guard_bytes > need.guard_bytes) need.guard_bytes = o.guard_bytes;
     }
-    return planned_warps(need.table_align, need.table_bytes, 2ull * need.slot_bytes, dyn_smem, sh.part_bytes(npad), need.guard_bytes);
+    return planned_warps(need.table_align, need.table_bytes, (uint64_t)sh.slots * need.slot_bytes, dyn_smem, sh.part_bytes(npad), need.guard_bytes);
 }
 bool tc_fits(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const TcShape &sh, uint32_t flat, uint32_t dyn_smem) {
     return tc_room(d, n, npad, sh, flat, dyn_smem) >= sh.decoders();
@@ -168,10 +168,10 @@ bool tc_fits(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const TcSh
 // have room, where whole tiles would be eight (large records, as FP16 has: a CTA of eight warps waits for its lookups).
 // False: it does not fit or apply.
 constexpr uint32_t kTcShapes = 5;
-bool tc_shape(const huffllm_desc *const *d, uint32_t n, uint32_t npad, uint32_t which, uint32_t flat, uint32_t dyn_smem, TcShape *sh) {
+bool tc_shape(const huffllm_desc *const *d, uint32_t n, uint32_t npad, uint32_t which, uint32_t flat, uint32_t dyn_smem, TcShape *sh, uint32_t slots = 2) {
     const uint32_t slices = which < 2 || which == 4 ? 1 : which == 2 ? 2 : 4;
     // three stages, two at the widest batch padding, where tensor memory holds no more; the CTA's last warp issues the MMAs
-    *sh = TcShape{4 / slices, slices, npad == 64 ? 2u : 3u, 32 / slices - (which == 1 ? 2 : 1)};
+    *sh = TcShape{4 / slices, slices, npad == 64 ? 2u : 3u, 32 / slices - (which == 1 ? 2 : 1), slots};
     if (which == 0) {
         for (; sh->na; --sh->na) {
             sh->row_groups = sh->na == 4 ? 31 : 8 * sh->na;
@@ -291,9 +291,9 @@ TcPlan tc_plan(const huffllm_desc *d, uint32_t npad, uint32_t sms, const TcShape
 // columns instead of 1024.)  Only where no plan of any shape is within both, the cut shape-0 plan is the measure.
 // False: no shape fits.
 bool tc_best(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const uint32_t *cta, uint32_t flat, uint32_t dyn_smem, size_t max_bytes,
-             TcShape *shape, TcPlan *plans) {
+             TcShape *shape, TcPlan *plans, uint32_t slots = 2) {
     TcShape base;
-    if (!tc_shape(d, n, npad, 0, flat, dyn_smem, &base)) return false;
+    if (!tc_shape(d, n, npad, 0, flat, dyn_smem, &base, slots)) return false;
     for (size_t base_bytes = ~(size_t)0;; base_bytes = max_bytes) {
         uint64_t best_span = ~0ull;
         uint32_t most[kMaxMats], ranges[kMaxMats];
@@ -313,7 +313,7 @@ bool tc_best(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const uint
                 for (uint32_t i = 0; i < n; ++i) pays = pays && d[i]->n_chunks >= 32ull * cta[i];
                 if (!pays) continue;
             }
-            if (which && !tc_shape(d, n, npad, which, flat, dyn_smem, &sh)) continue;
+            if (which && !tc_shape(d, n, npad, which, flat, dyn_smem, &sh, slots)) continue;
             TcPlan p[kMaxMats];
             uint64_t span = 0;
             for (uint32_t i = 0; i < n; ++i) {
@@ -341,17 +341,17 @@ bool tc_best(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const uint
 // vectors in chunks of 2048 took 121.5 us and was 4.9e-6 from 64 bits, with sixteen copies 117.8 and 1.7e-6; in chunks of 1024, where
 // all tiles fit either way, 8192 x 8192 at 24 took 56.0 us with a copy per lane and 58.0 with sixteen.
 bool tc_choose_anew(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const uint32_t *cta, uint32_t *flat, uint32_t dyn_smem, size_t max_bytes,
-                    TcShape *shape, TcPlan *plans) {
+                    TcShape *shape, TcPlan *plans, uint32_t slots) {
     // (room for 32 decoders beside the larger table and the most stages that a shape has: every shape fits beside either table, and
     // so the plans are the same)
     const uint32_t slices = npad == 64 ? 2 : 4;
-    if (*flat == kFlatBoth && tc_fits(d, n, npad, TcShape{4 / slices, slices, npad == 64 ? 2u : 3u, 32 / slices}, kFlatBothLanes, dyn_smem))
+    if (*flat == kFlatBoth && tc_fits(d, n, npad, TcShape{4 / slices, slices, npad == 64 ? 2u : 3u, 32 / slices, slots}, kFlatBothLanes, dyn_smem))
         *flat = kFlatBothLanes;
-    if (*flat != kFlatBoth) return tc_best(d, n, npad, cta, *flat, dyn_smem, max_bytes, shape, plans);
+    if (*flat != kFlatBoth) return tc_best(d, n, npad, cta, *flat, dyn_smem, max_bytes, shape, plans, slots);
     TcShape wide;
     TcPlan wide_plans[kMaxMats];
-    const bool tight = tc_best(d, n, npad, cta, kFlatBoth, dyn_smem, ~(size_t)0, shape, plans);
-    bool lanes = tc_best(d, n, npad, cta, kFlatBothLanes, dyn_smem, ~(size_t)0, &wide, wide_plans);
+    const bool tight = tc_best(d, n, npad, cta, kFlatBoth, dyn_smem, ~(size_t)0, shape, plans, slots);
+    bool lanes = tc_best(d, n, npad, cta, kFlatBothLanes, dyn_smem, ~(size_t)0, &wide, wide_plans, slots);
     for (uint32_t i = 0; lanes && tight && i < n; ++i) lanes = wide_plans[i].chunks <= plans[i].chunks;
     if (!lanes && !tight) return false;
     if (lanes) {
@@ -360,14 +360,14 @@ bool tc_choose_anew(const huffllm_desc *const *d, uint32_t n, uint32_t npad, con
         for (uint32_t i = 0; i < n; ++i) plans[i] = wide_plans[i];
     }
     for (uint32_t i = 0; i < n; ++i)
-        if (plans[i].bytes > max_bytes) return tc_best(d, n, npad, cta, *flat, dyn_smem, max_bytes, shape, plans);
+        if (plans[i].bytes > max_bytes) return tc_best(d, n, npad, cta, *flat, dyn_smem, max_bytes, shape, plans, slots);
     return true;
 }
 
 // The same, remembered: a plan is worked out from a few dozen numbers in 3 to 5 us, as long as a small product takes on the GPU, and a program asks for
 // the same few plans at every step.  A thread keeps the last ones by those numbers (all that the functions above read).
 struct TcQuestion {
-    uint32_t n, npad, flat, dyn_smem;
+    uint32_t n, npad, flat, dyn_smem, single_ok, reserved;
     uint64_t max_bytes;
     struct {
         uint32_t cta, dtype, lut_bits, flat_fields, max_words, chunk_cols, row_groups, col_chunks;
@@ -382,7 +382,7 @@ struct TcAnswer {
     TcPlan plans[kMaxMats];
 };
 bool tc_choose(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const uint32_t *cta, uint32_t *flat, uint32_t dyn_smem, size_t max_bytes,
-               TcShape *shape, TcPlan *plans) {
+               TcShape *shape, TcPlan *plans, bool single_ok = false) {
     constexpr uint32_t kKept = 16;
     static thread_local TcAnswer kept[kKept];
     TcQuestion q;
@@ -392,6 +392,7 @@ bool tc_choose(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const ui
     q.flat = *flat;
     q.dyn_smem = dyn_smem;
     q.max_bytes = max_bytes;
+    q.single_ok = single_ok;
     uint64_t hash = 0;
     for (uint32_t i = 0; i < n; ++i) {
         q.m[i] = {cta[i], d[i]->dtype, d[i]->lut_bits, d[i]->flat_fields, d[i]->max_words, d[i]->chunk_cols, d[i]->row_groups, d[i]->col_chunks, d[i]->n_chunks};
@@ -401,7 +402,29 @@ bool tc_choose(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const ui
     if (!a.known || memcmp(&a.of, &q, sizeof(q)) != 0) {
         a.known = false;
         a.flat = *flat;
-        a.fits = tc_choose_anew(d, n, npad, cta, &a.flat, dyn_smem, max_bytes, &a.shape, a.plans);
+        a.fits = tc_choose_anew(d, n, npad, cta, &a.flat, dyn_smem, max_bytes, &a.shape, a.plans, 2);
+        // Single slots (kernels with epilogues) where two leave fewer than 28 warps to decode and the estimate says that the launch gets a seventh shorter.
+        // A warp then waits for its next record at every chunk's start, which the stage ring mostly hides.  (Two slots / one, us, and the ratio of the
+        // estimates: FP16 11008 x 4096 at 32 vectors, chunks of 2048 38.9 / 36.8, 1.19, of 4096 65.7 / 38.9, 2.4; 20000 x 1024 at 64, chunks of 2048 40.4 / 28.4, 1.7;
+        // BF16 11008 x 4096 at 32, chunks of 8192 34.1 / 31.6, 1.4, of 16384 69.4 / 40.5, 1.5; 2048 x 4096 at 12, chunks of 8192 12.5 / 14.5, 1.09, of 16384 15.2 /
+        // 18.2, 1.0; bf16-trained FP16 20000 x 1024 at 64, chunks of 2048 33.2 / 39.8, 0.83.)
+        if (single_ok && a.fits && a.shape.decoders() < 28) {
+            uint32_t single_flat = *flat;
+            TcShape single;
+            TcPlan single_plans[kMaxMats];
+            if (tc_choose_anew(d, n, npad, cta, &single_flat, dyn_smem, max_bytes, &single, single_plans, 1)) {
+                uint64_t two_span = 0, one_span = 0;
+                for (uint32_t i = 0; i < n; ++i) {
+                    if (a.plans[i].span > two_span) two_span = a.plans[i].span;
+                    if (single_plans[i].span > one_span) one_span = single_plans[i].span;
+                }
+                if (6 * two_span >= 7 * one_span) {
+                    a.flat = single_flat;
+                    a.shape = single;
+                    for (uint32_t i = 0; i < n; ++i) a.plans[i] = single_plans[i];
+                }
+            }
+        }
         a.of = q;
         a.known = true;
     }
@@ -459,8 +482,8 @@ void set_tc_shape(KernelArgs *k, uint32_t npad, const TcShape &sh, uint32_t flat
     k->fp16_flat = flat;
     if (k->fmt && k->lut_bits <= 8) k->lut_size = fp16_table_bytes(flat);
     k->part_bytes = sh.part_bytes(npad);
-    k->slots = 2;
-    k->pair_recip = (uint32_t)(0x100000000ull / (2ull * k->slot_bytes));
+    k->slots = sh.slots;
+    k->pair_recip = (uint32_t)(0x100000000ull / ((uint64_t)sh.slots * k->slot_bytes));
     k->tc_npad = npad;
     k->tc_tiles = sh.na;
     k->tc_slices = sh.slices;
@@ -823,7 +846,7 @@ static huffllm_status product_multi(uint32_t n, const huffllm_desc *const *descs
         for (uint32_t i = 0; i < n; ++i) cta[i] = k.m[i].cta_count;
         TcShape sh;
         TcPlan plans[kMaxMats];
-        if (!tc_choose(descs, n, npad, cta, &flat, k.dyn_smem_bytes, workspace_bytes_each, &sh, plans))
+        if (!tc_choose(descs, n, npad, cta, &flat, k.dyn_smem_bytes, workspace_bytes_each, &sh, plans, eps != nullptr))
             return eps ? HUFFLLM_OK : fail(HUFFLLM_ERR_UNSUPPORTED, "chunk records too large for the tensor-core kernel's slots");
         set_tc_shape(&k, npad, sh, flat);
         uint32_t first = 0;
@@ -944,7 +967,7 @@ static huffllm_status product_one(const huffllm_desc *desc, const void *blob, co
         TcShape sh;
         TcPlan tp;
         uint32_t flat = flat_of(desc);
-        if (!tc_choose(&desc, 1, npad, &cta, &flat, (uint32_t)dev.smem_optin - kStaticSmem, workspace_bytes, &sh, &tp))
+        if (!tc_choose(&desc, 1, npad, &cta, &flat, (uint32_t)dev.smem_optin - kStaticSmem, workspace_bytes, &sh, &tp, ep != nullptr))
             return HUFFLLM_OK;      // records too large for this kernel's slots
         TcArgs t;
         memset(&t, 0, sizeof(t));

@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
         o1 = __ldg(index + cb + 1);
         if (cb + 1 < ce) o2 = __ldg(index + cb + 2);
     }
-    const SmemPlan plan = plan_smem(smem_base, A, n_dec);
+    const SmemPlan plan = plan_smem(smem_base, A, n_dec, EPI != 0 ? A.slots : 2u);
     if (plan.warps < n_dec) {                                   // the entry point sizes shared memory so that this cannot happen
         pdl_wait_prior_grid();
         if (tid == 0 && A.err) atomicExch(A.err, -3);
@@ -245,7 +245,11 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
     if (NPAD < 64) asm volatile("mov.u32 %0, %0;" : "+r"(ring));
     auto empty_bar = [&](uint32_t st) -> uint32_t { return ring + st * 8u; };
     auto full_bar = [&](uint32_t st) -> uint32_t { return ring + kTcStages * 8u + st * 8u; };
-    const uint32_t slot0 = slot_addr(plan, decodes ? slice * n_rg + rgi : 0u, 0, A.slot_bytes);    // (this kernel always runs with two slots per warp)
+    // (without epilogues always two slots per warp)
+    const bool single = EPI != 0 && A.slots == 1u;
+    const uint32_t slot0 = single ? slot_addr_single(plan, decodes ? slice * n_rg + rgi : 0u, A.slot_bytes)
+                                  : slot_addr(plan, decodes ? slice * n_rg + rgi : 0u, 0, A.slot_bytes);
+    auto slot_of = [&](uint32_t which) -> uint32_t { return slot0 + (single ? 0u : which * A.slot_bytes); };
     auto record_ok = [&](uint32_t r0, uint32_t r1, uint32_t nkb) -> bool {
         return r1 > r0 && r1 <= k.payload_units && (r1 - r0) * 128u > raw_part(nkb) &&
                (r1 - r0) * 128u - raw_part(nkb) <= A.slot_bytes;
@@ -255,7 +259,7 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
         if (record_ok(r0, r1, nkb)) {
             uint32_t bytes = (r1 - r0) * 128u - raw_part(nkb);
             mbar_expect_tx(bar, bytes);
-            bulk_g2s(slot0 + which * A.slot_bytes, payload + (uint64_t)r0 * 128u + raw_part(nkb), bytes, bar);
+            bulk_g2s(slot_of(which), payload + (uint64_t)r0 * 128u + raw_part(nkb), bytes, bar);
         } else {
             mbar_expect_tx(bar, 0);
         }
@@ -295,7 +299,7 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             const uint32_t kc_b = cb % KC;
             issue_record(kc_b, 0, o0, o1);
-            if (cb + 1 < ce) issue_record(kc_b + 1, 1, o1, o2);
+            if (cb + 1 < ce && !single) issue_record(kc_b + 1, 1, o1, o2);
         }
         if constexpr (EPI != 0) {
             if (tid < sizeof(EpiMat) / 4) s_epi[tid] = ((const uint32_t *)&T.e[MULTI ? mi : 0])[tid];
@@ -684,7 +688,7 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
             const uint32_t c_beg = rg * KC + kc0, c_end = rg * KC + kc1;
             if (lane == 0 && !primed) {
                 issue(c_beg, 0);
-                if (c_beg + 1 < c_end) issue(c_beg + 1, 1);
+                if (c_beg + 1 < c_end && !single) issue(c_beg + 1, 1);
             }
             uint32_t kc = kc0;
             // record offsets are known two chunks ahead, the first raw block of a record is asked for in the last block of the
@@ -715,7 +719,7 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
                     for (uint32_t kb = 0; kb < nkb; ++kb) stage_block(zero, kb & 1u, (kb & 1u) || kb + 1 < nkb ? 2u : 1u);
                     raw_there = false;
                 } else {
-                    uint32_t pa = (slot0 + which * A.slot_bytes) / 8u + start_of(D), pb = pa;
+                    uint32_t pa = slot_of(which) / 8u + start_of(D), pb = pa;
                     // one block: fetch the next block's raw bytes into the other register set (behind the record's last one: the
                     // next record's first, an address inside the blob whatever its offsets turn out to be), decode this one, hand
                     // it to the tensor core
@@ -749,7 +753,8 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
                 if (slices > 1u)
                     for (uint32_t p = (nkb + 1u) >> 1; p < full_stages; ++p) stage_nothing();
                 __syncwarp();
-                if (lane == 0 && c + 2 < c_end) issue_record(kc + 2, which, r2, r3);
+                if (lane == 0 && !single && c + 2 < c_end) issue_record(kc + 2, which, r2, r3);
+                if (EPI != 0 && lane == 0 && single && c + 1 < c_end) issue_record(kc + 1, which ^ 1u, r1, r2);   // (the barriers still take turns)
                 r0 = r1;
                 r1 = r2;
                 r2 = r3;
@@ -777,7 +782,7 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
             if (item_chunks(behind, nb, ne)) {
                 if (lane == 0) {
                     issue(nb, 0);
-                    if (nb + 1 < ne) issue(nb + 1, 1);
+                    if (nb + 1 < ne && !single) issue(nb + 1, 1);
                 }
                 primed = true;
             }

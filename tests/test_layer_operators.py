@@ -315,6 +315,8 @@ PRODUCTS = [
     (130, 1056, "fp16", 1024, 0),
     (515, 512, "fp16", 1024, 7),          # tables of 128 entries
     (64, 8192, "bf16", 16384, 0),         # single slots
+    (2000, 1024, "bf16", 16384, 0),       # single slots on the tensor-core path too
+    (1500, 1056, "fp16", 4096, 0),
 ]
 
 
