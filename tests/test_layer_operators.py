@@ -855,3 +855,63 @@ def test_offsets_past_32_bits(hl, torch):
     torch.cuda.synchronize()
     got = np.stack([values(big[b * near:b * near + rows]) for b in range(9)])
     check(got, *Sums(bits_to_f64(w, "bf16"), bits_to_f64(x, "bf16")).through("relu"), "bf16")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols", [65, 1000, 9001])
+@pytest.mark.parametrize("strides", [(0, 0, 0, 0), (8, 16, 24, 40), (3, 11, 19, 35), (1, 2, 3, 4), (4, 8, 4, 8)])
+@pytest.mark.parametrize("vectors", [5, 700])
+def test_norms_whose_buffers_have_strides_of_their_own(hl, torch, cols, strides, vectors):
+    """x, delta, sum and out each with their own distance between vectors: alike modulo eight values, multiples of 16 bytes, neither."""
+    g = torch.Generator(device="cuda").manual_seed(cols + vectors)
+    lds = [cols + k for k in strides]
+    x = torch.randn(vectors * lds[0], generator=g, device="cuda")
+    d = torch.randn(vectors * lds[1], generator=g, device="cuda").to(torch.float16)
+    s = torch.full((vectors * lds[2],), 55.0, device="cuda")
+    o = torch.full((vectors * lds[3],), 55.0, dtype=torch.float16, device="cuda")
+    gain = (1 + 0.2 * torch.randn(cols, generator=g, device="cuda")).to(torch.float16)
+    hl.add_rms_norm(hl.Norm(hl.FP16, vectors, cols, x, hl.ELEM_F32, gain, 1e-5, o, d, hl.ELEM_16, s, *lds))
+    torch.cuda.synchronize()
+    of = lambda t, ld: values(t.view(vectors, ld)[:, :cols])
+    h = of(x, lds[0]) + of(d, lds[1])
+    add = F32 * (np.abs(of(x, lds[0])) + np.abs(of(d, lds[1])))
+    want = norm64(h, values(gain), 1e-5)
+    rms = np.sqrt(np.mean(h * h, axis=1, keepdims=True) + 1e-5)
+    check(of(s, lds[2]), h, add, "f32")
+    check(of(o, lds[3]), want, add / rms * np.abs(values(gain)) + np.abs(want) * ((cols + 8) * F32 / 2 + 2 * F32 + 2.0 ** -22), "fp16")
+    assert torch.all(s.view(vectors, lds[2])[:, cols:] == 55.0) and torch.all(o.view(vectors, lds[3])[:, cols:] == 55.0)
+
+
+@pytest.mark.gpu
+def test_one_workspace_for_every_batch_and_kind_of_call(hl, torch):
+    """A feed-forward workspace larger than asked for, at changing batches; a product's workspace under plain calls and calls with epilogues in
+    turn, on the register path and on the tensor cores: what a call leaves behind does not reach the next one."""
+    c = FfnCase(hl, torch, 512, 640, "bf16", seed=5)
+    size = hl.ffn_workspace_bytes(c.ffn, 64) + 1000
+    ws = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    hs = {b: torch.randn((b, 512), device="cuda") for b in (1, 6, 12, 64)}
+    def sub_layer(b, w):
+        out = torch.empty_like(hs[b])
+        hl.decode_ffn(c.ffn, hs[b], b, out, hl.ELEM_F32, w, w.numel(), err)
+        return out
+    want = {b: sub_layer(b, torch.zeros(size, dtype=torch.uint8, device="cuda")) for b in hs}
+    for b in (64, 1, 12, 6, 64, 12, 1):
+        assert torch.equal(sub_layer(b, ws), want[b]), b
+
+    rows, cols = 40000, 1024                                    # more work items than CTAs in chunks of 512
+    blob = Blob(hl, torch, wl.gaussian_weights(rows, cols, 0.05, 6), "bf16", 512)
+    n, (ws,) = workspace(hl, torch, [blob], 64)
+    xs = {b: up(torch, x_of(b, cols, b, "bf16"), "bf16") for b in (1, 12, 40)}
+    def product(b, kind, w):
+        out = torch.empty((b, rows), device="cuda")
+        if kind:
+            hl.decode_gemm_epilogue(blob.desc, blob.dev, xs[b], b, hl.Epilogue(hl.ACT_RELU), out, w, n, err)
+        else:
+            hl.decode_gemm(blob.desc, blob.dev, xs[b], b, out, w, n, err)
+        return out
+    want = {(b, k): product(b, k, torch.zeros_like(ws)) for b in xs for k in (0, 1)}
+    for b, k in ((40, 1), (40, 0), (1, 1), (40, 1), (12, 1), (12, 0), (1, 0), (40, 1), (12, 1)):
+        assert torch.equal(product(b, k, ws), want[b, k]), (b, k)
+    torch.cuda.synchronize()
+    assert_clean(hl, blob, ws, err)
