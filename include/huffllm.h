@@ -449,7 +449,8 @@ huffllm_status huffllm_stack_gate_up_device(const uint16_t *gate_dev, const uint
  * added up in fp32 in a fixed order (they overflow for |h| above 1e19).  x, sum: x_type; delta: delta_type; gain, out: 16-bit words
  * of `dtype`, what the products take as x.  delta, sum and gain may be null (no addition, not wanted, ones).  sum may be x or delta
  * itself (same pointer, stride and type); out must not overlap the inputs.  Any alignment of the types is taken; 16-byte
- * aligned pointers, cols % 8 == 0 and strides of whole 16 bytes are faster.  Strides count values; 0 = packed.
+ * aligned pointers are faster, with cols % 8 == 0 and strides of whole 16 bytes, or with strides that are alike modulo 8 (packed vectors
+ * of any length).  Strides count values; 0 = packed.  Nothing is read before the kernel in front on the stream has finished.
  */
 typedef struct huffllm_norm {
     uint32_t dtype;                  /* huffllm_dtype of all 16-bit values */
