@@ -160,8 +160,7 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
     __shared__ __align__(8) uint64_t ring_bars[2 * kTcStages];   // stage may be refilled (arrived on by tcgen05.commit); every decoder warp's share is in place
     __shared__ uint32_t s_tmem_base, s_last;
     __shared__ __align__(16) uint32_t s_epi[EPI ? sizeof(EpiMat) / 4 : 1];     // the matrix's epilogue
-    __shared__ __align__(8) uint64_t s_next_bar;               // (EPI) the item behind the one at hand has been fetched, to
-    __shared__ uint32_t s_next[2];                             // these two places by turns
+    __shared__ uint32_t s_next[2];                             // (EPI) the item behind the one at hand, in these two places by turns
 
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     pdl_launch_dependents();   // the next kernel in the stream may be scheduled early; it waits for this one before it reads results
@@ -283,12 +282,6 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
         if (tid < S) {
             mbar_init(empty_bar(tid), 1);
             mbar_init(full_bar(tid), tiles == 4u ? 31u : tiles * 8u + 1u);      // (every warp but the issuer, decoding or not)
-        }
-        if constexpr (EPI != 0) {
-            if (tid == 0) {
-                mbar_init(smem_u32(&s_next_bar), 1);
-                s_next[0] = s_next[1] = ~0u;
-            }
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         if (warp == issuer) {
@@ -653,10 +646,8 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
                     if (sl < slices) least = min(least, nkb[sl]);
                 }
                 if constexpr (EPI != 0) {
-                    if (fetches && j + 1 == steps && lane == 0) {
+                    if (fetches && j + 1 == steps && lane == 0)
                         *(volatile uint32_t *)&s_next[turn & 1u] = n_cta + atomicAdd(T.fetched[MULTI ? mi : 0], 1u);
-                        mbar_arrive(smem_u32(&s_next_bar));
-                    }
                     __syncwarp();
                 }
                 for (uint32_t p = 0; p < n_st; ++p) {
@@ -771,7 +762,12 @@ __global__ void __launch_bounds__(1024, 1) huff_gemm_tc_kernel(const __grid_cons
         if constexpr (EPI != 0) {
             next = n_items;
             if (fetches) {
-                bounded_wait(smem_u32(&s_next_bar), turn & 1u);
+                // All warps that are left meet here and go on with the same item, behind a wait that ran out too (sums across slices and the teardown have
+                // barriers of the whole CTA).  A place is written again two meetings after it was read.  (An mbarrier on which the issuer arrived could be
+                // two phases ahead of a warp still waiting for the first: in an item of one step it arrives before it has waited for anybody.  The tiles'
+                // warps wait for the last stage's MMAs next, and with them for each other.)
+                __syncwarp();
+                asm volatile("bar.sync 1, %0;" ::"r"(tiles == 4u ? 1024u : tiles * 256u + 64u) : "memory");   // (the tiles' warps, x's and the issuer)
                 next = *(volatile uint32_t *)&s_next[turn & 1u];
                 ++turn;
             }
