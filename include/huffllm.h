@@ -422,6 +422,16 @@ huffllm_status huffllm_decode_gemm_epilogue(const huffllm_desc *desc, const void
                                             const huffllm_epilogue *epilogue, void *out_dev, void *workspace_dev,
                                             size_t workspace_bytes, int32_t *err_flag_dev, huffllm_stream stream);
 
+/*
+ * huffllm_gemm_launch_plan for a product with epilogues (of one matrix, or of several in one launch), which the tensor-core kernel takes for blobs of every
+ * max_code_len.  slots_per_warp: shared-memory slots of a decoder warp, 2 or 1 (see huffllm_decode_launch_plan), or 0, and nothing else is written, where the
+ * register path takes the call first (9..16 vectors over several matrices).  HUFFLLM_ERR_UNSUPPORTED where the kernel has no room for the blobs' records: the
+ * call then takes the register path.
+ */
+huffllm_status huffllm_gemm_epilogue_launch_plan(uint32_t n, const huffllm_desc *const *descs, uint32_t batch, size_t workspace_bytes_each,
+                                                 uint32_t *slots_per_warp, uint32_t *column_slices, uint32_t *row_groups, uint32_t *ranges,
+                                                 uint32_t *work_items, uint32_t *chunks_per_sum);
+
 /* huffllm_decode_gemm_multi with an epilogue per matrix (q, k and v with their biases, say): epilogues is a host array of n.  Every batch
  * takes blobs of every max_code_len (more than 8 vectors of blobs whose records are too large for the tensor-core kernel take launches of their own). */
 huffllm_status huffllm_decode_gemm_multi_epilogue(uint32_t n, const huffllm_desc *const *descs, const void *const *blobs_dev,

@@ -104,6 +104,8 @@ _SIGNATURES = {
     "huffllm_decode_gemm_static": [C.POINTER(Desc), C.c_void_p, C.c_void_p, C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p],
     "huffllm_decode_gemm_epilogue": [C.POINTER(Desc), C.c_void_p, C.c_void_p, C.c_uint32, C.POINTER(Epilogue), C.c_void_p, C.c_void_p,
                                      C.c_size_t, C.c_void_p, C.c_void_p],
+    "huffllm_gemm_epilogue_launch_plan": [C.c_uint32, C.c_void_p, C.c_uint32, C.c_size_t, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                          C.c_void_p],
     "huffllm_decode_gemm_multi_epilogue": [C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p,
                                            C.c_size_t, C.c_void_p, C.c_void_p],
     "huffllm_stacked_rows": [C.c_uint64, C.POINTER(C.c_uint64)],
@@ -472,6 +474,19 @@ def decode_gemm_epilogue(desc: Desc, blob_dev, x_dev, batch: int, epilogue: Epil
     """huffllm_decode_gemm_epilogue: a product with bias, activation, residual and rounding, or a gated product."""
     _check(lib().huffllm_decode_gemm_epilogue(C.byref(desc), _ptr(blob_dev), _ptr(x_dev), batch, C.byref(epilogue), _ptr(out_dev),
                                               _ptr(workspace_dev), workspace_bytes_, _ptr(err_flag_dev), _stream(stream)))
+
+
+def gemm_epilogue_launch_plan(descs, batch: int, workspace_bytes_each: int = 0) -> dict:
+    """huffllm_gemm_epilogue_launch_plan: the plan of a product with epilogues on the tensor cores; {"slots_per_warp": 0} where the register path takes it."""
+    n = len(descs)
+    desc_arr = (C.POINTER(Desc) * n)(*[C.pointer(d) for d in descs])
+    slots, sl, rg = C.c_uint32(), C.c_uint32(), C.c_uint32()
+    ranges, items, chunks = (C.c_uint32 * n)(), (C.c_uint32 * n)(), (C.c_uint32 * n)()
+    _check(lib().huffllm_gemm_epilogue_launch_plan(n, desc_arr, batch, workspace_bytes_each, C.byref(slots), C.byref(sl), C.byref(rg), ranges, items, chunks))
+    if slots.value == 0:
+        return {"slots_per_warp": 0}
+    return {"slots_per_warp": slots.value, "column_slices": sl.value, "row_groups": rg.value, "ranges": list(ranges), "work_items": list(items),
+            "chunks_per_sum": list(chunks)}
 
 
 class PreparedEpilogue:

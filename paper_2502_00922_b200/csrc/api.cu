@@ -623,6 +623,21 @@ huffllm_status make_epilogue(const huffllm_epilogue &ep, const huffllm_desc *des
     return HUFFLLM_OK;
 }
 
+bool two_tile_blobs(uint32_t n, const huffllm_desc *const *descs) {
+    for (uint32_t i = 0; i < n; ++i)
+        if (!two_tile_blob(descs[i])) return false;
+    return true;
+}
+// Several matrices with epilogues: 9..16 vectors go to the tensor cores too, but for long records of blobs that the register path takes.
+// (4096 + 1024 + 1024 rows x 4096 at 9 and at 16 vectors, register path / tensor cores, us: chunks of 1024 28.4 / 22.3, 28.1 / 22.4, of 4096
+// 23.7 / 18.4, 24.9 / 18.6, of 8192 19.5 / 22.1, 20.9 / 22.3; 2 x 14336 rows 56.4 / 57.9, 60.6 / 58.2.)
+bool register_path_first(uint32_t n, const huffllm_desc *const *descs, uint32_t batch) {
+    if (batch > kTwoTileBatch || !two_tile_blobs(n, descs)) return false;
+    for (uint32_t i = 0; i < n; ++i)
+        if (descs[i]->chunk_cols > 256) return true;
+    return false;
+}
+
 // Launch a described product: with the epilogues of its matrices, or (epi null) with fp32 sums to y.
 cudaError_t launch_product(const KernelArgs &k, const EpiMat *epi, uint32_t grid, cudaStream_t stream) {
     if (!epi) return launch_gemm(k, grid, stream);
@@ -717,9 +732,10 @@ huffllm_status huffllm_decode_launch_plan(const huffllm_desc *desc, uint32_t bat
     return HUFFLLM_OK;
 }
 
-huffllm_status huffllm_gemm_launch_plan(uint32_t n, const huffllm_desc *const *descs, uint32_t batch, size_t workspace_bytes_each,
-                                        uint32_t *column_slices, uint32_t *row_groups, uint32_t *ranges, uint32_t *work_items,
-                                        uint32_t *chunks_per_sum) {
+// The plan of the tensor-core kernel for a launch over n matrices, with epilogues (`slots` then gets the slots per warp, 0: the register path takes the
+// call first) or without.
+static huffllm_status launch_plan(uint32_t n, const huffllm_desc *const *descs, uint32_t batch, size_t workspace_bytes_each, bool epilogues, uint32_t *slots,
+                                  uint32_t *column_slices, uint32_t *row_groups, uint32_t *ranges, uint32_t *work_items, uint32_t *chunks_per_sum) {
     clear_error();
     if (!descs) return fail(HUFFLLM_ERR_INVALID_ARG, "null pointer");
     if (n == 0 || n > kMaxMats) return fail(HUFFLLM_ERR_INVALID_ARG, "between 1 and %u matrices per call", kMaxMats);
@@ -736,15 +752,20 @@ huffllm_status huffllm_gemm_launch_plan(uint32_t n, const huffllm_desc *const *d
     huffllm_status st;
     for (uint32_t i = 0; i < n; ++i) {
         if ((st = add_matrix(&k, descs[i], (const void *)256)) != HUFFLLM_OK) return st;     // (the pointer is only checked for alignment)
-        if (!tc_blob(descs[i])) return fail(HUFFLLM_ERR_UNSUPPORTED, "the tensor-core path takes tables of up to 9 bits (FP16: 8)");
+        if (!epilogues && !tc_blob(descs[i])) return fail(HUFFLLM_ERR_UNSUPPORTED, "the tensor-core path takes tables of up to 9 bits (FP16: 8)");
     }
     uint32_t flat = k.fp16_flat;
     if (n > 1 && (st = finish_args(&k, true, dev, &grid)) != HUFFLLM_OK) return st;
     for (uint32_t i = 0; i < n; ++i) cta[i] = n > 1 ? k.m[i].cta_count : (uint32_t)dev.sms;
+    if (epilogues && n > 1 && register_path_first(n, descs, batch)) {
+        if (slots) *slots = 0;
+        return HUFFLLM_OK;
+    }
     TcShape sh;
     TcPlan plans[kMaxMats];
-    if (!tc_choose(descs, n, tc_npad_of(batch), cta, &flat, k.dyn_smem_bytes, workspace_bytes_each ? workspace_bytes_each : ~(size_t)0, &sh, plans))
+    if (!tc_choose(descs, n, tc_npad_of(batch), cta, &flat, k.dyn_smem_bytes, workspace_bytes_each ? workspace_bytes_each : ~(size_t)0, &sh, plans, epilogues))
         return fail(HUFFLLM_ERR_UNSUPPORTED, "chunk records too large for the tensor-core kernel's slots");
+    if (slots) *slots = sh.slots;
     if (column_slices) *column_slices = sh.slices;
     if (row_groups) *row_groups = sh.row_groups;
     for (uint32_t i = 0; i < n; ++i) {
@@ -753,6 +774,18 @@ huffllm_status huffllm_gemm_launch_plan(uint32_t n, const huffllm_desc *const *d
         if (chunks_per_sum) chunks_per_sum[i] = plans[i].chunks;
     }
     return HUFFLLM_OK;
+}
+
+huffllm_status huffllm_gemm_launch_plan(uint32_t n, const huffllm_desc *const *descs, uint32_t batch, size_t workspace_bytes_each,
+                                        uint32_t *column_slices, uint32_t *row_groups, uint32_t *ranges, uint32_t *work_items,
+                                        uint32_t *chunks_per_sum) {
+    return launch_plan(n, descs, batch, workspace_bytes_each, false, nullptr, column_slices, row_groups, ranges, work_items, chunks_per_sum);
+}
+
+huffllm_status huffllm_gemm_epilogue_launch_plan(uint32_t n, const huffllm_desc *const *descs, uint32_t batch, size_t workspace_bytes_each,
+                                                 uint32_t *slots_per_warp, uint32_t *column_slices, uint32_t *row_groups, uint32_t *ranges,
+                                                 uint32_t *work_items, uint32_t *chunks_per_sum) {
+    return launch_plan(n, descs, batch, workspace_bytes_each, true, slots_per_warp, column_slices, row_groups, ranges, work_items, chunks_per_sum);
 }
 
 huffllm_status huffllm_decode(const huffllm_desc *desc, const void *blob, uint16_t *out, int32_t *err_flag, huffllm_stream stream) {
@@ -808,19 +841,10 @@ static huffllm_status product_multi(uint32_t n, const huffllm_desc *const *descs
     }
     DeviceInfo dev;
     if ((st = device_info(&dev)) != HUFFLLM_OK) return st;
-    // 9..16 vectors with epilogues: tensor cores too, but for long records of blobs that the register path takes.  (4096 + 1024 + 1024 rows x 4096 at 9 and
-    // at 16 vectors, register path / tensor cores, us: chunks of 1024 28.4 / 22.3, 28.1 / 22.4, of 4096 23.7 / 18.4, 24.9 / 18.6, of 8192 19.5 / 22.1,
-    // 20.9 / 22.3; 2 x 14336 rows 56.4 / 57.9, 60.6 / 58.2.)
     bool tensor_cores = batch > kTwoTileBatch, two_tiles = false;     // (two_tiles: the register path can take over)
     if (eps && batch > kKernelBatch && !tensor_cores) {
-        bool shorter = true;
-        two_tiles = true;
-        tensor_cores = true;
-        for (uint32_t i = 0; i < n; ++i) {
-            two_tiles = two_tiles && two_tile_blob(descs[i]);
-            shorter = shorter && descs[i]->chunk_cols <= 256;
-        }
-        tensor_cores = tensor_cores && (shorter || !two_tiles);
+        two_tiles = two_tile_blobs(n, descs);
+        tensor_cores = !register_path_first(n, descs, batch);
     }
     bool done = false;
     auto on_tensor_cores = [&]() -> huffllm_status {
