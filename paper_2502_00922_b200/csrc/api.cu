@@ -247,19 +247,18 @@ uint64_t tc_span(const huffllm_desc *d, const TcShape &sh, TcCost price, uint32_
 }
 // `sms`: the CTAs this matrix can have (all SMs, or its share of a launch over several matrices); `max_bytes`: the workspace
 // at hand (column ranges whose pieces would not fit are not considered: a share of the SMs can favour more ranges than the
-// whole GPU, for which workspaces are sized); `max_chunks`: the most column chunks that one accumulator may add up; `min_ranges`: the
+// whole GPU, for which workspaces are sized); `base`: shape 0; `max_chunks`: the most column chunks that one accumulator may add up; `min_ranges`: the
 // fewest ranges.
-TcPlan tc_plan(const huffllm_desc *d, uint32_t npad, uint32_t sms, const TcShape &sh, size_t max_bytes, uint32_t max_chunks,
+TcPlan tc_plan(const huffllm_desc *d, uint32_t npad, uint32_t sms, const TcShape &sh, size_t max_bytes, bool base = true, uint32_t max_chunks = ~0u,
                uint32_t min_ranges = 1) {
     TcPlan p;
     p.m_tiles = (d->row_groups + sh.row_groups - 1) / sh.row_groups;
     const size_t item_bytes = (size_t)32 * sh.piece_columns(npad) * 32 * sizeof(float);
-    // Column ranges: in shape 0 (no limit on the chunks) the count whose items are done first, their sums not considered (fewer,
+    // Column ranges: in shape 0 the count whose items are done first, their sums not considered (fewer,
     // longer ranges would be a little faster, but an accumulator's error grows with the columns it adds up: 1e-6 for 1024,
     // 3.8e-6 for 3584); in the others all costs count, and no accumulator may add up more columns than in shape 0.  For row groups that
     // fill no tile ranges are counted as if blocks and items were cheaper than they are, which makes for more of them and shorter
     // sums (20000 x 1024 FP16 at 32 in two ranges 30.3 us and 6.4e-7 from 64 bits, in four 32.5 and 3.4e-7); whether it pays is up to what they cost.
-    const bool base = max_chunks == ~0u;
     const TcCost price = tc_cost(sh, npad, d->dtype == HUFFLLM_FP16);
     const TcCost ranges_price = sh.part_filled() ? TcCost{kTcUnit * (14 + sh.row_groups) / (14 + 8), 5 * kTcUnit} : price;
     uint32_t best = 0;
@@ -289,14 +288,18 @@ TcPlan tc_plan(const huffllm_desc *d, uint32_t npad, uint32_t sms, const TcShape
 // workspace: what a caller hands over as workspace decides about time, not about rounding.  (With the limit taken from a shape-0
 // plan that the workspace had already cut, 28672 x 4096 at 64 vectors in a workspace of exactly the size asked for added up 2048
 // columns instead of 1024.)  Only where no plan of any shape is within both, the cut shape-0 plan is the measure.
+// `limits`: sums as short as these, whatever this launch's shape 0 would do (plans of single slots).
 // False: no shape fits.
+struct TcLimits {
+    uint32_t chunks[kMaxMats], ranges[kMaxMats];      // of every matrix: the most column chunks of a sum, the fewest ranges of shape 4
+};
 bool tc_best(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const uint32_t *cta, uint32_t flat, uint32_t dyn_smem, size_t max_bytes,
-             TcShape *shape, TcPlan *plans, uint32_t slots = 2) {
+             TcShape *shape, TcPlan *plans, uint32_t slots = 2, const TcLimits *limits = nullptr) {
     TcShape base;
     if (!tc_shape(d, n, npad, 0, flat, dyn_smem, &base, slots)) return false;
-    for (size_t base_bytes = ~(size_t)0;; base_bytes = max_bytes) {
+    for (size_t base_bytes = limits ? max_bytes : ~(size_t)0;; base_bytes = max_bytes) {
         uint64_t best_span = ~0ull;
-        uint32_t most[kMaxMats], ranges[kMaxMats];
+        TcLimits own;
         for (uint32_t which = 0; which < kTcShapes; ++which) {
             TcShape sh = base;
             // Row groups that fill no tile can pay where a CTA of whole tiles has eight and every CTA has 32 chunks or more to decode; the
@@ -317,12 +320,14 @@ bool tc_best(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const uint
             TcPlan p[kMaxMats];
             uint64_t span = 0;
             for (uint32_t i = 0; i < n; ++i) {
-                p[i] = tc_plan(d[i], npad, cta[i], sh, which ? max_bytes : base_bytes, which ? most[i] : ~0u, which == 4 ? ranges[i] : 1u);
+                const TcLimits &in = limits ? *limits : own;
+                p[i] = tc_plan(d[i], npad, cta[i], sh, which ? max_bytes : base_bytes, which == 0, which || limits ? in.chunks[i] : ~0u,
+                               which == 4 ? in.ranges[i] : 1u);
                 const uint64_t t = p[i].bytes > max_bytes ? ~0ull : p[i].span;
                 if (t > span) span = t;
                 if (which == 0) {
-                    most[i] = p[i].chunks;
-                    ranges[i] = p[i].ksplit ? p[i].ksplit : 1u;
+                    own.chunks[i] = p[i].chunks;
+                    own.ranges[i] = p[i].ksplit ? p[i].ksplit : 1u;
                 }
             }
             if (span < best_span) {
@@ -341,17 +346,17 @@ bool tc_best(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const uint
 // vectors in chunks of 2048 took 121.5 us and was 4.9e-6 from 64 bits, with sixteen copies 117.8 and 1.7e-6; in chunks of 1024, where
 // all tiles fit either way, 8192 x 8192 at 24 took 56.0 us with a copy per lane and 58.0 with sixteen.
 bool tc_choose_anew(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const uint32_t *cta, uint32_t *flat, uint32_t dyn_smem, size_t max_bytes,
-                    TcShape *shape, TcPlan *plans, uint32_t slots) {
+                    TcShape *shape, TcPlan *plans, uint32_t slots, const TcLimits *limits = nullptr) {
     // (room for 32 decoders beside the larger table and the most stages that a shape has: every shape fits beside either table, and
     // so the plans are the same)
     const uint32_t slices = npad == 64 ? 2 : 4;
     if (*flat == kFlatBoth && tc_fits(d, n, npad, TcShape{4 / slices, slices, npad == 64 ? 2u : 3u, 32 / slices, slots}, kFlatBothLanes, dyn_smem))
         *flat = kFlatBothLanes;
-    if (*flat != kFlatBoth) return tc_best(d, n, npad, cta, *flat, dyn_smem, max_bytes, shape, plans, slots);
+    if (*flat != kFlatBoth) return tc_best(d, n, npad, cta, *flat, dyn_smem, max_bytes, shape, plans, slots, limits);
     TcShape wide;
     TcPlan wide_plans[kMaxMats];
-    const bool tight = tc_best(d, n, npad, cta, kFlatBoth, dyn_smem, ~(size_t)0, shape, plans, slots);
-    bool lanes = tc_best(d, n, npad, cta, kFlatBothLanes, dyn_smem, ~(size_t)0, &wide, wide_plans, slots);
+    const bool tight = tc_best(d, n, npad, cta, kFlatBoth, dyn_smem, ~(size_t)0, shape, plans, slots, limits);
+    bool lanes = tc_best(d, n, npad, cta, kFlatBothLanes, dyn_smem, ~(size_t)0, &wide, wide_plans, slots, limits);
     for (uint32_t i = 0; lanes && tight && i < n; ++i) lanes = wide_plans[i].chunks <= plans[i].chunks;
     if (!lanes && !tight) return false;
     if (lanes) {
@@ -360,14 +365,47 @@ bool tc_choose_anew(const huffllm_desc *const *d, uint32_t n, uint32_t npad, con
         for (uint32_t i = 0; i < n; ++i) plans[i] = wide_plans[i];
     }
     for (uint32_t i = 0; i < n; ++i)
-        if (plans[i].bytes > max_bytes) return tc_best(d, n, npad, cta, *flat, dyn_smem, max_bytes, shape, plans, slots);
+        if (plans[i].bytes > max_bytes) return tc_best(d, n, npad, cta, *flat, dyn_smem, max_bytes, shape, plans, slots, limits);
+    return true;
+}
+
+// The same for a launch with epilogues, whose kernels exist with single slots too.
+// Single slots where two leave fewer than 28 warps to decode and the estimate says that the launch gets a seventh shorter.
+// A warp then waits for its next record at every chunk's start, which the stage ring mostly hides.  (Two slots / one, us, and the ratio of the
+// estimates: FP16 11008 x 4096 at 32 vectors, chunks of 2048 38.9 / 36.8, 1.19, of 4096 65.7 / 38.9, 2.4; 20000 x 1024 at 64, chunks of 2048 40.4 / 28.4, 1.7;
+// BF16 11008 x 4096 at 32, chunks of 8192 34.1 / 31.6, 1.4, of 16384 69.4 / 40.5, 1.5; 2048 x 4096 at 12, chunks of 8192 12.5 / 14.5, 1.09, of 16384 15.2 /
+// 18.2, 1.0; bf16-trained FP16 20000 x 1024 at 64, chunks of 2048 33.2 / 39.8, 0.83.)
+// No sum gets longer for it: the limits are those of two slots, from its shape 0 without a limit on the workspace.
+bool tc_choose_epilogues(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const uint32_t *cta, uint32_t *flat, uint32_t dyn_smem, size_t max_bytes,
+                         TcShape *shape, TcPlan *plans) {
+    uint32_t single_flat = *flat, free_flat = *flat;
+    if (!tc_choose_anew(d, n, npad, cta, flat, dyn_smem, max_bytes, shape, plans, 2)) return false;
+    if (shape->decoders() >= 28) return true;
+    TcShape single;
+    TcPlan single_plans[kMaxMats];
+    TcLimits limits;
+    if (!tc_choose_anew(d, n, npad, cta, &free_flat, dyn_smem, ~(size_t)0, &single, single_plans, 2)) return true;
+    for (uint32_t i = 0; i < n; ++i) {
+        limits.chunks[i] = single_plans[i].chunks;
+        limits.ranges[i] = single_plans[i].ksplit;
+    }
+    if (!tc_choose_anew(d, n, npad, cta, &single_flat, dyn_smem, max_bytes, &single, single_plans, 1, &limits)) return true;
+    uint64_t two_span = 0, one_span = 0;
+    for (uint32_t i = 0; i < n; ++i) {
+        if (plans[i].span > two_span) two_span = plans[i].span;
+        if (single_plans[i].span > one_span) one_span = single_plans[i].span;
+    }
+    if (6 * two_span < 7 * one_span) return true;
+    *flat = single_flat;
+    *shape = single;
+    for (uint32_t i = 0; i < n; ++i) plans[i] = single_plans[i];
     return true;
 }
 
 // The same, remembered: a plan is worked out from a few dozen numbers in 3 to 5 us, as long as a small product takes on the GPU, and a program asks for
 // the same few plans at every step.  A thread keeps the last ones by those numbers (all that the functions above read).
 struct TcQuestion {
-    uint32_t n, npad, flat, dyn_smem, single_ok, reserved;
+    uint32_t n, npad, flat, dyn_smem, epilogues, reserved;
     uint64_t max_bytes;
     struct {
         uint32_t cta, dtype, lut_bits, flat_fields, max_words, chunk_cols, row_groups, col_chunks;
@@ -382,7 +420,7 @@ struct TcAnswer {
     TcPlan plans[kMaxMats];
 };
 bool tc_choose(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const uint32_t *cta, uint32_t *flat, uint32_t dyn_smem, size_t max_bytes,
-               TcShape *shape, TcPlan *plans, bool single_ok = false) {
+               TcShape *shape, TcPlan *plans, bool epilogues = false) {
     constexpr uint32_t kKept = 16;
     static thread_local TcAnswer kept[kKept];
     TcQuestion q;
@@ -392,7 +430,7 @@ bool tc_choose(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const ui
     q.flat = *flat;
     q.dyn_smem = dyn_smem;
     q.max_bytes = max_bytes;
-    q.single_ok = single_ok;
+    q.epilogues = epilogues;
     uint64_t hash = 0;
     for (uint32_t i = 0; i < n; ++i) {
         q.m[i] = {cta[i], d[i]->dtype, d[i]->lut_bits, d[i]->flat_fields, d[i]->max_words, d[i]->chunk_cols, d[i]->row_groups, d[i]->col_chunks, d[i]->n_chunks};
@@ -402,29 +440,8 @@ bool tc_choose(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const ui
     if (!a.known || memcmp(&a.of, &q, sizeof(q)) != 0) {
         a.known = false;
         a.flat = *flat;
-        a.fits = tc_choose_anew(d, n, npad, cta, &a.flat, dyn_smem, max_bytes, &a.shape, a.plans, 2);
-        // Single slots (kernels with epilogues) where two leave fewer than 28 warps to decode and the estimate says that the launch gets a seventh shorter.
-        // A warp then waits for its next record at every chunk's start, which the stage ring mostly hides.  (Two slots / one, us, and the ratio of the
-        // estimates: FP16 11008 x 4096 at 32 vectors, chunks of 2048 38.9 / 36.8, 1.19, of 4096 65.7 / 38.9, 2.4; 20000 x 1024 at 64, chunks of 2048 40.4 / 28.4, 1.7;
-        // BF16 11008 x 4096 at 32, chunks of 8192 34.1 / 31.6, 1.4, of 16384 69.4 / 40.5, 1.5; 2048 x 4096 at 12, chunks of 8192 12.5 / 14.5, 1.09, of 16384 15.2 /
-        // 18.2, 1.0; bf16-trained FP16 20000 x 1024 at 64, chunks of 2048 33.2 / 39.8, 0.83.)
-        if (single_ok && a.fits && a.shape.decoders() < 28) {
-            uint32_t single_flat = *flat;
-            TcShape single;
-            TcPlan single_plans[kMaxMats];
-            if (tc_choose_anew(d, n, npad, cta, &single_flat, dyn_smem, max_bytes, &single, single_plans, 1)) {
-                uint64_t two_span = 0, one_span = 0;
-                for (uint32_t i = 0; i < n; ++i) {
-                    if (a.plans[i].span > two_span) two_span = a.plans[i].span;
-                    if (single_plans[i].span > one_span) one_span = single_plans[i].span;
-                }
-                if (6 * two_span >= 7 * one_span) {
-                    a.flat = single_flat;
-                    a.shape = single;
-                    for (uint32_t i = 0; i < n; ++i) a.plans[i] = single_plans[i];
-                }
-            }
-        }
+        a.fits = epilogues ? tc_choose_epilogues(d, n, npad, cta, &a.flat, dyn_smem, max_bytes, &a.shape, a.plans)
+                           : tc_choose_anew(d, n, npad, cta, &a.flat, dyn_smem, max_bytes, &a.shape, a.plans, 2);
         a.of = q;
         a.known = true;
     }
@@ -684,7 +701,7 @@ huffllm_status huffllm_workspace_bytes(const huffllm_desc *desc, uint32_t batch,
                 if (!tc_best(&desc, 1, npad, &cta, flat, dyn, ~(size_t)0, &sh, &p)) continue;
                 if (p.bytes > *bytes) *bytes = p.bytes;
                 if (!tc_shape(&desc, 1, npad, 0, flat, dyn, &sh)) continue;
-                p = tc_plan(desc, npad, cta, sh, ~(size_t)0, ~0u);
+                p = tc_plan(desc, npad, cta, sh, ~(size_t)0);
                 if (p.bytes > *bytes) *bytes = p.bytes;
             }
     }

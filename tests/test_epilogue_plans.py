@@ -48,3 +48,42 @@ def test_plans_are_refused(hl):
     assert status(lambda: hl.gemm_epilogue_launch_plan([good, d], 32)) == "UNSUPPORTED"    # types differ
     assert status(lambda: hl.gemm_epilogue_launch_plan([good] * 9, 32)) == "INVALID_ARG"
     assert hl.lib().huffllm_gemm_epilogue_launch_plan(1, None, 32, 0, None, None, None, None, None, None) == 1
+
+
+# Records so large that two slots a warp leave few warps a place: (rows, cols, dtype, chunk, limit).
+LARGE_RECORDS = [(22016, 4096, FP16, 2048, 0), (11008, 4096, FP16, 4096, 0), (10000, 4096, FP16, 2048, 0), (28672, 1024, FP16, 4096, 0), (10086, 4576, FP16, 4096, 0),
+                 (54663, 14080, FP16, 4096, 0), (30673, 1184, FP16, 4096, 0), (17996, 22208, FP16, 4096, 0), (8999, 4544, FP16, 4096, 0), (11008, 4096, BF16, 8192, 0),
+                 (33485, 13536, BF16, 8192, 0), (20000, 2048, BF16, 8192, 9), (11008, 4096, BF16, 16384, 0), (7528, 8832, BF16, 16384, 0), (2000, 4096, FP16, 2048, 7)]
+
+
+@pytest.mark.parametrize("rows,cols,dtype,chunk,limit", LARGE_RECORDS)
+@pytest.mark.parametrize("batch", [9, 12, 16, 17, 24, 32, 33, 45, 56, 64])
+def test_single_slots_make_no_sum_longer(hl, rows, cols, dtype, chunk, limit, batch):
+    """Rounding is not traded for time: no accumulator adds up more columns than with two slots a warp, as in the call without an epilogue."""
+    d = planned_desc(rows, cols, chunk, limit, dtype)
+    plan = hl.gemm_epilogue_launch_plan([d], batch)
+    if limit != 7:
+        assert plan["chunks_per_sum"][0] <= hl.gemm_launch_plan([d], batch)["chunks_per_sum"][0]
+
+
+def test_single_slots_are_taken(hl):
+    taken = {(rows, chunk, batch) for rows, cols, dtype, chunk, limit in LARGE_RECORDS for batch in (12, 32, 64)
+             if hl.gemm_epilogue_launch_plan([planned_desc(rows, cols, chunk, limit, dtype)], batch)["slots_per_warp"] == 1}
+    assert {(22016, 2048, 32), (11008, 4096, 32), (28672, 4096, 12), (11008, 16384, 32)} <= taken
+
+
+def test_single_slots_make_no_sum_longer_whatever_the_shape(hl):
+    import random
+    rng = random.Random(11)
+    single = 0
+    for _ in range(300):
+        dtype = rng.choice([BF16, FP16])
+        chunk = rng.choice([4096, 8192, 16384] if dtype == BF16 else [2048, 4096])
+        d = planned_desc(int(200 * 280 ** rng.random()), 32 * int(10 * 90 ** rng.random()), chunk, rng.choice([0, 9]) if dtype == BF16 else 0, dtype)
+        batch = rng.randrange(9, 65)
+        if status(lambda: hl.gemm_launch_plan([d], batch)) == "UNSUPPORTED":
+            continue                                       # (records that the kernel has no room for)
+        plan = hl.gemm_epilogue_launch_plan([d], batch)
+        single += plan["slots_per_warp"] == 1
+        assert plan["chunks_per_sum"][0] <= hl.gemm_launch_plan([d], batch)["chunks_per_sum"][0], (d.rows, d.cols, dtype, chunk, batch)
+    assert single > 100
