@@ -256,25 +256,27 @@ TcPlan tc_plan(const huffllm_desc *d, uint32_t npad, uint32_t sms, const TcShape
     const size_t item_bytes = (size_t)32 * sh.piece_columns(npad) * 32 * sizeof(float);
     // Column ranges: in shape 0 the count whose items are done first, their sums not considered (fewer,
     // longer ranges would be a little faster, but an accumulator's error grows with the columns it adds up: 1e-6 for 1024,
-    // 3.8e-6 for 3584); in the others all costs count, and no accumulator may add up more columns than in shape 0.  For row groups that
+    // 3.8e-6 for 3584); in the others, and wherever `max_chunks` bounds the sums, all costs count, and no accumulator may add up more columns than in
+    // shape 0.  For row groups that
     // fill no tile ranges are counted as if blocks and items were cheaper than they are, which makes for more of them and shorter
     // sums (20000 x 1024 FP16 at 32 in two ranges 30.3 us and 6.4e-7 from 64 bits, in four 32.5 and 3.4e-7); whether it pays is up to what they cost.
     const TcCost price = tc_cost(sh, npad, d->dtype == HUFFLLM_FP16);
     const TcCost ranges_price = sh.part_filled() ? TcCost{kTcUnit * (14 + sh.row_groups) / (14 + 8), 5 * kTcUnit} : price;
+    const bool all_costs = !base || max_chunks != ~0u;
     uint32_t best = 0;
     uint64_t best_span = ~0ull;
     for (uint32_t ks = min_ranges; ks <= 16 && ks <= d->col_chunks; ++ks) {
         if (ks > 1 && ws_partial_offset(d) + (size_t)p.m_tiles * ks * item_bytes > max_bytes) break;
         const uint32_t range = (d->col_chunks + ks - 1) / ks;
         if ((range + sh.slices - 1) / sh.slices > max_chunks) continue;
-        const uint64_t span = tc_span(d, sh, ranges_price, p.m_tiles, ks, sms) + (base ? 0 : tc_sum_cost(sh, npad, ks));
+        const uint64_t span = tc_span(d, sh, ranges_price, p.m_tiles, ks, sms) + (all_costs ? tc_sum_cost(sh, npad, ks) : 0);
         if (span < best_span) { best_span = span; best = ks; }
     }
-    if (best && sh.part_filled()) best_span = tc_span(d, sh, price, p.m_tiles, best, sms) + tc_sum_cost(sh, npad, best);
+    if (best && (all_costs || sh.part_filled())) best_span = tc_span(d, sh, price, p.m_tiles, best, sms);
     p.ksplit = best;                                     // (0: no number of ranges is within the limits)
     p.items = p.m_tiles * best;
     // (at the widest padding an issuer that carries the activations of four tiles as well makes a block take an eighth longer)
-    p.span = !best ? ~0ull : !base ? best_span : (npad == 64 && sh.na == 4 ? best_span * 9 / 8 : best_span) + tc_sum_cost(sh, npad, best);
+    p.span = !best ? ~0ull : (base && npad == 64 && sh.na == 4 ? best_span * 9 / 8 : best_span) + tc_sum_cost(sh, npad, best);
     p.chunks = best ? ((d->col_chunks + best - 1) / best + sh.slices - 1) / sh.slices : 0;
     // the counters' region is sized for the smallest tile (most row tiles), so that plans for different batch sizes
     // sharing one workspace never put partial sums where another plan keeps counters
@@ -297,7 +299,7 @@ bool tc_best(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const uint
              TcShape *shape, TcPlan *plans, uint32_t slots = 2, const TcLimits *limits = nullptr) {
     TcShape base;
     if (!tc_shape(d, n, npad, 0, flat, dyn_smem, &base, slots)) return false;
-    for (size_t base_bytes = limits ? max_bytes : ~(size_t)0;; base_bytes = max_bytes) {
+    for (size_t base_bytes = ~(size_t)0;; base_bytes = max_bytes) {
         uint64_t best_span = ~0ull;
         TcLimits own;
         for (uint32_t which = 0; which < kTcShapes; ++which) {
@@ -371,34 +373,46 @@ bool tc_choose_anew(const huffllm_desc *const *d, uint32_t n, uint32_t npad, con
 
 // The same for a launch with epilogues, whose kernels exist with single slots too.
 // Single slots where two leave fewer than 28 warps to decode and the estimate says that the launch gets a seventh shorter.
-// A warp then waits for its next record at every chunk's start, which the stage ring mostly hides.  (Two slots / one, us, and the ratio of the
-// estimates: FP16 11008 x 4096 at 32 vectors, chunks of 2048 38.9 / 36.8, 1.19, of 4096 65.7 / 38.9, 2.4; 20000 x 1024 at 64, chunks of 2048 40.4 / 28.4, 1.7;
-// BF16 11008 x 4096 at 32, chunks of 8192 34.1 / 31.6, 1.4, of 16384 69.4 / 40.5, 1.5; 2048 x 4096 at 12, chunks of 8192 12.5 / 14.5, 1.09, of 16384 15.2 /
-// 18.2, 1.0; bf16-trained FP16 20000 x 1024 at 64, chunks of 2048 33.2 / 39.8, 0.83.)
-// No sum gets longer for it: the limits are those of two slots, from its shape 0 without a limit on the workspace.
+// A warp then waits for its next record at every chunk's start, which the stage ring mostly hides.  (Two slots, the plain call / one, us: FP16
+// 11008 x 4096 at 24 vectors, chunks of 2048, 37.0 / 36.6, at 32, chunks of 4096, 58.3 / 51.0; 13230 x 3904 at 32, chunks of 4096, 69.1 / 40.7; 14336 x 4096 at
+// 16, chunks of 2048, 53.4 / 43.5; 20000 x 1024 at 64, the same, 33.4 / 28.4; BF16 11008 x 4096 at 32, chunks of 8192 33.4 / 31.8, of 16384 54.9 / 41.2; 28672 x
+// 8192 at 64, chunks of 8192, 168 / 146.  Of 48 plans that took them three were slower: BF16 of 9 bits 5145 x 2272 at 48 24.5 / 26.1, FP16 5461 x 1728 at 32
+// 14.4 / 15.2, BF16 5847 x 7648 at 48 38.3 / 39.2.)
+// No sum gets longer for it than in the two-slot plan of a workspace without limit, and that workspace decides as well whether single slots are taken:
+// a smaller one can only take them back.
 bool tc_choose_epilogues(const huffllm_desc *const *d, uint32_t n, uint32_t npad, const uint32_t *cta, uint32_t *flat, uint32_t dyn_smem, size_t max_bytes,
                          TcShape *shape, TcPlan *plans) {
-    uint32_t single_flat = *flat, free_flat = *flat;
+    const uint32_t asked_flat = *flat;
     if (!tc_choose_anew(d, n, npad, cta, flat, dyn_smem, max_bytes, shape, plans, 2)) return false;
     if (shape->decoders() >= 28) return true;
+    auto span_of = [&](const TcPlan *p) -> uint64_t {
+        uint64_t span = 0;
+        for (uint32_t i = 0; i < n; ++i)
+            if (p[i].span > span) span = p[i].span;
+        return span;
+    };
     TcShape single;
-    TcPlan single_plans[kMaxMats];
+    TcPlan p[kMaxMats];
+    uint32_t two_flat = asked_flat, single_flat = asked_flat;
+    if (!tc_choose_anew(d, n, npad, cta, &two_flat, dyn_smem, ~(size_t)0, &single, p, 2) || single.decoders() >= 28) return true;
+    const uint64_t free_span = span_of(p);
     TcLimits limits;
-    if (!tc_choose_anew(d, n, npad, cta, &free_flat, dyn_smem, ~(size_t)0, &single, single_plans, 2)) return true;
     for (uint32_t i = 0; i < n; ++i) {
-        limits.chunks[i] = single_plans[i].chunks;
-        limits.ranges[i] = single_plans[i].ksplit;
+        limits.chunks[i] = p[i].chunks;
+        limits.ranges[i] = p[i].ksplit;
     }
-    if (!tc_choose_anew(d, n, npad, cta, &single_flat, dyn_smem, max_bytes, &single, single_plans, 1, &limits)) return true;
-    uint64_t two_span = 0, one_span = 0;
-    for (uint32_t i = 0; i < n; ++i) {
-        if (plans[i].span > two_span) two_span = plans[i].span;
-        if (single_plans[i].span > one_span) one_span = single_plans[i].span;
+    auto pays = [&](uint64_t two_span) -> bool { return 6 * two_span >= 7 * span_of(p); };
+    if (!tc_choose_anew(d, n, npad, cta, &single_flat, dyn_smem, ~(size_t)0, &single, p, 1, &limits) || !pays(free_span)) return true;
+    bool cut = false;
+    for (uint32_t i = 0; i < n; ++i) cut = cut || p[i].bytes > max_bytes;
+    if (cut) {
+        single_flat = asked_flat;
+        if (!tc_choose_anew(d, n, npad, cta, &single_flat, dyn_smem, max_bytes, &single, p, 1, &limits)) return true;
     }
-    if (6 * two_span < 7 * one_span) return true;
+    if (!pays(span_of(plans))) return true;
     *flat = single_flat;
     *shape = single;
-    for (uint32_t i = 0; i < n; ++i) plans[i] = single_plans[i];
+    for (uint32_t i = 0; i < n; ++i) plans[i] = p[i];
     return true;
 }
 
@@ -690,8 +704,8 @@ huffllm_status huffllm_workspace_bytes(const huffllm_desc *desc, uint32_t batch,
         const int sms = have ? dev.sms : 148;
         const uint32_t dyn = (have ? (uint32_t)dev.smem_optin : 232448u) - kStaticSmem;
         const uint32_t cta = (uint32_t)sms;
-        // The plan that will run for this and for every smaller batch, and the shape-0 plan, which a launch over several matrices
-        // may fall back on; with all three FP16 tables, and with those that flat codes leave.
+        // The plans that will run for this and for every smaller batch, without epilogues and with (single slots), and the shape-0 plan,
+        // which a launch over several matrices may fall back on; with all three FP16 tables, and with those that flat codes leave.
         for (uint32_t npad = 16; npad <= tc_npad_of(batch); npad *= 2)
             for (uint32_t flat : {kFlatNone, kFlatUpper, kFlatBoth, kFlatBothLanes}) {
                 const uint32_t have_flat = flat == kFlatBothLanes ? kFlatBoth : flat;
@@ -703,6 +717,8 @@ huffllm_status huffllm_workspace_bytes(const huffllm_desc *desc, uint32_t batch,
                 if (!tc_shape(&desc, 1, npad, 0, flat, dyn, &sh)) continue;
                 p = tc_plan(desc, npad, cta, sh, ~(size_t)0);
                 if (p.bytes > *bytes) *bytes = p.bytes;
+                uint32_t chosen = have_flat;
+                if (flat == have_flat && tc_choose_epilogues(&desc, 1, npad, &cta, &chosen, dyn, ~(size_t)0, &sh, &p) && p.bytes > *bytes) *bytes = p.bytes;
             }
     }
     return HUFFLLM_OK;

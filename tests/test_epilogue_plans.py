@@ -87,3 +87,84 @@ def test_single_slots_make_no_sum_longer_whatever_the_shape(hl):
         single += plan["slots_per_warp"] == 1
         assert plan["chunks_per_sum"][0] <= hl.gemm_launch_plan([d], batch)["chunks_per_sum"][0], (d.rows, d.cols, dtype, chunk, batch)
     assert single > 100
+
+
+@pytest.mark.parametrize("rows,cols,dtype,chunk,limit", LARGE_RECORDS)
+def test_the_plan_is_the_same_in_the_workspace_asked_for_and_in_any(hl, rows, cols, dtype, chunk, limit):
+    """A buffer's size decides neither about rounding nor about time, also when it was sized for more vectors."""
+    d = planned_desc(rows, cols, chunk, limit, dtype)
+    for batch in (9, 12, 16, 17, 24, 32, 33, 45, 56, 64):
+        free = hl.gemm_epilogue_launch_plan([d], batch)
+        for sized_for in sorted({batch, 16, 32, 64}):
+            if sized_for >= batch:
+                assert hl.gemm_epilogue_launch_plan([d], batch, hl.workspace_bytes(d, sized_for)) == free, (batch, sized_for)
+
+
+def test_the_plan_is_the_same_in_the_workspace_asked_for_whatever_the_shape(hl):
+    import random
+    rng = random.Random(12)
+    for _ in range(300):
+        dtype = rng.choice([BF16, FP16])
+        chunk = rng.choice([1024, 4096, 8192, 16384] if dtype == BF16 else [1024, 2048, 4096])
+        limit = rng.choice([0, 0, 9, 12]) if dtype == BF16 else rng.choice([0, 0, 7, 9, 12])
+        d = planned_desc(int(200 * 280 ** rng.random()), 32 * int(10 * 90 ** rng.random()), chunk, limit, dtype)
+        batch = rng.randrange(9, 65)
+        if status(lambda: hl.gemm_epilogue_launch_plan([d], batch)) == "UNSUPPORTED":
+            continue                                       # (records that the kernel has no room for)
+        assert hl.gemm_epilogue_launch_plan([d], batch, hl.workspace_bytes(d, batch)) == hl.gemm_epilogue_launch_plan([d], batch), (d.rows, d.cols, dtype, chunk, limit, batch)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols,dtype,chunk,limit,batch", [(28672, 1024, "fp16", 4096, 0, 12), (28672, 1024, "fp16", 4096, 0, 56), (11008, 4096, "fp16", 4096, 0, 32),
+                                                               (20000, 2048, "bf16", 8192, 9, 17), (22016, 1024, "bf16", 16384, 0, 40), (11008, 4096, "fp16", 4096, 7, 24)])
+def test_single_slots_in_the_workspace_asked_for(hl, rows, cols, dtype, chunk, limit, batch):
+    """The plans above at work: one slot a warp, some with more work items than CTAs; against 64 bits on sampled rows, twice the same bits,
+    and no further from 64 bits than the bound of an accumulator of that many columns."""
+    import numpy as np
+    import torch
+
+    import workloads as wl
+    from test_layer_operators import Blob, Sums, assert_clean, bits_to_f64, check, up, values, workspace
+    w = wl.gaussian_weights(rows, cols, 0.05, rows + cols, dtype)
+    blob = Blob(hl, torch, w, dtype, chunk, limit)
+    n, (ws,) = workspace(hl, torch, [blob], batch)
+    plan = hl.gemm_epilogue_launch_plan([blob.desc], batch, n)
+    assert plan["slots_per_warp"] == 1 and plan == hl.gemm_epilogue_launch_plan([blob.desc], batch)
+    x = wl.activations(batch, cols, 3, dtype)
+    xd = up(torch, x, dtype)
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    outs = []
+    for _ in range(2):
+        outs.append(torch.empty((batch, rows), dtype=torch.float32, device="cuda"))
+        hl.decode_gemm_epilogue(blob.desc, blob.dev, xd, batch, hl.Epilogue(hl.ACT_RELU), outs[-1], ws, n, err)
+        torch.cuda.synchronize()
+        assert_clean(hl, blob, ws, err)
+    assert torch.equal(*outs)
+    pick = np.unique(np.concatenate([np.arange(0, rows, 37), np.arange(rows - 40, rows)]))
+    check(values(outs[0])[:, pick], *Sums(bits_to_f64(w[pick], dtype), bits_to_f64(x, dtype)).through("relu"), "f32")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch", [12, 24, 64])
+@pytest.mark.parametrize("dtype,chunk", [("bf16", 512), ("fp16", 4096)])
+def test_several_matrices_with_more_items_than_ctas_each(hl, dtype, chunk, batch):
+    """Every matrix of a launch has a counter of its own in its own workspace."""
+    import torch
+
+    import workloads as wl
+    from test_layer_operators import Blob, Sums, assert_clean, bits_to_f64, check, up, values, workspace
+    shapes = [(60000, 256), (20000, 512), (60000, 128)]
+    ws_ = [wl.gaussian_weights(r, c, 0.05, r + c, dtype) for r, c in shapes]
+    blobs = [Blob(hl, torch, w, dtype, chunk) for w in ws_]
+    n, wss = workspace(hl, torch, blobs, batch)
+    xs = [wl.activations(batch, c, c, dtype) for _, c in shapes]
+    xd = [up(torch, x, dtype) for x in xs]
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for act in ("relu", "silu"):
+        outs = [torch.empty((batch, r), dtype=torch.float32, device="cuda") for r, _ in shapes]
+        eps = [hl.Epilogue(getattr(hl, "ACT_" + act.upper()))] * 3
+        hl.decode_gemm_multi_epilogue([b.desc for b in blobs], [b.dev for b in blobs], xd, batch, eps, outs, wss, n, err)
+        torch.cuda.synchronize()
+        for b, w, x, ws, out in zip(blobs, ws_, xs, wss, outs):
+            assert_clean(hl, b, ws, err)
+            check(values(out), *Sums(bits_to_f64(w, dtype), bits_to_f64(x, dtype)).through(act), "f32")
