@@ -61,3 +61,11 @@ def test_several_matrices(hl, torch, kind, batch, chunk):  # noqa: F811
 @pytest.mark.parametrize("h16,hidden,n", [(True, 96, 2080), (False, 288, 800)])
 def test_the_sub_layer(hl, torch, kind, batch, h16, hidden, n):  # noqa: F811
     ops.test_the_feed_forward_sub_layer(hl, torch, batch, "fp16", h16, hidden, n)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("limit", [7, 9, 12])
+@pytest.mark.parametrize("batch", [1, 6, 16, 24, 64])
+def test_other_table_sizes(hl, torch, kind, limit, batch):  # noqa: F811
+    w = wl.gaussian_weights(300, 1056, 0.05, limit, "fp16")
+    ops.run_product(hl, torch, w, "fp16", batch, "silu", True, True, True, 1024, limit, seed=batch)
