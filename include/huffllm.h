@@ -413,10 +413,11 @@ typedef struct huffllm_epilogue {
 } huffllm_epilogue;
 
 /*
- * huffllm_decode_gemm with an epilogue: the same kernels, workspace, limits and error flag (which kernel runs at 9..16 vectors is chosen
- * anew, and blobs of long codes take the tensor cores above 8 vectors too, so the sums may differ from the plain call's in their last bits
- * there).  out: device memory (or pinned host memory
- * the device can address), aligned to its type.
+ * huffllm_decode_gemm with an epilogue: the same kernels, workspace, limits and error flag.  The sums may differ from the plain call's in
+ * their last bits: at 9..16 vectors, where the kernel is chosen anew; above 8 vectors for blobs of long codes, which take the tensor cores
+ * too; and at 9..64 for blobs whose records are so large that warps get one slot (huffllm_gemm_epilogue_launch_plan), where no accumulator
+ * adds up more columns than in the plain call.  They do not depend on the size of a workspace of at least huffllm_workspace_bytes.
+ * out: device memory (or pinned host memory the device can address), aligned to its type.
  */
 huffllm_status huffllm_decode_gemm_epilogue(const huffllm_desc *desc, const void *blob_dev, const uint16_t *x_dev, uint32_t batch,
                                             const huffllm_epilogue *epilogue, void *out_dev, void *workspace_dev,

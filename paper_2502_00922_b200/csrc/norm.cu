@@ -213,7 +213,7 @@ static cudaError_t launch_norm_items(const NormArgs &a, uint32_t vectors, cudaSt
         const uint64_t t = ((groups + items - 1) / items + 31) / 32 * 32;
         return (uint32_t)(t < (uint64_t)kNormMaxThreads ? t : (uint64_t)kNormMaxThreads);
     };
-    // One group of eight a thread where that makes a CTA of at most 1024 threads; where there are vectors for many rounds of CTAs anyway, two or
+    // One group of eight a thread where that makes a CTA of at most 1024 threads; where there are vectors for many rounds of CTAs anyway (eight a B200's SM), two or
     // four from 513 threads on, so that an SM's CTAs are more and wait for their sums at different times.  (us with one / two / four groups:
     // 296 x 8192 in 16 bits 5.3 / 6.0 / 6.3, 2048 x 8192 25.4 / 23.8 / 25.5; 2048 x 4096 in fp32 19.5 / 21.1 / 23.7; 4096 x 16384 - / 105 / 88.)
     const bool many = vectors >= 8 * 148;
