@@ -433,7 +433,9 @@ huffllm_status huffllm_gemm_epilogue_launch_plan(uint32_t n, const huffllm_desc 
                                                  uint32_t *slots_per_warp, uint32_t *column_slices, uint32_t *row_groups, uint32_t *ranges,
                                                  uint32_t *work_items, uint32_t *chunks_per_sum);
 
-/* huffllm_decode_gemm_multi with an epilogue per matrix (q, k and v with their biases, say): epilogues is a host array of n.  Every batch
+/* huffllm_decode_gemm_multi with an epilogue per matrix (q, k and v with their biases, say): epilogues is a host array of n.  No out may share a
+ * value with another one (side by side in one buffer, with its stride, they may lie), or with an x, bias or residual of the call other than its own residual:
+ * nothing orders the matrices of a launch.  Every batch
  * takes blobs of every max_code_len (more than 8 vectors of blobs whose records are too large for the tensor-core kernel take launches of their own). */
 huffllm_status huffllm_decode_gemm_multi_epilogue(uint32_t n, const huffllm_desc *const *descs, const void *const *blobs_dev,
                                                   const uint16_t *const *xs_dev, uint32_t batch, const huffllm_epilogue *epilogues,
@@ -457,7 +459,8 @@ huffllm_status huffllm_stack_gate_up_device(const uint16_t *gate_dev, const uint
  * Residual addition and root-mean-square norm between two products, one launch:
  *     h = x + delta;   sum = h;   out = h / sqrt(mean(h^2) + eps) * gain
  * for `vectors` vectors of `cols` values.  h is kept in fp32 (out is computed from it, not from the rounded sum); the squares are
- * added up in fp32 in a fixed order (they overflow for |h| above 1e19).  x, sum: x_type; delta: delta_type; gain, out: 16-bit words
+ * added up in fp32 in a fixed order (they overflow for |h| above 1e19 and vanish below 1e-22, which shows with eps = 0 alone: a vector
+ * of zeros then gives NaN).  x, sum: x_type; delta: delta_type; gain, out: 16-bit words
  * of `dtype`, what the products take as x.  delta, sum and gain may be null (no addition, not wanted, ones).  sum may be x or delta
  * itself (same pointer, stride and type); out must not overlap the inputs.  Any alignment of the types is taken; 16-byte
  * aligned pointers are faster, with cols % 8 == 0 and strides of whole 16 bytes, or with strides that are alike modulo 8 (packed vectors

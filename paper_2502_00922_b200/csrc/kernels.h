@@ -53,7 +53,7 @@ struct KernelArgs {
     // (behind the matrices, so that the fields the hot loops read keep their places)
     uint32_t slots;            // slots per decoder warp: 2 (the next record lands while this one is decoded), or 1 where two would
                                // leave too few warps a slot (large records: the feeder then waits for a slot before every copy).
-                               // Kernels with single slots exist for FP16 blobs and for BF16 blobs with 8-bit tables.
+                               // Kernels with single slots exist for FP16 blobs and for BF16 blobs with 8-bit tables; on the tensor cores with epilogues alone, for all.
     uint32_t fp16_flat;        // FP16 blobs: which mantissa halves of every matrix of the launch carry the flat 5-bit code
 };
 // (kFlatBoth: the exponent's table with sixteen copies of an entry, kFlatBothLanes: with one per lane; the lower half alone is not made use of)

@@ -168,3 +168,26 @@ def test_several_matrices_with_more_items_than_ctas_each(hl, dtype, chunk, batch
         for b, w, x, ws, out in zip(blobs, ws_, xs, wss, outs):
             assert_clean(hl, b, ws, err)
             check(values(out), *Sums(bits_to_f64(w, dtype), bits_to_f64(x, dtype)).through(act), "f32")
+
+
+def test_remembered_plans_are_those_worked_out_anew(hl):
+    """Questions with and without epilogues in several orders against threads that have kept nothing."""
+    import random
+    import threading
+    descs = [planned_desc(rows, cols, chunk, limit, dtype) for rows, cols, dtype, chunk, limit in LARGE_RECORDS if limit != 7]
+    questions = [(epi, d, b, w) for d in descs for b in (12, 33) for w in (0, hl.workspace_bytes(d, b), hl.workspace_bytes(d, 9)) for epi in (False, True)]
+
+    def ask(q):
+        epi, d, batch, ws = q
+        return (hl.gemm_epilogue_launch_plan if epi else hl.gemm_launch_plan)([d], batch, ws)
+    anew = []
+    for q in questions:
+        t = threading.Thread(target=lambda: anew.append(ask(q)))
+        t.start()
+        t.join()
+    assert len(anew) == len(questions)
+    order = list(range(len(questions)))
+    for seed in range(3):
+        random.Random(seed).shuffle(order)
+        for i in order + order[::-1]:
+            assert ask(questions[i]) == anew[i]

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 import workloads as wl
-from test_layer_operators import Blob, FfnCase, assert_clean, f_to_bits, hl, torch, up, workspace, x_of  # noqa: F401
+from test_layer_operators import Blob, FfnCase, assert_clean, f_to_bits, hl, norm_case, torch, up, workspace, x_of  # noqa: F401
 
 
 @pytest.mark.gpu
@@ -136,3 +136,52 @@ def test_captured_graphs_and_calls_take_turns_on_a_workspace(hl, torch, batch): 
         assert torch.equal(outs[i], want[i])
     for b, w in zip(blobs, wss):
         assert_clean(hl, b, w, err)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols", [32769, 40001, 65536])
+@pytest.mark.parametrize("over", ["x", "delta"])
+def test_long_vectors_updated_in_place(hl, torch, cols, over):  # noqa: F811
+    """Vectors that a CTA goes through twice: the second time every value is read by the thread that then writes it."""
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    for t, elem in ((torch.bfloat16, hl.ELEM_16), (torch.float32, hl.ELEM_F32)):
+        x, d = (torch.randn((3, cols), generator=g, device="cuda").to(t) for _ in range(2))
+        results = []
+        for place in (None, over):
+            a, b = x.clone(), d.clone()
+            s = torch.empty_like(a) if place is None else a if place == "x" else b
+            o = torch.empty((3, cols), dtype=torch.bfloat16, device="cuda")
+            hl.add_rms_norm(hl.Norm(hl.BF16, 3, cols, a, elem, None, 1e-6, o, b, elem, s))
+            torch.cuda.synchronize()
+            results.append((s.clone(), o))
+        assert torch.equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("x16,delta", [(True, "16"), (False, "f32"), (False, None)])
+def test_very_long_vectors(hl, torch, x16, delta):  # noqa: F811
+    norm_case(hl, torch, 2, 1_000_003, "bf16", x16, delta, True, True, pad=5, seed=1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch", [1, 5, 12, 40])
+@pytest.mark.parametrize("out16", [True, False])
+def test_outs_side_by_side_in_one_buffer(hl, torch, batch, out16):  # noqa: F811
+    """q, k and v of a token next to each other, as attention wants them: three outs with the buffer's stride; the same values as in buffers of their own."""
+    cols, rows = 512, (512, 128, 130)
+    blobs = [Blob(hl, torch, wl.gaussian_weights(r, cols, 0.05, i), "bf16") for i, r in enumerate(rows)]
+    n, wss = workspace(hl, torch, blobs, batch)
+    x = up(torch, x_of(batch, cols, 1, "bf16"), "bf16")
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    t, elem = (torch.bfloat16, hl.ELEM_16) if out16 else (torch.float32, hl.ELEM_F32)
+    ld = sum(rows) + 6
+    buf = torch.full((batch, ld), 77.0, dtype=t, device="cuda")
+    at = [0, rows[0], rows[0] + rows[1]]
+    own = [torch.empty((batch, r), dtype=t, device="cuda") for r in rows]
+    for eps, outs in (([hl.Epilogue(hl.ACT_SILU, elem, out_stride=ld)] * 3, [buf[:, a:] for a in at]), ([hl.Epilogue(hl.ACT_SILU, elem)] * 3, own)):
+        hl.decode_gemm_multi_epilogue([b.desc for b in blobs], [b.dev for b in blobs], [x] * 3, batch, eps, outs, wss, n, err)
+    torch.cuda.synchronize()
+    assert int(err.item()) == 0
+    for a, r, o in zip(at, rows, own):
+        assert torch.equal(buf[:, a:a + r], o)
+    assert torch.all(buf[:, sum(rows):] == 77.0)
