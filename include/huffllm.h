@@ -502,6 +502,129 @@ huffllm_status huffllm_decode_ffn(const huffllm_ffn *ffn, const void *h_dev, uin
                                   uint64_t out_stride, uint32_t h_type, void *workspace_dev, size_t workspace_bytes,
                                   int32_t *err_flag_dev, huffllm_stream stream);
 
+/* ------------------------------------------------ device: between and behind the products of a decode step */
+
+/*
+ * Rotary positions with one or several axes (time, height and width of image and video tokens), for q and k in one launch.
+ * Pair i of a head's first rotary_dim channels turns by the angle  positions[axis(i)][token] * frequencies[i]:
+ *     (a, b) -> (a cos - b sin, b cos + a sin)
+ * The angle is that of the exact product, however far the position; sines and cosines are fp32, the result is rounded once.  Channels from
+ * rotary_dim on are copied.  sections[a] is the number of pairs of axis a; they add up to rotary_dim / 2, and lie one axis behind the
+ * other, or (in_turn) are dealt to the axes in turn, an axis that has had all of its pairs being passed over.
+ * q and k: [tokens][heads][head_dim] words of dtype, a stride being the values from one token to the next (0 = packed).  k may be null (no
+ * keys), or q.  An out may be its input itself (same pointer, same stride); other overlaps are not allowed.
+ */
+typedef enum {
+    HUFFLLM_PAIR_HALVES = 0,       /* channels i and i + rotary_dim / 2 */
+    HUFFLLM_PAIR_NEIGHBOURS = 1    /* channels 2 i and 2 i + 1          */
+} huffllm_pairing;
+#define HUFFLLM_MAX_AXES 4
+typedef struct huffllm_rotary {
+    uint32_t dtype, pairing;               /* huffllm_dtype, huffllm_pairing                   */
+    uint32_t head_dim, rotary_dim;         /* rotary_dim even, at most head_dim, which is at most 1024 */
+    uint32_t axes, in_turn;                /* 1 .. HUFFLLM_MAX_AXES                            */
+    uint32_t sections[HUFFLLM_MAX_AXES];
+    uint64_t tokens;
+    uint32_t q_heads, k_heads;
+    const int32_t *positions;              /* device [axes][tokens]                            */
+    const float *frequencies;              /* device [rotary_dim / 2]: radians per position    */
+    const uint16_t *q, *k;                 /* device                                           */
+    uint16_t *q_out, *k_out;
+    uint64_t q_stride, k_stride, q_out_stride, k_out_stride;
+} huffllm_rotary;
+huffllm_status huffllm_apply_rotary(const huffllm_rotary *args, huffllm_stream stream);
+
+/*
+ * A cache of keys and values held in 4 bits, in pages.
+ * For every token and head, 32 channels share an fp16 offset m = fp16(smallest) and scale s = fp16((largest - smallest) / 15, computed in
+ * fp32); a channel x has the code (x - m) / s rounded to the nearest whole number (ties to even), 0 .. 15 (s = 0: code 0), and stands for
+ * s * code + m: 5 bits a channel.  A group whose s or m would not be finite (NaN, infinities, values beyond fp16) stands for NaN.
+ *
+ * The pool is [pages][kv_heads][page_tokens / 16] blocks of 16 tokens; a block's bytes are the attention's business (cache_layout.h).
+ * table[sequence][i] is the page of tokens i * page_tokens ..; entries that no token of the sequence lies on are never looked at.
+ * lengths[sequence] counts all of its tokens, those of the call included.  Table and lengths are read on the device, so a captured call
+ * follows them as they grow.  Several sequences may share pages that are only read.
+ * The calls set *err_flag (device, may be null) to sequence + 1 where a length is negative or beyond the table's row, a page is not one of the
+ * pool's, or starts do not ascend within the rows of the call; what lies on such a page is neither written nor seen, nothing is read or
+ * written out of place, and other sequences are served.
+ * A pool needs no initialisation.  huffllm_cache_bytes: its size for the given pages, heads and channels (pool, table and lengths may
+ * be null there).
+ */
+typedef struct huffllm_cache {
+    uint32_t dtype;                        /* huffllm_dtype of keys, values, queries and outputs            */
+    uint32_t kv_heads, head_dim;           /* head_dim: 64, 96, 128, 192 or 256                             */
+    uint32_t page_tokens;                  /* a multiple of 16, at most 65536                               */
+    uint64_t pages;
+    void *pool;                            /* device, 256-byte aligned                                      */
+    uint32_t sequences, table_stride;      /* table_stride: entries of a sequence, at least 1               */
+    const int32_t *table, *lengths;        /* device [sequences][table_stride], [sequences]                 */
+} huffllm_cache;
+huffllm_status huffllm_cache_bytes(const huffllm_cache *cache, size_t *bytes);
+
+/*
+ * The rows of a call: sequence b has rows starts[b] .. starts[b + 1] - 1, its last tokens in order (row r is token
+ * lengths[b] - starts[b + 1] + r; a row in front of token 0 is no token: not written to the cache, and its attention is 0).  starts (device,
+ * sequences + 1 entries) null: one row per sequence.  `rows` bounds them: a sequence with a start beyond it is an error (see above).
+ * Rows of the tensors that are no sequence's are left as they were.
+ *
+ * huffllm_cache_append writes k and v (device, [rows][kv_heads][head_dim] words of the cache's dtype) into the cache.  The same token twice
+ * (two sequences sharing a page that is written) leaves either.  huffllm_cache_read gives back what the cache holds for those rows, as fp32
+ * or rounded to dtype; either output may be null.  Strides count values between rows; 0 = packed.
+ */
+huffllm_status huffllm_cache_append(const huffllm_cache *cache, const uint16_t *k_dev, const uint16_t *v_dev, uint64_t k_stride,
+                                    uint64_t v_stride, uint64_t rows, const int32_t *starts_dev, int32_t *err_flag_dev, huffllm_stream stream);
+huffllm_status huffllm_cache_read(const huffllm_cache *cache, void *k_dev, void *v_dev, uint32_t type, uint64_t k_stride, uint64_t v_stride,
+                                  uint64_t rows, const int32_t *starts_dev, int32_t *err_flag_dev, huffllm_stream stream);
+
+/*
+ * Causal attention of the rows' queries over the cache (rows and starts as above; their own keys and values appended before):
+ *     out = sum_j p_j v_j,   p = softmax(scale * q k_j) over the tokens j that the row's token i sees:
+ *     j <= i, and, where window is not 0, j > i - window or j < sinks (the first tokens stay visible)
+ * Query heads h * heads / kv_heads .. share key head h.  q and out: [rows][heads][head_dim] words of the cache's dtype; out must not overlap q.
+ * A row that sees nothing is 0.  Tokens that are not seen have no influence, whatever the cache holds for them.  Sums and softmax are fp32;
+ * probabilities and queries are multiplied in 11 bits or more; codes, scales and offsets exactly.  Results are the same from run to run.
+ * The workspace (256-byte aligned, huffllm_attention_workspace_bytes or more) is zero-filled once after allocation; its first
+ * huffllm_attention_control_bytes bytes are counters that every call leaves zero; the rest is overwritten freely.  One workspace serves every
+ * call that it is large enough for, one call at a time.
+ */
+typedef struct huffllm_attention {
+    uint32_t heads;                        /* a multiple of the cache's kv_heads */
+    float scale;
+    uint32_t window, sinks;                /* window 0: everything up to the row's token */
+    uint64_t rows, q_stride, out_stride;   /* strides 0 = packed */
+    const uint16_t *q;                     /* device */
+    uint16_t *out;                         /* device */
+    const int32_t *starts;                 /* device, or null */
+} huffllm_attention;
+huffllm_status huffllm_attention_workspace_bytes(const huffllm_cache *cache, const huffllm_attention *args, size_t *bytes);
+huffllm_status huffllm_attention_control_bytes(const huffllm_cache *cache, const huffllm_attention *args, size_t *bytes);
+huffllm_status huffllm_cache_attention(const huffllm_cache *cache, const huffllm_attention *args, void *workspace_dev, size_t workspace_bytes,
+                                       int32_t *err_flag_dev, huffllm_stream stream);
+
+/*
+ * The next token of every row of logits, from a given random number each.  With w_i = exp((x_i - max x) / temperature), and the tokens in the
+ * order of their logits, the largest first, the lower index first among equals:
+ *     top_k   the first top_k stay                                         (0 or less: all)
+ *     top_p   of these the shortest row with at least top_p of their mass  (at least the first; 1 or more: all)
+ *     min_p   of these the ones with w_i >= min_p                          (0 or less: all; 1 or more: the largest)
+ * The token is the first one (in the order of indexes) of those that stay up to which their mass is more than uniform * all of it.
+ * temperature 0 or less: the first of the largest.  A NaN logit is as good as minus infinity; where there is plus infinity, only such
+ * tokens have a mass, the same each.  A row with nothing above minus infinity gives -1.
+ * The four settings are device arrays of a value per row, or null (temperature 1, the others off); uniform is in [0, 1) (outside: the first or
+ * the last that stays).  Masses are added up in 32 bits or more, the same way in every call.  No workspace.
+ */
+typedef struct huffllm_sampling {
+    uint32_t logits_type, dtype;           /* huffllm_elem; dtype: of 16-bit logits                */
+    uint64_t rows, vocab, stride;          /* vocab at most 2^31 - 1; stride 0 = packed            */
+    const void *logits;                    /* device                                               */
+    const float *temperature;              /* device [rows] or null, like the next three           */
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+    const float *uniform;                  /* device [rows]                                        */
+    int32_t *tokens;                       /* device [rows]                                        */
+} huffllm_sampling;
+huffllm_status huffllm_sample(const huffllm_sampling *args, huffllm_stream stream);
+
 /*
  * Reference point for the compressed path: y = W x for an UNCOMPRESSED bf16 matrix (device,
  * row-major, 16-byte aligned rows, cols a multiple of 8), same fp32 accumulation, written as a

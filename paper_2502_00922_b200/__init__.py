@@ -10,4 +10,6 @@ from .binding import (  # noqa: F401
     stage_copy, split_counts_size, split_histogram, split_entropy, build_codebook_from_counts, encode_device_scratch_bytes, encode_device,
     ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH, ELEM_F32, ELEM_16, Epilogue, Norm, Ffn, decode_gemm_epilogue, gemm_epilogue_launch_plan, decode_gemm_multi_epilogue, PreparedEpilogue,
     stacked_rows, stack_gate_up, stack_gate_up_device, add_rms_norm, PreparedNorm, ffn_workspace_bytes, decode_ffn, PreparedFfn,
+    PAIR_HALVES, PAIR_NEIGHBOURS, MAX_AXES, Rotary, PreparedRotary, apply_rotary, Cache, cache_bytes, PreparedAppend, cache_append, PreparedRead, cache_read,
+    Attention, attention_workspace_bytes, attention_control_bytes, PreparedAttention, cache_attention, Sampling, PreparedSampling, sample,
 )

@@ -10,6 +10,8 @@ BF16, FP16 = 0, 1
 SPLIT_PAPER, SPLIT_WHOLE_EXPONENT = 0, 1
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = range(5)
 ELEM_F32, ELEM_16 = 0, 1
+PAIR_HALVES, PAIR_NEIGHBOURS = 0, 1
+MAX_AXES = 4
 _SO = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libhuffllm.so")
 _lib = None
 
@@ -76,6 +78,65 @@ class Ffn(C.Structure):
                          _ptr(gate_up_bias), _ptr(down_bias))
         self._keep = (gate_up, gate_up_blob, down, down_blob, gain, gate_up_bias, down_bias)
 
+
+class Rotary(C.Structure):
+    """huffllm_rotary: the arguments of rotary positions (the tensors must stay alive and in place)."""
+    _fields_ = [("dtype", C.c_uint32), ("pairing", C.c_uint32), ("head_dim", C.c_uint32), ("rotary_dim", C.c_uint32), ("axes", C.c_uint32),
+                ("in_turn", C.c_uint32), ("sections", C.c_uint32 * MAX_AXES), ("tokens", C.c_uint64), ("q_heads", C.c_uint32),
+                ("k_heads", C.c_uint32), ("positions", C.c_void_p), ("frequencies", C.c_void_p), ("q", C.c_void_p), ("k", C.c_void_p),
+                ("q_out", C.c_void_p), ("k_out", C.c_void_p), ("q_stride", C.c_uint64), ("k_stride", C.c_uint64), ("q_out_stride", C.c_uint64),
+                ("k_out_stride", C.c_uint64)]
+
+    def __init__(self, dtype: int, tokens: int, head_dim: int, positions, frequencies, q, q_heads: int, q_out, k=None, k_heads: int = 0, k_out=None,
+                 rotary_dim: int = 0, sections=None, in_turn: bool = False, pairing: int = PAIR_HALVES, q_stride: int = 0, k_stride: int = 0,
+                 q_out_stride: int = 0, k_out_stride: int = 0):
+        rotary_dim = rotary_dim or head_dim
+        sections = list(sections) if sections is not None else [rotary_dim // 2]
+        if not 1 <= len(sections) <= MAX_AXES:
+            raise ValueError(f"1 to {MAX_AXES} sections")
+        super().__init__(dtype, pairing, head_dim, rotary_dim, len(sections), int(in_turn), (C.c_uint32 * MAX_AXES)(*sections), tokens, q_heads,
+                         k_heads, _ptr(positions), _ptr(frequencies), _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), q_stride, k_stride,
+                         q_out_stride, k_out_stride)
+        self._keep = _one_device(positions, frequencies, q, k, q_out, k_out)
+
+
+class Cache(C.Structure):
+    """huffllm_cache: pages of keys and values held in 4 bits, with the page table and lengths (the tensors must stay alive and in place)."""
+    _fields_ = [("dtype", C.c_uint32), ("kv_heads", C.c_uint32), ("head_dim", C.c_uint32), ("page_tokens", C.c_uint32), ("pages", C.c_uint64),
+                ("pool", C.c_void_p), ("sequences", C.c_uint32), ("table_stride", C.c_uint32), ("table", C.c_void_p), ("lengths", C.c_void_p)]
+
+    def __init__(self, dtype: int, kv_heads: int, head_dim: int, page_tokens: int, pages: int, pool=None, table=None, lengths=None,
+                 sequences: int = 0, table_stride: int = 0):
+        """table: [sequences][table_stride] int32 tensor, lengths: [sequences]; the two numbers are taken from a table that has a shape."""
+        if table is not None and not isinstance(table, int):
+            sequences, table_stride = sequences or table.shape[0], table_stride or table.shape[1]
+        super().__init__(dtype, kv_heads, head_dim, page_tokens, pages, _ptr(pool), sequences, table_stride, _ptr(table), _ptr(lengths))
+        self._keep = _one_device(pool, table, lengths)
+
+
+class Attention(C.Structure):
+    """huffllm_attention: queries, outputs and mask of an attention over a cache (the tensors must stay alive and in place)."""
+    _fields_ = [("heads", C.c_uint32), ("scale", C.c_float), ("window", C.c_uint32), ("sinks", C.c_uint32), ("rows", C.c_uint64),
+                ("q_stride", C.c_uint64), ("out_stride", C.c_uint64), ("q", C.c_void_p), ("out", C.c_void_p), ("starts", C.c_void_p)]
+
+    def __init__(self, q, heads: int, out, rows: int, scale: float, starts=None, window: int = 0, sinks: int = 0, q_stride: int = 0,
+                 out_stride: int = 0):
+        super().__init__(heads, scale, window, sinks, rows, q_stride, out_stride, _ptr(q), _ptr(out), _ptr(starts))
+        self._keep = _one_device(q, out, starts)
+
+
+class Sampling(C.Structure):
+    """huffllm_sampling: logits, settings and random numbers of a choice of tokens (the tensors must stay alive and in place)."""
+    _fields_ = [("logits_type", C.c_uint32), ("dtype", C.c_uint32), ("rows", C.c_uint64), ("vocab", C.c_uint64), ("stride", C.c_uint64),
+                ("logits", C.c_void_p), ("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p),
+                ("uniform", C.c_void_p), ("tokens", C.c_void_p)]
+
+    def __init__(self, logits, logits_type: int, rows: int, vocab: int, uniform, tokens, dtype: int = BF16, temperature=None, top_k=None,
+                 top_p=None, min_p=None, stride: int = 0):
+        super().__init__(logits_type, dtype, rows, vocab, stride, _ptr(logits), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
+                         _ptr(uniform), _ptr(tokens))
+        self._keep = _one_device(logits, temperature, top_k, top_p, min_p, uniform, tokens)
+
 _SIGNATURES = {
     "huffllm_build_codebook": [C.c_void_p, C.c_uint64, C.c_uint64, C.c_int, C.c_uint32, C.POINTER(C.c_void_p)],
     "huffllm_build_codebook_split": [C.c_void_p, C.c_uint64, C.c_uint64, C.c_int, C.c_int, C.c_uint32, C.POINTER(C.c_void_p)],
@@ -115,6 +176,15 @@ _SIGNATURES = {
     "huffllm_ffn_workspace_bytes": [C.POINTER(Ffn), C.c_uint32, C.POINTER(C.c_size_t)],
     "huffllm_decode_ffn": [C.POINTER(Ffn), C.c_void_p, C.c_uint64, C.c_uint32, C.c_void_p, C.c_uint64, C.c_uint32, C.c_void_p, C.c_size_t,
                            C.c_void_p, C.c_void_p],
+    "huffllm_apply_rotary": [C.POINTER(Rotary), C.c_void_p],
+    "huffllm_cache_bytes": [C.POINTER(Cache), C.POINTER(C.c_size_t)],
+    "huffllm_cache_append": [C.POINTER(Cache), C.c_void_p, C.c_void_p, C.c_uint64, C.c_uint64, C.c_uint64, C.c_void_p, C.c_void_p, C.c_void_p],
+    "huffllm_cache_read": [C.POINTER(Cache), C.c_void_p, C.c_void_p, C.c_uint32, C.c_uint64, C.c_uint64, C.c_uint64, C.c_void_p, C.c_void_p,
+                           C.c_void_p],
+    "huffllm_attention_workspace_bytes": [C.POINTER(Cache), C.POINTER(Attention), C.POINTER(C.c_size_t)],
+    "huffllm_attention_control_bytes": [C.POINTER(Cache), C.POINTER(Attention), C.POINTER(C.c_size_t)],
+    "huffllm_cache_attention": [C.POINTER(Cache), C.POINTER(Attention), C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p],
+    "huffllm_sample": [C.POINTER(Sampling), C.c_void_p],
     "huffllm_stage_copy": [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p],
     "huffllm_plain_gemv": [C.c_void_p, C.c_uint64, C.c_uint64, C.c_void_p, C.c_void_p, C.c_void_p],
     "huffllm_plain_gemv_multi": [C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p],
@@ -176,6 +246,14 @@ def _ptr(t):
     if isinstance(t, np.ndarray):
         return t.ctypes.data
     return t.data_ptr()
+
+
+def _one_device(*tensors):
+    """The tensors, for keeping; a call's tensors lie on one device."""
+    devices = {t.device for t in tensors if hasattr(t, "device") and getattr(t, "is_cuda", False)}
+    if len(devices) > 1:
+        raise ValueError("tensors of one call on different devices: " + ", ".join(sorted(map(str, devices))))
+    return tensors
 
 
 def _stream(stream):
@@ -593,3 +671,104 @@ def decode_ffn(ffn: Ffn, h_dev, batch: int, out_dev, h_type: int, workspace_dev,
                h_stride: int = 0, out_stride: int = 0, stream=None):
     """huffllm_decode_ffn: out = h + down(act(gate(norm(h))) * up(norm(h))), from compressed weights."""
     PreparedFfn(ffn, h_dev, batch, out_dev, h_type, workspace_dev, workspace_bytes_, err_flag_dev, h_stride, out_stride).run(_stream(stream))
+
+
+class _Prepared:
+    """A call marshalled once; `stream` is the raw cudaStream_t value."""
+
+    def run(self, stream: int):
+        st = self._fn(*self._args, C.c_void_p(stream))
+        if st:
+            _check(st)
+
+
+class PreparedRotary(_Prepared):
+    """A huffllm_apply_rotary call, marshalled once (the tensors must stay alive and in place; so in the next classes)."""
+
+    def __init__(self, rotary: Rotary):
+        self.rotary, self._fn, self._args = rotary, _unconverted("huffllm_apply_rotary"), (C.byref(rotary),)
+
+
+def apply_rotary(rotary: Rotary, stream=None):
+    """huffllm_apply_rotary: q and k turned by their tokens' positions."""
+    PreparedRotary(rotary).run(_stream(stream))
+
+
+def cache_bytes(cache: Cache) -> int:
+    """huffllm_cache_bytes: bytes of the pool."""
+    n = C.c_size_t()
+    _check(lib().huffllm_cache_bytes(C.byref(cache), C.byref(n)))
+    return n.value
+
+
+class PreparedAppend(_Prepared):
+    """A huffllm_cache_append call, marshalled once."""
+
+    def __init__(self, cache: Cache, k_dev, v_dev, rows: int, starts=None, k_stride: int = 0, v_stride: int = 0, err_flag_dev=None):
+        self._keep = cache, _one_device(cache._keep[0], k_dev, v_dev, starts, err_flag_dev)
+        ptr = lambda t: C.c_void_p(_ptr(t))
+        self._fn = _unconverted("huffllm_cache_append")
+        self._args = (C.byref(cache), ptr(k_dev), ptr(v_dev), C.c_uint64(k_stride), C.c_uint64(v_stride), C.c_uint64(rows), ptr(starts),
+                      ptr(err_flag_dev))
+
+
+def cache_append(cache: Cache, k_dev, v_dev, rows: int, starts=None, k_stride: int = 0, v_stride: int = 0, err_flag_dev=None, stream=None):
+    """huffllm_cache_append: the rows' keys and values into the cache."""
+    PreparedAppend(cache, k_dev, v_dev, rows, starts, k_stride, v_stride, err_flag_dev).run(_stream(stream))
+
+
+class PreparedRead(_Prepared):
+    """A huffllm_cache_read call, marshalled once."""
+
+    def __init__(self, cache: Cache, k_dev, v_dev, elem_type: int, rows: int, starts=None, k_stride: int = 0, v_stride: int = 0, err_flag_dev=None):
+        self._keep = cache, _one_device(cache._keep[0], k_dev, v_dev, starts, err_flag_dev)
+        ptr = lambda t: C.c_void_p(_ptr(t))
+        self._fn = _unconverted("huffllm_cache_read")
+        self._args = (C.byref(cache), ptr(k_dev), ptr(v_dev), C.c_uint32(elem_type), C.c_uint64(k_stride), C.c_uint64(v_stride), C.c_uint64(rows),
+                      ptr(starts), ptr(err_flag_dev))
+
+
+def cache_read(cache: Cache, k_dev, v_dev, elem_type: int, rows: int, starts=None, k_stride: int = 0, v_stride: int = 0, err_flag_dev=None,
+               stream=None):
+    """huffllm_cache_read: what the cache holds for the rows, as fp32 or 16 bits."""
+    PreparedRead(cache, k_dev, v_dev, elem_type, rows, starts, k_stride, v_stride, err_flag_dev).run(_stream(stream))
+
+
+def attention_workspace_bytes(cache: Cache, attention: Attention) -> int:
+    n = C.c_size_t()
+    _check(lib().huffllm_attention_workspace_bytes(C.byref(cache), C.byref(attention), C.byref(n)))
+    return n.value
+
+
+def attention_control_bytes(cache: Cache, attention: Attention) -> int:
+    """huffllm_attention_control_bytes: the leading bytes of a workspace that are zero between calls."""
+    n = C.c_size_t()
+    _check(lib().huffllm_attention_control_bytes(C.byref(cache), C.byref(attention), C.byref(n)))
+    return n.value
+
+
+class PreparedAttention(_Prepared):
+    """A huffllm_cache_attention call, marshalled once."""
+
+    def __init__(self, cache: Cache, attention: Attention, workspace_dev, workspace_bytes_: int, err_flag_dev=None):
+        self._keep = cache, attention, _one_device(cache._keep[0], attention._keep[0], workspace_dev, err_flag_dev)
+        ptr = lambda t: C.c_void_p(_ptr(t))
+        self._fn = _unconverted("huffllm_cache_attention")
+        self._args = (C.byref(cache), C.byref(attention), ptr(workspace_dev), C.c_size_t(workspace_bytes_), ptr(err_flag_dev))
+
+
+def cache_attention(cache: Cache, attention: Attention, workspace_dev, workspace_bytes_: int, err_flag_dev=None, stream=None):
+    """huffllm_cache_attention: causal attention of the rows over the cache, with an optional window and first tokens that stay visible."""
+    PreparedAttention(cache, attention, workspace_dev, workspace_bytes_, err_flag_dev).run(_stream(stream))
+
+
+class PreparedSampling(_Prepared):
+    """A huffllm_sample call, marshalled once."""
+
+    def __init__(self, sampling: Sampling):
+        self.sampling, self._fn, self._args = sampling, _unconverted("huffllm_sample"), (C.byref(sampling),)
+
+
+def sample(sampling: Sampling, stream=None):
+    """huffllm_sample: a token for every row of logits, from given random numbers."""
+    PreparedSampling(sampling).run(_stream(stream))

@@ -10,7 +10,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(os.path.dirname(PKG), "include")
 SO = os.path.join(PKG, "libhuffllm.so")
 SOURCES = ["host_codec.cpp", "api.cu", "kernels.cu", "kernels_epilogue.cu", "kernels_tc.cu", "kernels_tc_epilogue.cu", "kernels_tc_epilogue_fp16.cu",
-           "norm.cu", "split_explorer.cu", "encode_device.cu"]
+           "norm.cu", "split_explorer.cu", "encode_device.cu", "api_step.cu", "rotary.cu", "cache.cu", "attention.cu", "sampling.cu"]
 
 
 def needs_build() -> bool:

@@ -24,10 +24,10 @@ struct DeviceSlot {
     std::atomic<int> sms{0}, smem_optin{0};
 };
 DeviceSlot g_dev[64];
-struct DeviceInfo {
-    int sms = 0, smem_optin = 0;
-};
 
+}  // namespace
+
+namespace huffllm {
 huffllm_status device_info(DeviceInfo *out) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -47,6 +47,9 @@ huffllm_status device_info(DeviceInfo *out) {
     out->smem_optin = d.smem_optin.load(std::memory_order_relaxed);
     return HUFFLLM_OK;
 }
+}  // namespace huffllm
+
+namespace {
 
 // Scratch layout of one matrix's workspace:
 //   [0, 4096)            arrival counters of the register-path kernel (one per CTA: 2048 bytes), and behind them two counters of the

@@ -29,6 +29,12 @@ constexpr uint64_t kTailSlack = 4096;
 huffllm_status fail(huffllm_status st, const char *fmt, ...);
 void clear_error();
 
+// The current device's facts (api.cu).
+struct DeviceInfo {
+    int sms = 0, smem_optin = 0;
+};
+huffllm_status device_info(DeviceInfo *out);
+
 // Geometry checks common to host and device calls; returns OK or sets the error.
 huffllm_status check_desc(const huffllm_desc *d);
 
