@@ -178,11 +178,13 @@ huffllm_status huffllm_attention_control_bytes(const huffllm_cache *cache, const
     if (!bytes) return fail(HUFFLLM_ERR_INVALID_ARG, "bytes is null");
     const huffllm_status st = check_attention(cache, args, false);
     if (st != HUFFLLM_OK) return st;
-    *bytes = 4096;
+    *bytes = kAttentionCtas * sizeof(unsigned int);
     return HUFFLLM_OK;
 }
 huffllm_status huffllm_attention_workspace_bytes(const huffllm_cache *cache, const huffllm_attention *args, size_t *bytes) {
-    return huffllm_attention_control_bytes(cache, args, bytes);
+    const huffllm_status st = huffllm_attention_control_bytes(cache, args, bytes);
+    if (st == HUFFLLM_OK) *bytes += (size_t)kAttentionCtas * 2 * kAttentionPartial * sizeof(float);
+    return st;
 }
 
 huffllm_status huffllm_cache_attention(const huffllm_cache *cache, const huffllm_attention *args, void *workspace, size_t workspace_bytes,
@@ -213,6 +215,8 @@ huffllm_status huffllm_cache_attention(const huffllm_cache *cache, const huffllm
     k.sinks = a.sinks;
     k.scale = a.scale;
     k.err = err_flag;
+    k.tickets = (unsigned int *)workspace;
+    k.partials = (float *)((uint8_t *)workspace + kAttentionCtas * sizeof(unsigned int));
     DeviceInfo dev;
     if ((st = device_info(&dev)) != HUFFLLM_OK) return st;
     return launched(launch_attention(k, dev.sms, (cudaStream_t)stream), "attention");

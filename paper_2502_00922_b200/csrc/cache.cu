@@ -70,6 +70,8 @@ __global__ void __launch_bounds__(kCacheThreads) cache_append_kernel(const __gri
         if (lane == 0) {
             *(__half *)(block + (side ? value_scale_at(C.dim, r, g) : key_scale_at(C.dim, r, g))) = s;
             *(__half *)(block + (side ? value_offset_at(C.dim, r, g) : key_offset_at(C.dim, r, g))) = m;
+            // (keys' offsets are read in pairs, and what is read is multiplied by 0: it must be a number)
+            if (side == 0 && g + 1 == cache_groups(C.dim) && g % 2 == 0) *(__half *)(block + key_offset_at(C.dim, r, g + 1)) = __ushort_as_half(0);
         }
     }
 }

@@ -2,6 +2,7 @@
 // sampling.
 #pragma once
 #include <cuda_runtime.h>
+#include <atomic>
 #include <cstdint>
 
 namespace huffllm {
@@ -35,6 +36,8 @@ struct CacheRows {
 cudaError_t launch_cache_append(const CacheArgs &c, const CacheRows &r, uint32_t sms, cudaStream_t stream);
 cudaError_t launch_cache_read(const CacheArgs &c, const CacheRows &r, uint32_t sms, cudaStream_t stream);
 
+constexpr uint32_t kAttentionCtas = 512;                  // most CTAs of a launch
+constexpr uint32_t kAttentionPartial = 16 * 132;          // most floats of a piece (a column's channels and four more: 16 columns of 128, eight of 256)
 struct AttentionArgs {
     CacheArgs c;
     const uint16_t *q;
@@ -46,7 +49,7 @@ struct AttentionArgs {
     float scale;
     int32_t *err;                  // may be null
     unsigned int *tickets;         // zero between calls
-    float *partials;
+    float *partials;               // two pieces a CTA
 };
 cudaError_t launch_attention(const AttentionArgs &a, uint32_t sms, cudaStream_t stream);
 
