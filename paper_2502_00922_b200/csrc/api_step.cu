@@ -213,6 +213,8 @@ huffllm_status huffllm_cache_attention(const huffllm_cache *cache, const huffllm
     k.group = a.heads / cache->kv_heads;
     k.window = a.window;
     k.sinks = a.sinks;
+    const uint64_t page_blocks = cache->page_tokens / kCacheBlock;
+    k.page_recip = page_blocks == 1 ? 0xFFFFFFFFu : (uint32_t)((1ull << 32) / page_blocks);
     k.scale = a.scale;
     k.err = err_flag;
     k.tickets = (unsigned int *)workspace;

@@ -8,9 +8,9 @@
 //            sum is a product of its own too, and a row of ones in it gives the sum of the p_t
 // The tokens are the rows of the first product and the columns of the second: its B operand is the first's result transposed (movmatrix).
 //
-// Work is cut evenly: the steps of 32 tokens of all (sequence, tile of rows, key head) stand in one line, of which every CTA takes the same
-// length; its warps deal the steps of a piece among themselves and add up in shared memory.  Pieces of one line segment that more than one CTA
-// works on meet in the workspace, where the last CTA to arrive adds them up in their order.
+// Work is cut evenly: the steps of 32 tokens of all units (sequence, key head, tile of rows) stand in one line, of which every CTA takes the
+// same length, and of that every warp.  A warp that has all of a unit writes its output; what warps of one CTA have of a unit meets in shared
+// memory, behind the line's end, and what CTAs have of one in the workspace, where the last CTA to arrive adds it up, in the line's order.
 #include <cuda_runtime.h>
 
 #include "cache_rows.cuh"
@@ -21,18 +21,19 @@ namespace huffllm {
 
 constexpr uint32_t kStepTokens = 2 * kCacheBlock;
 constexpr uint32_t kWaitTries = 1u << 22;
+constexpr int kSlack = 4;                        // a weight's exponent is set this far below its cap, so that few later ones are above it
 
 template <int DIM, int NT>
 struct AttentionShape {
     static constexpr int kGroups = DIM / 32, kCols = 8 * NT;
-    static constexpr int kWarps = DIM * NT <= 128 ? 16 : 8;
-    static constexpr int kStages = 2;
+    static constexpr int kWarps = DIM * NT <= 128 ? 12 : 8;
+    static constexpr int kStages = DIM * NT == 256 && DIM == 128 ? 3 : 2;
     static constexpr uint32_t kBlockBytes = cache_block_bytes(DIM);
     static constexpr uint32_t kRingBytes = kWarps * kStages * 2 * kBlockBytes;
     static constexpr uint32_t kRow = DIM + 4;                    // floats of a column's sums: two of the last four are its reference and weight
-    static constexpr uint32_t kMergeBytes = kWarps * kCols * kRow * 4;
-    static constexpr uint32_t kSmem = kRingBytes + kMergeBytes;
-    static constexpr uint32_t kPartial = kCols * kRow;           // floats of a piece in the workspace
+    static constexpr uint32_t kPiece = kCols * kRow;             // floats of what is known of a unit
+    static constexpr uint32_t kSmem = kRingBytes + kWarps * kPiece * 4;
+    static_assert(kStages * 2 * kBlockBytes >= kPiece * 4, "a warp's last piece lies where its copies did");
 };
 
 // Steps that some row of a sequence sees: the first tokens', then from the window's on.
@@ -46,7 +47,7 @@ __device__ __forceinline__ Steps steps_of(const Sequence &S, uint32_t window, ui
     const uint32_t end = (uint32_t)(S.tokens - 1) / kStepTokens + 1;
     if (window) {
         const int64_t first = (int64_t)S.tokens - S.rows - window + 1;
-        if (first > 0) s.from = (uint32_t)(first / kStepTokens);
+        if (first > 0) s.from = (uint32_t)first / kStepTokens;
         const uint32_t seen = min(sinks, (uint32_t)S.tokens);
         s.sink_end = min((seen + kStepTokens - 1) / kStepTokens, s.from);
     }
@@ -54,20 +55,38 @@ __device__ __forceinline__ Steps steps_of(const Sequence &S, uint32_t window, ui
     return s;
 }
 
+// What is known of a unit that a warp had a part of.
+struct Piece {
+    uint64_t begin;                                              // where in the line the unit begins
+    uint32_t count;                                              // its steps (0: no piece)
+    uint32_t first_row, rows, head, row0;                        // of the sequence: its first row, all its rows times heads; of the unit: key head, first row
+};
 // A stretch of the line: one unit (sequence, key head, tile of rows), its steps x .. end - 1.
 struct Walk {
-    uint64_t left;                                               // steps of the CTA behind this stretch
-    uint32_t b, unit, units, x, end;
+    uint64_t left;                                               // steps of the warp behind this stretch
+    uint32_t b, unit, units, x, end, tiles;
+    uint32_t head, row0;                                         // of the unit: key head, first row of the tile
+    int32_t lo, hi, from;                                        // tokens of the tile's first and last row; the first one that the first row's window has
     Sequence S;
     Steps steps;
-    uint32_t tiles;
     __device__ __forceinline__ void load(const AttentionArgs &A, uint32_t cols) {
         S = sequence_of(A.c, A.starts, A.rows, b);
         steps = steps_of(S, A.window, A.sinks);
         tiles = (S.rows * A.group + cols - 1) / cols;
         units = tiles * A.c.kv_heads;
     }
-    // on to the next unit; false at the end of the CTA's line
+    __device__ __forceinline__ void take(const AttentionArgs &A, uint32_t cols) {
+        head = unit / tiles;
+        row0 = unit % tiles * cols;
+        const int32_t first = S.tokens - (int32_t)S.rows;
+        lo = first + (int32_t)(row0 / A.group);
+        hi = first + (int32_t)((min(row0 + cols, S.rows * A.group) - 1) / A.group);
+        from = first_seen(A, lo);
+        const uint32_t room = steps.count - x;
+        end = left < room ? x + (uint32_t)left : steps.count;
+        left -= end - x;
+    }
+    // on to the next unit; false at the end of the warp's line
     __device__ __forceinline__ bool next(const AttentionArgs &A, uint32_t cols) {
         if (left == 0) return false;
         ++unit;
@@ -77,13 +96,19 @@ struct Walk {
             load(A, cols);
         }
         x = 0;
-        take();
+        take(A, cols);
         return true;
     }
-    __device__ __forceinline__ void take() {
-        const uint32_t room = steps.count - x;
-        end = left < room ? x + (uint32_t)left : steps.count;
-        left -= end - x;
+    static __device__ __forceinline__ int32_t first_seen(const AttentionArgs &A, int32_t pos) {
+        return A.window && (int64_t)pos >= (int64_t)A.window ? pos - (int32_t)A.window + 1 : 0;
+    }
+    // does some row of the tile see one of the tokens t .. t + n - 1?
+    __device__ __forceinline__ bool any_seen(const AttentionArgs &A, uint32_t t, uint32_t n) const {
+        return (int32_t)t <= hi && ((int32_t)(t + n) > from || t < A.sinks);
+    }
+    // does every row see all tokens of the step from t on?
+    __device__ __forceinline__ bool all_seen(const AttentionArgs &A, uint32_t t) const {
+        return (int32_t)(t + kStepTokens) <= lo + 1 && ((int32_t)t >= first_seen(A, hi) || t + kStepTokens <= A.sinks);
     }
 };
 
@@ -137,6 +162,14 @@ __device__ __forceinline__ void lds_words(uint32_t at, uint32_t *w) {
 __device__ __forceinline__ float low_half(uint32_t w) { return __half2float(__ushort_as_half((uint16_t)w)); }
 __device__ __forceinline__ float high_half(uint32_t w) { return __half2float(__ushort_as_half((uint16_t)(w >> 16))); }
 
+// Products alone, without a sum to add them to
+__device__ __forceinline__ void mma_f16_16816_new(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+}
+__device__ __forceinline__ void sts32(uint32_t at, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
+
 template <int DIM, int NT>
 __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32, 1) attention_kernel(const __grid_constant__ AttentionArgs A) {
     using Shape = AttentionShape<DIM, NT>;
@@ -146,122 +179,116 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32, 1) atten
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) uint64_t s_bar[W * STAGES];
     __shared__ uint32_t s_here[W * STAGES][2];                   // blocks of a stage that are there
-    __shared__ uint64_t s_scan[W + 1], s_found_left;
-    __shared__ uint32_t s_found_b, s_last;
-    float *const merge = (float *)(smem + Shape::kRingBytes);
+    __shared__ Piece s_piece[W][2];
+    __shared__ uint32_t s_last[2];
+    float *const first_pieces = (float *)(smem + Shape::kRingBytes);
+    auto piece_at = [&](uint32_t w, uint32_t which) { return which ? (float *)(smem + w * STAGES * 2 * BLOCK) : first_pieces + w * Shape::kPiece; };
     const CacheArgs &C = A.c;
     const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32, g = lane / 4, t4 = lane % 4;
 
     if (lane < STAGES) mbar_init(smem_u32(&s_bar[warp * STAGES + lane]), 1);
+    if (lane < 2) s_piece[warp][lane].count = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     pdl_launch_dependents();
     pdl_wait_prior_grid();
     if (blockIdx.x == 0) report_faults(C, A.starts, A.rows, A.err);
 
-    // The line: how long it is, and where in it this CTA starts.
+    // The line: how long it is, and where in it this CTA starts (every warp finds out by itself).
     auto weight_of = [&](uint32_t b) -> uint64_t {
         if (b >= C.sequences) return 0;
         const Sequence S = sequence_of(C, A.starts, A.rows, b);
         return (uint64_t)((S.rows * A.group + COLS - 1) / COLS) * C.kv_heads * steps_of(S, A.window, A.sinks).count;
     };
-    uint64_t total = 0, mine = weight_of(tid);
-    for (uint32_t b0 = 0; b0 < C.sequences; b0 += THREADS) {
-        uint64_t w = b0 ? weight_of(b0 + tid) : mine;
-        for (int o = 16; o; o >>= 1) w += __shfl_xor_sync(kFull, w, o);
-        total += w;
-    }
-    if (lane == 0) s_scan[warp] = total;
-    if (tid == 0) s_found_b = 0, s_found_left = 0;
-    __syncthreads();
-    total = 0;
-    for (int i = 0; i < W; ++i) total += s_scan[i];
+    const uint64_t first = weight_of(lane);
+    uint64_t total = first;
+    for (uint32_t b0 = 32; b0 < C.sequences; b0 += 32) total += weight_of(b0 + lane);
+    for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(kFull, total, o);
     if (total == 0) return;
-    // (as many CTAs as find at least a step for every other warp)
+    // (as many CTAs as find at least a step for every other of their warps)
     const uint64_t ctas = min((uint64_t)gridDim.x, max((uint64_t)1, (total + W / 2 - 1) / (W / 2)));
     if (blockIdx.x >= ctas) return;
-    const uint64_t line_from = blockIdx.x * total / ctas, line_to = (blockIdx.x + 1) * total / ctas;
+    const uint64_t cta_from = blockIdx.x * total / ctas, cta_to = (blockIdx.x + 1) * total / ctas;
+    // (warps without a step are the last ones: a unit's pieces are those of warps that follow each other)
+    const uint64_t each = (cta_to - cta_from) / W, rest = (cta_to - cta_from) % W;
+    const uint64_t line_from = cta_from + each * warp + min((uint64_t)warp, rest), line_to = line_from + each + (warp < rest ? 1 : 0);
+
+    if (line_from < line_to) {
+    Walk ahead;                                                  // the stretch that copies are asked for; `at` is the one worked on
     uint64_t before = 0;
-    for (uint32_t b0 = 0; b0 < C.sequences; b0 += THREADS) {
-        const uint64_t w = b0 ? weight_of(b0 + tid) : mine;
+    for (uint32_t b0 = 0;; b0 += 32) {
+        const uint64_t w = b0 ? weight_of(b0 + lane) : first;
         uint64_t sum = w;
         for (int o = 1; o < 32; o <<= 1) {
             const uint64_t up = __shfl_up_sync(kFull, sum, o);
             if (lane >= o) sum += up;
         }
-        __syncthreads();
-        if (lane == 31) s_scan[warp] = sum;
-        __syncthreads();
-        uint64_t ahead = before;
-        for (uint32_t i = 0; i < W; ++i) {
-            if (i < warp) ahead += s_scan[i];
-            before += s_scan[i];
+        const uint32_t behind = __ballot_sync(kFull, before + sum > line_from);
+        if (behind) {                                            // (there is one: the line goes on behind its start)
+            const int k = __ffs(behind) - 1;
+            ahead.b = b0 + k;
+            before += __shfl_sync(kFull, sum - w, k);
+            break;
         }
-        const uint64_t to = ahead + sum, from = to - w;
-        if (from <= line_from && line_from < to) s_found_b = b0 + tid, s_found_left = line_from - from;
+        before += __shfl_sync(kFull, sum, 31);
     }
-    __syncthreads();
-
-    Walk ahead;                                                  // the stretch that copies are asked for; `at` is the one worked on
-    ahead.b = s_found_b;
     ahead.load(A, COLS);
-    ahead.unit = (uint32_t)(s_found_left / ahead.steps.count);
-    ahead.x = (uint32_t)(s_found_left % ahead.steps.count);
+    ahead.unit = (uint32_t)((line_from - before) / ahead.steps.count);
+    ahead.x = (uint32_t)((line_from - before) % ahead.steps.count);
     ahead.left = line_to - line_from;
-    ahead.take();
+    ahead.take(A, COLS);
     Walk at = ahead;
     uint64_t at_first = line_from - at.x;                        // where in the line the unit begins
     bool more = true;
-    uint32_t next_x = ahead.x + warp;
+    uint32_t next_x = ahead.x;
 
     const uint32_t ring = smem_u32(smem) + warp * STAGES * 2 * BLOCK;
     const uint32_t bars = smem_u32(&s_bar[warp * STAGES]);
-    // Rows of a unit's tile: positions of its first and last token, and its key head.
-    auto tile_of = [&](const Walk &w, int32_t &lo, int32_t &hi) {
-        const uint32_t tile = w.unit % w.tiles, r0 = tile * COLS, r1 = min(r0 + COLS, w.S.rows * A.group) - 1;
-        const int32_t first = w.S.tokens - (int32_t)w.S.rows;
-        lo = first + (int32_t)(r0 / A.group);
-        hi = first + (int32_t)(r1 / A.group);
-    };
-    // Does a row of the tile see one of tokens t .. t + n - 1?
-    auto any_seen = [&](uint32_t t, uint32_t n, int32_t lo, int32_t hi) -> bool {
-        return (int32_t)t <= hi && (!A.window || (int64_t)t + n > (int64_t)lo - A.window + 1 || t < A.sinks);
-    };
-    // Ask for the warp's next step.
-    auto ask = [&](uint32_t stage) {
+    // The warp's next step: the page of a block (lanes 0 and 1 have one each) is looked up when the step in front of it is asked for.
+    const uint32_t page_blocks = C.page_tokens / kCacheBlock;
+    uint32_t in_page = 0;
+    int32_t page = -1;
+    bool wanted = false;
+    auto look_up = [&]() {
         while (more && next_x >= ahead.end) {
             more = ahead.next(A, COLS);
-            next_x = ahead.x + warp;
+            next_x = ahead.x;
         }
+        wanted = false;
+        if (more && lane < 2) {
+            const uint32_t block = ahead.steps.step(next_x) * 2 + lane;
+            wanted = ahead.any_seen(A, block * kCacheBlock, kCacheBlock);
+            uint32_t i = __umulhi(block, A.page_recip);          // block / page_blocks, or one less
+            in_page = block - i * page_blocks;
+            if (in_page >= page_blocks) ++i, in_page -= page_blocks;
+            if (wanted) page = __ldcg(C.table + (uint64_t)ahead.b * C.table_stride + i);
+        }
+    };
+    auto ask = [&](uint32_t stage) {
         if (!more) return;
-        const uint8_t *src = nullptr;
-        if (lane < 2) {
-            int32_t lo, hi;
-            tile_of(ahead, lo, hi);
-            const uint32_t t = ahead.steps.step(next_x) * kStepTokens + lane * kCacheBlock;
-            if (any_seen(t, kCacheBlock, lo, hi)) {
-                src = block_of(C, ahead.b, t, ahead.unit / ahead.tiles);
-                if (!src && A.err) *A.err = (int32_t)ahead.b + 1;
-            }
-            s_here[warp * STAGES + stage][lane] = src != nullptr;
-        }
-        const uint32_t count = __popc(__ballot_sync(kFull, src != nullptr));
+        const bool here = wanted && page >= 0 && (uint32_t)page < C.pages;
+        if (wanted && !here && A.err) *A.err = (int32_t)ahead.b + 1;
+        if (lane < 2) s_here[warp * STAGES + stage][lane] = here;
+        const uint32_t count = __popc(__ballot_sync(kFull, here));
         if (lane == 0) mbar_expect_tx(bars + 8 * stage, count * BLOCK);
         __syncwarp();
-        if (src) bulk_g2s(ring + (stage * 2 + lane) * BLOCK, src, BLOCK, bars + 8 * stage);
-        next_x += W;
+        if (here) {
+            const uint64_t block = ((uint64_t)page * C.kv_heads + ahead.head) * page_blocks + in_page;
+            bulk_g2s(ring + (stage * 2 + lane) * BLOCK, C.pool + block * BLOCK, BLOCK, bars + 8 * stage);
+        }
+        ++next_x;
+        look_up();
     };
     __syncwarp();
+    look_up();
     for (uint32_t s = 0; s < STAGES; ++s) ask(s);
 
     uint32_t stage = 0, phase = 0;
     for (bool on = true; on; at_first += at.steps.count, on = at.next(A, COLS)) {
         // ---- the tile's queries, as B operands: column n of a lane is its g, rows its t4's eight channels of a group
-        const uint32_t head = at.unit / at.tiles, row0 = at.unit % at.tiles * COLS, rows_all = at.S.rows * A.group;
+        const uint32_t head = at.head, row0 = at.row0, rows_all = at.S.rows * A.group;
         uint32_t q[NT][G][4], q_sum[NT][2];
         float factor[NT][2];
         int32_t pos[NT][2];
-        int32_t lo, hi;
-        tile_of(at, lo, hi);
         const bool wide = !(((uintptr_t)A.q & 15) || A.q_stride % 8);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -331,8 +358,9 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32, 1) atten
             }
         }
 
-        float acc[NT][2 * G][4], off[NT][4], top[NT][2], ref[NT][2];
-        int head_room = 15;                                      // weights are at most 2^head_room: below 2^14 times the largest scale yet
+        float acc[NT][2 * G][4], off[NT][4], ref[NT][2];         // weights are 2^(score - ref)
+        float cap[NT][2];                                        // ... of at most 2^cap (minus infinity: the row has not seen a token yet)
+        int room = 15;                                           // the next cap: 2^room times the largest scale of the values yet is below 2^14
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -341,10 +369,11 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32, 1) atten
                 for (int c = 0; c < 4; ++c) acc[n][j][c] = 0.0f;
 #pragma unroll
             for (int c = 0; c < 4; ++c) off[n][c] = 0.0f;
-            top[n][0] = top[n][1] = ref[n][0] = ref[n][1] = -INFINITY;
+            ref[n][0] = ref[n][1] = 0.0f;
+            cap[n][0] = cap[n][1] = -INFINITY;
         }
 
-        for (uint32_t x = at.x + warp; x < at.end; x += W) {
+        for (uint32_t x = at.x; x < at.end; ++x) {
             {
                 uint32_t tries = 0;
                 while (!mbar_try_wait(bars + 8 * stage, phase) && ++tries < kWaitTries) {}
@@ -353,9 +382,21 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32, 1) atten
             const uint32_t base = at.steps.step(x) * kStepTokens, slot = ring + stage * 2 * BLOCK;
             const bool here0 = s_here[warp * STAGES + stage][0], here1 = s_here[warp * STAGES + stage][1];
             if (here0 || here1) {
-                // every token of the step seen by every row?
-                const bool whole = here0 && here1 && (int32_t)(base + kStepTokens - 1) <= lo &&
-                                   (!A.window || (int64_t)base > (int64_t)hi - A.window || base + kStepTokens <= A.sinks);
+                const bool whole = here0 && here1 && at.all_seen(A, base);
+                if (!whole) {
+                    // what nobody sees may hold anything: its scales and offsets of values become 0, its scores (below) minus infinity
+#pragma unroll 1
+                    for (uint32_t w = lane; w < 16 * G; w += 32) {
+                        const uint32_t k = w / (8 * G), i = w % (8 * G), t = base + k * kCacheBlock + i / (2 * G) * 2 + (i & 1) * 8;
+                        const bool here = k ? here1 : here0;
+                        const uint32_t mask = (here && at.any_seen(A, t, 1) ? 0xFFFFu : 0u) | (here && at.any_seen(A, t + 1, 1) ? 0xFFFF0000u : 0u);
+                        const uint32_t s_at = slot + k * BLOCK + value_scale_at(DIM, 0, 0) + i * 4, m_at = slot + k * BLOCK + value_offset_at(DIM, 0, 0) + i * 4;
+                        sts32(s_at, lds32(s_at) & mask);
+                        sts32(m_at, lds32(m_at) & mask);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                }
                 float score[2][NT][4];
                 uint32_t most2 = 0;
 #pragma unroll
@@ -380,8 +421,8 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32, 1) atten
                     const uint32_t mb = t4 < HW ? lds32(blk + key_offset_at(DIM, 0, 0) + ((g + 8) * HW + t4) * 4) : 0u;
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        float d[4] = {0, 0, 0, 0};
-                        mma_f16_16816(d, ma, mb, ma, mb, q_sum[n][0], q_sum[n][1]);
+                        float d[4];
+                        mma_f16_16816_new(d, ma, mb, ma, mb, q_sum[n][0], q_sum[n][1]);
 #pragma unroll
                         for (int c = 0; c < 4; ++c) score[k][n][c] = d[c] * 0x1p-19f;
                     }
@@ -391,8 +432,8 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32, 1) atten
                         const uint32_t a8 = wa[i] >> 8, b8 = wb[i] >> 8;
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            float d[4] = {0, 0, 0, 0};
-                            mma_f16_16816(d, wa[i] & 0x000F000Fu, wb[i] & 0x000F000Fu, wa[i] & 0x00F000F0u, wb[i] & 0x00F000F0u, q[n][i][0], q[n][i][1]);
+                            float d[4];
+                            mma_f16_16816_new(d, wa[i] & 0x000F000Fu, wb[i] & 0x000F000Fu, wa[i] & 0x00F000F0u, wb[i] & 0x00F000F0u, q[n][i][0], q[n][i][1]);
                             mma_f16_16816(d, a8 & 0x000F000Fu, b8 & 0x000F000Fu, a8 & 0x00F000F0u, b8 & 0x00F000F0u, q[n][i][2], q[n][i][3]);
                             score[k][n][0] = fmaf(d[0], fa, score[k][n][0]);
                             score[k][n][1] = fmaf(d[1], fa, score[k][n][1]);
@@ -400,57 +441,100 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32, 1) atten
                             score[k][n][3] = fmaf(d[3], fb, score[k][n][3]);
                         }
                     }
-                    // the largest scale of the block's values
+                    // the largest scale of the block's values (as whole numbers: they are not negative, and a NaN is larger than any)
 #pragma unroll
-                    for (int i = 0; i < 8 * G; i += 32) {
-                        const uint32_t w = i + lane;
-                        uint32_t s2 = w < 8 * G ? lds32(blk + value_scale_at(DIM, 0, 0) + w * 4) : 0u;
-                        if (!whole) {                            // (tokens that nobody sees may hold anything)
-                            const uint32_t t = base + k * kCacheBlock + w / (2 * G) * 2 + (w & 1) * 8;
-                            const bool here = k ? here1 : here0;
-                            if (!here || !any_seen(t, 1, lo, hi)) s2 &= 0xFFFF0000u;
-                            if (!here || !any_seen(t + 1, 1, lo, hi)) s2 &= 0x0000FFFFu;
-                        }
-                        const __half2 h = __hmax2(*(const __half2 *)&most2, *(const __half2 *)&s2);
-                        most2 = *(const uint32_t *)&h;
-                    }
+                    for (int i = 0; i < 8 * G; i += 32)
+                        if (8 * G % 32 == 0 || i + lane < 8 * G) most2 = __vmaxu2(most2, lds32(blk + value_scale_at(DIM, 0, 0) + (i + lane) * 4));
                 }
-                const uint32_t most = __reduce_max_sync(kFull, max(most2 & 0xFFFFu, most2 >> 16));
-                head_room = min(head_room, 28 - (int)(most >> 10));
+                // to exponents of the weights
+                bool over = (max(most2 & 0xFFFFu, most2 >> 16) >> 10) > (uint32_t)(28 - room);
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    float alpha[2];
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        float m = -INFINITY;
+                    for (int k = 0; k < 2; ++k)
 #pragma unroll
-                        for (int k = 0; k < 2; ++k)
+                        for (int c = 0; c < 4; ++c) score[k][n][c] = fmaf(score[k][n][c], factor[n][c & 1], -ref[n][c & 1]);
+                if (!whole) {
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                float v = score[k][n][2 * h + c] * factor[n][c];
-                                if (!whole) {
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            const int32_t seen_from = Walk::first_seen(A, pos[n][c]);
+#pragma unroll
+                            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) {
                                     const int32_t t = (int32_t)(base + k * kCacheBlock + h * 8 + g);
-                                    const bool seen = (k ? here1 : here0) && t <= pos[n][c] &&
-                                                      (!A.window || (int64_t)t > (int64_t)pos[n][c] - A.window || (uint32_t)t < A.sinks);
-                                    v = seen ? v : -INFINITY;
+                                    const bool seen = (k ? here1 : here0) && t <= pos[n][c] && (t >= seen_from || (uint32_t)t < A.sinks);
+                                    if (!seen) score[k][n][2 * h + c] = -INFINITY;
                                 }
-                                score[k][n][2 * h + c] = v;
-                                m = fmaxf(m, v);
-                            }
-                        m = fmaxf(m, __shfl_xor_sync(kFull, m, 4));
-                        m = fmaxf(m, __shfl_xor_sync(kFull, m, 8));
-                        m = fmaxf(m, __shfl_xor_sync(kFull, m, 16));
-                        top[n][c] = fmaxf(top[n][c], m);
-                        const float r = top[n][c] - (float)head_room;
-                        alpha[c] = r == -INFINITY ? 0.0f : ex2(ref[n][c] - r);
-                        ref[n][c] = r;
-                    }
+                        }
+                }
 #pragma unroll
-                    for (int j = 0; j < 2 * G; ++j) {
-                        acc[n][j][0] *= alpha[0], acc[n][j][1] *= alpha[1];
-                        acc[n][j][2] *= alpha[0], acc[n][j][3] *= alpha[1];
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+                        over = over || fmaxf(fmaxf(score[0][n][c], score[0][n][2 + c]), fmaxf(score[1][n][c], score[1][n][2 + c])) > cap[n][c];
+                if (__any_sync(kFull, over)) {
+                    // weights too large for what they are relative to, the first that a row sees, or scales larger than any yet
+                    uint32_t most = __reduce_max_sync(kFull, max(most2 & 0xFFFFu, most2 >> 16));
+                    if (most >= 0x7C00u) {
+                        // groups of values that stand for NaN: the rows that see one get it by way of the offsets, and its scale becomes 0
+                        most = 0;
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const uint32_t scales = slot + k * BLOCK + value_scale_at(DIM, 0, 0);
+                            uint2 s = make_uint2(0, 0);
+                            if (g < G) s = lds64(scales + (t4 * G + g) * 8);
+                            auto nans = [](uint32_t h2) { return ((h2 & 0x7FFFu) > 0x7C00u ? 0x3C00u : 0u) | ((h2 & 0x7FFF0000u) > 0x7C000000u ? 0x3C000000u : 0u); };
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) {
+                                auto seen = [&](int c) { return score[k][n][c] > -INFINITY ? 1.0f : 0.0f; };
+                                const uint32_t b0 = transposed(pack_half2(seen(0), seen(1))), b1 = transposed(pack_half2(seen(2), seen(3)));
+                                float d[4];
+                                mma_f16_16816_new(d, nans(s.x), 0u, nans(s.y), 0u, b0, b1);
+                                off[n][0] = d[0] > 0.0f ? NAN : off[n][0];
+                                off[n][1] = d[1] > 0.0f ? NAN : off[n][1];
+                            }
+                            __syncwarp();
+#pragma unroll 1
+                            for (uint32_t w = lane; w < 8 * G; w += 32) {
+                                uint32_t h2 = lds32(scales + w * 4);
+                                h2 &= ((h2 & 0x7FFFu) > 0x7C00u ? 0u : 0xFFFFu) | ((h2 & 0x7FFF0000u) > 0x7C000000u ? 0u : 0xFFFF0000u);
+                                sts32(scales + w * 4, h2);
+                                most = max(most, max(h2 & 0xFFFFu, h2 >> 16));
+                            }
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        most = __reduce_max_sync(kFull, most);
                     }
-                    off[n][0] *= alpha[0], off[n][1] *= alpha[1], off[n][2] *= alpha[0], off[n][3] *= alpha[1];
+                    room = min(room, 28 - (int)(most >> 10));
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        float alpha[2];
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            float m = fmaxf(fmaxf(score[0][n][c], score[0][n][2 + c]), fmaxf(score[1][n][c], score[1][n][2 + c]));
+                            m = fmaxf(m, __shfl_xor_sync(kFull, m, 4));
+                            m = fmaxf(m, __shfl_xor_sync(kFull, m, 8));
+                            m = fmaxf(m, __shfl_xor_sync(kFull, m, 16));
+                            const bool none = cap[n][c] == -INFINITY;        // (nothing seen yet)
+                            float by = 0.0f;
+                            if (m > fminf(cap[n][c], (float)room)) by = m - (float)(room - kSlack);
+                            alpha[c] = none ? 0.0f : ex2(-by);
+                            ref[n][c] += by;
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) score[k][n][c] -= by, score[k][n][2 + c] -= by;
+                            if (!none || m > -INFINITY) cap[n][c] = (float)room;
+                        }
+#pragma unroll
+                        for (int j = 0; j < 2 * G; ++j) {
+                            acc[n][j][0] *= alpha[0], acc[n][j][1] *= alpha[1];
+                            acc[n][j][2] *= alpha[0], acc[n][j][3] *= alpha[1];
+                        }
+                        off[n][0] *= alpha[0], off[n][1] *= alpha[1], off[n][2] *= alpha[0], off[n][3] *= alpha[1];
+                    }
                 }
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
@@ -458,18 +542,11 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32, 1) atten
                     uint32_t p[NT][2];
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        const float r0 = ref[n][0] == -INFINITY ? 0.0f : ref[n][0], r1 = ref[n][1] == -INFINITY ? 0.0f : ref[n][1];
-                        p[n][0] = transposed(pack_half2(ex2(score[k][n][0] - r0), ex2(score[k][n][1] - r1)));
-                        p[n][1] = transposed(pack_half2(ex2(score[k][n][2] - r0), ex2(score[k][n][3] - r1)));
+                        p[n][0] = transposed(pack_half2(ex2(score[k][n][0]), ex2(score[k][n][1])));
+                        p[n][1] = transposed(pack_half2(ex2(score[k][n][2]), ex2(score[k][n][3])));
                     }
                     uint2 m = make_uint2(0, 0);
                     if (g < G) m = lds64(blk + value_offset_at(DIM, 0, 0) + (t4 * G + g) * 8);
-                    if (!whole) {
-                        const bool here = k ? here1 : here0;
-                        const uint32_t t = base + k * kCacheBlock + 2 * t4;
-                        m.x &= (here && any_seen(t, 1, lo, hi) ? 0xFFFFu : 0u) | (here && any_seen(t + 1, 1, lo, hi) ? 0xFFFF0000u : 0u);
-                        m.y &= (here && any_seen(t + 8, 1, lo, hi) ? 0xFFFFu : 0u) | (here && any_seen(t + 9, 1, lo, hi) ? 0xFFFF0000u : 0u);
-                    }
                     const uint32_t ones = g == 0 ? 0x3C003C00u : 0u;
 #pragma unroll
                     for (int n = 0; n < NT; ++n) mma_f16_16816(off[n], m.x, ones, m.y, ones, p[n][0], p[n][1]);
@@ -485,11 +562,7 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32, 1) atten
                         const uint2 s = lds64(blk + value_scale_at(DIM, 0, 0) + (t4 * G + i) * 8);
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            uint32_t p0 = mul_half2(p[n][0], s.x), p1 = mul_half2(p[n][1], s.y);
-                            if (!whole) {                        // (what a row does not see is nothing, whatever its scale)
-                                p0 &= ((p[n][0] & 0x7FFFu) ? 0xFFFFu : 0u) | ((p[n][0] & 0x7FFF0000u) ? 0xFFFF0000u : 0u);
-                                p1 &= ((p[n][1] & 0x7FFFu) ? 0xFFFFu : 0u) | ((p[n][1] & 0x7FFF0000u) ? 0xFFFF0000u : 0u);
-                            }
+                            const uint32_t p0 = mul_half2(p[n][0], s.x), p1 = mul_half2(p[n][1], s.y);
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
                                 const uint32_t v = w[2 * i + h], v8 = v >> 8;
@@ -504,77 +577,158 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32, 1) atten
             if (++stage == STAGES) stage = 0, phase ^= 1;
         }
 
-        // ---- the warps' sums meet: a column's channels, then its reference and weight
+        // ---- the unit's channels; a column's reference (minus infinity: nothing seen) and weight
+        if (at.x == 0 && at.end == at.steps.count) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n) {
+                float by[2];
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                float *const to = merge + (warp * COLS + n * 8 + 2 * t4 + c) * ROW;
+                for (int c = 0; c < 2; ++c) {
+                    const float weight = __shfl_sync(kFull, off[n][2 + c], t4);
+                    by[c] = weight == 0.0f ? 0.0f : 1.0f / weight;
+                }
+                const uint32_t r = row0 + n * 8 + g;             // (behind the transposition a lane has one row, two channels)
+                uint16_t *const to = A.out + (uint64_t)(at.S.first_row + r / A.group) * A.out_stride + (uint64_t)(head * A.group + r % A.group) * DIM + 2 * t4;
+                const bool in = r < rows_all, paired = ((uintptr_t)to & 3) == 0;
 #pragma unroll
                 for (int j = 0; j < 2 * G; ++j) {
-                    const float m = __shfl_sync(kFull, off[n][c], (j / 2) * 4 + t4);
-                    to[16 * j + g] = fmaf(acc[n][j][c], 0x1p24f, m);
-                    to[16 * j + 8 + g] = fmaf(acc[n][j][2 + c], 0x1p20f, m);
+                    const float m0 = __shfl_sync(kFull, off[n][0], (j / 2) * 4 + t4), m1 = __shfl_sync(kFull, off[n][1], (j / 2) * 4 + t4);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float up = h ? 0x1p20f : 0x1p24f;
+                        float o0 = fmaf(acc[n][j][2 * h], up, m0) * by[0], o1 = fmaf(acc[n][j][2 * h + 1], up, m1) * by[1];
+                        const uint32_t v = transposed(C.fp16 ? round16<true>(o0) | (uint32_t)round16<true>(o1) << 16
+                                                             : round16<false>(o0) | (uint32_t)round16<false>(o1) << 16);
+                        uint16_t *const o = to + 16 * j + 8 * h;
+                        if (in && paired) *(uint32_t *)o = v;
+                        else if (in) o[0] = (uint16_t)v, o[1] = (uint16_t)(v >> 16);
+                    }
                 }
-                if (g == 0) to[DIM] = ref[n][c], to[DIM + 1] = off[n][2 + c];
             }
-        __syncthreads();
-        const uint32_t n_warps = min((uint32_t)W, at.end - at.x);
-        const bool complete = at.x == 0 && at.end == at.steps.count;
-        const uint64_t first_cta = ((at_first + 1) * ctas - 1) / total, last_cta = ((at_first + at.steps.count) * ctas - 1) / total;
-        float *const piece = A.partials + (2 * (uint64_t)blockIdx.x + (at.x ? 0 : 1)) * Shape::kPartial;
-        auto put = [&](uint32_t col, uint32_t d, float value, float weight) {
-            const uint32_t r = row0 + col;
-            if (r >= rows_all) return;
-            const float o = weight == 0.0f ? 0.0f : value / weight;
-            A.out[(uint64_t)(at.S.first_row + r / A.group) * A.out_stride + (uint64_t)(head * A.group + r % A.group) * DIM + d] =
-                C.fp16 ? round16<true>(o) : round16<false>(o);
-        };
-        for (uint32_t i = tid; i < COLS * DIM; i += THREADS) {
-            const uint32_t col = i / DIM, d = i % DIM;
-            float all = -INFINITY, value = 0.0f, weight = 0.0f;
-            for (uint32_t w = 0; w < n_warps; ++w) all = fmaxf(all, merge[(w * COLS + col) * ROW + DIM]);
-            for (uint32_t w = 0; w < n_warps; ++w) {
-                const float *from = merge + (w * COLS + col) * ROW;
-                const float scale = from[DIM] == -INFINITY ? (from[DIM + 1] == 0.0f ? 0.0f : NAN) : ex2(from[DIM] - all);
-                value = fmaf(scale, from[d], value);
-                weight = fmaf(scale, from[DIM + 1], weight);
-            }
-            if (complete) {
-                put(col, d, value, weight);
+        } else {
+            const uint32_t which = at.x ? 0 : 1;
+            float *const piece = piece_at(warp, which);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float *const to = piece + (n * 8 + 2 * t4 + c) * ROW;
+#pragma unroll
+                    for (int j = 0; j < 2 * G; ++j) {
+                        const float m = __shfl_sync(kFull, off[n][c], (j / 2) * 4 + t4);
+                        to[16 * j + g] = fmaf(acc[n][j][c], 0x1p24f, m);
+                        to[16 * j + 8 + g] = fmaf(acc[n][j][2 + c], 0x1p20f, m);
+                    }
+                    if (g == 0) *(float2 *)(to + DIM) = make_float2(cap[n][c] == -INFINITY ? -INFINITY : ref[n][c], off[n][2 + c]);
+                }
+            if (lane == 0) s_piece[warp][which] = Piece{at_first, at.steps.count, at.S.first_row, rows_all, head, row0};
+        }
+    }
+    }
+    __syncthreads();
+
+    // ---- units of which more than one warp has a piece: a run of pieces in the order of the line
+    auto join = [&](uint32_t count, auto load4, auto load2, float4 &value, float2 &tail) {
+        value = make_float4(0, 0, 0, 0);
+        tail = make_float2(-INFINITY, 0.0f);
+#pragma unroll 8
+        for (uint32_t i = 0; i < count; ++i) tail.x = fmaxf(tail.x, load2(i).x);
+#pragma unroll 4
+        for (uint32_t i = 0; i < count; ++i) {
+            const float4 v = load4(i);
+            const float2 t = load2(i);
+            const float scale = t.x == -INFINITY ? (t.y == 0.0f ? 0.0f : NAN) : ex2(t.x - tail.x);
+            value.x = fmaf(scale, v.x, value.x), value.y = fmaf(scale, v.y, value.y);
+            value.z = fmaf(scale, v.z, value.z), value.w = fmaf(scale, v.w, value.w);
+            tail.y = fmaf(scale, t.y, tail.y);
+        }
+    };
+    auto put = [&](const Piece &P, uint32_t col, uint32_t d, float4 v, float weight) {
+        const uint32_t r = P.row0 + col;
+        if (r >= P.rows) return;
+        const float by = weight == 0.0f ? 0.0f : 1.0f / weight;
+        uint16_t *const to = A.out + (uint64_t)(P.first_row + r / A.group) * A.out_stride + (uint64_t)(P.head * A.group + r % A.group) * DIM + d;
+        uint16_t o[4];
+        if (C.fp16) o[0] = round16<true>(v.x * by), o[1] = round16<true>(v.y * by), o[2] = round16<true>(v.z * by), o[3] = round16<true>(v.w * by);
+        else o[0] = round16<false>(v.x * by), o[1] = round16<false>(v.y * by), o[2] = round16<false>(v.z * by), o[3] = round16<false>(v.w * by);
+        if (((uintptr_t)to & 7) == 0) {
+            *(uint2 *)to = make_uint2(o[0] | (uint32_t)o[1] << 16, o[2] | (uint32_t)o[3] << 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) to[i] = o[i];
+        }
+    };
+    constexpr uint32_t ITEMS = COLS * DIM / 4;
+    uint32_t open[2] = {~0u, ~0u};                               // runs whose units other CTAs have a part of: began in front of this one, go on behind it
+    for (uint32_t from = 0; from < 2 * W;) {
+        const Piece P = s_piece[from / 2][from % 2];
+        if (P.count == 0) {
+            ++from;
+            continue;
+        }
+        uint32_t to = from + 1, count = 1;                       // (a warp that has the middle of a unit has no last piece)
+        for (uint32_t i = to; i < 2 * W; ++i) {
+            if (s_piece[i / 2][i % 2].count == 0) continue;
+            if (s_piece[i / 2][i % 2].begin != P.begin) break;
+            to = i + 1;
+            ++count;
+        }
+        const bool closed = P.begin >= cta_from && P.begin + P.count <= cta_to;
+        const uint32_t which = P.begin < cta_from ? 0 : 1;
+        if (!closed) open[which] = from;
+        float *const piece = A.partials + (2 * (uint64_t)blockIdx.x + which) * Shape::kPiece;
+        for (uint32_t i = tid; i < ITEMS; i += THREADS) {
+            const uint32_t col = i / (DIM / 4), d = i % (DIM / 4) * 4;
+            float4 value;
+            float2 tail;
+            // (a run is every warp's first piece, but for its beginning, which may be a last one)
+            const uint32_t w0 = (from + 1) / 2;
+            auto src = [&](uint32_t k) { return (from % 2 == 0 ? piece_at(w0 + k, 0) : k == 0 ? piece_at(w0 - 1, 1) : piece_at(w0 + k - 1, 0)) + col * ROW; };
+            join(count, [&](uint32_t k) { return *(const float4 *)(src(k) + d); }, [&](uint32_t k) { return *(const float2 *)(src(k) + DIM); }, value, tail);
+            if (closed) {
+                put(P, col, d, value, tail.y);
             } else {
-                __stcg(piece + col * ROW + d, value);
-                if (d == 0) __stcg(piece + col * ROW + DIM, all), __stcg(piece + col * ROW + DIM + 1, weight);
+                __stcg((float4 *)(piece + col * ROW + d), value);
+                if (d == 0) __stcg((float2 *)(piece + col * ROW + DIM), tail);
             }
         }
-        __syncthreads();                                         // (the sums are read, the pieces written)
-        if (!complete) {
-            if (tid == 0) {
-                __threadfence();
-                const uint32_t count = (uint32_t)(last_cta - first_cta) + 1;
-                const bool last = arrive_acq_rel(A.tickets + first_cta) == count - 1;
-                if (last) A.tickets[first_cta] = 0;
-                __threadfence();
-                s_last = last;
-            }
-            __syncthreads();
-            if (s_last) {
-                for (uint32_t i = tid; i < COLS * DIM; i += THREADS) {
-                    const uint32_t col = i / DIM, d = i % DIM;
-                    float all = -INFINITY, value = 0.0f, weight = 0.0f;
-                    for (uint64_t c = first_cta; c <= last_cta; ++c)
-                        all = fmaxf(all, __ldcg(A.partials + (2 * c + (c == first_cta)) * Shape::kPartial + col * ROW + DIM));
-                    for (uint64_t c = first_cta; c <= last_cta; ++c) {
-                        const float *from = A.partials + (2 * c + (c == first_cta)) * Shape::kPartial + col * ROW;
-                        const float r = __ldcg(from + DIM), l = __ldcg(from + DIM + 1);
-                        const float scale = r == -INFINITY ? (l == 0.0f ? 0.0f : NAN) : ex2(r - all);
-                        value = fmaf(scale, __ldcg(from + d), value);
-                        weight = fmaf(scale, l, weight);
-                    }
-                    put(col, d, value, weight);
-                }
-            }
-            __syncthreads();
+        from = to;
+    }
+    if (open[0] == ~0u && open[1] == ~0u) return;
+
+    // ---- and units of which more than one CTA has: the last one to arrive adds up
+    __syncthreads();                                             // (the CTA's pieces are written)
+    uint64_t first_cta[2] = {0, 0};
+    uint32_t cta_count[2] = {0, 0};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        if (open[k] == ~0u) continue;
+        const Piece &P = s_piece[open[k] / 2][open[k] % 2];
+        first_cta[k] = ((P.begin + 1) * ctas - 1) / total;
+        cta_count[k] = (uint32_t)(((P.begin + P.count) * ctas - 1) / total - first_cta[k]) + 1;
+        if (tid == k) {
+            __threadfence();
+            const bool last = arrive_acq_rel(A.tickets + first_cta[k]) == cta_count[k] - 1;
+            if (last) A.tickets[first_cta[k]] = 0;
+            __threadfence();
+            s_last[k] = last;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        if (open[k] == ~0u || !s_last[k]) continue;
+        const Piece P = s_piece[open[k] / 2][open[k] % 2];
+        // (the unit's first CTA has its piece in the second place, see above)
+        const float *const pieces = A.partials + 2 * first_cta[k] * Shape::kPiece;
+        for (uint32_t i = tid; i < ITEMS; i += THREADS) {
+            const uint32_t col = i / (DIM / 4), d = i % (DIM / 4) * 4;
+            auto src = [&](uint32_t w) { return pieces + (w ? 2 * w : 1) * Shape::kPiece + col * ROW; };
+            float4 value;
+            float2 tail;
+            join(cta_count[k], [&](uint32_t w) { return __ldcg((const float4 *)(src(w) + d)); }, [&](uint32_t w) { return __ldcg((const float2 *)(src(w) + DIM)); },
+                 value, tail);
+            put(P, col, d, value, tail.y);
         }
     }
 }
@@ -582,8 +736,8 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32, 1) atten
 template <int DIM, int NT>
 static cudaError_t launch_shape(const AttentionArgs &a, uint32_t sms, cudaStream_t stream) {
     using Shape = AttentionShape<DIM, NT>;
-    static_assert(Shape::kSmem + 1024 <= 232448, "shared memory of a CTA");
-    static_assert(Shape::kPartial <= kAttentionPartial, "a piece's place in the workspace");
+    static_assert(Shape::kSmem + 1536 <= 232448, "shared memory of a CTA");
+    static_assert(Shape::kPiece <= kAttentionPartial, "a piece's place in the workspace");
     static std::atomic<bool> attr_set[64];   // set twice by racing threads at worst: the call is idempotent
     int dev = 0;
     cudaGetDevice(&dev);

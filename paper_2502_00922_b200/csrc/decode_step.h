@@ -46,6 +46,7 @@ struct AttentionArgs {
     const int32_t *starts;         // may be null
     uint32_t rows, heads, group;   // group: query heads of a key head
     uint32_t window, sinks;
+    uint32_t page_recip;           // floor(2^32 / blocks of a page) (one block: less one)
     float scale;
     int32_t *err;                  // may be null
     unsigned int *tickets;         // zero between calls
