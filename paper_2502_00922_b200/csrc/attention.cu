@@ -20,13 +20,14 @@
 namespace huffllm {
 
 constexpr uint32_t kStepTokens = 2 * kCacheBlock;
-constexpr uint32_t kWaitTries = 1u << 22;
+// A wait gives up after about a second: so many tries of one that sleeps for some microseconds, and of one that does not.
+constexpr uint32_t kWaitTries = 1u << 17, kPollTries = 1u << 25;
 constexpr int kSlack = 4;                        // a weight's exponent is set this far below its cap, so that few later ones are above it
 
 template <int DIM, int NT>
 struct AttentionShape {
     static constexpr int kGroups = DIM / 32, kCols = 8 * NT;
-    static constexpr int kWarps = DIM * NT <= 128 ? 12 : 8;
+    static constexpr int kWarps = DIM * NT <= 128 ? 15 : 7;      // that compute; one more asks for their copies
     static constexpr int kStages = DIM * NT == 256 && DIM == 128 ? 3 : 2;
     static constexpr uint32_t kBlockBytes = cache_block_bytes(DIM);
     static constexpr uint32_t kRingBytes = kWarps * kStages * 2 * kBlockBytes;
@@ -171,13 +172,15 @@ __device__ __forceinline__ void mma_f16_16816_new(float (&d)[4], uint32_t a0, ui
 __device__ __forceinline__ void sts32(uint32_t at, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
 
 template <int DIM, int NT>
-__global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32, 1) attention_kernel(const __grid_constant__ AttentionArgs A) {
+__global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) attention_kernel(const __grid_constant__ AttentionArgs A) {
     using Shape = AttentionShape<DIM, NT>;
-    constexpr int G = Shape::kGroups, COLS = Shape::kCols, W = Shape::kWarps, STAGES = Shape::kStages, THREADS = W * 32;
+    constexpr int G = Shape::kGroups, COLS = Shape::kCols, W = Shape::kWarps, STAGES = Shape::kStages, THREADS = W * 32 + 32;
     constexpr uint32_t BLOCK = Shape::kBlockBytes, ROW = Shape::kRow;
     constexpr uint32_t kFull = 0xFFFFFFFFu;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(8) uint64_t s_bar[W * STAGES];
+    __shared__ __align__(8) uint64_t s_bar[2][W * STAGES];      // a stage's copies have arrived; a stage has been read
+    __shared__ uint64_t s_start[W];                              // where in the line the first sequence of a warp begins
+    __shared__ uint32_t s_start_b[W];                            // ... and which one it is
     __shared__ uint32_t s_here[W * STAGES][2];                   // blocks of a stage that are there
     __shared__ Piece s_piece[W][2];
     __shared__ uint32_t s_last[2];
@@ -186,8 +189,8 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32, 1) atten
     const CacheArgs &C = A.c;
     const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32, g = lane / 4, t4 = lane % 4;
 
-    if (lane < STAGES) mbar_init(smem_u32(&s_bar[warp * STAGES + lane]), 1);
-    if (lane < 2) s_piece[warp][lane].count = 0;
+    if (warp < W && lane < STAGES) mbar_init(smem_u32(&s_bar[0][warp * STAGES + lane]), 1), mbar_init(smem_u32(&s_bar[1][warp * STAGES + lane]), 1);
+    if (warp < W && lane < 2) s_piece[warp][lane].count = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     pdl_launch_dependents();
     pdl_wait_prior_grid();
@@ -210,78 +213,95 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32, 1) atten
     const uint64_t cta_from = blockIdx.x * total / ctas, cta_to = (blockIdx.x + 1) * total / ctas;
     // (warps without a step are the last ones: a unit's pieces are those of warps that follow each other)
     const uint64_t each = (cta_to - cta_from) / W, rest = (cta_to - cta_from) % W;
-    const uint64_t line_from = cta_from + each * warp + min((uint64_t)warp, rest), line_to = line_from + each + (warp < rest ? 1 : 0);
-
-    if (line_from < line_to) {
-    Walk ahead;                                                  // the stretch that copies are asked for; `at` is the one worked on
-    uint64_t before = 0;
-    for (uint32_t b0 = 0;; b0 += 32) {
-        const uint64_t w = b0 ? weight_of(b0 + lane) : first;
-        uint64_t sum = w;
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint64_t up = __shfl_up_sync(kFull, sum, o);
-            if (lane >= o) sum += up;
+    const uint32_t reader = warp < W ? warp : min(lane, W - 1);  // the last warp's lanes ask for a warp's copies each
+    const uint64_t line_from = cta_from + each * reader + min((uint64_t)reader, rest), line_to = line_from + each + (reader < rest ? 1 : 0);
+    if (warp < W && line_from < line_to) {
+        uint64_t before = 0;
+        for (uint32_t b0 = 0;; b0 += 32) {
+            const uint64_t w = b0 ? weight_of(b0 + lane) : first;
+            uint64_t sum = w;
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint64_t up = __shfl_up_sync(kFull, sum, o);
+                if (lane >= o) sum += up;
+            }
+            const uint32_t behind = __ballot_sync(kFull, before + sum > line_from);
+            if (behind) {                                        // (there is one: the line goes on behind its start)
+                const int k = __ffs(behind) - 1;
+                before += __shfl_sync(kFull, sum - w, k);
+                if (lane == 0) s_start[warp] = before, s_start_b[warp] = b0 + k;
+                break;
+            }
+            before += __shfl_sync(kFull, sum, 31);
         }
-        const uint32_t behind = __ballot_sync(kFull, before + sum > line_from);
-        if (behind) {                                            // (there is one: the line goes on behind its start)
-            const int k = __ffs(behind) - 1;
-            ahead.b = b0 + k;
-            before += __shfl_sync(kFull, sum - w, k);
-            break;
-        }
-        before += __shfl_sync(kFull, sum, 31);
     }
-    ahead.load(A, COLS);
-    ahead.unit = (uint32_t)((line_from - before) / ahead.steps.count);
-    ahead.x = (uint32_t)((line_from - before) % ahead.steps.count);
-    ahead.left = line_to - line_from;
-    ahead.take(A, COLS);
-    Walk at = ahead;
-    uint64_t at_first = line_from - at.x;                        // where in the line the unit begins
-    bool more = true;
-    uint32_t next_x = ahead.x;
-
-    const uint32_t ring = smem_u32(smem) + warp * STAGES * 2 * BLOCK;
-    const uint32_t bars = smem_u32(&s_bar[warp * STAGES]);
-    // The warp's next step: the page of a block (lanes 0 and 1 have one each) is looked up when the step in front of it is asked for.
-    const uint32_t page_blocks = C.page_tokens / kCacheBlock;
-    uint32_t in_page = 0;
-    int32_t page = -1;
-    bool wanted = false;
-    auto look_up = [&]() {
-        while (more && next_x >= ahead.end) {
-            more = ahead.next(A, COLS);
-            next_x = ahead.x;
-        }
-        wanted = false;
-        if (more && lane < 2) {
-            const uint32_t block = ahead.steps.step(next_x) * 2 + lane;
-            wanted = ahead.any_seen(A, block * kCacheBlock, kCacheBlock);
+    __syncthreads();
+    const uint32_t ring = smem_u32(smem) + reader * STAGES * 2 * BLOCK;
+    const uint32_t bars = smem_u32(&s_bar[0][reader * STAGES]), read_bars = smem_u32(&s_bar[1][reader * STAGES]);
+    Walk at;
+    if (line_from < line_to) {
+        at.b = s_start_b[reader];
+        at.load(A, COLS);
+        at.unit = (uint32_t)((line_from - s_start[reader]) / at.steps.count);
+        at.x = (uint32_t)((line_from - s_start[reader]) % at.steps.count);
+        at.left = line_to - line_from;
+        at.take(A, COLS);
+    }
+    if (warp == W) {
+        // The copies: a lane looks up its warp's next pages, and asks for them as soon as their stage has been read.
+        const uint32_t page_blocks = C.page_tokens / kCacheBlock;
+        bool more = lane < W && line_from < line_to;
+        uint32_t x = more ? at.x : 0, stage = 0, phase = 1, in_page[2] = {0, 0};   // (a fresh barrier's phase in front of its first is over)
+        int32_t page[2] = {-1, -1};
+        bool wanted[2] = {false, false};
+        auto look_up = [&]() {
+            if (x >= at.end) {
+                more = at.next(A, COLS);
+                x = at.x;
+                if (!more) return;
+            }
+            const uint32_t block = at.steps.step(x) * 2;
             uint32_t i = __umulhi(block, A.page_recip);          // block / page_blocks, or one less
-            in_page = block - i * page_blocks;
-            if (in_page >= page_blocks) ++i, in_page -= page_blocks;
-            if (wanted) page = __ldcg(C.table + (uint64_t)ahead.b * C.table_stride + i);
+            in_page[0] = block - i * page_blocks;
+            if (in_page[0] >= page_blocks) ++i, in_page[0] -= page_blocks;
+            const int32_t *const entry = C.table + (uint64_t)at.b * C.table_stride + i;
+            const bool turns = in_page[0] + 1 == page_blocks;
+            in_page[1] = turns ? 0 : in_page[0] + 1;
+            wanted[0] = at.any_seen(A, block * kCacheBlock, kCacheBlock);
+            wanted[1] = at.any_seen(A, block * kCacheBlock + kCacheBlock, kCacheBlock);
+            if (wanted[0] || (wanted[1] && !turns)) page[0] = __ldcg(entry);
+            if (wanted[1] && turns) page[1] = __ldcg(entry + 1);
+            else page[1] = page[0];
+        };
+        if (more) look_up();
+        for (uint32_t tries = 0; __any_sync(kFull, more) && tries < kPollTries; ++tries) {
+            const bool ready = more && mbar_test_wait(read_bars + 8 * stage, phase);
+            if (__any_sync(kFull, ready)) tries = 0;
+            if (ready) {
+                bool here[2];
+                const uint8_t *src[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    here[k] = wanted[k] && page[k] >= 0 && (uint32_t)page[k] < C.pages;
+                    if (wanted[k] && !here[k] && A.err) *A.err = (int32_t)at.b + 1;
+                    src[k] = C.pool + (((uint64_t)(uint32_t)page[k] * C.kv_heads + at.head) * page_blocks + in_page[k]) * BLOCK;
+                    s_here[reader * STAGES + stage][k] = here[k];
+                }
+                mbar_expect_tx(bars + 8 * stage, (here[0] + here[1]) * BLOCK);
+                const uint32_t to = ring + stage * 2 * BLOCK;
+                if (here[0] && here[1] && src[1] == src[0] + BLOCK) {
+                    bulk_g2s(to, src[0], 2 * BLOCK, bars + 8 * stage);
+                } else {
+                    if (here[0]) bulk_g2s(to, src[0], BLOCK, bars + 8 * stage);
+                    if (here[1]) bulk_g2s(to + BLOCK, src[1], BLOCK, bars + 8 * stage);
+                }
+                if (++stage == STAGES) stage = 0, phase ^= 1;
+                ++x;
+                look_up();
+            }
         }
-    };
-    auto ask = [&](uint32_t stage) {
-        if (!more) return;
-        const bool here = wanted && page >= 0 && (uint32_t)page < C.pages;
-        if (wanted && !here && A.err) *A.err = (int32_t)ahead.b + 1;
-        if (lane < 2) s_here[warp * STAGES + stage][lane] = here;
-        const uint32_t count = __popc(__ballot_sync(kFull, here));
-        if (lane == 0) mbar_expect_tx(bars + 8 * stage, count * BLOCK);
-        __syncwarp();
-        if (here) {
-            const uint64_t block = ((uint64_t)page * C.kv_heads + ahead.head) * page_blocks + in_page;
-            bulk_g2s(ring + (stage * 2 + lane) * BLOCK, C.pool + block * BLOCK, BLOCK, bars + 8 * stage);
-        }
-        ++next_x;
-        look_up();
-    };
-    __syncwarp();
-    look_up();
-    for (uint32_t s = 0; s < STAGES; ++s) ask(s);
-
+        if (more && A.err) *A.err = -1;
+    } else if (line_from < line_to) {
+    uint64_t at_first = line_from - at.x;                        // where in the line the unit begins
     uint32_t stage = 0, phase = 0;
     for (bool on = true; on; at_first += at.steps.count, on = at.next(A, COLS)) {
         // ---- the tile's queries, as B operands: column n of a lane is its g, rows its t4's eight channels of a group
@@ -573,7 +593,7 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32, 1) atten
                 }
             }
             __syncwarp();
-            ask(stage);
+            if (lane == 0) mbar_arrive(read_bars + 8 * stage);
             if (++stage == STAGES) stage = 0, phase ^= 1;
         }
 
@@ -746,7 +766,7 @@ static cudaError_t launch_shape(const AttentionArgs &a, uint32_t sms, cudaStream
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
     }
-    return launch_behind(attention_kernel<DIM, NT>, dim3(sms < kAttentionCtas ? sms : kAttentionCtas), Shape::kWarps * 32, Shape::kSmem, stream, a);
+    return launch_behind(attention_kernel<DIM, NT>, dim3(sms < kAttentionCtas ? sms : kAttentionCtas), Shape::kWarps * 32 + 32, Shape::kSmem, stream, a);
 }
 
 // One tile of eight rows where a key head has no more than eight, two where it has (and registers hold them).
