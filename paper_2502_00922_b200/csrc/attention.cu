@@ -113,6 +113,8 @@ struct Walk {
     }
 };
 
+// (a division of 64 bits is some hundred instructions, and hardly a line is that long)
+__device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b) { return (a | b) >> 32 ? a / b : (uint32_t)a / (uint32_t)b; }
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -183,7 +185,7 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
     __shared__ uint32_t s_start_b[W];                            // ... and which one it is
     __shared__ uint32_t s_here[W * STAGES][2];                   // blocks of a stage that are there
     __shared__ Piece s_piece[W][2];
-    __shared__ uint32_t s_last[2];
+    __shared__ uint2 s_join[2];                                  // units that this CTA is the last to arrive at: first CTA and number of pieces
     float *const first_pieces = (float *)(smem + Shape::kRingBytes);
     auto piece_at = [&](uint32_t w, uint32_t which) { return which ? (float *)(smem + w * STAGES * 2 * BLOCK) : first_pieces + w * Shape::kPiece; };
     const CacheArgs &C = A.c;
@@ -194,12 +196,12 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     pdl_launch_dependents();
     pdl_wait_prior_grid();
-    if (blockIdx.x == 0) report_faults(C, A.starts, A.rows, A.err);
 
     // The line: how long it is, and where in it this CTA starts (every warp finds out by itself).
     auto weight_of = [&](uint32_t b) -> uint64_t {
         if (b >= C.sequences) return 0;
         const Sequence S = sequence_of(C, A.starts, A.rows, b);
+        if (S.bad && tid < 32 && blockIdx.x == 0 && A.err) *A.err = (int32_t)b + 1;
         return (uint64_t)((S.rows * A.group + COLS - 1) / COLS) * C.kv_heads * steps_of(S, A.window, A.sinks).count;
     };
     const uint64_t first = weight_of(lane);
@@ -208,9 +210,14 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
     for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(kFull, total, o);
     if (total == 0) return;
     // (as many CTAs as find at least a step for every other of their warps)
-    const uint64_t ctas = min((uint64_t)gridDim.x, max((uint64_t)1, (total + W / 2 - 1) / (W / 2)));
+    const uint32_t ctas = (uint32_t)min((uint64_t)gridDim.x, (total + W / 2 - 1) / (W / 2));
     if (blockIdx.x >= ctas) return;
-    const uint64_t cta_from = blockIdx.x * total / ctas, cta_to = (blockIdx.x + 1) * total / ctas;
+    const uint64_t cta_each = quotient(total, ctas), cta_rest = total - cta_each * ctas;       // (the first cta_rest CTAs have a step more)
+    const uint64_t cta_from = cta_each * blockIdx.x + min((uint64_t)blockIdx.x, cta_rest), cta_to = cta_from + cta_each + (blockIdx.x < cta_rest ? 1 : 0);
+    auto cta_of = [&](uint64_t step) -> uint32_t {
+        const uint64_t longer = cta_rest * (cta_each + 1);
+        return (uint32_t)(step < longer ? quotient(step, cta_each + 1) : cta_rest + quotient(step - longer, cta_each));
+    };
     // (warps without a step are the last ones: a unit's pieces are those of warps that follow each other)
     const uint64_t each = (cta_to - cta_from) / W, rest = (cta_to - cta_from) % W;
     const uint32_t reader = warp < W ? warp : min(lane, W - 1);  // the last warp's lanes ask for a warp's copies each
@@ -241,8 +248,9 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
     if (line_from < line_to) {
         at.b = s_start_b[reader];
         at.load(A, COLS);
-        at.unit = (uint32_t)((line_from - s_start[reader]) / at.steps.count);
-        at.x = (uint32_t)((line_from - s_start[reader]) % at.steps.count);
+        const uint64_t in = line_from - s_start[reader];
+        at.unit = (uint32_t)quotient(in, at.steps.count);
+        at.x = (uint32_t)(in - (uint64_t)at.unit * at.steps.count);
         at.left = line_to - line_from;
         at.take(A, COLS);
     }
@@ -647,108 +655,118 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
     }
     __syncthreads();
 
-    // ---- units of which more than one warp has a piece: a run of pieces in the order of the line
-    auto join = [&](uint32_t count, auto load4, auto load2, float4 &value, float2 &tail) {
-        value = make_float4(0, 0, 0, 0);
-        tail = make_float2(-INFINITY, 0.0f);
-#pragma unroll 8
-        for (uint32_t i = 0; i < count; ++i) tail.x = fmaxf(tail.x, load2(i).x);
-#pragma unroll 4
-        for (uint32_t i = 0; i < count; ++i) {
-            const float4 v = load4(i);
-            const float2 t = load2(i);
-            const float scale = t.x == -INFINITY ? (t.y == 0.0f ? 0.0f : NAN) : ex2(t.x - tail.x);
-            value.x = fmaf(scale, v.x, value.x), value.y = fmaf(scale, v.y, value.y);
-            value.z = fmaf(scale, v.z, value.z), value.w = fmaf(scale, v.w, value.w);
-            tail.y = fmaf(scale, t.y, tail.y);
-        }
-    };
-    auto put = [&](const Piece &P, uint32_t col, uint32_t d, float4 v, float weight) {
-        const uint32_t r = P.row0 + col;
-        if (r >= P.rows) return;
-        const float by = weight == 0.0f ? 0.0f : 1.0f / weight;
-        uint16_t *const to = A.out + (uint64_t)(P.first_row + r / A.group) * A.out_stride + (uint64_t)(P.head * A.group + r % A.group) * DIM + d;
-        uint16_t o[4];
-        if (C.fp16) o[0] = round16<true>(v.x * by), o[1] = round16<true>(v.y * by), o[2] = round16<true>(v.z * by), o[3] = round16<true>(v.w * by);
-        else o[0] = round16<false>(v.x * by), o[1] = round16<false>(v.y * by), o[2] = round16<false>(v.z * by), o[3] = round16<false>(v.w * by);
-        if (((uintptr_t)to & 7) == 0) {
-            *(uint2 *)to = make_uint2(o[0] | (uint32_t)o[1] << 16, o[2] | (uint32_t)o[3] << 16);
-        } else {
+    // ---- units of which more than one warp has a piece: a run of pieces in the order of the line; a warp joins a column of a run
+    // Joins `count` pieces (N channels, every 32nd, of one column): value gets the sums, the result is their reference and weight.
+    auto join = [&](uint32_t count, auto tails, auto src, auto in, auto &value) -> float2 {
+        constexpr int N = (int)(sizeof(value) / sizeof(float));
+        float ref = -INFINITY, weight = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) to[i] = o[i];
-        }
-    };
-    constexpr uint32_t ITEMS = COLS * DIM / 4;
-    uint32_t open[2] = {~0u, ~0u};                               // runs whose units other CTAs have a part of: began in front of this one, go on behind it
-    for (uint32_t from = 0; from < 2 * W;) {
-        const Piece P = s_piece[from / 2][from % 2];
-        if (P.count == 0) {
-            ++from;
-            continue;
-        }
-        uint32_t to = from + 1, count = 1;                       // (a warp that has the middle of a unit has no last piece)
-        for (uint32_t i = to; i < 2 * W; ++i) {
-            if (s_piece[i / 2][i % 2].count == 0) continue;
-            if (s_piece[i / 2][i % 2].begin != P.begin) break;
-            to = i + 1;
-            ++count;
-        }
-        const bool closed = P.begin >= cta_from && P.begin + P.count <= cta_to;
-        const uint32_t which = P.begin < cta_from ? 0 : 1;
-        if (!closed) open[which] = from;
-        float *const piece = A.partials + (2 * (uint64_t)blockIdx.x + which) * Shape::kPiece;
-        for (uint32_t i = tid; i < ITEMS; i += THREADS) {
-            const uint32_t col = i / (DIM / 4), d = i % (DIM / 4) * 4;
-            float4 value;
-            float2 tail;
-            // (a run is every warp's first piece, but for its beginning, which may be a last one)
-            const uint32_t w0 = (from + 1) / 2;
-            auto src = [&](uint32_t k) { return (from % 2 == 0 ? piece_at(w0 + k, 0) : k == 0 ? piece_at(w0 - 1, 1) : piece_at(w0 + k - 1, 0)) + col * ROW; };
-            join(count, [&](uint32_t k) { return *(const float4 *)(src(k) + d); }, [&](uint32_t k) { return *(const float2 *)(src(k) + DIM); }, value, tail);
-            if (closed) {
-                put(P, col, d, value, tail.y);
-            } else {
-                __stcg((float4 *)(piece + col * ROW + d), value);
-                if (d == 0) __stcg((float2 *)(piece + col * ROW + DIM), tail);
+        for (int j = 0; j < N; ++j) value[j] = 0.0f;
+        for (uint32_t base = 0; base < count; base += 32) {      // a lane has the reference and weight of one of 32 pieces
+            const uint32_t have = min(32u, count - base);
+            const float2 t = lane < have ? in(tails(base + lane) + DIM) : make_float2(-INFINITY, 0.0f);
+            float top = fmaxf(ref, t.x);
+            for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
+            const float scale = t.x == -INFINITY ? (t.y == 0.0f ? 0.0f : NAN) : ex2(t.x - top);
+            float sum = scale * t.y;
+            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
+            if (base) {
+                const float keep = ref == -INFINITY ? 1.0f : ex2(ref - top);
+                weight *= keep;
+#pragma unroll
+                for (int j = 0; j < N; ++j) value[j] *= keep;
+            }
+            weight += sum;
+            ref = top;
+#pragma unroll 8
+            for (uint32_t i = 0; i < have; ++i) {
+                const float *const from = src(base + i) + lane;
+                const float by = __shfl_sync(kFull, scale, i);
+#pragma unroll
+                for (int j = 0; j < N; ++j) value[j] = fmaf(by, in.one(from + 32 * j), value[j]);
             }
         }
-        from = to;
+        return make_float2(ref, weight);
+    };
+    struct FromShared {
+        __device__ __forceinline__ float2 operator()(const float *p) const { return *(const float2 *)p; }
+        __device__ __forceinline__ float one(const float *p) const { return *p; }
+    };
+    struct FromGlobal {
+        __device__ __forceinline__ float2 operator()(const float *p) const { return __ldcg((const float2 *)p); }
+        __device__ __forceinline__ float one(const float *p) const { return __ldcg(p); }
+    };
+    auto put = [&](const Piece &P, uint32_t col, uint32_t d, float v) {
+        const uint32_t r = P.row0 + col;
+        if (r >= P.rows) return;
+        uint16_t *const to = A.out + (uint64_t)(P.first_row + r / A.group) * A.out_stride + (uint64_t)(P.head * A.group + r % A.group) * DIM + d;
+        *to = C.fp16 ? round16<true>(v) : round16<false>(v);
+    };
+    const Piece *const all_pieces = &s_piece[0][0];
+    const bool there = lane < 2 * W && all_pieces[lane].count != 0;
+    const uint64_t begin = there ? all_pieces[lane].begin : 0;
+    const uint32_t places = __ballot_sync(kFull, there), ahead = places & ((1u << lane) - 1);
+    const uint64_t begin_ahead = __shfl_sync(kFull, begin, 31 - __clz(ahead | 1u));
+    const uint32_t runs = __ballot_sync(kFull, there && (ahead == 0 || begin_ahead != begin));
+    // the unit that began in front of this CTA, and the one that goes on behind it and began here
+    const bool open_lane = (runs >> lane & 1) && (begin < cta_from || begin + all_pieces[lane].count > cta_to);
+    const uint32_t open_before = __ballot_sync(kFull, open_lane && begin < cta_from), open_behind = __ballot_sync(kFull, open_lane && begin >= cta_from);
+    for (uint32_t item = warp; item < __popc(runs) * COLS; item += W + 1) {
+        uint32_t left = runs;
+        for (uint32_t i = item / COLS; i; --i) left &= left - 1;
+        const uint32_t run = __ffs(left) - 1, col = item % COLS;
+        const uint32_t later = runs & ~((2u << run) - 1), members = places & ~((1u << run) - 1) & (later ? (1u << (__ffs(later) - 1)) - 1 : kFull);
+        const Piece P = all_pieces[run];
+        const uint32_t w0 = run / 2, odd = run % 2;              // (a run is every warp's first piece, but for its beginning, which may be a last one)
+        auto src = [&](uint32_t k) -> const float * { return (k == 0 && odd ? piece_at(w0, 1) : first_pieces + (w0 + k) * Shape::kPiece) + col * ROW; };
+        float value[G];
+        const float2 tail = join(__popc(members), src, src, FromShared{}, value);
+        const bool open = (open_before | open_behind) >> run & 1;
+        float *const piece = A.partials + (2 * (uint64_t)blockIdx.x + (open_before >> run & 1 ? 0 : 1)) * Shape::kPiece + col * ROW;
+        const float by = tail.y == 0.0f ? 0.0f : 1.0f / tail.y;
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+            if (open) __stcg(piece + 32 * j + lane, value[j]);
+            else put(P, col, 32 * j + lane, value[j] * by);
+        }
+        if (open && lane == 0) __stcg((float2 *)(piece + DIM), tail);
     }
-    if (open[0] == ~0u && open[1] == ~0u) return;
+    if (!(open_before | open_behind)) return;
 
     // ---- and units of which more than one CTA has: the last one to arrive adds up
     __syncthreads();                                             // (the CTA's pieces are written)
-    uint64_t first_cta[2] = {0, 0};
-    uint32_t cta_count[2] = {0, 0};
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        if (open[k] == ~0u) continue;
-        const Piece &P = s_piece[open[k] / 2][open[k] % 2];
-        first_cta[k] = ((P.begin + 1) * ctas - 1) / total;
-        cta_count[k] = (uint32_t)(((P.begin + P.count) * ctas - 1) / total - first_cta[k]) + 1;
-        if (tid == k) {
-            __threadfence();
-            const bool last = arrive_acq_rel(A.tickets + first_cta[k]) == cta_count[k] - 1;
-            if (last) A.tickets[first_cta[k]] = 0;
-            __threadfence();
-            s_last[k] = last;
+    if (warp < 2) {
+        const uint32_t which = warp ? open_behind : open_before;
+        bool last = false;
+        if (which) {
+            const Piece &P = all_pieces[__ffs(which) - 1];
+            const uint32_t first_cta = cta_of(P.begin), count = cta_of(P.begin + P.count - 1) - first_cta + 1;
+            if (lane == 0) {
+                last = arrive_acq_rel(A.tickets + first_cta) == count - 1;
+                if (last) A.tickets[first_cta] = 0;
+                s_join[warp] = make_uint2(first_cta, last ? count : 0);
+            }
+        } else if (lane == 0) {
+            s_join[warp] = make_uint2(0, 0);
         }
     }
     __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        if (open[k] == ~0u || !s_last[k]) continue;
-        const Piece P = s_piece[open[k] / 2][open[k] % 2];
+    for (uint32_t k = 0; k < 2; ++k) {
+        const uint2 J = s_join[k];
+        if (J.y == 0) continue;
+        const Piece P = all_pieces[__ffs(k ? open_behind : open_before) - 1];
         // (the unit's first CTA has its piece in the second place, see above)
-        const float *const pieces = A.partials + 2 * first_cta[k] * Shape::kPiece;
-        for (uint32_t i = tid; i < ITEMS; i += THREADS) {
-            const uint32_t col = i / (DIM / 4), d = i % (DIM / 4) * 4;
-            auto src = [&](uint32_t w) { return pieces + (w ? 2 * w : 1) * Shape::kPiece + col * ROW; };
-            float4 value;
-            float2 tail;
-            join(cta_count[k], [&](uint32_t w) { return __ldcg((const float4 *)(src(w) + d)); }, [&](uint32_t w) { return __ldcg((const float2 *)(src(w) + DIM)); },
-                 value, tail);
-            put(P, col, d, value, tail.y);
+        const float *const pieces = A.partials + 2 * (uint64_t)J.x * Shape::kPiece;
+        constexpr uint32_t PARTS = G % 2 ? 1 : 2;                // of a column's channels
+        for (uint32_t item = warp; item < COLS * PARTS; item += W + 1) {
+            const uint32_t col = item / PARTS, d = item % PARTS * (DIM / PARTS);
+            auto src = [&](uint32_t i) { return pieces + (i ? 2 * i : 1) * Shape::kPiece + col * ROW; };
+            float value[G / PARTS];
+            auto shifted = [&](uint32_t i) { return src(i) + d; };
+            const float2 tail = join(J.y, src, shifted, FromGlobal{}, value);
+            const float by = tail.y == 0.0f ? 0.0f : 1.0f / tail.y;
+#pragma unroll
+            for (int j = 0; j < G / PARTS; ++j) put(P, col, d + 32 * j + lane, value[j] * by);
         }
     }
 }
