@@ -54,6 +54,7 @@ struct AttentionArgs {
 };
 cudaError_t launch_attention(const AttentionArgs &a, uint32_t sms, cudaStream_t stream);
 
+constexpr uint32_t kSampleMostSmem = 227 * 1024;
 struct SamplingArgs {
     const void *logits;
     uint64_t stride;
@@ -62,6 +63,7 @@ struct SamplingArgs {
     const float *top_p, *min_p, *uniform;
     int32_t *tokens;
     uint32_t rows, vocab, type;    // type 0: fp32, 1: BF16, 2: FP16
+    uint32_t part, kept_pieces;    // (the launcher's) logits of a CTA; how many 16-byte pieces of them it keeps in shared memory
 };
 cudaError_t launch_sampling(const SamplingArgs &a, uint32_t sms, cudaStream_t stream);
 

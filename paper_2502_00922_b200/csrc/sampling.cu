@@ -1,160 +1,635 @@
 // The next token of a row of logits, from a given random number.
 //
-// What stays is a beginning of the order (largest logit first, lower index first among equals), so it is told by its last logit's key and
-// by how many of those with that very key stay.  Both cuts (top_k by number, top_p by mass) are found by halving the keys' range.
+// What stays is a beginning of the order (largest logit first, lower index first among equals), so it is told by its last logit, the cut, and by
+// how many of those equal to it stay; which ones these are, and the draw, go by index and need no order.  A cluster of CTAs reads a row once and
+// keeps it in shared memory.  2048 bins of equal width in the logit (at most 1/64 in the weight's exponent) count the tokens above every edge, and
+// the weights' mass: a bin adds up, in whole numbers and so in any order, how far its weights are below that of its upper edge.  The bin in
+// which top_k or top_p end goes to a list of the first CTA, which finds the cut by halving the range of its values.
+//
+// Bound by the instructions per logit (load, largest, bin, two additions in shared memory, draw) where rows are many, and by the cluster's
+// barriers, some ten, where they are few.
+#include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
 #include "decode_common.cuh"
 #include "decode_step.h"
 #include "epilogue.cuh"
 
+namespace cg = cooperative_groups;
+
 namespace huffllm {
 
-constexpr uint32_t kSampleThreads = 1024;
+constexpr uint32_t kSampleThreads = 512, kSampleWarps = kSampleThreads / 32;
+constexpr uint32_t kBins = 2048;
+constexpr uint32_t kMostList = 2 * kBins;              // a bin with fewer logits is searched in shared memory, in a list that lies where the bins were
+constexpr uint32_t kMostCluster = 8;
+constexpr uint32_t kFull = 0xFFFFFFFFu;
 
-// Ascending with the value; NaN and minus infinity lowest, both zeros alike.
+// Ascending with the value, both zeros alike.
 __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t u = __float_as_uint(x == 0.0f ? 0.0f : x);
-    return x != x ? 0x007FFFFFu : u & 0x80000000u ? ~u : u | 0x80000000u;
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
-constexpr uint32_t kLowestKey = 0x007FFFFFu;
 
+// Values of a 16-byte piece, widened
 template <int TYPE>
-__device__ __forceinline__ float logit_at(const void *p, uint64_t i) {
-    if (TYPE == 0) return __ldcg((const float *)p + i);
-    return widen16<TYPE == 2>(__ldcg((const unsigned short *)p + i));
-}
+struct Piece16 {
+    static constexpr int N = TYPE == 0 ? 4 : 8;
+    float x[N];
+    __device__ __forceinline__ explicit Piece16(uint4 v) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (TYPE == 0) x[i] = __uint_as_float(w[i]);
+            else x[2 * i] = widen16<TYPE == 2>((uint16_t)w[i]), x[2 * i + 1] = widen16<TYPE == 2>((uint16_t)(w[i] >> 16));
+        }
+    }
+};
 
-template <typename T, typename Op>
-__device__ T block_reduce(T v, Op op, T *scratch) {
-    const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    for (int o = 16; o; o >>= 1) v = op(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
-    __syncthreads();
-    if (lane == 0) scratch[warp] = v;
-    __syncthreads();
-    v = scratch[lane];
-    for (int o = 16; o; o >>= 1) v = op(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+struct alignas(16) SampleShared {
+    uint32_t count[kBins];                             // a CTA's bins; later, in the first CTA, the list
+    uint32_t below[kBins];
+    uint32_t all_count[kBins];                         // the first CTA: all CTAs' bins
+    float all_mass[kBins];
+    double warp_mass[kSampleWarps], scan_mass[kSampleWarps];
+    uint32_t warp_equal[kSampleWarps], scan_count[kSampleWarps], sums[2][kSampleWarps];
+    float warp_top[kSampleWarps], warp_least[kSampleWarps];
+    float cta_top, cta_least;
+    double table_mass[kMostCluster * kSampleWarps];
+    uint32_t table_equal[kMostCluster * kSampleWarps];
+    uint32_t found_bin, found_count, listed;
+    double found_mass;
+    struct {
+        uint32_t bin, lowest;
+        double want;
+    } named[2];                                        // what the first CTA searches: by count, by mass
+    float cut;                                         // the outcome: logits above it stay, and `ties` of those that equal it
+    uint32_t ties;
+};
+
+// One row, as a CTA sees it: `pieces` pieces of 16 bytes, of which the first `kept` lie in shared memory.  Values outside the CTA's part of the
+// row are NaN, which is neither above nor equal to anything.
+template <int TYPE>
+struct RowPart {
+    static constexpr int N = Piece16<TYPE>::N;
+    using Raw = std::conditional_t<TYPE == 0, uint32_t, uint16_t>;
+    const Raw *first;                                  // the CTA's first value in memory
+    uint4 *data;
+    uint32_t count, phase, pieces, kept;
+    __device__ __forceinline__ uint4 from_memory(uint32_t piece) const {
+        const int64_t at = (int64_t)piece * N - phase;
+        if (at >= 0 && at + N <= count) return __ldcg((const uint4 *)(first + at));
+        Raw v[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = at + j >= 0 && at + j < count ? __ldcg(first + at + j) : (Raw)0x7FFFFFFFu;
+        uint4 r;
+        if constexpr (TYPE == 0) r = make_uint4(v[0], v[1], v[2], v[3]);
+        else r = make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16, v[6] | (uint32_t)v[7] << 16);
+        return r;
+    }
+    __device__ __forceinline__ Piece16<TYPE> piece(uint32_t i) const { return Piece16<TYPE>(i < kept ? data[i] : from_memory(i)); }
+};
+
+__device__ __forceinline__ float warp_max(float v) {
+    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kFull, v, o));
+    return v;
+}
+__device__ __forceinline__ float warp_min(float v) {
+    for (int o = 16; o; o >>= 1) v = fminf(v, __shfl_xor_sync(kFull, v, o));
     return v;
 }
 
 template <int TYPE>
 __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_constant__ SamplingArgs A) {
-    __shared__ double s_d[32];
-    __shared__ uint32_t s_u[32];
-    __shared__ double s_part[kSampleThreads];
+    extern __shared__ __align__(16) uint8_t dynamic[];
+    SampleShared &S = *(SampleShared *)dynamic;
+    cg::cluster_group cluster = cg::this_cluster();
+    const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32, ctas = cluster.num_blocks(), rank = cluster.block_rank();
+    const uint32_t row = blockIdx.x / ctas;
+    SampleShared &S0 = *cluster.map_shared_rank(&S, 0);
     pdl_launch_dependents();
+    for (uint32_t i = tid; i < kBins; i += kSampleThreads) S.count[i] = S.below[i] = 0;
     pdl_wait_prior_grid();
-    const uint32_t tid = threadIdx.x, row = blockIdx.x, n = A.vocab;
-    const uint64_t base = row * A.stride;
-    const float t = A.temperature ? __ldcg(A.temperature + row) : 1.0f;
-    const bool greedy = !(t > 0.0f);
-    const float u = __ldcg(A.uniform + row), top_p = A.top_p ? __ldcg(A.top_p + row) : 1.0f, given = A.min_p ? __ldcg(A.min_p + row) : 0.0f, least = given > 1.0f ? 1.0f : given;
-    const int32_t k = greedy ? 1 : A.top_k ? __ldcg(A.top_k + row) : 0;
-    auto add_u = [](uint32_t a, uint32_t b) { return a + b; };
-    auto add_d = [](double a, double b) { return a + b; };
-    auto max_u = [](uint32_t a, uint32_t b) { return max(a, b); };
-    uint32_t top = 0;
-    for (uint32_t i = tid; i < n; i += kSampleThreads) top = max(top, key_of(logit_at<TYPE>(A.logits, base + i)));
-    top = block_reduce(top, max_u, s_u);
-    if (top <= kLowestKey) {
-        if (tid == 0) A.tokens[row] = -1;
-        return;
-    }
-    const float most = value_of(top);
-    auto weight = [&](uint32_t key) -> float { return key == top ? 1.0f : greedy || most == INFINITY ? 0.0f : expf((value_of(key) - most) / t); };
-    auto key_at = [&](uint32_t i) { return key_of(logit_at<TYPE>(A.logits, base + i)); };
-    // how many keys (and what mass) are above `cut`
-    auto above = [&](uint32_t cut, double *mass) -> uint32_t {
-        uint32_t c = 0;
-        double m = 0.0;
-        for (uint32_t i = tid; i < n; i += kSampleThreads) {
-            const uint32_t key = key_at(i);
-            if (key > cut) {
-                ++c;
-                m += weight(key);
+
+    RowPart<TYPE> R;
+    using Raw = typename RowPart<TYPE>::Raw;
+    const uint32_t i0 = min(A.vocab, rank * A.part);
+    R.first = (const Raw *)A.logits + row * A.stride + i0;
+    R.data = (uint4 *)(dynamic + sizeof(SampleShared));
+    R.count = min(A.vocab - i0, A.part);
+    R.phase = (uint32_t)((uintptr_t)R.first % 16 / sizeof(Raw));
+    R.pieces = R.count ? (R.phase + R.count + R.N - 1) / R.N : 0;
+    R.kept = min(R.pieces, A.kept_pieces);
+
+    const float t_given = A.temperature ? __ldcg(A.temperature + row) : 1.0f, p = A.top_p ? __ldcg(A.top_p + row) : 1.0f, u = __ldcg(A.uniform + row);
+    const float min_given = A.min_p ? __ldcg(A.min_p + row) : 0.0f, least_weight = min_given > 1.0f ? 1.0f : min_given;
+    const int32_t k_given = A.top_k ? __ldcg(A.top_k + row) : 0;
+    const bool first_only = !(t_given > 1e-30f) || p <= 0.0f || k_given == 1;
+    const float temperature = t_given > 1e-30f ? t_given : 1.0f;
+
+    // ---- the row into shared memory; its largest and smallest logit
+    float top = -INFINITY, least = INFINITY;
+    for (uint32_t i0 = tid; i0 < R.pieces; i0 += 4 * kSampleThreads) {
+        uint4 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t i = i0 + j * kSampleThreads;
+            v[j] = i < R.pieces ? R.from_memory(i) : make_uint4(kFull, kFull, kFull, kFull);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t i = i0 + j * kSampleThreads;
+            if (i < R.kept) R.data[i] = v[j];
+            const Piece16<TYPE> x(v[j]);
+#pragma unroll
+            for (int e = 0; e < R.N; ++e) {
+                top = fmaxf(top, x.x[e]);
+                least = fminf(least, x.x[e] == -INFINITY ? INFINITY : x.x[e]);
             }
         }
-        c = block_reduce(c, add_u, s_u);
-        *mass = block_reduce(m, add_d, s_d);
-        return c;
+    }
+    top = warp_max(top);
+    least = warp_min(least);
+    if (lane == 0) S.warp_top[warp] = top, S.warp_least[warp] = least;
+    __syncthreads();
+    if (warp == 0) {
+        top = warp_max(lane < kSampleWarps ? S.warp_top[lane] : -INFINITY);
+        least = warp_min(lane < kSampleWarps ? S.warp_least[lane] : INFINITY);
+        if (lane == 0) S.cta_top = top, S.cta_least = least, S.listed = 0;
+    }
+    cluster.sync();
+    {
+        const SampleShared &other = *cluster.map_shared_rank(&S, lane % ctas);
+        top = warp_max(other.cta_top);
+        least = warp_min(other.cta_least);
+    }
+    if (top == -INFINITY) {                            // (every CTA of the row comes here)
+        if (rank == 0 && tid == 0) A.tokens[row] = -1;
+        cluster.sync();
+        return;
+    }
+    // Exponents of weights in bins: most 1/64 wide, narrower where the row's logits are closer together.
+    const float scale = fmaxf(64.0f / temperature, fminf((float)(kBins - 1) / (top - least), 1e30f));
+    const float width = 1.0f / (scale * temperature), to_log2 = -1.4426950408889634f / temperature;
+    auto place = [&](float x) { return x == top ? 0.0f : (top - x) * scale; };
+    auto weight = [&](float x) { return x == top ? 1.0f : exp2f((top - x) * to_log2); };
+    // (a weight's distance from that of its bin's upper edge, in 2^-22 of it: 1 - exp(-r) for r up to 1/64)
+    auto below_edge = [&](float place, uint32_t bin) {
+        const float r = (place - (float)bin) * width;
+        return (uint32_t)__float2int_rn(r * (1.0f - r * (0.5f - r * 0.16666667f)) * 4194304.0f);
     };
-    // the cut: keys above `cut` stay, and `ties` of those that equal it
-    uint32_t cut = kLowestKey, ties = 0;
-    double mass;
-    uint32_t count = above(cut, &mass);
-    if (k > 0 && (uint32_t)k < count) {
-        uint32_t lo = kLowestKey, hi = top;              // fewer than k above hi, k or more above lo
-        while (hi - lo > 1) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            if (above(mid, &mass) < (uint32_t)k) hi = mid;
-            else lo = mid;
+
+    float cut = -INFINITY;                             // (what equals minus infinity has no weight)
+    uint32_t ties = 0;
+    const bool by_count = !first_only && k_given > 0 && (uint32_t)k_given < A.vocab, by_mass = !first_only && p < 1.0f;
+    if (first_only) {
+        cut = top;
+        ties = 1;
+    } else if (by_count || by_mass) {
+        // ---- the bins
+        for (uint32_t i = tid; i < R.pieces; i += kSampleThreads) {
+            const Piece16<TYPE> x = R.piece(i);
+#pragma unroll
+            for (int e = 0; e < R.N; ++e) {
+                const float at = place(x.x[e]);
+                if (at < (float)kBins) {
+                    const uint32_t bin = (uint32_t)at;
+                    atomicAdd(&S.count[bin], 1u);
+                    if (by_mass) atomicAdd(&S.below[bin], below_edge(at, bin));
+                }
+            }
         }
-        cut = hi;
-        ties = (uint32_t)k - above(cut, &mass);
-        mass += (double)ties * weight(cut);
-    }
-    if (top_p < 1.0f) {
-        const double want = fmax((double)top_p, 0.0) * mass;
-        uint32_t lo = cut, hi = top;                     // less than `want` above hi; `want` or more above lo, or lo is the cut
-        double m;
-        while (hi - lo > 1) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            above(mid, &m);
-            if (m < want) hi = mid;
-            else lo = mid;
+        cluster.sync();
+        const uint32_t share = kBins / ctas;
+        for (uint32_t i = tid; i < share; i += kSampleThreads) {
+            const uint32_t bin = rank * share + i;
+            uint32_t count = 0;
+            uint64_t below = 0;
+            for (uint32_t r = 0; r < ctas; ++r) {
+                const SampleShared &other = *cluster.map_shared_rank(&S, r);
+                count += other.count[bin];
+                below += other.below[bin];
+            }
+            S0.all_count[bin] = count;
+            S0.all_mass[bin] = expf(-(float)bin * width) * (float)((double)count - (double)below * 0x1p-22);
         }
-        above(lo, &m);
-        const bool at_cut = lo == cut && m < want;       // (the cut's own ties are needed too)
-        const uint32_t edge = at_cut ? cut : hi;
-        const uint32_t over = above(edge, &m), at = at_cut ? ties : above(edge - 1, &mass) - over;
-        const double each = weight(edge), left = want - m;
-        const double need = each > 0.0 ? ceil(left / each) : (double)at;
-        cut = edge;
-        ties = (uint32_t)fmin(fmax(need, over ? 0.0 : 1.0), (double)at);
-    }
-    // the draw, in the order of indexes: a thread's share follows the one before
-    const uint32_t share = (n + kSampleThreads - 1) / kSampleThreads, from = min(n, tid * share), to = min(n, from + share);
-    uint32_t equal = 0;
-    for (uint32_t i = from; i < to; ++i) equal += key_at(i) == cut;
-    s_part[tid] = equal;
-    __syncthreads();
-    uint32_t before = 0;
-    for (uint32_t i = 0; i < tid; ++i) before += (uint32_t)s_part[i];
-    __syncthreads();
-    auto stays = [&](uint32_t key, uint32_t &seen) -> double {
-        const bool in = key > cut || (key == cut && seen++ < ties);
-        const float w = in ? weight(key) : 0.0f;
-        return w < least ? 0.0 : (double)w;
-    };
-    double part = 0.0;
-    uint32_t seen = before;
-    for (uint32_t i = from; i < to; ++i) part += stays(key_at(i), seen);
-    s_part[tid] = part;
-    __syncthreads();
-    double total = 0.0, ahead = 0.0;
-    for (uint32_t i = 0; i < kSampleThreads; ++i) {
-        if (i == tid) ahead = total;
-        total += s_part[i];
-    }
-    const double aim = fmin(fmax((double)u, 0.0), 1.0) * total;
-    if (part > 0.0) {
-        double run = ahead;
-        int32_t found = -1, last = -1;
-        seen = before;
-        for (uint32_t i = from; i < to && found < 0; ++i) {
-            const double w = stays(key_at(i), seen);
-            if (w > 0.0) last = (int32_t)i;
-            run += w;
-            if (w > 0.0 && run > aim) found = (int32_t)i;
+        cluster.sync();
+
+        // ---- the first CTA: up to where in the bins
+        constexpr uint32_t PER = kBins / kSampleThreads;
+        uint32_t count_to = 0, counts[PER] = {};
+        double mass_to = 0.0;
+        float masses[PER] = {};
+        if (rank == 0) {
+            uint32_t c = 0;
+            double m = 0.0;
+#pragma unroll
+            for (uint32_t j = 0; j < PER; ++j) {
+                counts[j] = S.all_count[tid * PER + j];
+                masses[j] = S.all_mass[tid * PER + j];
+                c += counts[j];
+                m += masses[j];
+            }
+            uint32_t ci = c;
+            double mi = m;
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t cu = __shfl_up_sync(kFull, ci, o);
+                const double mu = __shfl_up_sync(kFull, mi, o);
+                if (lane >= o) ci += cu, mi += mu;
+            }
+            if (lane == 31) S.scan_count[warp] = ci, S.scan_mass[warp] = mi;
+            __syncthreads();
+            count_to = ci - c;
+            mass_to = mi - m;
+            for (uint32_t w = 0; w < warp; ++w) count_to += S.scan_count[w], mass_to += S.scan_mass[w];
         }
-        if (found >= 0 && ahead <= aim) A.tokens[row] = found;
-        if (found < 0 && ahead + part >= total && aim >= total) A.tokens[row] = last;
+        // The bin in which the count, or the mass, reaches what is wanted (kBins: in none); `limit`: bins from there on do not count.
+        auto find = [&](bool counted, uint32_t want_count, double want_mass, uint32_t limit) {
+            if (tid == 0) S.found_bin = kBins;
+            __syncthreads();
+            uint32_t c = count_to;
+            double m = mass_to;
+#pragma unroll
+            for (uint32_t j = 0; j < PER; ++j) {
+                const uint32_t c1 = c + counts[j], bin = tid * PER + j;
+                const double m1 = m + masses[j];
+                if (bin < limit && counts[j] && (counted ? c < want_count && c1 >= want_count : m < want_mass && m1 >= want_mass))
+                    S.found_bin = bin, S.found_count = c, S.found_mass = m;
+                c = c1;
+                m = m1;
+            }
+            __syncthreads();
+        };
+        float *const list = (float *)S.count;
+        // All of a bin's logits into the first CTA's list.
+        auto gather = [&](uint32_t bin) {
+            for (uint32_t i = tid; i - lane < R.pieces; i += kSampleThreads) {
+                Piece16<TYPE> x = i < R.pieces ? R.piece(i) : Piece16<TYPE>(make_uint4(kFull, kFull, kFull, kFull));
+                uint32_t hits = 0;
+#pragma unroll
+                for (int e = 0; e < R.N; ++e) {
+                    const float at = place(x.x[e]);
+                    if (at < (float)kBins && (uint32_t)at == bin) hits |= 1u << e;
+                }
+                if (hits) {
+                    uint32_t to = atomicAdd(&S0.listed, __popc(hits));
+                    float *const list0 = (float *)S0.count;
+#pragma unroll
+                    for (int e = 0; e < R.N; ++e)
+                        if (hits >> e & 1) {
+                            if (to < kMostList) list0[to] = x.x[e];
+                            ++to;
+                        }
+                }
+            }
+        };
+        // Searches the keys of a bin: the first key, from above, at which the count (or the mass, in 2^-20 of the bin's upper edge) of all
+        // keys down to it reaches `want`.  above: of the keys above it; equal: how many have it.
+        struct Edge {
+            uint32_t key, equal;
+            double above;
+            bool by_row;                               // every CTA has found it
+        };
+        auto mass20 = [&](float x, uint32_t bin) { return 1048576u - (below_edge(place(x), bin) >> 2); };
+        auto block_sum = [&](uint32_t v, uint32_t turn) {
+            v = __reduce_add_sync(kFull, v);
+            if (lane == 0) S.sums[turn & 1][warp] = v;
+            __syncthreads();
+            return __reduce_add_sync(kFull, lane < kSampleWarps ? S.sums[turn & 1][lane] : 0u);
+        };
+        auto search_list = [&](uint32_t n, uint32_t bin, bool counted, double want, uint32_t lowest) -> Edge {
+            constexpr uint32_t EACH = kMostList / kSampleThreads;
+            uint32_t key[EACH], part[EACH], low = kFull, high = 0;
+#pragma unroll
+            for (uint32_t j = 0; j < EACH; ++j) {
+                const uint32_t i = tid + j * kSampleThreads;
+                key[j] = 0, part[j] = 0;
+                if (i < n) {
+                    key[j] = key_of(list[i]);
+                    part[j] = counted ? 1u : mass20(list[i], bin);
+                    low = min(low, key[j]);
+                    high = max(high, key[j]);
+                }
+            }
+            low = __reduce_min_sync(kFull, low);
+            high = __reduce_max_sync(kFull, high);
+            if (lane == 0) S.sums[0][warp] = low, S.sums[1][warp] = high;
+            __syncthreads();
+            low = __reduce_min_sync(kFull, lane < kSampleWarps ? S.sums[0][lane] : kFull);
+            high = __reduce_max_sync(kFull, lane < kSampleWarps ? S.sums[1][lane] : 0u);
+            __syncthreads();
+            low = max(low, lowest) - 1;                // `want` or more above it (or as much as there is); less above `high`
+            uint32_t turn = 0;
+            auto above = [&](uint32_t mid) {
+                uint32_t v = 0;
+#pragma unroll
+                for (uint32_t j = 0; j < EACH; ++j) v += key[j] > mid ? part[j] : 0u;
+                return block_sum(v, turn++);
+            };
+            while (high - low > 1) {
+                const uint32_t mid = low + (high - low) / 2;
+                if ((double)above(mid) < want) high = mid;
+                else low = mid;
+            }
+            Edge e;
+            e.key = high;
+            e.above = (double)above(high);
+            uint32_t v = 0;
+#pragma unroll
+            for (uint32_t j = 0; j < EACH; ++j) v += key[j] == high;
+            e.equal = block_sum(v, turn++);
+            e.by_row = false;
+            __syncthreads();
+            return e;
+        };
+        // The same where a bin has more logits than the list: every CTA goes through its part of the row at every turn.
+        enum { kCountAbove, kMassAbove, kCountEqual };
+        auto row_total = [&](uint32_t bin, uint32_t edge, int what) -> double {
+            uint64_t v = 0;
+            for (uint32_t i = tid; i < R.pieces; i += kSampleThreads) {
+                const Piece16<TYPE> x = R.piece(i);
+#pragma unroll
+                for (int e = 0; e < R.N; ++e) {
+                    const float at = place(x.x[e]);
+                    if (!(at < (float)kBins) || (uint32_t)at != bin) continue;
+                    const uint32_t key = key_of(x.x[e]);
+                    if (what == kCountEqual ? key == edge : key > edge) v += what == kMassAbove ? mass20(x.x[e], bin) : 1u;
+                }
+            }
+            for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+            if (lane == 0) S.warp_mass[warp] = (double)v;
+            cluster.sync();
+            double sum = 0.0;
+            for (uint32_t r = 0; r < ctas; ++r) {
+                const SampleShared &other = *cluster.map_shared_rank(&S, r);
+                for (uint32_t w = 0; w < kSampleWarps; ++w) sum += other.warp_mass[w];
+            }
+            cluster.sync();
+            return sum;
+        };
+        auto search_row = [&](uint32_t bin, bool counted, double want, uint32_t lowest) -> Edge {
+            uint32_t low = max(key_of(-INFINITY), lowest) - 1, high = key_of(top);
+            while (high - low > 1) {
+                const uint32_t mid = low + (high - low) / 2;
+                if (row_total(bin, mid, counted ? kCountAbove : kMassAbove) < want) high = mid;
+                else low = mid;
+            }
+            Edge e;
+            e.key = high;
+            e.above = row_total(bin, high, counted ? kCountAbove : kMassAbove);
+            e.equal = (uint32_t)row_total(bin, high, kCountEqual);
+            e.by_row = true;
+            return e;
+        };
+        // Gathers and searches a bin that the first CTA names (kBins: none).
+        uint32_t gathered = kBins;
+        auto search = [&](uint32_t bin0, bool counted, double want0, uint32_t lowest0) -> Edge {
+            if (rank == 0 && tid < ctas) {
+                auto &to = cluster.map_shared_rank(&S, tid)->named[counted ? 0 : 1];
+                to.bin = bin0, to.want = want0, to.lowest = lowest0;
+            }
+            cluster.sync();
+            const auto &named = S.named[counted ? 0 : 1];
+            const uint32_t bin = named.bin, lowest = named.lowest;
+            const double want = named.want;
+            Edge e{0, 0, 0.0, false};
+            if (bin == kBins) return e;
+            if (bin != gathered) {
+                if (rank == 0 && tid == 0) S.listed = 0;
+                cluster.sync();
+                gather(bin);
+                cluster.sync();
+                gathered = bin;
+            }
+            const uint32_t n = S0.listed;
+            if (n >= kMostList) return search_row(bin, counted, want, lowest);
+            if (rank == 0) e = search_list(n, bin, counted, want, lowest);
+            return e;
+        };
+
+        double mass = 0.0;                             // of what top_k leaves
+        uint32_t limit = kBins, lowest = 0;
+        if (rank == 0)
+            for (uint32_t w = 0; w < kSampleWarps; ++w) mass += S.scan_mass[w];
+        if (by_count) {
+            uint32_t bin = kBins, before = 0;
+            double mass_before = 0.0;
+            if (rank == 0) {
+                find(true, (uint32_t)k_given, 0.0, kBins);
+                bin = S.found_bin, before = S.found_count, mass_before = S.found_mass;
+                __syncthreads();
+            }
+            const Edge e = search(bin, true, (double)((uint32_t)k_given - before), 0);
+            const double row_mass = e.by_row && by_mass ? row_total(S.named[0].bin, e.key, kMassAbove) : 0.0;
+            if (rank == 0 && bin < kBins) {
+                cut = value_of(e.key);
+                ties = (uint32_t)k_given - before - (uint32_t)e.above;
+                limit = bin + 1;
+                lowest = e.key;
+                if (by_mass) {
+                    // the mass of what stays of the bin: its keys above the cut, and the ties
+                    double inside = row_mass;
+                    if (!e.by_row) {
+                        uint32_t v = 0;
+                        for (uint32_t i = tid; i < S.listed; i += kSampleThreads) v += key_of(list[i]) > e.key ? mass20(list[i], bin) : 0u;
+                        inside = (double)block_sum(v, 0);
+                        __syncthreads();
+                    }
+                    mass = mass_before + exp((double)(-(float)bin * width)) * 0x1p-20 * (inside + (double)ties * mass20(cut, bin));
+                }
+            }
+        }
+        if (by_mass) {
+            uint32_t bin = kBins;
+            double want = (double)p * mass, part = 0.0;
+            if (rank == 0) {
+                find(false, 0, want, limit);
+                bin = S.found_bin;
+                part = (want - S.found_mass) * exp((double)((float)bin * width)) * 0x1p20;
+                __syncthreads();
+            }
+            const Edge e = search(bin, false, part, bin + 1 == limit ? lowest : 0);
+            if (rank == 0 && bin < kBins) {
+                const uint32_t have = bin + 1 == limit && e.key == lowest ? ties : e.equal;
+                const float edge = value_of(e.key);
+                const double need = ceil((part - e.above) / (double)mass20(edge, bin));
+                cut = edge;
+                ties = (uint32_t)fmin(fmax(need, 1.0), (double)have);
+            }
+        }
+        __syncthreads();
+        if (rank == 0 && tid < ctas) {
+            SampleShared &other = *cluster.map_shared_rank(&S, tid);
+            other.cut = cut, other.ties = ties;
+        }
+        cluster.sync();
+        cut = S.cut;
+        ties = S.ties;
     }
+
+    // ---- the draw, in the order of indexes: warps have stretches of the row, lanes pieces of 16 bytes that follow each other
+    const uint32_t stretch = (R.pieces + kSampleWarps * 32 - 1) / (kSampleWarps * 32) * 32, from = warp * stretch, to = min(R.pieces, from + stretch);
+    {
+        float sum = 0.0f;
+        uint32_t equal = 0;
+        for (uint32_t i = from + lane; i < to; i += 32) {
+            const Piece16<TYPE> x = R.piece(i);
+#pragma unroll
+            for (int e = 0; e < R.N; ++e) {
+                if (x.x[e] > cut) {
+                    const float w = weight(x.x[e]);
+                    sum += w < least_weight ? 0.0f : w;
+                }
+                equal += x.x[e] == cut;
+            }
+        }
+        double m = sum;
+        for (int o = 16; o; o >>= 1) m += __shfl_xor_sync(kFull, m, o);
+        equal = __reduce_add_sync(kFull, equal);
+        if (lane == 0) S.warp_mass[warp] = m, S.warp_equal[warp] = equal;
+    }
+    cluster.sync();
+    for (uint32_t i = tid; i < ctas * kSampleWarps; i += kSampleThreads) {
+        const SampleShared &other = *cluster.map_shared_rank(&S, i / kSampleWarps);
+        S.table_mass[i] = other.warp_mass[i % kSampleWarps];
+        S.table_equal[i] = other.warp_equal[i % kSampleWarps];
+    }
+    cluster.sync();                                    // (the last look at another CTA's shared memory)
+    const float cut_weight_given = cut == -INFINITY ? 0.0f : weight(cut), cut_weight = cut_weight_given < least_weight ? 0.0f : cut_weight_given;
+    // every warp: the stretch in which the mass exceeds what is drawn
+    const uint32_t stretches = ctas * kSampleWarps, own = rank * kSampleWarps + warp;
+    uint32_t equal_before = 0, equal_own = 0;
+    double run = 0.0, own_from = 0.0, total = 0.0;
+    int32_t chosen = -1, last = -1;
+    for (int turn = 0; turn < 2; ++turn) {             // (all of the mass, then where)
+        const double aim = fmin(fmax((double)u, 0.0), 1.0) * total;
+        uint32_t equals = 0;
+        run = 0.0;
+        for (uint32_t base = 0; base < stretches; base += 32) {
+            const uint32_t i = base + lane;
+            const uint32_t eq = i < stretches ? S.table_equal[i] : 0;
+            uint32_t eq_to = eq;
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t up = __shfl_up_sync(kFull, eq_to, o);
+                if (lane >= o) eq_to += up;
+            }
+            const uint32_t eq_from = equals + eq_to - eq, stay = eq_from < ties ? min(eq, ties - eq_from) : 0;
+            double m = i < stretches ? S.table_mass[i] + (double)stay * cut_weight : 0.0, m_to = m;
+            for (int o = 1; o < 32; o <<= 1) {
+                const double up = __shfl_up_sync(kFull, m_to, o);
+                if (lane >= o) m_to += up;
+            }
+            if (turn) {
+                const uint32_t over = __ballot_sync(kFull, m > 0.0 && run + m_to > aim), some = __ballot_sync(kFull, m > 0.0);
+                if (chosen < 0 && over) chosen = base + __ffs(over) - 1;
+                if (some) last = base + 31 - __clz(some);
+                if (own >= base && own < base + 32) {
+                    own_from = run + __shfl_sync(kFull, m_to - m, own - base);
+                    equal_before = __shfl_sync(kFull, eq_from, own - base);
+                    equal_own = __shfl_sync(kFull, eq, own - base);
+                }
+            }
+            equals += __shfl_sync(kFull, eq_to, 31);
+            run += __shfl_sync(kFull, m_to, 31);
+        }
+        total = run;
+    }
+    if (own != (uint32_t)(chosen >= 0 ? chosen : last)) return;
+    // the stretch's warp: the token (its sums may round otherwise than all of it did: then its last one)
+    const double aim = chosen >= 0 ? fmin(fmax((double)u, 0.0), 1.0) * total : INFINITY;
+    int32_t token = -1;
+    run = own_from;
+    for (uint32_t i0 = from; i0 < to; i0 += 32) {
+        const uint32_t i = i0 + lane;
+        const Piece16<TYPE> x = i < to ? R.piece(i) : Piece16<TYPE>(make_uint4(kFull, kFull, kFull, kFull));
+        float w[R.N];
+        uint32_t eq = 0, any = 0;
+#pragma unroll
+        for (int e = 0; e < R.N; ++e) eq += x.x[e] == cut, any |= x.x[e] >= cut;
+        if (!__any_sync(kFull, any)) continue;
+        uint32_t eq_to = eq;
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t up = __shfl_up_sync(kFull, eq_to, o);
+            if (lane >= o) eq_to += up;
+        }
+        uint32_t seen = equal_before + eq_to - eq;
+        double m = 0.0;
+#pragma unroll
+        for (int e = 0; e < R.N; ++e) {
+            w[e] = 0.0f;
+            if (x.x[e] > cut) w[e] = weight(x.x[e]);
+            if (x.x[e] == cut && seen++ < ties) w[e] = cut_weight;
+            if (w[e] < least_weight) w[e] = 0.0f;
+            m += w[e];
+        }
+        double m_to = m;
+        for (int o = 1; o < 32; o <<= 1) {
+            const double up = __shfl_up_sync(kFull, m_to, o);
+            if (lane >= o) m_to += up;
+        }
+        const uint32_t over = __ballot_sync(kFull, m > 0.0 && run + m_to > aim), some = __ballot_sync(kFull, m > 0.0);
+        if (some) {
+            const int who = over ? __ffs(over) - 1 : 31 - __clz(some);
+            if (lane == who) {
+                double r = run + m_to - m;
+                int e = -1;
+#pragma unroll
+                for (int j = 0; j < R.N; ++j) {
+                    const bool was_over = e >= 0 && r > aim;
+                    if (w[j] > 0.0f && !was_over) {
+                        r += w[j];
+                        e = j;
+                    }
+                }
+                token = (int32_t)(i * R.N + e) - (int32_t)R.phase;
+            }
+            token = __shfl_sync(kFull, token, who);
+            if (over) break;
+        }
+        equal_before += __shfl_sync(kFull, eq_to, 31);
+        run += __shfl_sync(kFull, m_to, 31);
+    }
+    if (lane == 0) A.tokens[row] = (int32_t)i0 + token;
 }
 
-cudaError_t launch_sampling(const SamplingArgs &a, uint32_t, cudaStream_t stream) {
-    return launch_behind(a.type == 0 ? sample_kernel<0> : a.type == 1 ? sample_kernel<1> : sample_kernel<2>, dim3(a.rows), kSampleThreads, 0, stream, a);
+template <int TYPE>
+static cudaError_t launch_type(const SamplingArgs &a, uint32_t ctas, uint32_t smem, cudaStream_t stream) {
+    static std::atomic<bool> attr_set[64];             // set twice by racing threads at worst: the call is idempotent
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (dev < 0 || dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
+        const cudaError_t e = cudaFuncSetAttribute(sample_kernel<TYPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSampleMostSmem);
+        if (e != cudaSuccess) return e;
+        if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(a.rows * ctas);
+    cfg.blockDim = dim3(kSampleThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, sample_kernel<TYPE>, a);
+}
+
+cudaError_t launch_sampling(const SamplingArgs &args, uint32_t sms, cudaStream_t stream) {
+    SamplingArgs a = args;
+    const uint32_t size = a.type == 0 ? 4 : 2;
+    // As many CTAs a row as keep it at 80 KB each (two CTAs an SM), and more while SMs are idle and a CTA has more than 2048 logits.
+    uint32_t ctas = 1;
+    while (ctas < kMostCluster && ((uint64_t)a.vocab * size > ctas * 81920ull || ((uint64_t)a.rows * ctas * 2 <= sms && a.vocab > ctas * 2048u))) ctas *= 2;
+    a.part = (uint32_t)(((uint64_t)a.vocab + ctas - 1) / ctas);
+    const uint64_t pieces = ((uint64_t)a.part * size + 30) / 16, room = (kSampleMostSmem - sizeof(SampleShared)) / 16;
+    a.kept_pieces = (uint32_t)(pieces < room ? pieces : room);
+    const uint32_t smem = (uint32_t)sizeof(SampleShared) + a.kept_pieces * 16;
+    return a.type == 0 ? launch_type<0>(a, ctas, smem, stream) : a.type == 1 ? launch_type<1>(a, ctas, smem, stream) : launch_type<2>(a, ctas, smem, stream);
 }
 
 }  // namespace huffllm

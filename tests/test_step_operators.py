@@ -608,6 +608,28 @@ def test_sample_ties_go_to_the_lowest_index(hl, torch):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("vocab,rows", [(30011, 3), (150001, 2), (9001, 160)])
+def test_sample_crowded_logits(hl, torch, vocab, rows):
+    """Thousands of tokens next to each other in their logits, a few distinct values of them or many; very high and very low temperatures."""
+    rng = np.random.default_rng(vocab)
+    for kind in range(4):
+        x = [rng.integers(0, 3, (rows, vocab)) * 1e-3, 5 + rng.random((rows, vocab)) * 1e-3, np.full((rows, vocab), -2.5),
+             np.where(rng.random((rows, vocab)) < 0.5, 1.0, rng.standard_normal((rows, vocab)))][kind]
+        x[:, vocab // 2] = 5.5
+        for t in (1.0, 1e-4, 50.0):
+            # (cuts by mass between the borders of whole groups of equals, where 1e-5 of the mass is less than a token)
+            settings = {"temperature": [t] * rows, "top_k": [[vocab // 3, 0, 7000][i % 3] for i in range(rows)],
+                        "top_p": [[0.61234, 0.5, 1.0, 0.87654][i % 4] for i in range(rows)], "min_p": [0.0] * rows}
+            u = rng.random(rows)
+            tokens, seen = run_sample(hl, torch, x, "f32", settings, u)
+            for i in range(rows):
+                want, near, kept = sample64(seen[i], np.float64(np.float32(t)), settings["top_k"][i], float(np.float32(settings["top_p"][i])), 0.0, float(np.float32(u[i])))
+                # weights of up to 150000 like tokens lie 7e-6 of the mass apart: a draw lands within a few tokens of the exact one
+                place, got = np.searchsorted(kept, want), np.searchsorted(kept, tokens[i])
+                assert 0 <= got < len(kept) + 1 and abs(int(got) - int(place)) <= 2 + 1e-5 * len(kept) * 2, (kind, t, i, tokens[i], want)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "fp16"])
 def test_sample_masked_logits(hl, torch, dtype):
     """Minus infinity, the type's lowest value, NaN, plus infinity; rows with one token left, and with none."""
