@@ -512,7 +512,7 @@ huffllm_status huffllm_decode_ffn(const huffllm_ffn *ffn, const void *h_dev, uin
  * rotary_dim on are copied.  sections[a] is the number of pairs of axis a; they add up to rotary_dim / 2, and lie one axis behind the
  * other, or (in_turn) are dealt to the axes in turn, an axis that has had all of its pairs being passed over.
  * q and k: [tokens][heads][head_dim] words of dtype, a stride being the values from one token to the next (0 = packed).  k may be null (no
- * keys), or q.  An out may be its input itself (same pointer, same stride); other overlaps are not allowed.
+ * keys).  An out may be its input itself (same pointer, same stride); other overlaps are not allowed.
  */
 typedef enum {
     HUFFLLM_PAIR_HALVES = 0,       /* channels i and i + rotary_dim / 2 */

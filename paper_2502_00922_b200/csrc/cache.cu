@@ -1,4 +1,9 @@
 // The 4-bit cache: new tokens written, tokens read back.
+//
+// A warp has the tokens that a call brings of one block (up to 16), of one head, of its keys or of its values.  A lane has eight channels of a
+// token, which come and go as 16 bytes, four lanes have a group.  Eight codes are a word of the keys as it lies; of the values, a word has four
+// tokens of two channels, so these change places in shared memory, four by four bytes.  Bound by memory where rows are many (the
+// instructions are about ten a value), by latency where they are few: rows are then a CTA each, and heads spread over more of them.
 #include <cuda_runtime.h>
 
 #include "cache_rows.cuh"
@@ -7,121 +12,281 @@
 
 namespace huffllm {
 
-constexpr uint32_t kCacheThreads = 256;
+constexpr uint32_t kCacheWarps = 8;
 
-// Scale and offset of a group from its smallest and largest value; false where it stands for NaN.
-__device__ __forceinline__ bool scale_of(float low, float high, bool finite, __half &s, __half &m) {
-    s = __float2half_rn(__fdiv_rn(high - low, 15.0f));
-    m = __float2half_rn(low);
-    if (finite && __half2float(s) < INFINITY && fabsf(__half2float(m)) < INFINITY) return true;
-    s = __ushort_as_half(0x7FFFu);
-    m = __ushort_as_half(0u);
-    return false;
-}
-// The code of x: (x - m) / s, exactly rounded.  The quotient in fp32 is off by less than 1e-5, so 64 bits decide only next to a border.
-__device__ __forceinline__ uint32_t code_of(float x, float s, float m) {
-    if (s == 0.0f) return 0;
-    float q = (x - m) / s;
-    if (fabsf(q - floorf(q) - 0.5f) < 1e-4f) q = (float)rint(((double)x - (double)m) / (double)s);
-    return (uint32_t)fminf(fmaxf(rintf(q), 0.0f), 15.0f);
+// The rows of a call that lie in one block.
+struct BlockRows {
+    uint32_t row, count;           // the first of them, and how many
+    uint32_t r;                    // its place in the block
+    int64_t block;                 // number of the block of head 0 among the pool's, or -1
+    uint32_t head_step;            // from there to the next head's
+};
+
+// Calls f(BlockRows) for every block that begins among the CTA's `rows` rows; a warp at a time, all lanes alike.
+template <typename F>
+__device__ __forceinline__ void for_blocks(const CacheArgs &C, const CacheRows &R, uint32_t rows, F f) {
+    constexpr uint32_t kFull = 0xFFFFFFFFu;
+    const uint32_t lane = threadIdx.x % 32, row = blockIdx.x * rows + lane;
+    if (blockIdx.x == 0 && blockIdx.y == 0) report_faults(C, R.starts, R.rows, R.err);
+    BlockRows B{row, 0, 0, -1, C.page_tokens / kCacheBlock};
+    if (lane < rows && row < R.rows) {
+        const uint32_t b = sequence_of_row(R.starts, C.sequences, row);
+        const Sequence S = sequence_of(C, R.starts, R.rows, b < C.sequences ? b : 0);
+        const uint32_t i = row - S.first_row;
+        const int32_t at = S.tokens - (int32_t)S.rows + (int32_t)i;
+        if (b < C.sequences && !S.bad && row >= S.first_row && i < S.rows && at >= 0 && (at % kCacheBlock == 0 || i == 0 || at == 0)) {
+            B.r = at % kCacheBlock;
+            B.count = min(kCacheBlock - B.r, S.rows - i);
+            const int32_t page = __ldcg(C.table + (uint64_t)b * C.table_stride + at / C.page_tokens);
+            if (page >= 0 && (uint32_t)page < C.pages) B.block = (int64_t)page * C.kv_heads * B.head_step + at % C.page_tokens / kCacheBlock;
+            else if (R.err) *R.err = (int32_t)b + 1;
+        }
+    }
+    for (uint32_t who = __ballot_sync(kFull, B.block >= 0); who; who &= who - 1) {
+        const int l = __ffs(who) - 1;
+        f(BlockRows{__shfl_sync(kFull, B.row, l), __shfl_sync(kFull, B.count, l), __shfl_sync(kFull, B.r, l), (int64_t)__shfl_sync(kFull, (long long)B.block, l), B.head_step});
+    }
 }
 
-// A warp per row, head and side (keys, values); a lane has channel `lane` of a group.
-template <bool F16>
-__global__ void __launch_bounds__(kCacheThreads) cache_append_kernel(const __grid_constant__ CacheArgs C, const __grid_constant__ CacheRows R) {
+// Four words, a byte of each into every word of the result: out[i] has byte i of in[0], in[1], in[2], in[3].
+__device__ __forceinline__ void transpose_bytes(const uint32_t (&in)[4], uint32_t (&out)[4]) {
+    const uint32_t a = prmt(in[0], in[1], 0x5140), b = prmt(in[2], in[3], 0x5140), c = prmt(in[0], in[1], 0x7362), d = prmt(in[2], in[3], 0x7362);
+    out[0] = prmt(a, b, 0x5410), out[1] = prmt(a, b, 0x7632), out[2] = prmt(c, d, 0x5410), out[3] = prmt(c, d, 0x7632);
+}
+// Token i of the four in a word of values, t4's.
+__device__ __forceinline__ uint32_t token_of(uint32_t t4, uint32_t i) { return 2 * t4 + (i >> 1) + (i & 1) * 8; }
+
+// Words 4 half .. 4 half + 3 of value rows (g) and tile j of 16 channels, tokens t4's: items of a block are 2 * dim.  Neighbouring items are neighbours in
+// memory: the words of a lane, then the lanes of a row.
+template <uint32_t DIM>
+struct ValueItem {
+    uint32_t t4, j, half, word;                            // word: into the block's words, of row g = 4 half; the next g is 4 lanes on
+    static constexpr uint32_t kItems = DIM / 16 * 8;
+    __device__ __forceinline__ explicit ValueItem(uint32_t i) {
+        t4 = i / 4 % 4;
+        half = i / 16 % 2;
+        j = i % 4 + i / 32 * 4;
+    }
+    __device__ __forceinline__ bool exists() const { return j < DIM / 16; }
+    __device__ __forceinline__ uint32_t at(uint32_t g) const { return value_byte_at(DIM, 2 * t4, 16 * j + 4 * half + g); }   // bytes into the block
+};
+
+template <uint32_t DIM, bool F16>
+__global__ void __launch_bounds__(kCacheWarps * 32) cache_append_kernel(const __grid_constant__ CacheArgs C, const __grid_constant__ CacheRows R,
+                                                                        const uint32_t rows) {
+    constexpr uint32_t CHUNKS = DIM / 8, EACH = kCacheBlock * CHUNKS / 32, G = cache_groups(DIM), kFull = 0xFFFFFFFFu;
+    __shared__ uint32_t s_codes[kCacheWarps][kCacheBlock * DIM / 8];       // [token][16 channels][2]: a byte is two channels, eight apart
     pdl_launch_dependents();
     pdl_wait_prior_grid();
-    if (blockIdx.x == 0) report_faults(C, R.starts, R.rows, R.err);
-    const uint32_t lane = threadIdx.x % 32;
-    const uint64_t item = (uint64_t)blockIdx.x * (kCacheThreads / 32) + threadIdx.x / 32;
-    const uint32_t row = (uint32_t)(item / (2 * C.kv_heads)), h = (uint32_t)(item % (2 * C.kv_heads)) / 2, side = item % 2;
-    if (row >= R.rows) return;
-    const uint32_t b = sequence_of_row(R.starts, C.sequences, row);
-    if (b >= C.sequences) return;
-    const Sequence S = sequence_of(C, R.starts, R.rows, b);
-    if (S.bad || row < S.first_row || row - S.first_row >= S.rows) return;
-    const int32_t at = S.tokens - (int32_t)S.rows + (int32_t)(row - S.first_row);
-    if (at < 0) return;
-    uint8_t *const block = block_of(C, b, at, h);
-    if (!block) {
-        if (R.err && lane == 0) *R.err = (int32_t)b + 1;
-        return;
-    }
-    const uint32_t r = at % kCacheBlock;
-    const uint16_t *x = (side ? R.v + row * R.v_stride : R.k + row * R.k_stride) + h * C.dim;
-    for (uint32_t g = 0; g < cache_groups(C.dim); ++g) {
-        const float v = widen16<F16>(__ldcg(x + g * kCacheGroup + lane));
-        float low = v, high = v;
-        for (int o = 16; o; o >>= 1) {
-            low = fminf(low, __shfl_xor_sync(0xFFFFFFFFu, low, o));
-            high = fmaxf(high, __shfl_xor_sync(0xFFFFFFFFu, high, o));
+    const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const bool wide = !(((uintptr_t)R.k | (uintptr_t)R.v) & 15) && R.k_stride % 8 == 0 && R.v_stride % 8 == 0;
+    for_blocks(C, R, rows, [&](const BlockRows &B) {
+        for (uint32_t task = blockIdx.y * kCacheWarps + warp; task < 2 * C.kv_heads; task += gridDim.y * kCacheWarps) {
+            const uint32_t head = task / 2, side = task % 2;
+            const uint16_t *const x = (side ? R.v : R.k) + head * DIM;
+            const uint64_t stride = side ? R.v_stride : R.k_stride;
+            uint8_t *const block = C.pool + (uint64_t)(B.block + (int64_t)head * B.head_step) * cache_block_bytes(DIM);
+            uint4 raw[EACH];
+#pragma unroll
+            for (uint32_t k = 0; k < EACH; ++k) {
+                const uint32_t i = k * 32 + lane, token = i / CHUNKS, chunk = i % CHUNKS;
+                raw[k] = make_uint4(0, 0, 0, 0);
+                if (token - B.r >= B.count) continue;      // (wraps in front of the first)
+                const uint16_t *const from = x + (uint64_t)(B.row + token - B.r) * stride + chunk * 8;
+                if (wide) {
+                    raw[k] = __ldcg((const uint4 *)from);
+                } else {
+                    uint32_t e[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) e[j] = __ldcg((const unsigned short *)from + j);
+                    raw[k] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+                }
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < EACH; ++k) {
+                const uint32_t i = k * 32 + lane, token = i / CHUNKS, chunk = i % CHUNKS, group = chunk / 4, t4 = chunk % 4;
+                const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+                float v[8], low, high;
+                uint32_t most = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[2 * j] = widen16<F16>((uint16_t)w[j]), v[2 * j + 1] = widen16<F16>((uint16_t)(w[j] >> 16));
+                    most = __vmaxu2(most, w[j] & 0x7FFF7FFFu);
+                    low = j ? fminf(low, fminf(v[2 * j], v[2 * j + 1])) : fminf(v[0], v[1]);
+                    high = j ? fmaxf(high, fmaxf(v[2 * j], v[2 * j + 1])) : fmaxf(v[0], v[1]);
+                }
+#pragma unroll
+                for (int o = 1; o < 4; o <<= 1) {
+                    low = fminf(low, __shfl_xor_sync(kFull, low, o));
+                    high = fmaxf(high, __shfl_xor_sync(kFull, high, o));
+                    most = __vmaxu2(most, __shfl_xor_sync(kFull, most, o));
+                }
+                __half s = __float2half_rn(__fdiv_rn(high - low, 15.0f)), m = __float2half_rn(low);
+                const uint32_t infinite = F16 ? 0x7C00u : 0x7F80u;
+                const bool sound = max(most & 0xFFFFu, most >> 16) < infinite && __half2float(s) < INFINITY && fabsf(__half2float(m)) < INFINITY;
+                if (!sound) s = __ushort_as_half(0x7FFFu), m = __ushort_as_half(0);
+                const float fs = __half2float(s), fm = __half2float(m), by = sound && fs != 0.0f ? 1.0f / fs : 0.0f;
+                // The code is (x - m) / s rounded.  In fp32 the quotient is off by less than 1e-5: 64 bits decide next to a border alone.
+                uint32_t code[8];
+                float edge = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float q = fminf(fmaxf((v[j] - fm) * by, 0.0f), 15.0f), up = q + 12582912.0f;   // (1.5 * 2^23: the sum is whole)
+                    edge = fmaxf(edge, fabsf(q - (up - 12582912.0f)));
+                    code[j] = __float_as_uint(up) & 15u;
+                }
+                if (edge > 0.49998f && by != 0.0f) {
+#pragma unroll 1
+                    for (int j = 0; j < 8; ++j) {
+                        const double q = ((double)widen16<F16>((uint16_t)(w[j >> 1] >> (j & 1) * 16)) - (double)fm) / (double)fs;
+                        const uint32_t c = (uint32_t)fmin(fmax(rint(q), 0.0), 15.0);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) code[k] = k == j ? c : code[k];
+                    }
+                }
+                const bool here = token - B.r < B.count;
+                if (side == 0) {
+                    uint32_t word = 0;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) word |= code[j] << ((j & 1) * 16 + (j >> 1) * 4);
+                    if (here) *(uint32_t *)(block + key_word_at(DIM, token, group, t4)) = word;
+                } else {
+                    // eight channels of 16 come from this lane, the others from its neighbour; each gets half of their bytes
+                    uint32_t nibbles[2] = {code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24, code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24};
+                    const uint32_t other = __shfl_xor_sync(kFull, lane & 1 ? nibbles[0] : nibbles[1], 1);
+                    s_codes[warp][token * (DIM / 8) + chunk] = lane & 1 ? other | nibbles[1] << 4 : nibbles[0] | other << 4;
+                }
+                if (here && t4 == 0) {
+                    *(__half *)(block + (side ? value_scale_at(DIM, token, group) : key_scale_at(DIM, token, group))) = s;
+                    *(__half *)(block + (side ? value_offset_at(DIM, token, group) : key_offset_at(DIM, token, group))) = m;
+                    // (keys' offsets are read in pairs, and what is read is multiplied by 0: it must be a number)
+                    if (G % 2 && side == 0 && group + 1 == G) *(__half *)(block + key_offset_at(DIM, token, group + 1)) = __ushort_as_half(0);
+                }
+            }
+            if (side == 0) continue;
+            __syncwarp();
+#pragma unroll
+            for (uint32_t i = 0; i < (ValueItem<DIM>::kItems + 31) / 32 * 32; i += 32) {
+                const ValueItem<DIM> item(i + lane);
+                if (!item.exists()) continue;
+                uint32_t in[4], out[4], mask = 0;
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j) {
+                    const uint32_t token = token_of(item.t4, j);
+                    in[j] = s_codes[warp][token * (DIM / 8) + item.j * 2 + item.half];
+                    mask |= token - B.r < B.count ? 1u << j : 0u;
+                }
+                transpose_bytes(in, out);
+#pragma unroll
+                for (uint32_t g = 0; g < 4; ++g) {
+                    uint8_t *const to = block + item.at(g);
+                    if (mask == 15u) {
+                        *(uint32_t *)to = out[g];
+                    } else {
+#pragma unroll
+                        for (uint32_t j = 0; j < 4; ++j)
+                            if (mask >> j & 1) to[j] = (uint8_t)(out[g] >> 8 * j);
+                    }
+                }
+            }
+            __syncwarp();
         }
-        __half s, m;
-        const bool sound = scale_of(low, high, __all_sync(0xFFFFFFFFu, fabsf(v) < INFINITY), s, m);
-        const uint32_t code = sound ? code_of(v, __half2float(s), __half2float(m)) : 0u;
-        if (side == 0) {
-            uint32_t word = code << ((lane & 1) * 16 + (lane % 8 >> 1) * 4);
-            for (int o = 1; o < 8; o <<= 1) word |= __shfl_xor_sync(0xFFFFFFFFu, word, o);
-            if (lane % 8 == 0) *(uint32_t *)(block + key_word_at(C.dim, r, g, lane / 8)) = word;
-        } else {
-            const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, code, 8);
-            if (lane % 16 < 8) block[value_byte_at(C.dim, r, g * kCacheGroup + lane)] = (uint8_t)(code | other << 4);
-        }
-        if (lane == 0) {
-            *(__half *)(block + (side ? value_scale_at(C.dim, r, g) : key_scale_at(C.dim, r, g))) = s;
-            *(__half *)(block + (side ? value_offset_at(C.dim, r, g) : key_offset_at(C.dim, r, g))) = m;
-            // (keys' offsets are read in pairs, and what is read is multiplied by 0: it must be a number)
-            if (side == 0 && g + 1 == cache_groups(C.dim) && g % 2 == 0) *(__half *)(block + key_offset_at(C.dim, r, g + 1)) = __ushort_as_half(0);
-        }
-    }
+    });
 }
 
-template <bool F16>
-__global__ void __launch_bounds__(kCacheThreads) cache_read_kernel(const __grid_constant__ CacheArgs C, const __grid_constant__ CacheRows R) {
+template <uint32_t DIM, bool F16>
+__global__ void __launch_bounds__(kCacheWarps * 32) cache_read_kernel(const __grid_constant__ CacheArgs C, const __grid_constant__ CacheRows R,
+                                                                      const uint32_t rows) {
+    constexpr uint32_t CHUNKS = DIM / 8, EACH = kCacheBlock * CHUNKS / 32;
+    __shared__ uint32_t s_codes[kCacheWarps][kCacheBlock * DIM / 8];
     pdl_launch_dependents();
     pdl_wait_prior_grid();
-    if (blockIdx.x == 0) report_faults(C, R.starts, R.rows, R.err);
-    const uint32_t lane = threadIdx.x % 32;
-    const uint64_t item = (uint64_t)blockIdx.x * (kCacheThreads / 32) + threadIdx.x / 32;
-    const uint32_t row = (uint32_t)(item / (2 * C.kv_heads)), h = (uint32_t)(item % (2 * C.kv_heads)) / 2, side = item % 2;
-    if (row >= R.rows) return;
-    const uint32_t b = sequence_of_row(R.starts, C.sequences, row);
-    if (b >= C.sequences) return;
-    const Sequence S = sequence_of(C, R.starts, R.rows, b);
-    if (S.bad || row < S.first_row || row - S.first_row >= S.rows) return;
-    const int32_t at = S.tokens - (int32_t)S.rows + (int32_t)(row - S.first_row);
-    if (at < 0) return;
-    const uint8_t *const block = block_of(C, b, at, h);
-    if (!block) {
-        if (R.err && lane == 0) *R.err = (int32_t)b + 1;
-        return;
-    }
-    const uint32_t r = at % kCacheBlock;
-    void *const out = side ? (void *)R.v : (void *)R.k;
-    if (!out) return;
-    const uint64_t to = row * (side ? R.v_stride : R.k_stride) + h * C.dim;
-    for (uint32_t g = 0; g < cache_groups(C.dim); ++g) {
-        const uint32_t d = g * kCacheGroup + lane;
-        uint32_t code;
-        if (side == 0) code = *(const uint32_t *)(block + key_word_at(C.dim, r, g, lane / 8)) >> ((lane & 1) * 16 + (lane % 8 >> 1) * 4) & 15u;
-        else code = block[value_byte_at(C.dim, r, lane % 16 < 8 ? d : d - 8)] >> (lane % 16 < 8 ? 0 : 4) & 15u;
-        const float s = __half2float(*(const __half *)(block + (side ? value_scale_at(C.dim, r, g) : key_scale_at(C.dim, r, g))));
-        const float m = __half2float(*(const __half *)(block + (side ? value_offset_at(C.dim, r, g) : key_offset_at(C.dim, r, g))));
-        const float v = fmaf(s, (float)code, m);
-        if (R.f32) ((float *)out)[to + d] = v;
-        else ((uint16_t *)out)[to + d] = round16<F16>(v);
-    }
+    const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const bool wide = !(((uintptr_t)R.k | (uintptr_t)R.v) & 15) && R.k_stride % 8 == 0 && R.v_stride % 8 == 0;
+    for_blocks(C, R, rows, [&](const BlockRows &B) {
+        for (uint32_t task = blockIdx.y * kCacheWarps + warp; task < 2 * C.kv_heads; task += gridDim.y * kCacheWarps) {
+            const uint32_t head = task / 2, side = task % 2;
+            uint16_t *const base = side ? R.v : R.k;
+            if (!base) continue;
+            const uint64_t stride = side ? R.v_stride : R.k_stride;
+            const uint8_t *const block = C.pool + (uint64_t)(B.block + (int64_t)head * B.head_step) * cache_block_bytes(DIM);
+            if (side) {
+#pragma unroll
+                for (uint32_t i = 0; i < (ValueItem<DIM>::kItems + 31) / 32 * 32; i += 32) {
+                    const ValueItem<DIM> item(i + lane);
+                    if (!item.exists()) continue;
+                    uint32_t in[4], out[4];
+#pragma unroll
+                    for (uint32_t g = 0; g < 4; ++g) in[g] = __ldcg((const uint32_t *)(block + item.at(g)));
+                    transpose_bytes(in, out);
+#pragma unroll
+                    for (uint32_t j = 0; j < 4; ++j) s_codes[warp][token_of(item.t4, j) * (DIM / 8) + item.j * 2 + item.half] = out[j];
+                }
+                __syncwarp();
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < EACH; ++k) {
+                const uint32_t i = k * 32 + lane, token = i / CHUNKS, chunk = i % CHUNKS, group = chunk / 4, t4 = chunk % 4;
+                if (token - B.r >= B.count) continue;
+                const float s = __half2float(__ushort_as_half(__ldcg((const unsigned short *)(block + (side ? value_scale_at(DIM, token, group) : key_scale_at(DIM, token, group))))));
+                const float m = __half2float(__ushort_as_half(__ldcg((const unsigned short *)(block + (side ? value_offset_at(DIM, token, group) : key_offset_at(DIM, token, group))))));
+                float v[8];
+                if (side) {
+                    const uint32_t pair = token * (DIM / 8) + chunk / 2 * 2, shift = chunk % 2 * 4;
+                    const uint32_t c0 = s_codes[warp][pair] >> shift, c1 = s_codes[warp][pair + 1] >> shift;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = fmaf(s, (float)(c0 >> 8 * j & 15u), m), v[4 + j] = fmaf(s, (float)(c1 >> 8 * j & 15u), m);
+                } else {
+                    const uint32_t word = __ldcg((const uint32_t *)(block + key_word_at(DIM, token, group, t4)));
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = fmaf(s, (float)(word >> ((j & 1) * 16 + (j >> 1) * 4) & 15u), m);
+                }
+                const uint64_t to = (uint64_t)(B.row + token - B.r) * stride + head * DIM + chunk * 8;
+                if (R.f32) {
+                    float *const o = (float *)base + to;
+                    if (wide) {
+                        ((float4 *)o)[0] = make_float4(v[0], v[1], v[2], v[3]);
+                        ((float4 *)o)[1] = make_float4(v[4], v[5], v[6], v[7]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) o[j] = v[j];
+                    }
+                } else {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = round16<F16>(v[2 * j]) | (uint32_t)round16<F16>(v[2 * j + 1]) << 16;
+                    if (wide) {
+                        *(uint4 *)(base + to) = make_uint4(w[0], w[1], w[2], w[3]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) base[to + j] = (uint16_t)(w[j >> 1] >> (j & 1) * 16);
+                    }
+                }
+            }
+            if (side) __syncwarp();
+        }
+    });
 }
 
-static uint32_t items_grid(const CacheArgs &c, const CacheRows &r) {
-    const uint64_t warps = (uint64_t)r.rows * c.kv_heads * 2;
-    return (uint32_t)((warps + kCacheThreads / 32 - 1) / (kCacheThreads / 32));
+template <uint32_t DIM>
+static cudaError_t launch_move(bool append, const CacheArgs &c, const CacheRows &r, uint32_t sms, cudaStream_t stream) {
+    // Sixteen rows a CTA, as many as a block has, where that leaves every SM some CTAs (rows find their blocks lane by lane); else one.
+    const uint32_t tasks = (2 * c.kv_heads + kCacheWarps - 1) / kCacheWarps;
+    const uint32_t rows = (uint64_t)(r.rows / kCacheBlock) * tasks >= 2 * (uint64_t)sms ? kCacheBlock : 1;
+    const dim3 grid((r.rows + rows - 1) / rows, tasks);
+    auto kernel = append ? (c.fp16 ? cache_append_kernel<DIM, true> : cache_append_kernel<DIM, false>) : (c.fp16 ? cache_read_kernel<DIM, true> : cache_read_kernel<DIM, false>);
+    return launch_behind(kernel, grid, kCacheWarps * 32, 0, stream, c, r, rows);
 }
-cudaError_t launch_cache_append(const CacheArgs &c, const CacheRows &r, uint32_t, cudaStream_t stream) {
-    return launch_behind(c.fp16 ? cache_append_kernel<true> : cache_append_kernel<false>, dim3(items_grid(c, r)), kCacheThreads, 0, stream, c, r);
+static cudaError_t launch_dim(bool append, const CacheArgs &c, const CacheRows &r, uint32_t sms, cudaStream_t stream) {
+    switch (c.dim) {
+        case 64: return launch_move<64>(append, c, r, sms, stream);
+        case 96: return launch_move<96>(append, c, r, sms, stream);
+        case 128: return launch_move<128>(append, c, r, sms, stream);
+        case 192: return launch_move<192>(append, c, r, sms, stream);
+        default: return launch_move<256>(append, c, r, sms, stream);
+    }
 }
-cudaError_t launch_cache_read(const CacheArgs &c, const CacheRows &r, uint32_t, cudaStream_t stream) {
-    return launch_behind(c.fp16 ? cache_read_kernel<true> : cache_read_kernel<false>, dim3(items_grid(c, r)), kCacheThreads, 0, stream, c, r);
-}
+cudaError_t launch_cache_append(const CacheArgs &c, const CacheRows &r, uint32_t sms, cudaStream_t stream) { return launch_dim(true, c, r, sms, stream); }
+cudaError_t launch_cache_read(const CacheArgs &c, const CacheRows &r, uint32_t sms, cudaStream_t stream) { return launch_dim(false, c, r, sms, stream); }
 
 }  // namespace huffllm

@@ -70,8 +70,87 @@ __global__ void __launch_bounds__(128) rotary_kernel(const __grid_constant__ Rot
     }
 }
 
+// Heads whose channels lie on 16-byte boundaries: a thread turns eight channels with the eight half a rotary_dim away (or four pairs of
+// neighbours), in as many heads as threads leave it.  A CTA has a token; its sines and cosines meet in shared memory while the
+// heads are on their way.  Bound by memory for many tokens, by the way there and back for few.
+constexpr uint32_t kRotaryThreads = 256, kRotaryEach = 2;
+template <bool F16, bool NEIGHBOURS>
+__global__ void __launch_bounds__(kRotaryThreads) rotary_wide_kernel(const __grid_constant__ RotaryArgs A) {
+    __shared__ float2 s_turn[512];
+    pdl_launch_dependents();
+    pdl_wait_prior_grid();
+    const uint32_t token = blockIdx.x, pairs = A.rot / 2, tid = threadIdx.x;
+    const uint32_t turned = NEIGHBOURS ? A.rot / 8 : A.rot / 16;          // items of a head: turned ones, and pieces that are copied
+    const uint32_t items = turned + (A.dim - A.rot) / 8, all = items * (A.heads[0] + A.heads[1]);
+    const uint32_t step = blockDim.x * kRotaryEach;
+    bool known = false;
+    for (uint32_t base = 0; base < all; base += step) {
+        uint4 x[kRotaryEach], y[kRotaryEach];
+        const uint16_t *from[kRotaryEach];
+        uint16_t *to[kRotaryEach];
+        uint32_t part[kRotaryEach];
+#pragma unroll
+        for (uint32_t k = 0; k < kRotaryEach; ++k) {
+            const uint32_t i = base + k * blockDim.x + tid, h = i / items;
+            part[k] = i % items;
+            const uint32_t which = h < A.heads[0] ? 0 : 1, head = which ? h - A.heads[0] : h;
+            const uint32_t at = head * A.dim + (part[k] < turned ? part[k] * 8 : A.rot + (part[k] - turned) * 8);
+            from[k] = A.in[which] + token * A.in_stride[which] + at;
+            to[k] = A.out[which] + token * A.out_stride[which] + at;
+            if (i >= all) {
+                to[k] = nullptr;
+                continue;
+            }
+            x[k] = __ldcg((const uint4 *)from[k]);
+            if (!NEIGHBOURS && part[k] < turned) y[k] = __ldcg((const uint4 *)(from[k] + pairs));
+        }
+        if (!known) {
+            for (uint32_t i = tid; i < pairs; i += blockDim.x)
+                s_turn[i] = turn_of(__ldcg(A.positions + (uint64_t)axis_of(A, i) * A.tokens + token), __ldcg(A.frequencies + i));
+            __syncthreads();
+            known = true;
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kRotaryEach; ++k) {
+            if (!to[k]) continue;
+            if (part[k] >= turned) {
+                if (to[k] != from[k]) *(uint4 *)to[k] = x[k];
+                continue;
+            }
+            const uint32_t a[4] = {x[k].x, x[k].y, x[k].z, x[k].w}, b[4] = {y[k].x, y[k].y, y[k].z, y[k].w};
+            uint32_t c[4], d[4];
+            auto lo = [](uint32_t w) { return widen16<F16>((uint16_t)w); };
+            auto hi = [](uint32_t w) { return widen16<F16>((uint16_t)(w >> 16)); };
+            auto both = [](float l, float h) { return round16<F16>(l) | (uint32_t)round16<F16>(h) << 16; };
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                if constexpr (NEIGHBOURS) {
+                    const float2 t = s_turn[part[k] * 4 + j];
+                    c[j] = both(lo(a[j]) * t.x - hi(a[j]) * t.y, hi(a[j]) * t.x + lo(a[j]) * t.y);
+                } else {
+                    const float2 t = s_turn[part[k] * 8 + 2 * j], u = s_turn[part[k] * 8 + 2 * j + 1];
+                    c[j] = both(lo(a[j]) * t.x - lo(b[j]) * t.y, hi(a[j]) * u.x - hi(b[j]) * u.y);
+                    d[j] = both(lo(b[j]) * t.x + lo(a[j]) * t.y, hi(b[j]) * u.x + hi(a[j]) * u.y);
+                }
+            }
+            *(uint4 *)to[k] = make_uint4(c[0], c[1], c[2], c[3]);
+            if (!NEIGHBOURS) *(uint4 *)(to[k] + pairs) = make_uint4(d[0], d[1], d[2], d[3]);
+        }
+    }
+}
+
 cudaError_t launch_rotary(const RotaryArgs &a, cudaStream_t stream) {
-    return launch_behind(a.fp16 ? rotary_kernel<true> : rotary_kernel<false>, dim3(a.tokens), 128, 0, stream, a);
+    bool wide = a.dim % 8 == 0 && a.rot % (a.neighbours ? 8 : 16) == 0;
+    for (int w = 0; w < 2; ++w)
+        if (a.heads[w]) wide = wide && !(((uintptr_t)a.in[w] | (uintptr_t)a.out[w]) & 15) && a.in_stride[w] % 8 == 0 && a.out_stride[w] % 8 == 0;
+    if (!wide) return launch_behind(a.fp16 ? rotary_kernel<true> : rotary_kernel<false>, dim3(a.tokens), 128, 0, stream, a);
+    const uint32_t items = ((a.neighbours ? a.rot / 8 : a.rot / 16) + (a.dim - a.rot) / 8) * (a.heads[0] + a.heads[1]);
+    // (as few threads as go through a token's items in whole rounds)
+    const uint32_t rounds = (items + kRotaryThreads * kRotaryEach - 1) / (kRotaryThreads * kRotaryEach), each = rounds * kRotaryEach;
+    const uint32_t threads = ((items + each - 1) / each + 31) / 32 * 32;
+    auto kernel = a.neighbours ? (a.fp16 ? rotary_wide_kernel<true, true> : rotary_wide_kernel<false, true>)
+                               : (a.fp16 ? rotary_wide_kernel<true, false> : rotary_wide_kernel<false, false>);
+    return launch_behind(kernel, dim3(a.tokens), threads, 0, stream, a);
 }
 
 }  // namespace huffllm

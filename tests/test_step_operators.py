@@ -241,8 +241,8 @@ def test_cache_holds_the_format(hl, torch, dim, kv, page, dtype, kind):
         total += counts
         p.lengths.copy_(ints(torch, total))
         rows = sum(counts) + 5                            # five rows behind the last sequence
-        pad = 8 if kind == "normal" else 0                # between the rows
-        new = [to_bits(kv_values(rng, (rows, kv * dim + pad), "normal" if pad else kind), dtype) for _ in range(2)]
+        pad = {"normal": 8, "far": 3, "flat": 4}.get(kind, 0)      # between the rows
+        new = [to_bits(kv_values(rng, (rows, kv * dim + pad), "normal" if kind == "flat" else kind), dtype) for _ in range(2)]
         hl.cache_append(p.cache, up(torch, new[0], dtype), up(torch, new[1], dtype), rows, starts=p.starts(counts), k_stride=kv * dim + pad,
                         v_stride=kv * dim + pad, err_flag_dev=p.err)
         at = 0
