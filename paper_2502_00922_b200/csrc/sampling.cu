@@ -22,6 +22,7 @@ namespace huffllm {
 constexpr uint32_t kSampleThreads = 512, kSampleWarps = kSampleThreads / 32;
 constexpr uint32_t kBins = 2048;
 constexpr uint32_t kMostList = 2 * kBins;              // a bin with fewer logits is searched in shared memory, in a list that lies where the bins were
+constexpr uint32_t kShortList = 256;
 constexpr uint32_t kMostCluster = 8;
 constexpr uint32_t kFull = 0xFFFFFFFFu;
 
@@ -47,6 +48,22 @@ struct Piece16 {
     }
 };
 
+// The largest and the smallest value of a piece (a NaN is none).
+template <int TYPE>
+__device__ __forceinline__ float piece_max(uint4 v) {
+    if constexpr (TYPE == 0) return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+    using Two = std::conditional_t<TYPE == 1, __nv_bfloat162, __half2>;
+    const Two m = __hmax2(__hmax2(*(const Two *)&v.x, *(const Two *)&v.y), __hmax2(*(const Two *)&v.z, *(const Two *)&v.w));
+    return fmaxf(widen16<TYPE == 2>((uint16_t)*(const uint32_t *)&m), widen16<TYPE == 2>((uint16_t)(*(const uint32_t *)&m >> 16)));
+}
+template <int TYPE>
+__device__ __forceinline__ float piece_min(uint4 v) {
+    if constexpr (TYPE == 0) return fminf(fminf(__uint_as_float(v.x), __uint_as_float(v.y)), fminf(__uint_as_float(v.z), __uint_as_float(v.w)));
+    using Two = std::conditional_t<TYPE == 1, __nv_bfloat162, __half2>;
+    const Two m = __hmin2(__hmin2(*(const Two *)&v.x, *(const Two *)&v.y), __hmin2(*(const Two *)&v.z, *(const Two *)&v.w));
+    return fminf(widen16<TYPE == 2>((uint16_t)*(const uint32_t *)&m), widen16<TYPE == 2>((uint16_t)(*(const uint32_t *)&m >> 16)));
+}
+
 struct alignas(16) SampleShared {
     uint32_t count[kBins];                             // a CTA's bins; later, in the first CTA, the list
     uint32_t below[kBins];
@@ -58,12 +75,14 @@ struct alignas(16) SampleShared {
     float cta_top, cta_least;
     double table_mass[kMostCluster * kSampleWarps];
     uint32_t table_equal[kMostCluster * kSampleWarps];
-    uint32_t found_bin, found_count, listed;
+    uint32_t found_bin, found_count, listed[2];
     double found_mass;
     struct {
         uint32_t bin, lowest;
         double want;
     } named[2];                                        // what the first CTA searches: by count, by mass
+    uint32_t draw_stretch, draw_equal;                 // where the draw ends; of the equals in front of it, the mass there, and what it has to exceed
+    double draw_from, draw_aim;
     float cut;                                         // the outcome: logits above it stay, and `ties` of those that equal it
     uint32_t ties;
 };
@@ -88,9 +107,15 @@ struct RowPart {
         else r = make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16, v[6] | (uint32_t)v[7] << 16);
         return r;
     }
-    __device__ __forceinline__ Piece16<TYPE> piece(uint32_t i) const { return Piece16<TYPE>(i < kept ? data[i] : from_memory(i)); }
+    __device__ __forceinline__ uint4 raw(uint32_t i) const { return i < kept ? data[i] : from_memory(i); }
+    __device__ __forceinline__ Piece16<TYPE> piece(uint32_t i) const { return Piece16<TYPE>(raw(i)); }
 };
 
+__device__ __forceinline__ float exp2_approx(float x) {   // off by 2^-22 of itself
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 __device__ __forceinline__ float warp_max(float v) {
     for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kFull, v, o));
     return v;
@@ -141,14 +166,11 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
         for (int j = 0; j < 4; ++j) {
             const uint32_t i = i0 + j * kSampleThreads;
             if (i < R.kept) R.data[i] = v[j];
-            const Piece16<TYPE> x(v[j]);
-#pragma unroll
-            for (int e = 0; e < R.N; ++e) {
-                top = fmaxf(top, x.x[e]);
-                least = fminf(least, x.x[e] == -INFINITY ? INFINITY : x.x[e]);
-            }
+            top = fmaxf(top, piece_max<TYPE>(v[j]));
+            least = fminf(least, piece_min<TYPE>(v[j]));
         }
     }
+    const float own_top = top;                         // of the thread's logits
     top = warp_max(top);
     least = warp_min(least);
     if (lane == 0) S.warp_top[warp] = top, S.warp_least[warp] = least;
@@ -156,7 +178,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
     if (warp == 0) {
         top = warp_max(lane < kSampleWarps ? S.warp_top[lane] : -INFINITY);
         least = warp_min(lane < kSampleWarps ? S.warp_least[lane] : INFINITY);
-        if (lane == 0) S.cta_top = top, S.cta_least = least, S.listed = 0;
+        if (lane == 0) S.cta_top = top, S.cta_least = least, S.listed[0] = S.listed[1] = 0;
     }
     cluster.sync();
     {
@@ -169,34 +191,59 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
         cluster.sync();
         return;
     }
-    // Exponents of weights in bins: most 1/64 wide, narrower where the row's logits are closer together.
+    // Exponents of weights in bins: most 1/64 wide, narrower where the row's logits are closer together (and none is minus infinity).
     const float scale = fmaxf(64.0f / temperature, fminf((float)(kBins - 1) / (top - least), 1e30f));
     const float width = 1.0f / (scale * temperature), to_log2 = -1.4426950408889634f / temperature;
-    auto place = [&](float x) { return x == top ? 0.0f : (top - x) * scale; };
-    auto weight = [&](float x) { return x == top ? 1.0f : exp2f((top - x) * to_log2); };
-    // (a weight's distance from that of its bin's upper edge, in 2^-22 of it: 1 - exp(-r) for r up to 1/64)
-    auto below_edge = [&](float place, uint32_t bin) {
-        const float r = (place - (float)bin) * width;
-        return (uint32_t)__float2int_rn(r * (1.0f - r * (0.5f - r * 0.16666667f)) * 4194304.0f);
+    auto place = [&](float x) { return (top - x) * scale; };
+    auto weight = [&](float x) { return x == top ? 1.0f : exp2_approx((top - x) * to_log2); };
+    // The bin of a place below kBins (2^23 and more has no fraction, and its low bits are the whole number; conversions go through a slower
+    // pipe), and a weight's distance from that of the bin's upper edge, in 2^-22 of it: 1 - exp(-r) for r up to 1/64.
+    auto bin_of = [](float place) { return __float_as_uint(__fadd_rd(place, 8388608.0f)) & (2 * kBins - 1); };
+    auto below_edge = [&](float place) {
+        const float r = (place - (__fadd_rd(place, 8388608.0f) - 8388608.0f)) * width;
+        return __float_as_uint(fmaf(r * (1.0f - r * (0.5f - r * 0.16666667f)), 4194304.0f, 12582912.0f)) & 0x1FFFFu;
     };
 
     float cut = -INFINITY;                             // (what equals minus infinity has no weight)
     uint32_t ties = 0;
     const bool by_count = !first_only && k_given > 0 && (uint32_t)k_given < A.vocab, by_mass = !first_only && p < 1.0f;
-    if (first_only) {
+    const bool infinite = top == INFINITY;             // (equal weights: how many stay shows when all of them are counted, for the draw)
+    if (first_only || infinite) {
         cut = top;
         ties = 1;
     } else if (by_count || by_mass) {
         // ---- the bins
+        // Where top_k is small, most of the row need not be looked at closely: of the threads' largest logits, which are that many tokens, the
+        // top_k-th largest is not above the cut.  (Halving its range sixteen times is near enough.)
+        float floor = -INFINITY;
+        if (by_count && (uint32_t)k_given <= kSampleThreads / 8 * 7) {
+            const uint32_t key = own_top > -INFINITY ? key_of(own_top) : 0u;
+            uint32_t low = 0, high = key_of(top) + 1;  // so many threads or more have `low` or more
+            for (int turn = 0; turn < 20; ++turn) {
+                const uint32_t mid = low + (high - low) / 2;
+                if ((uint32_t)__syncthreads_count(key >= mid) >= (uint32_t)k_given) low = mid;
+                else high = mid;
+            }
+            if (low > key_of(-INFINITY)) floor = value_of(low);
+        }
+        const uint32_t counts_at = (uint32_t)__cvta_generic_to_shared(S.count), below_at = (uint32_t)__cvta_generic_to_shared(S.below);
         for (uint32_t i = tid; i < R.pieces; i += kSampleThreads) {
-            const Piece16<TYPE> x = R.piece(i);
+            const uint4 v = R.raw(i);
+            if (by_count && !(piece_max<TYPE>(v) >= floor)) continue;
+            const Piece16<TYPE> x(v);
 #pragma unroll
             for (int e = 0; e < R.N; ++e) {
-                const float at = place(x.x[e]);
-                if (at < (float)kBins) {
-                    const uint32_t bin = (uint32_t)at;
-                    atomicAdd(&S.count[bin], 1u);
-                    if (by_mass) atomicAdd(&S.below[bin], below_edge(at, bin));
+                const float at = x.x[e] >= floor ? place(x.x[e]) : INFINITY;
+                const uint32_t bin = bin_of(at) * 4;
+                // (with predicates: a branch for every logit costs more than what is behind it)
+                if (by_mass) {
+                    asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.f32 p, %0, %1;\n\t@p red.shared.add.u32 [%2], 1;\n\t@p red.shared.add.u32 [%3], %4;\n\t}" ::"f"(at),
+                                 "f"((float)kBins), "r"(counts_at + bin), "r"(below_at + bin), "r"(below_edge(at))
+                                 : "memory");
+                } else {
+                    asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.f32 p, %0, %1;\n\t@p red.shared.add.u32 [%2], 1;\n\t}" ::"f"(at), "f"((float)kBins),
+                                 "r"(counts_at + bin)
+                                 : "memory");
                 }
             }
         }
@@ -263,17 +310,23 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
         };
         float *const list = (float *)S.count;
         // All of a bin's logits into the first CTA's list.
-        auto gather = [&](uint32_t bin) {
-            for (uint32_t i = tid; i - lane < R.pieces; i += kSampleThreads) {
-                Piece16<TYPE> x = i < R.pieces ? R.piece(i) : Piece16<TYPE>(make_uint4(kFull, kFull, kFull, kFull));
+        auto gather = [&](uint32_t bin, uint32_t which) {
+            // (most pieces have none within a bin and a half of its middle)
+            const float middle = top - ((float)bin + 0.5f) / scale, reach = 1.0f / scale + fabsf(middle) * 1e-6f;
+            for (uint32_t i = tid; i < R.pieces; i += kSampleThreads) {
+                const Piece16<TYPE> x = R.piece(i);
+                float nearest = INFINITY;
+#pragma unroll
+                for (int e = 0; e < R.N; ++e) nearest = fminf(nearest, fabsf(x.x[e] - middle));
+                if (nearest > reach) continue;
                 uint32_t hits = 0;
 #pragma unroll
                 for (int e = 0; e < R.N; ++e) {
                     const float at = place(x.x[e]);
-                    if (at < (float)kBins && (uint32_t)at == bin) hits |= 1u << e;
+                    if (at < (float)kBins && bin_of(at) == bin) hits |= 1u << e;
                 }
                 if (hits) {
-                    uint32_t to = atomicAdd(&S0.listed, __popc(hits));
+                    uint32_t to = atomicAdd(&S0.listed[which], __popc(hits));
                     float *const list0 = (float *)S0.count;
 #pragma unroll
                     for (int e = 0; e < R.N; ++e)
@@ -291,15 +344,51 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
             double above;
             bool by_row;                               // every CTA has found it
         };
-        auto mass20 = [&](float x, uint32_t bin) { return 1048576u - (below_edge(place(x), bin) >> 2); };
+        auto mass20 = [&](float x) { return 1048576u - (below_edge(place(x)) >> 2); };
         auto block_sum = [&](uint32_t v, uint32_t turn) {
             v = __reduce_add_sync(kFull, v);
             if (lane == 0) S.sums[turn & 1][warp] = v;
             __syncthreads();
             return __reduce_add_sync(kFull, lane < kSampleWarps ? S.sums[turn & 1][lane] : 0u);
         };
-        auto search_list = [&](uint32_t n, uint32_t bin, bool counted, double want, uint32_t lowest) -> Edge {
+        // (a short list: every warp by itself)
+        auto search_short = [&](uint32_t n, bool counted, double want, uint32_t lowest) -> Edge {
+            constexpr uint32_t EACH = kShortList / 32;
+            const uint32_t whole_want = (uint32_t)fmin(ceil(want), 4294967295.0);
+            uint32_t key[EACH], part[EACH], low = kFull, high = 0;
+#pragma unroll
+            for (uint32_t j = 0; j < EACH; ++j) {
+                const uint32_t i = lane + j * 32;
+                key[j] = 0, part[j] = 0;
+                if (i < n) {
+                    key[j] = key_of(list[i]);
+                    part[j] = counted ? 1u : mass20(list[i]);
+                    low = min(low, key[j]);
+                    high = max(high, key[j]);
+                }
+            }
+            low = max(__reduce_min_sync(kFull, low), lowest) - 1;
+            high = __reduce_max_sync(kFull, high);
+            auto above = [&](uint32_t mid) {
+                uint32_t v = 0;
+#pragma unroll
+                for (uint32_t j = 0; j < EACH; ++j) v += key[j] > mid ? part[j] : 0u;
+                return __reduce_add_sync(kFull, v);
+            };
+            while (high - low > 1) {
+                const uint32_t mid = low + (high - low) / 2;
+                if (above(mid) < whole_want) high = mid;
+                else low = mid;
+            }
+            uint32_t v = 0;
+#pragma unroll
+            for (uint32_t j = 0; j < EACH; ++j) v += key[j] == high;
+            return Edge{high, __reduce_add_sync(kFull, v), (double)above(high), false};
+        };
+        auto search_list = [&](uint32_t n, bool counted, double want, uint32_t lowest) -> Edge {
+            if (n <= kShortList) return search_short(n, counted, want, lowest);
             constexpr uint32_t EACH = kMostList / kSampleThreads;
+            const uint32_t whole_want = (uint32_t)fmin(ceil(want), 4294967295.0);
             uint32_t key[EACH], part[EACH], low = kFull, high = 0;
 #pragma unroll
             for (uint32_t j = 0; j < EACH; ++j) {
@@ -307,7 +396,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
                 key[j] = 0, part[j] = 0;
                 if (i < n) {
                     key[j] = key_of(list[i]);
-                    part[j] = counted ? 1u : mass20(list[i], bin);
+                    part[j] = counted ? 1u : mass20(list[i]);
                     low = min(low, key[j]);
                     high = max(high, key[j]);
                 }
@@ -329,7 +418,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
             };
             while (high - low > 1) {
                 const uint32_t mid = low + (high - low) / 2;
-                if ((double)above(mid) < want) high = mid;
+                if (above(mid) < whole_want) high = mid;
                 else low = mid;
             }
             Edge e;
@@ -352,9 +441,9 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
 #pragma unroll
                 for (int e = 0; e < R.N; ++e) {
                     const float at = place(x.x[e]);
-                    if (!(at < (float)kBins) || (uint32_t)at != bin) continue;
+                    if (!(at < (float)kBins) || bin_of(at) != bin) continue;
                     const uint32_t key = key_of(x.x[e]);
-                    if (what == kCountEqual ? key == edge : key > edge) v += what == kMassAbove ? mass20(x.x[e], bin) : 1u;
+                    if (what == kCountEqual ? key == edge : key > edge) v += what == kMassAbove ? mass20(x.x[e]) : 1u;
                 }
             }
             for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
@@ -383,7 +472,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
             return e;
         };
         // Gathers and searches a bin that the first CTA names (kBins: none).
-        uint32_t gathered = kBins;
+        uint32_t gathered = kBins, list_of = 0;
         auto search = [&](uint32_t bin0, bool counted, double want0, uint32_t lowest0) -> Edge {
             if (rank == 0 && tid < ctas) {
                 auto &to = cluster.map_shared_rank(&S, tid)->named[counted ? 0 : 1];
@@ -396,15 +485,14 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
             Edge e{0, 0, 0.0, false};
             if (bin == kBins) return e;
             if (bin != gathered) {
-                if (rank == 0 && tid == 0) S.listed = 0;
-                cluster.sync();
-                gather(bin);
+                list_of = counted ? 0 : 1;
+                gather(bin, list_of);
                 cluster.sync();
                 gathered = bin;
             }
-            const uint32_t n = S0.listed;
+            const uint32_t n = S0.listed[list_of];
             if (n >= kMostList) return search_row(bin, counted, want, lowest);
-            if (rank == 0) e = search_list(n, bin, counted, want, lowest);
+            if (rank == 0) e = search_list(n, counted, want, lowest);
             return e;
         };
 
@@ -432,11 +520,11 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
                     double inside = row_mass;
                     if (!e.by_row) {
                         uint32_t v = 0;
-                        for (uint32_t i = tid; i < S.listed; i += kSampleThreads) v += key_of(list[i]) > e.key ? mass20(list[i], bin) : 0u;
+                        for (uint32_t i = tid; i < S.listed[0]; i += kSampleThreads) v += key_of(list[i]) > e.key ? mass20(list[i]) : 0u;
                         inside = (double)block_sum(v, 0);
                         __syncthreads();
                     }
-                    mass = mass_before + exp((double)(-(float)bin * width)) * 0x1p-20 * (inside + (double)ties * mass20(cut, bin));
+                    mass = mass_before + exp((double)(-(float)bin * width)) * 0x1p-20 * (inside + (double)ties * mass20(cut));
                 }
             }
         }
@@ -453,7 +541,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
             if (rank == 0 && bin < kBins) {
                 const uint32_t have = bin + 1 == limit && e.key == lowest ? ties : e.equal;
                 const float edge = value_of(e.key);
-                const double need = ceil((part - e.above) / (double)mass20(edge, bin));
+                const double need = ceil((part - e.above) / (double)mass20(edge));
                 cut = edge;
                 ties = (uint32_t)fmin(fmax(need, 1.0), (double)have);
             }
@@ -497,49 +585,65 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
     }
     cluster.sync();                                    // (the last look at another CTA's shared memory)
     const float cut_weight_given = cut == -INFINITY ? 0.0f : weight(cut), cut_weight = cut_weight_given < least_weight ? 0.0f : cut_weight_given;
-    // every warp: the stretch in which the mass exceeds what is drawn
-    const uint32_t stretches = ctas * kSampleWarps, own = rank * kSampleWarps + warp;
-    uint32_t equal_before = 0, equal_own = 0;
-    double run = 0.0, own_from = 0.0, total = 0.0;
-    int32_t chosen = -1, last = -1;
-    for (int turn = 0; turn < 2; ++turn) {             // (all of the mass, then where)
-        const double aim = fmin(fmax((double)u, 0.0), 1.0) * total;
-        uint32_t equals = 0;
-        run = 0.0;
-        for (uint32_t base = 0; base < stretches; base += 32) {
-            const uint32_t i = base + lane;
-            const uint32_t eq = i < stretches ? S.table_equal[i] : 0;
-            uint32_t eq_to = eq;
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t up = __shfl_up_sync(kFull, eq_to, o);
-                if (lane >= o) eq_to += up;
-            }
-            const uint32_t eq_from = equals + eq_to - eq, stay = eq_from < ties ? min(eq, ties - eq_from) : 0;
-            double m = i < stretches ? S.table_mass[i] + (double)stay * cut_weight : 0.0, m_to = m;
-            for (int o = 1; o < 32; o <<= 1) {
-                const double up = __shfl_up_sync(kFull, m_to, o);
-                if (lane >= o) m_to += up;
-            }
-            if (turn) {
-                const uint32_t over = __ballot_sync(kFull, m > 0.0 && run + m_to > aim), some = __ballot_sync(kFull, m > 0.0);
-                if (chosen < 0 && over) chosen = base + __ffs(over) - 1;
-                if (some) last = base + 31 - __clz(some);
-                if (own >= base && own < base + 32) {
-                    own_from = run + __shfl_sync(kFull, m_to - m, own - base);
-                    equal_before = __shfl_sync(kFull, eq_from, own - base);
-                    equal_own = __shfl_sync(kFull, eq, own - base);
-                }
-            }
-            equals += __shfl_sync(kFull, eq_to, 31);
-            run += __shfl_sync(kFull, m_to, 31);
+    // the first warp: the stretch in which the mass exceeds what is drawn; a lane has four that follow each other
+    static_assert(kMostCluster * kSampleWarps <= 4 * 32, "a lane's stretches");
+    if (warp == 0) {
+        const uint32_t stretches = ctas * kSampleWarps;
+        uint32_t eq[4], eq_to = 0;
+        double m[4], m_to = 0.0;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            const uint32_t i = lane * 4 + j;
+            eq[j] = i < stretches ? S.table_equal[i] : 0;
+            m[j] = i < stretches ? S.table_mass[i] : 0.0;
+            eq_to += eq[j];
         }
-        total = run;
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t up = __shfl_up_sync(kFull, eq_to, o);
+            if (lane >= o) eq_to += up;
+        }
+        uint32_t before = eq_to - eq[0] - eq[1] - eq[2] - eq[3];
+        const uint32_t equal_from = before;
+        if (infinite && !first_only) {
+            const uint32_t all_equal = __shfl_sync(kFull, eq_to, 31);
+            ties = by_count ? min((uint32_t)k_given, all_equal) : all_equal;
+            if (by_mass) ties = max(1u, min(ties, (uint32_t)ceil((double)p * ties)));
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            m[j] += (double)(before < ties ? min(eq[j], ties - before) : 0) * cut_weight;
+            before += eq[j];
+            m_to += m[j];
+        }
+        const double own = m_to;
+        for (int o = 1; o < 32; o <<= 1) {
+            const double up = __shfl_up_sync(kFull, m_to, o);
+            if (lane >= o) m_to += up;
+        }
+        const double all = __shfl_sync(kFull, m_to, 31), aim = fmin(fmax((double)u, 0.0), 1.0) * all;
+        const uint32_t over = __ballot_sync(kFull, own > 0.0 && m_to > aim), some = __ballot_sync(kFull, own > 0.0);
+        // (lanes' sums may round so that none exceeds what is drawn, or none of a lane's stretches does: then the last that has a mass)
+        if (lane == (over ? __ffs(over) - 1 : 31 - __clz(some | 1u))) {
+            double r = m_to - own, from = 0.0;
+            uint32_t seen = equal_from, equal = 0, at = lane * 4;
+            bool done = false;
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                if (m[j] > 0.0 && !done) from = r, equal = seen, at = lane * 4 + j, done = over && r + m[j] > aim;
+                r += m[j];
+                seen += eq[j];
+            }
+            S.draw_stretch = at, S.draw_equal = equal, S.ties = ties, S.draw_from = from, S.draw_aim = done ? aim : INFINITY;
+        }
     }
-    if (own != (uint32_t)(chosen >= 0 ? chosen : last)) return;
+    __syncthreads();
+    if (rank * kSampleWarps + warp != S.draw_stretch) return;
+    uint32_t equal_before = S.draw_equal;
+    ties = S.ties;
+    double run = S.draw_from;
+    const double aim = S.draw_aim;
     // the stretch's warp: the token (its sums may round otherwise than all of it did: then its last one)
-    const double aim = chosen >= 0 ? fmin(fmax((double)u, 0.0), 1.0) * total : INFINITY;
     int32_t token = -1;
-    run = own_from;
     for (uint32_t i0 = from; i0 < to; i0 += 32) {
         const uint32_t i = i0 + lane;
         const Piece16<TYPE> x = i < to ? R.piece(i) : Piece16<TYPE>(make_uint4(kFull, kFull, kFull, kFull));
