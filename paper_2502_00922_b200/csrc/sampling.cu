@@ -19,10 +19,11 @@ namespace cg = cooperative_groups;
 
 namespace huffllm {
 
-constexpr uint32_t kSampleThreads = 512, kSampleWarps = kSampleThreads / 32;
+constexpr uint32_t kSampleThreads = 256, kSampleEach = 4,   // CTAs an SM has room for
+                    kSampleWarps = kSampleThreads / 32;
 constexpr uint32_t kBins = 2048;
 constexpr uint32_t kMostList = 2 * kBins;              // a bin with fewer logits is searched in shared memory, in a list that lies where the bins were
-constexpr uint32_t kShortList = 256;
+constexpr uint32_t kShortList = 256, kMostNear = 2048;
 constexpr uint32_t kMostCluster = 8;
 constexpr uint32_t kFull = 0xFFFFFFFFu;
 
@@ -69,13 +70,14 @@ struct alignas(16) SampleShared {
     uint32_t below[kBins];
     uint32_t all_count[kBins];                         // the first CTA: all CTAs' bins
     float all_mass[kBins];
+    float near[kMostNear];                             // a CTA's logits that may be above the cut, where top_k is small
     double warp_mass[kSampleWarps], scan_mass[kSampleWarps];
     uint32_t warp_equal[kSampleWarps], scan_count[kSampleWarps], sums[2][kSampleWarps];
     float warp_top[kSampleWarps], warp_least[kSampleWarps];
     float cta_top, cta_least;
     double table_mass[kMostCluster * kSampleWarps];
     uint32_t table_equal[kMostCluster * kSampleWarps];
-    uint32_t found_bin, found_count, listed[2];
+    uint32_t found_bin, found_count, listed[2], nears;
     double found_mass;
     struct {
         uint32_t bin, lowest;
@@ -108,7 +110,17 @@ struct RowPart {
         return r;
     }
     __device__ __forceinline__ uint4 raw(uint32_t i) const { return i < kept ? data[i] : from_memory(i); }
-    __device__ __forceinline__ Piece16<TYPE> piece(uint32_t i) const { return Piece16<TYPE>(raw(i)); }
+    // f(piece) for the pieces first, first + step .. below end; four are on their way together (they may come from L2).
+    template <typename F>
+    __device__ __forceinline__ void each(uint32_t first, uint32_t end, uint32_t step, F f) const {
+        for (uint32_t i0 = first; i0 < end; i0 += 4 * step) {
+            uint4 v[4];
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) v[j] = i0 + j * step < end ? raw(i0 + j * step) : make_uint4(kFull, kFull, kFull, kFull);
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) f(v[j]);
+        }
+    }
 };
 
 __device__ __forceinline__ float exp2_approx(float x) {   // off by 2^-22 of itself
@@ -126,7 +138,7 @@ __device__ __forceinline__ float warp_min(float v) {
 }
 
 template <int TYPE>
-__global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_constant__ SamplingArgs A) {
+__global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(const __grid_constant__ SamplingArgs A) {
     extern __shared__ __align__(16) uint8_t dynamic[];
     SampleShared &S = *(SampleShared *)dynamic;
     cg::cluster_group cluster = cg::this_cluster();
@@ -154,7 +166,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
     const float temperature = t_given > 1e-30f ? t_given : 1.0f;
 
     // ---- the row into shared memory; its largest and smallest logit
-    float top = -INFINITY, least = INFINITY;
+    float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, least = INFINITY;   // of four parts of the thread's logits
     for (uint32_t i0 = tid; i0 < R.pieces; i0 += 4 * kSampleThreads) {
         uint4 v[4];
 #pragma unroll
@@ -166,19 +178,18 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
         for (int j = 0; j < 4; ++j) {
             const uint32_t i = i0 + j * kSampleThreads;
             if (i < R.kept) R.data[i] = v[j];
-            top = fmaxf(top, piece_max<TYPE>(v[j]));
+            tops[j] = fmaxf(tops[j], piece_max<TYPE>(v[j]));
             least = fminf(least, piece_min<TYPE>(v[j]));
         }
     }
-    const float own_top = top;                         // of the thread's logits
-    top = warp_max(top);
+    float top = warp_max(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
     least = warp_min(least);
     if (lane == 0) S.warp_top[warp] = top, S.warp_least[warp] = least;
     __syncthreads();
     if (warp == 0) {
         top = warp_max(lane < kSampleWarps ? S.warp_top[lane] : -INFINITY);
         least = warp_min(lane < kSampleWarps ? S.warp_least[lane] : INFINITY);
-        if (lane == 0) S.cta_top = top, S.cta_least = least, S.listed[0] = S.listed[1] = 0;
+        if (lane == 0) S.cta_top = top, S.cta_least = least, S.listed[0] = S.listed[1] = S.nears = 0;
     }
     cluster.sync();
     {
@@ -213,39 +224,77 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
         ties = 1;
     } else if (by_count || by_mass) {
         // ---- the bins
-        // Where top_k is small, most of the row need not be looked at closely: of the threads' largest logits, which are that many tokens, the
-        // top_k-th largest is not above the cut.  (Halving its range sixteen times is near enough.)
+        const float units = __uint_as_float((127u + min(22u, (uint32_t)__clz(A.part))) << 23);
+        // Where top_k is small, most of the row need not be looked at closely: of the largest logits of the threads' parts, which are that many
+        // tokens, the top_k-th largest is not above the cut.  (Halving their range 16 times is near enough.)
         float floor = -INFINITY;
-        if (by_count && (uint32_t)k_given <= kSampleThreads / 8 * 7) {
-            const uint32_t key = own_top > -INFINITY ? key_of(own_top) : 0u;
-            uint32_t low = 0, high = key_of(top) + 1;  // so many threads or more have `low` or more
-            for (int turn = 0; turn < 20; ++turn) {
-                const uint32_t mid = low + (high - low) / 2;
-                if ((uint32_t)__syncthreads_count(key >= mid) >= (uint32_t)k_given) low = mid;
+        if (by_count && (uint32_t)k_given <= kSampleThreads * 3 && (uint32_t)k_given < R.count / 8) {
+            uint32_t key[4], low = 0, high = key_of(top) + 1;          // so many parts or more have a largest of `low` or more
+#pragma unroll
+            for (int j = 0; j < 4; ++j) key[j] = tops[j] > -INFINITY ? key_of(tops[j]) : 0u;
+            for (uint32_t turn = 0; turn < 16; ++turn) {
+                const uint32_t mid = turn == 0 ? key_of(top - 16.0f * temperature) : low + (high - low) / 2;
+                const uint32_t count = __reduce_add_sync(kFull, (key[0] >= mid) + (key[1] >= mid) + (key[2] >= mid) + (key[3] >= mid));
+                if (lane == 0) S.sums[turn & 1][warp] = count;
+                __syncthreads();
+                if (__reduce_add_sync(kFull, lane < kSampleWarps ? S.sums[turn & 1][lane] : 0u) >= (uint32_t)k_given) low = mid;
                 else high = mid;
             }
             if (low > key_of(-INFINITY)) floor = value_of(low);
+            __syncthreads();
         }
         const uint32_t counts_at = (uint32_t)__cvta_generic_to_shared(S.count), below_at = (uint32_t)__cvta_generic_to_shared(S.below);
-        for (uint32_t i = tid; i < R.pieces; i += kSampleThreads) {
-            const uint4 v = R.raw(i);
-            if (by_count && !(piece_max<TYPE>(v) >= floor)) continue;
-            const Piece16<TYPE> x(v);
+        // (with predicates: a branch for every logit costs more than what is behind it)
+        auto count_one = [&](float x) {
+            const float at = place(x);
+            const uint32_t bin = bin_of(at) * 4;
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.f32 p, %0, %1;\n\t@p red.shared.add.u32 [%2], 1;\n\t}" ::"f"(at), "f"((float)kBins), "r"(counts_at + bin)
+                         : "memory");
+            if (by_mass)
+                asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.f32 p, %0, %1;\n\t@p red.shared.add.u32 [%2], %3;\n\t}" ::"f"(at), "f"((float)kBins), "r"(below_at + bin),
+                             "r"(below_edge(at))
+                             : "memory");
+        };
+        // Mass alone, in one addition: a weight in `units` of its bin's upper edge, as many as the CTA's logits leave of 32 bits (18 bits and more, 2^-19
+        // of a weight, where a CTA has up to 16384 logits).  units exp(-r) is a polynomial in how far the place is in its bin.
+        const float c1 = -units * width, c2 = 0.5f * units * width * width, c3 = -units * width * width * width / 6.0f;
+        auto weigh_one = [&](float x) {
+            const float at = place(x), whole = __fadd_rd(at, 8388608.0f), f = at - (whole - 8388608.0f);
+            const uint32_t bin = (__float_as_uint(whole) & (2 * kBins - 1)) * 4;
+            const uint32_t w = __float_as_uint(fmaf(fmaf(fmaf(c3, f, c2), f, c1), f, units + 8388608.0f)) & 0x7FFFFFu;
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.f32 p, %0, %1;\n\t@p red.shared.add.u32 [%2], %3;\n\t}" ::"f"(at), "f"((float)kBins), "r"(below_at + bin), "r"(w)
+                         : "memory");
+        };
+        if (floor > -INFINITY) {
+            R.each(tid, R.pieces, kSampleThreads, [&](uint4 v) {
+                if (!(piece_max<TYPE>(v) >= floor)) return;
+                const Piece16<TYPE> x(v);
+                uint32_t hits = 0;
 #pragma unroll
-            for (int e = 0; e < R.N; ++e) {
-                const float at = x.x[e] >= floor ? place(x.x[e]) : INFINITY;
-                const uint32_t bin = bin_of(at) * 4;
-                // (with predicates: a branch for every logit costs more than what is behind it)
-                if (by_mass) {
-                    asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.f32 p, %0, %1;\n\t@p red.shared.add.u32 [%2], 1;\n\t@p red.shared.add.u32 [%3], %4;\n\t}" ::"f"(at),
-                                 "f"((float)kBins), "r"(counts_at + bin), "r"(below_at + bin), "r"(below_edge(at))
-                                 : "memory");
-                } else {
-                    asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.f32 p, %0, %1;\n\t@p red.shared.add.u32 [%2], 1;\n\t}" ::"f"(at), "f"((float)kBins),
-                                 "r"(counts_at + bin)
-                                 : "memory");
+                for (int e = 0; e < R.N; ++e) hits |= x.x[e] >= floor ? 1u << e : 0u;
+                uint32_t to = atomicAdd(&S.nears, __popc(hits));
+#pragma unroll
+                for (int e = 0; e < R.N; ++e)
+                    if (hits >> e & 1) {
+                        if (to < kMostNear) S.near[to] = x.x[e];
+                        ++to;
+                    }
+            });
+            __syncthreads();
+        }
+        const uint32_t nears = S.nears;
+        const bool by_near = floor > -INFINITY && nears <= kMostNear;
+        if (by_near) {
+            for (uint32_t i = tid; i < nears; i += kSampleThreads) count_one(S.near[i]);
+        } else {
+            R.each(tid, R.pieces, kSampleThreads, [&](uint4 v) {
+                const Piece16<TYPE> x(v);
+#pragma unroll
+                for (int e = 0; e < R.N; ++e) {
+                    if (by_count) count_one(x.x[e]);
+                    else weigh_one(x.x[e]);
                 }
-            }
+            });
         }
         cluster.sync();
         const uint32_t share = kBins / ctas;
@@ -259,7 +308,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
                 below += other.below[bin];
             }
             S0.all_count[bin] = count;
-            S0.all_mass[bin] = expf(-(float)bin * width) * (float)((double)count - (double)below * 0x1p-22);
+            S0.all_mass[bin] = expf(-(float)bin * width) * (float)(by_count ? (double)count - (double)below * 0x1p-22 : (double)below / units);
         }
         cluster.sync();
 
@@ -301,7 +350,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
             for (uint32_t j = 0; j < PER; ++j) {
                 const uint32_t c1 = c + counts[j], bin = tid * PER + j;
                 const double m1 = m + masses[j];
-                if (bin < limit && counts[j] && (counted ? c < want_count && c1 >= want_count : m < want_mass && m1 >= want_mass))
+                if (bin < limit && (counted ? c < want_count && c1 >= want_count : m < want_mass && m1 >= want_mass))
                     S.found_bin = bin, S.found_count = c, S.found_mass = m;
                 c = c1;
                 m = m1;
@@ -311,23 +360,32 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
         float *const list = (float *)S.count;
         // All of a bin's logits into the first CTA's list.
         auto gather = [&](uint32_t bin, uint32_t which) {
+            float *const list0 = (float *)S0.count;
+            auto in_bin = [&](float x) {
+                const float at = place(x);
+                return at < (float)kBins && bin_of(at) == bin;
+            };
+            if (by_near) {
+                for (uint32_t i = tid; i < nears; i += kSampleThreads) {
+                    if (!in_bin(S.near[i])) continue;
+                    const uint32_t to = atomicAdd(&S0.listed[which], 1u);
+                    if (to < kMostList) list0[to] = S.near[i];
+                }
+                return;
+            }
             // (most pieces have none within a bin and a half of its middle)
             const float middle = top - ((float)bin + 0.5f) / scale, reach = 1.0f / scale + fabsf(middle) * 1e-6f;
-            for (uint32_t i = tid; i < R.pieces; i += kSampleThreads) {
-                const Piece16<TYPE> x = R.piece(i);
+            R.each(tid, R.pieces, kSampleThreads, [&](uint4 v) {
+                const Piece16<TYPE> x(v);
                 float nearest = INFINITY;
 #pragma unroll
                 for (int e = 0; e < R.N; ++e) nearest = fminf(nearest, fabsf(x.x[e] - middle));
-                if (nearest > reach) continue;
+                if (nearest > reach) return;
                 uint32_t hits = 0;
 #pragma unroll
-                for (int e = 0; e < R.N; ++e) {
-                    const float at = place(x.x[e]);
-                    if (at < (float)kBins && bin_of(at) == bin) hits |= 1u << e;
-                }
+                for (int e = 0; e < R.N; ++e) hits |= in_bin(x.x[e]) ? 1u << e : 0u;
                 if (hits) {
                     uint32_t to = atomicAdd(&S0.listed[which], __popc(hits));
-                    float *const list0 = (float *)S0.count;
 #pragma unroll
                     for (int e = 0; e < R.N; ++e)
                         if (hits >> e & 1) {
@@ -335,7 +393,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
                             ++to;
                         }
                 }
-            }
+            });
         };
         // Searches the keys of a bin: the first key, from above, at which the count (or the mass, in 2^-20 of the bin's upper edge) of all
         // keys down to it reaches `want`.  above: of the keys above it; equal: how many have it.
@@ -436,8 +494,8 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
         enum { kCountAbove, kMassAbove, kCountEqual };
         auto row_total = [&](uint32_t bin, uint32_t edge, int what) -> double {
             uint64_t v = 0;
-            for (uint32_t i = tid; i < R.pieces; i += kSampleThreads) {
-                const Piece16<TYPE> x = R.piece(i);
+            R.each(tid, R.pieces, kSampleThreads, [&](uint4 piece) {
+                const Piece16<TYPE> x(piece);
 #pragma unroll
                 for (int e = 0; e < R.N; ++e) {
                     const float at = place(x.x[e]);
@@ -445,7 +503,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
                     const uint32_t key = key_of(x.x[e]);
                     if (what == kCountEqual ? key == edge : key > edge) v += what == kMassAbove ? mass20(x.x[e]) : 1u;
                 }
-            }
+            });
             for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
             if (lane == 0) S.warp_mass[warp] = (double)v;
             cluster.sync();
@@ -557,12 +615,13 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
     }
 
     // ---- the draw, in the order of indexes: warps have stretches of the row, lanes pieces of 16 bytes that follow each other
-    const uint32_t stretch = (R.pieces + kSampleWarps * 32 - 1) / (kSampleWarps * 32) * 32, from = warp * stretch, to = min(R.pieces, from + stretch);
-    {
+    // a warp's mass above the cut of a stretch, and how many equal it, into the warp's place
+    auto sum_stretch = [&](uint32_t from, uint32_t to) {
         float sum = 0.0f;
         uint32_t equal = 0;
-        for (uint32_t i = from + lane; i < to; i += 32) {
-            const Piece16<TYPE> x = R.piece(i);
+        R.each(from + lane, to, 32, [&](uint4 v) {
+            if (!(piece_max<TYPE>(v) >= cut)) return;
+            const Piece16<TYPE> x(v);
 #pragma unroll
             for (int e = 0; e < R.N; ++e) {
                 if (x.x[e] > cut) {
@@ -571,12 +630,14 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
                 }
                 equal += x.x[e] == cut;
             }
-        }
+        });
         double m = sum;
         for (int o = 16; o; o >>= 1) m += __shfl_xor_sync(kFull, m, o);
         equal = __reduce_add_sync(kFull, equal);
         if (lane == 0) S.warp_mass[warp] = m, S.warp_equal[warp] = equal;
-    }
+    };
+    const uint32_t stretch = (R.pieces + kSampleWarps * 32 - 1) / (kSampleWarps * 32) * 32;
+    sum_stretch(min(R.pieces, warp * stretch), min(R.pieces, (warp + 1) * stretch));
     cluster.sync();
     for (uint32_t i = tid; i < ctas * kSampleWarps; i += kSampleThreads) {
         const SampleShared &other = *cluster.map_shared_rank(&S, i / kSampleWarps);
@@ -585,15 +646,15 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
     }
     cluster.sync();                                    // (the last look at another CTA's shared memory)
     const float cut_weight_given = cut == -INFINITY ? 0.0f : weight(cut), cut_weight = cut_weight_given < least_weight ? 0.0f : cut_weight_given;
-    // the first warp: the stretch in which the mass exceeds what is drawn; a lane has four that follow each other
-    static_assert(kMostCluster * kSampleWarps <= 4 * 32, "a lane's stretches");
+    // the first warp: the stretch in which the mass exceeds what is drawn; a lane has some that follow each other
+    constexpr uint32_t STRETCHES = kMostCluster * kSampleWarps / 32;    // of a lane
     if (warp == 0) {
         const uint32_t stretches = ctas * kSampleWarps;
-        uint32_t eq[4], eq_to = 0;
-        double m[4], m_to = 0.0;
+        uint32_t eq[STRETCHES], eq_to = 0;
+        double m[STRETCHES], m_to = 0.0;
 #pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) {
-            const uint32_t i = lane * 4 + j;
+        for (uint32_t j = 0; j < STRETCHES; ++j) {
+            const uint32_t i = lane * STRETCHES + j;
             eq[j] = i < stretches ? S.table_equal[i] : 0;
             m[j] = i < stretches ? S.table_mass[i] : 0.0;
             eq_to += eq[j];
@@ -602,7 +663,9 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
             const uint32_t up = __shfl_up_sync(kFull, eq_to, o);
             if (lane >= o) eq_to += up;
         }
-        uint32_t before = eq_to - eq[0] - eq[1] - eq[2] - eq[3];
+        uint32_t before = eq_to;
+#pragma unroll
+        for (uint32_t j = 0; j < STRETCHES; ++j) before -= eq[j];
         const uint32_t equal_from = before;
         if (infinite && !first_only) {
             const uint32_t all_equal = __shfl_sync(kFull, eq_to, 31);
@@ -610,7 +673,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
             if (by_mass) ties = max(1u, min(ties, (uint32_t)ceil((double)p * ties)));
         }
 #pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) {
+        for (uint32_t j = 0; j < STRETCHES; ++j) {
             m[j] += (double)(before < ties ? min(eq[j], ties - before) : 0) * cut_weight;
             before += eq[j];
             m_to += m[j];
@@ -625,11 +688,11 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
         // (lanes' sums may round so that none exceeds what is drawn, or none of a lane's stretches does: then the last that has a mass)
         if (lane == (over ? __ffs(over) - 1 : 31 - __clz(some | 1u))) {
             double r = m_to - own, from = 0.0;
-            uint32_t seen = equal_from, equal = 0, at = lane * 4;
+            uint32_t seen = equal_from, equal = 0, at = lane * STRETCHES;
             bool done = false;
 #pragma unroll
-            for (uint32_t j = 0; j < 4; ++j) {
-                if (m[j] > 0.0 && !done) from = r, equal = seen, at = lane * 4 + j, done = over && r + m[j] > aim;
+            for (uint32_t j = 0; j < STRETCHES; ++j) {
+                if (m[j] > 0.0 && !done) from = r, equal = seen, at = lane * STRETCHES + j, done = over && r + m[j] > aim;
                 r += m[j];
                 seen += eq[j];
             }
@@ -637,16 +700,37 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(const __grid_con
         }
     }
     __syncthreads();
-    if (rank * kSampleWarps + warp != S.draw_stretch) return;
-    uint32_t equal_before = S.draw_equal;
-    ties = S.ties;
+    if (S.draw_stretch / kSampleWarps != rank) return;
+    // the stretch's CTA: its warps share it, and the one that has the draw goes through its part
+    const uint32_t drawn = S.draw_stretch % kSampleWarps, drawn_from = min(R.pieces, drawn * stretch), drawn_to = min(R.pieces, drawn_from + stretch);
+    const uint32_t part = (drawn_to - drawn_from + kSampleWarps * 32 - 1) / (kSampleWarps * 32) * 32;
+    uint32_t equal_before = S.draw_equal, from = drawn_from, to = drawn_to;
     double run = S.draw_from;
     const double aim = S.draw_aim;
-    // the stretch's warp: the token (its sums may round otherwise than all of it did: then its last one)
+    ties = S.ties;
+    sum_stretch(min(drawn_to, drawn_from + warp * part), min(drawn_to, drawn_from + (warp + 1) * part));
+    __syncthreads();
+    {
+        uint32_t chosen = 0, equal_chosen = equal_before, equal = equal_before;
+        double run_chosen = run, r = run;
+        bool done = false;
+        for (uint32_t w = 0; w < kSampleWarps; ++w) {
+            const uint32_t eq = S.warp_equal[w];
+            const double m = S.warp_mass[w] + (double)(equal < ties ? min(eq, ties - equal) : 0) * cut_weight;
+            if (m > 0.0 && !done) chosen = w, equal_chosen = equal, run_chosen = r, done = r + m > aim;
+            r += m;
+            equal += eq;
+        }
+        if (warp != chosen) return;
+        equal_before = equal_chosen;
+        run = run_chosen;
+        from = min(drawn_to, drawn_from + warp * part);
+        to = min(drawn_to, from + part);
+    }
     int32_t token = -1;
     for (uint32_t i0 = from; i0 < to; i0 += 32) {
         const uint32_t i = i0 + lane;
-        const Piece16<TYPE> x = i < to ? R.piece(i) : Piece16<TYPE>(make_uint4(kFull, kFull, kFull, kFull));
+        const Piece16<TYPE> x(i < to ? R.raw(i) : make_uint4(kFull, kFull, kFull, kFull));
         float w[R.N];
         uint32_t eq = 0, any = 0;
 #pragma unroll
@@ -726,11 +810,16 @@ static cudaError_t launch_type(const SamplingArgs &a, uint32_t ctas, uint32_t sm
 cudaError_t launch_sampling(const SamplingArgs &args, uint32_t sms, cudaStream_t stream) {
     SamplingArgs a = args;
     const uint32_t size = a.type == 0 ? 4 : 2;
-    // As many CTAs a row as keep it at 80 KB each (two CTAs an SM), and more while SMs are idle and a CTA has more than 2048 logits.
+    // As many CTAs a row as keep what all that run together read again and again, 64 MB, in L2; more where that leaves SMs idle and CTAs with
+    // more than 2048 logits.  What shared memory has room for stays there.
+    const uint64_t slots = (uint64_t)sms * kSampleEach;
+    auto running = [&](uint64_t n) { return a.rows * n < slots ? a.rows * n : slots; };
     uint32_t ctas = 1;
-    while (ctas < kMostCluster && ((uint64_t)a.vocab * size > ctas * 81920ull || ((uint64_t)a.rows * ctas * 2 <= sms && a.vocab > ctas * 2048u))) ctas *= 2;
+    while (ctas < kMostCluster && (running(ctas) * ((uint64_t)a.vocab * size / ctas) > (64ull << 20) || (a.rows * (uint64_t)ctas * 2 <= slots && a.vocab > ctas * 2048u))) ctas *= 2;
     a.part = (uint32_t)(((uint64_t)a.vocab + ctas - 1) / ctas);
-    const uint64_t pieces = ((uint64_t)a.part * size + 30) / 16, room = (kSampleMostSmem - sizeof(SampleShared)) / 16;
+    const uint64_t each = (running(ctas) + sms - 1) / sms;             // CTAs of an SM
+    const uint64_t pieces = ((uint64_t)a.part * size + 30) / 16, all = kSampleMostSmem / each - (each > 1 ? 1024 : 0);
+    const uint64_t room = all > sizeof(SampleShared) ? (all - sizeof(SampleShared)) / 16 : 0;
     a.kept_pieces = (uint32_t)(pieces < room ? pieces : room);
     const uint32_t smem = (uint32_t)sizeof(SampleShared) + a.kept_pieces * 16;
     return a.type == 0 ? launch_type<0>(a, ctas, smem, stream) : a.type == 1 ? launch_type<1>(a, ctas, smem, stream) : launch_type<2>(a, ctas, smem, stream);
