@@ -65,12 +65,37 @@ __device__ __forceinline__ float piece_min(uint4 v) {
     return fminf(widen16<TYPE == 2>((uint16_t)*(const uint32_t *)&m), widen16<TYPE == 2>((uint16_t)(*(const uint32_t *)&m >> 16)));
 }
 
+// Which values of a piece are `floor` or more, which is a value of the type: bits 0 .. 3, or of 16-bit values i and i + 16 for the lower and
+// upper half of word i; and the value that such a bit stands for.
+template <int TYPE>
+__device__ __forceinline__ uint32_t at_least(uint4 v, float floor) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t hits = 0;
+    if constexpr (TYPE == 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) hits |= __uint_as_float(w[i]) >= floor ? 1u << i : 0u;
+    } else {
+        using Two = std::conditional_t<TYPE == 1, __nv_bfloat162, __half2>;
+        const uint32_t both = round16<TYPE == 2>(floor) * 0x10001u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) hits |= __hge2_mask(*(const Two *)&w[i], *(const Two *)&both) & 0x10001u << i;
+    }
+    return hits;
+}
+template <int TYPE>
+__device__ __forceinline__ float value_at(uint4 v, uint32_t bit) {
+    const uint32_t lo = bit & 1 ? v.y : v.x, hi = bit & 1 ? v.w : v.z, w = bit & 2 ? hi : lo;
+    if constexpr (TYPE == 0) return __uint_as_float(w);
+    return widen16<TYPE == 2>((uint16_t)(bit & 16 ? w >> 16 : w));
+}
+
 struct alignas(16) SampleShared {
     uint32_t count[kBins];                             // a CTA's bins; later, in the first CTA, the list
     uint32_t below[kBins];
     uint32_t all_count[kBins];                         // the first CTA: all CTAs' bins
     float all_mass[kBins];
-    float near[kMostNear];                             // a CTA's logits that may be above the cut, where top_k is small
+    float near[kMostNear];                             // a CTA's logits that may be above the cut, where top_k is small,
+    uint32_t near_piece[kMostNear];                    // and the pieces that have them
     double warp_mass[kSampleWarps], scan_mass[kSampleWarps];
     uint32_t warp_equal[kSampleWarps], scan_count[kSampleWarps], sums[2][kSampleWarps];
     float warp_top[kSampleWarps], warp_least[kSampleWarps];
@@ -110,7 +135,7 @@ struct RowPart {
         return r;
     }
     __device__ __forceinline__ uint4 raw(uint32_t i) const { return i < kept ? data[i] : from_memory(i); }
-    // f(piece) for the pieces first, first + step .. below end; four are on their way together (they may come from L2).
+    // f(piece, its number) for the pieces first, first + step .. below end; four are on their way together (they may come from L2).
     template <typename F>
     __device__ __forceinline__ void each(uint32_t first, uint32_t end, uint32_t step, F f) const {
         for (uint32_t i0 = first; i0 < end; i0 += 4 * step) {
@@ -118,7 +143,7 @@ struct RowPart {
 #pragma unroll
             for (uint32_t j = 0; j < 4; ++j) v[j] = i0 + j * step < end ? raw(i0 + j * step) : make_uint4(kFull, kFull, kFull, kFull);
 #pragma unroll
-            for (uint32_t j = 0; j < 4; ++j) f(v[j]);
+            for (uint32_t j = 0; j < 4; ++j) f(v[j], i0 + j * step);
         }
     }
 };
@@ -217,6 +242,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
 
     float cut = -INFINITY;                             // (what equals minus infinity has no weight)
     uint32_t ties = 0;
+    bool by_near = false;                              // what stays is in the list of near logits
     const bool by_count = !first_only && k_given > 0 && (uint32_t)k_given < A.vocab, by_mass = !first_only && p < 1.0f;
     const bool infinite = top == INFINITY;             // (equal weights: how many stay shows when all of them are counted, for the draw)
     if (first_only || infinite) {
@@ -226,21 +252,21 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
         // ---- the bins
         const float units = __uint_as_float((127u + min(22u, (uint32_t)__clz(A.part))) << 23);
         // Where top_k is small, most of the row need not be looked at closely: of the largest logits of the threads' parts, which are that many
-        // tokens, the top_k-th largest is not above the cut.  (Halving their range 16 times is near enough.)
+        // tokens, the top_k-th largest is not above the cut.  (Halving a range ten times is near enough.)
         float floor = -INFINITY;
         if (by_count && (uint32_t)k_given <= kSampleThreads * 3 && (uint32_t)k_given < R.count / 8) {
-            uint32_t key[4], low = 0, high = key_of(top) + 1;          // so many parts or more have a largest of `low` or more
-#pragma unroll
-            for (int j = 0; j < 4; ++j) key[j] = tops[j] > -INFINITY ? key_of(tops[j]) : 0u;
-            for (uint32_t turn = 0; turn < 16; ++turn) {
-                const uint32_t mid = turn == 0 ? key_of(top - 16.0f * temperature) : low + (high - low) / 2;
-                const uint32_t count = __reduce_add_sync(kFull, (key[0] >= mid) + (key[1] >= mid) + (key[2] >= mid) + (key[3] >= mid));
+            float high = top;                          // `floor` or more have so many parts or more
+            for (uint32_t turn = 0; turn < 11; ++turn) {
+                const float mid = turn == 0 ? top - 16.0f * temperature : 0.5f * (floor + high);
+                const uint32_t count = __reduce_add_sync(kFull, (tops[0] >= mid) + (tops[1] >= mid) + (tops[2] >= mid) + (tops[3] >= mid));
                 if (lane == 0) S.sums[turn & 1][warp] = count;
                 __syncthreads();
-                if (__reduce_add_sync(kFull, lane < kSampleWarps ? S.sums[turn & 1][lane] : 0u) >= (uint32_t)k_given) low = mid;
+                if (__reduce_add_sync(kFull, lane < kSampleWarps ? S.sums[turn & 1][lane] : 0u) >= (uint32_t)k_given) floor = mid;
                 else high = mid;
+                if (floor == -INFINITY) break;
             }
-            if (low > key_of(-INFINITY)) floor = value_of(low);
+            if constexpr (TYPE == 1) floor = __bfloat162float(__float2bfloat16_rd(floor));
+            if constexpr (TYPE == 2) floor = __half2float(__float2half_rd(floor));
             __syncthreads();
         }
         const uint32_t counts_at = (uint32_t)__cvta_generic_to_shared(S.count), below_at = (uint32_t)__cvta_generic_to_shared(S.below);
@@ -266,28 +292,21 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
                          : "memory");
         };
         if (floor > -INFINITY) {
-            R.each(tid, R.pieces, kSampleThreads, [&](uint4 v) {
-                if (!(piece_max<TYPE>(v) >= floor)) return;
-                const Piece16<TYPE> x(v);
-                uint32_t hits = 0;
-#pragma unroll
-                for (int e = 0; e < R.N; ++e) hits |= x.x[e] >= floor ? 1u << e : 0u;
+            R.each(tid, R.pieces, kSampleThreads, [&](uint4 v, uint32_t i) {
+                uint32_t hits = at_least<TYPE>(v, floor);
+                if (!hits) return;
                 uint32_t to = atomicAdd(&S.nears, __popc(hits));
-#pragma unroll
-                for (int e = 0; e < R.N; ++e)
-                    if (hits >> e & 1) {
-                        if (to < kMostNear) S.near[to] = x.x[e];
-                        ++to;
-                    }
+                for (; hits; hits &= hits - 1, ++to)
+                    if (to < kMostNear) S.near[to] = value_at<TYPE>(v, __ffs(hits) - 1), S.near_piece[to] = i;
             });
             __syncthreads();
         }
         const uint32_t nears = S.nears;
-        const bool by_near = floor > -INFINITY && nears <= kMostNear;
+        by_near = floor > -INFINITY && nears <= kMostNear;
         if (by_near) {
             for (uint32_t i = tid; i < nears; i += kSampleThreads) count_one(S.near[i]);
         } else {
-            R.each(tid, R.pieces, kSampleThreads, [&](uint4 v) {
+            R.each(tid, R.pieces, kSampleThreads, [&](uint4 v, uint32_t) {
                 const Piece16<TYPE> x(v);
 #pragma unroll
                 for (int e = 0; e < R.N; ++e) {
@@ -375,7 +394,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
             }
             // (most pieces have none within a bin and a half of its middle)
             const float middle = top - ((float)bin + 0.5f) / scale, reach = 1.0f / scale + fabsf(middle) * 1e-6f;
-            R.each(tid, R.pieces, kSampleThreads, [&](uint4 v) {
+            R.each(tid, R.pieces, kSampleThreads, [&](uint4 v, uint32_t) {
                 const Piece16<TYPE> x(v);
                 float nearest = INFINITY;
 #pragma unroll
@@ -494,7 +513,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
         enum { kCountAbove, kMassAbove, kCountEqual };
         auto row_total = [&](uint32_t bin, uint32_t edge, int what) -> double {
             uint64_t v = 0;
-            R.each(tid, R.pieces, kSampleThreads, [&](uint4 piece) {
+            R.each(tid, R.pieces, kSampleThreads, [&](uint4 piece, uint32_t) {
                 const Piece16<TYPE> x(piece);
 #pragma unroll
                 for (int e = 0; e < R.N; ++e) {
@@ -619,7 +638,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
     auto sum_stretch = [&](uint32_t from, uint32_t to) {
         float sum = 0.0f;
         uint32_t equal = 0;
-        R.each(from + lane, to, 32, [&](uint4 v) {
+        R.each(from + lane, to, 32, [&](uint4 v, uint32_t) {
             if (!(piece_max<TYPE>(v) >= cut)) return;
             const Piece16<TYPE> x(v);
 #pragma unroll
@@ -637,7 +656,22 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
         if (lane == 0) S.warp_mass[warp] = m, S.warp_equal[warp] = equal;
     };
     const uint32_t stretch = (R.pieces + kSampleWarps * 32 - 1) / (kSampleWarps * 32) * 32;
-    sum_stretch(min(R.pieces, warp * stretch), min(R.pieces, (warp + 1) * stretch));
+    if (by_near) {
+        // (the list is in no order: masses in whole numbers, 2^-40)
+        uint64_t sum = 0;
+        uint32_t equal = 0;
+        for (uint32_t i = lane; i < S.nears; i += 32) {
+            if (S.near_piece[i] / stretch != warp) continue;
+            const float x = S.near[i], w = x > cut ? weight(x) : 0.0f;
+            if (!(w < least_weight)) sum += (uint64_t)((double)w * 0x1p40);
+            equal += x == cut;
+        }
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
+        equal = __reduce_add_sync(kFull, equal);
+        if (lane == 0) S.warp_mass[warp] = (double)sum * 0x1p-40, S.warp_equal[warp] = equal;
+    } else {
+        sum_stretch(min(R.pieces, warp * stretch), min(R.pieces, (warp + 1) * stretch));
+    }
     cluster.sync();
     for (uint32_t i = tid; i < ctas * kSampleWarps; i += kSampleThreads) {
         const SampleShared &other = *cluster.map_shared_rank(&S, i / kSampleWarps);
