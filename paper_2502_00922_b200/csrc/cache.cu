@@ -72,9 +72,9 @@ struct ValueItem {
 };
 
 template <uint32_t DIM, bool F16>
-__global__ void __launch_bounds__(kCacheWarps * 32) cache_append_kernel(const __grid_constant__ CacheArgs C, const __grid_constant__ CacheRows R,
+__global__ void __launch_bounds__(kCacheWarps * 32, 3) cache_append_kernel(const __grid_constant__ CacheArgs C, const __grid_constant__ CacheRows R,
                                                                         const uint32_t rows) {
-    constexpr uint32_t CHUNKS = DIM / 8, EACH = kCacheBlock * CHUNKS / 32, G = cache_groups(DIM), kFull = 0xFFFFFFFFu;
+    constexpr uint32_t CHUNKS = DIM / 8, AT_ONCE = 4, G = cache_groups(DIM), kFull = 0xFFFFFFFFu;
     __shared__ uint32_t s_codes[kCacheWarps][kCacheBlock * DIM / 8];       // [token][16 channels][2]: a byte is two channels, eight apart
     pdl_launch_dependents();
     pdl_wait_prior_grid();
@@ -86,10 +86,13 @@ __global__ void __launch_bounds__(kCacheWarps * 32) cache_append_kernel(const __
             const uint16_t *const x = (side ? R.v : R.k) + head * DIM;
             const uint64_t stride = side ? R.v_stride : R.k_stride;
             uint8_t *const block = C.pool + (uint64_t)(B.block + (int64_t)head * B.head_step) * cache_block_bytes(DIM);
-            uint4 raw[EACH];
+            // four pieces of 16 bytes (a lane's, of two tokens or more) on their way together; tokens that the call does not bring are passed over
+#pragma unroll 1
+            for (uint32_t k0 = B.r * CHUNKS / 32; k0 * 32 < (B.r + B.count) * CHUNKS; k0 += AT_ONCE) {
+            uint4 raw[AT_ONCE];
 #pragma unroll
-            for (uint32_t k = 0; k < EACH; ++k) {
-                const uint32_t i = k * 32 + lane, token = i / CHUNKS, chunk = i % CHUNKS;
+            for (uint32_t k = 0; k < AT_ONCE; ++k) {
+                const uint32_t i = (k0 + k) * 32 + lane, token = i / CHUNKS, chunk = i % CHUNKS;
                 raw[k] = make_uint4(0, 0, 0, 0);
                 if (token - B.r >= B.count) continue;      // (wraps in front of the first)
                 const uint16_t *const from = x + (uint64_t)(B.row + token - B.r) * stride + chunk * 8;
@@ -103,8 +106,9 @@ __global__ void __launch_bounds__(kCacheWarps * 32) cache_append_kernel(const __
                 }
             }
 #pragma unroll
-            for (uint32_t k = 0; k < EACH; ++k) {
-                const uint32_t i = k * 32 + lane, token = i / CHUNKS, chunk = i % CHUNKS, group = chunk / 4, t4 = chunk % 4;
+            for (uint32_t k = 0; k < AT_ONCE; ++k) {
+                if ((k0 + k) * 32 >= (B.r + B.count) * CHUNKS) break;
+                const uint32_t i = (k0 + k) * 32 + lane, token = i / CHUNKS, chunk = i % CHUNKS, group = chunk / 4, t4 = chunk % 4;
                 const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
                 float v[8], low, high;
                 uint32_t most = 0;
@@ -125,14 +129,15 @@ __global__ void __launch_bounds__(kCacheWarps * 32) cache_append_kernel(const __
                 const uint32_t infinite = F16 ? 0x7C00u : 0x7F80u;
                 const bool sound = max(most & 0xFFFFu, most >> 16) < infinite && __half2float(s) < INFINITY && fabsf(__half2float(m)) < INFINITY;
                 if (!sound) s = __ushort_as_half(0x7FFFu), m = __ushort_as_half(0);
-                const float fs = __half2float(s), fm = __half2float(m), by = sound && fs != 0.0f ? 1.0f / fs : 0.0f;
-                // The code is (x - m) / s rounded.  In fp32 the quotient is off by less than 1e-5: 64 bits decide next to a border alone.
+                const float fs = __half2float(s), fm = __half2float(m), by = sound && fs != 0.0f ? 1.0f / (15.0f * fs) : 0.0f;
+                // The code is (x - m) / s rounded.  In fp32 the quotient is off by less than 1e-5: 64 bits decide next to a border alone.  (Taken as
+                // a part of 15, which cuts it off at both ends for nothing; 1.5 * 2^23 more is whole.)
                 uint32_t code[8];
                 float edge = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float q = fminf(fmaxf((v[j] - fm) * by, 0.0f), 15.0f), up = q + 12582912.0f;   // (1.5 * 2^23: the sum is whole)
-                    edge = fmaxf(edge, fabsf(q - (up - 12582912.0f)));
+                    const float q = __saturatef((v[j] - fm) * by), up = fmaf(q, 15.0f, 12582912.0f);
+                    edge = fmaxf(edge, fabsf(fmaf(q, 15.0f, 12582912.0f - up)));
                     code[j] = __float_as_uint(up) & 15u;
                 }
                 if (edge > 0.49998f && by != 0.0f) {
@@ -154,7 +159,7 @@ __global__ void __launch_bounds__(kCacheWarps * 32) cache_append_kernel(const __
                     // eight channels of 16 come from this lane, the others from its neighbour; each gets half of their bytes
                     uint32_t nibbles[2] = {code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24, code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24};
                     const uint32_t other = __shfl_xor_sync(kFull, lane & 1 ? nibbles[0] : nibbles[1], 1);
-                    s_codes[warp][token * (DIM / 8) + chunk] = lane & 1 ? other | nibbles[1] << 4 : nibbles[0] | other << 4;
+                    if (here) s_codes[warp][token * (DIM / 8) + chunk] = lane & 1 ? other | nibbles[1] << 4 : nibbles[0] | other << 4;
                 }
                 if (here && t4 == 0) {
                     *(__half *)(block + (side ? value_scale_at(DIM, token, group) : key_scale_at(DIM, token, group))) = s;
@@ -162,6 +167,7 @@ __global__ void __launch_bounds__(kCacheWarps * 32) cache_append_kernel(const __
                     // (keys' offsets are read in pairs, and what is read is multiplied by 0: it must be a number)
                     if (G % 2 && side == 0 && group + 1 == G) *(__half *)(block + key_offset_at(DIM, token, group + 1)) = __ushort_as_half(0);
                 }
+            }
             }
             if (side == 0) continue;
             __syncwarp();
@@ -176,6 +182,7 @@ __global__ void __launch_bounds__(kCacheWarps * 32) cache_append_kernel(const __
                     in[j] = s_codes[warp][token * (DIM / 8) + item.j * 2 + item.half];
                     mask |= token - B.r < B.count ? 1u << j : 0u;
                 }
+                if (mask == 0) continue;
                 transpose_bytes(in, out);
 #pragma unroll
                 for (uint32_t g = 0; g < 4; ++g) {
@@ -195,7 +202,7 @@ __global__ void __launch_bounds__(kCacheWarps * 32) cache_append_kernel(const __
 }
 
 template <uint32_t DIM, bool F16>
-__global__ void __launch_bounds__(kCacheWarps * 32) cache_read_kernel(const __grid_constant__ CacheArgs C, const __grid_constant__ CacheRows R,
+__global__ void __launch_bounds__(kCacheWarps * 32, 3) cache_read_kernel(const __grid_constant__ CacheArgs C, const __grid_constant__ CacheRows R,
                                                                       const uint32_t rows) {
     constexpr uint32_t CHUNKS = DIM / 8, EACH = kCacheBlock * CHUNKS / 32;
     __shared__ uint32_t s_codes[kCacheWarps][kCacheBlock * DIM / 8];
