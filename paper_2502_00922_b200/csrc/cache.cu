@@ -48,6 +48,9 @@ __device__ __forceinline__ void for_blocks(const CacheArgs &C, const CacheRows &
     }
 }
 
+// A code in 64 bits (a call: few values need it).
+static __device__ __noinline__ float exact_code(float v, float m, float s) { return (float)fmin(fmax(rint(((double)v - (double)m) / (double)s), 0.0), 15.0); }
+
 // Four words, a byte of each into every word of the result: out[i] has byte i of in[0], in[1], in[2], in[3].
 __device__ __forceinline__ void transpose_bytes(const uint32_t (&in)[4], uint32_t (&out)[4]) {
     const uint32_t a = prmt(in[0], in[1], 0x5140), b = prmt(in[2], in[3], 0x5140), c = prmt(in[0], in[1], 0x7362), d = prmt(in[2], in[3], 0x7362);
@@ -72,9 +75,9 @@ struct ValueItem {
 };
 
 template <uint32_t DIM, bool F16>
-__global__ void __launch_bounds__(kCacheWarps * 32, 3) cache_append_kernel(const __grid_constant__ CacheArgs C, const __grid_constant__ CacheRows R,
+__global__ void __launch_bounds__(kCacheWarps * 32, 4) cache_append_kernel(const __grid_constant__ CacheArgs C, const __grid_constant__ CacheRows R,
                                                                         const uint32_t rows) {
-    constexpr uint32_t CHUNKS = DIM / 8, AT_ONCE = 4, G = cache_groups(DIM), kFull = 0xFFFFFFFFu;
+    constexpr uint32_t CHUNKS = DIM / 8, AT_ONCE = 2, G = cache_groups(DIM), kFull = 0xFFFFFFFFu;
     __shared__ uint32_t s_codes[kCacheWarps][kCacheBlock * DIM / 8];       // [token][16 channels][2]: a byte is two channels, eight apart
     pdl_launch_dependents();
     pdl_wait_prior_grid();
@@ -110,56 +113,56 @@ __global__ void __launch_bounds__(kCacheWarps * 32, 3) cache_append_kernel(const
                 if ((k0 + k) * 32 >= (B.r + B.count) * CHUNKS) break;
                 const uint32_t i = (k0 + k) * 32 + lane, token = i / CHUNKS, chunk = i % CHUNKS, group = chunk / 4, t4 = chunk % 4;
                 const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
-                float v[8], low, high;
-                uint32_t most = 0;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    v[2 * j] = widen16<F16>((uint16_t)w[j]), v[2 * j + 1] = widen16<F16>((uint16_t)(w[j] >> 16));
-                    most = __vmaxu2(most, w[j] & 0x7FFF7FFFu);
-                    low = j ? fminf(low, fminf(v[2 * j], v[2 * j + 1])) : fminf(v[0], v[1]);
-                    high = j ? fmaxf(high, fmaxf(v[2 * j], v[2 * j + 1])) : fmaxf(v[0], v[1]);
-                }
+                // smallest and largest of the group, two at a time; a NaN stays one
+                using Two = std::conditional_t<F16, __half2, __nv_bfloat162>;
+                auto two = [](const uint32_t &u) { return *(const Two *)&u; };
+                auto word = [](const Two &t) { return *(const uint32_t *)&t; };
+                uint32_t low2 = word(__hmin2_nan(__hmin2_nan(two(w[0]), two(w[1])), __hmin2_nan(two(w[2]), two(w[3]))));
+                uint32_t high2 = word(__hmax2_nan(__hmax2_nan(two(w[0]), two(w[1])), __hmax2_nan(two(w[2]), two(w[3]))));
 #pragma unroll
                 for (int o = 1; o < 4; o <<= 1) {
-                    low = fminf(low, __shfl_xor_sync(kFull, low, o));
-                    high = fmaxf(high, __shfl_xor_sync(kFull, high, o));
-                    most = __vmaxu2(most, __shfl_xor_sync(kFull, most, o));
+                    const uint32_t l = __shfl_xor_sync(kFull, low2, o), h = __shfl_xor_sync(kFull, high2, o);
+                    low2 = word(__hmin2_nan(two(low2), two(l)));
+                    high2 = word(__hmax2_nan(two(high2), two(h)));
                 }
-                __half s = __float2half_rn(__fdiv_rn(high - low, 15.0f)), m = __float2half_rn(low);
-                const uint32_t infinite = F16 ? 0x7C00u : 0x7F80u;
-                const bool sound = max(most & 0xFFFFu, most >> 16) < infinite && __half2float(s) < INFINITY && fabsf(__half2float(m)) < INFINITY;
+                const uint32_t low_turned = prmt(low2, 0, 0x1032), high_turned = prmt(high2, 0, 0x1032);
+                const float low = widen16<F16>((uint16_t)word(__hmin2_nan(two(low2), two(low_turned))));
+                const float high = widen16<F16>((uint16_t)word(__hmax2_nan(two(high2), two(high_turned))));
+                // (high - low) / 15 as fp32 has it: the quotient by the reciprocal, and once more what that leaves over (Markstein's division)
+                const float span = high - low, first = span * (1.0f / 15.0f), span15 = fmaf(fmaf(-15.0f, first, span), 1.0f / 15.0f, first);
+                __half s = __float2half_rn(span15), m = __float2half_rn(low);
+                const bool sound = __half2float(s) < INFINITY && fabsf(__half2float(m)) < INFINITY;
                 if (!sound) s = __ushort_as_half(0x7FFFu), m = __ushort_as_half(0);
-                const float fs = __half2float(s), fm = __half2float(m), by = sound && fs != 0.0f ? 1.0f / (15.0f * fs) : 0.0f;
-                // The code is (x - m) / s rounded.  In fp32 the quotient is off by less than 1e-5: 64 bits decide next to a border alone.  (Taken as
+                const float fs = __half2float(s), fm = __half2float(m), by = sound && fs != 0.0f ? __fdividef(1.0f, 15.0f * fs) : 0.0f;
+                // The code is (x - m) / s rounded.  In fp32 the quotient is off by less than 15 * 2^-22: 64 bits decide next to a border alone.  (Taken as
                 // a part of 15, which cuts it off at both ends for nothing; 1.5 * 2^23 more is whole.)
-                uint32_t code[8];
-                float edge = 0.0f;
+                float code[8], edge = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float q = __saturatef((v[j] - fm) * by), up = fmaf(q, 15.0f, 12582912.0f);
-                    edge = fmaxf(edge, fabsf(fmaf(q, 15.0f, 12582912.0f - up)));
-                    code[j] = __float_as_uint(up) & 15u;
+                    const float v = widen16<F16>((uint16_t)(w[j >> 1] >> (j & 1) * 16)), q = __saturatef((v - fm) * by);
+                    code[j] = fmaf(q, 15.0f, 12582912.0f) - 12582912.0f;
+                    edge = fmaxf(edge, fabsf(fmaf(q, 15.0f, -code[j])));
                 }
-                if (edge > 0.49998f && by != 0.0f) {
-#pragma unroll 1
-                    for (int j = 0; j < 8; ++j) {
-                        const double q = ((double)widen16<F16>((uint16_t)(w[j >> 1] >> (j & 1) * 16)) - (double)fm) / (double)fs;
-                        const uint32_t c = (uint32_t)fmin(fmax(rint(q), 0.0), 15.0);
+                if (edge > 0.499995f && by != 0.0f) {
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) code[k] = k == j ? c : code[k];
+                    for (int j = 0; j < 8; ++j) {
+                        const float v = widen16<F16>((uint16_t)(w[j >> 1] >> (j & 1) * 16)), q = __saturatef((v - fm) * by);
+                        if (fabsf(fmaf(q, 15.0f, -code[j])) > 0.499995f) code[j] = exact_code(v, fm, fs);
                     }
                 }
+                // (whole numbers in fp32: 2^23 more has them in its low bits)
+                auto join2 = [](float a, float b, float by) { return __float_as_uint(fmaf(b, by, a + 8388608.0f)); };
                 const bool here = token - B.r < B.count;
                 if (side == 0) {
-                    uint32_t word = 0;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) word |= code[j] << ((j & 1) * 16 + (j >> 1) * 4);
-                    if (here) *(uint32_t *)(block + key_word_at(DIM, token, group, t4)) = word;
+                    const uint32_t even = __float_as_uint(fmaf(fmaf(fmaf(code[6], 16.0f, code[4]), 16.0f, code[2]), 16.0f, code[0] + 8388608.0f));
+                    const uint32_t odd = __float_as_uint(fmaf(fmaf(fmaf(code[7], 16.0f, code[5]), 16.0f, code[3]), 16.0f, code[1] + 8388608.0f));
+                    if (here) *(uint32_t *)(block + key_word_at(DIM, token, group, t4)) = prmt(even, odd, 0x5410);
                 } else {
                     // eight channels of 16 come from this lane, the others from its neighbour; each gets half of their bytes
-                    uint32_t nibbles[2] = {code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24, code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24};
-                    const uint32_t other = __shfl_xor_sync(kFull, lane & 1 ? nibbles[0] : nibbles[1], 1);
-                    if (here) s_codes[warp][token * (DIM / 8) + chunk] = lane & 1 ? other | nibbles[1] << 4 : nibbles[0] | other << 4;
+                    const uint32_t front = prmt(join2(code[0], code[1], 256.0f), join2(code[2], code[3], 256.0f), 0x5410);
+                    const uint32_t back = prmt(join2(code[4], code[5], 256.0f), join2(code[6], code[7], 256.0f), 0x5410);
+                    const uint32_t other = __shfl_xor_sync(kFull, lane & 1 ? front : back, 1);
+                    if (here) s_codes[warp][token * (DIM / 8) + chunk] = lane & 1 ? other | back << 4 : front | other << 4;
                 }
                 if (here && t4 == 0) {
                     *(__half *)(block + (side ? value_scale_at(DIM, token, group) : key_scale_at(DIM, token, group))) = s;
@@ -202,7 +205,7 @@ __global__ void __launch_bounds__(kCacheWarps * 32, 3) cache_append_kernel(const
 }
 
 template <uint32_t DIM, bool F16>
-__global__ void __launch_bounds__(kCacheWarps * 32, 3) cache_read_kernel(const __grid_constant__ CacheArgs C, const __grid_constant__ CacheRows R,
+__global__ void __launch_bounds__(kCacheWarps * 32, 5) cache_read_kernel(const __grid_constant__ CacheArgs C, const __grid_constant__ CacheRows R,
                                                                       const uint32_t rows) {
     constexpr uint32_t CHUNKS = DIM / 8, EACH = kCacheBlock * CHUNKS / 32;
     __shared__ uint32_t s_codes[kCacheWarps][kCacheBlock * DIM / 8];
@@ -237,16 +240,18 @@ __global__ void __launch_bounds__(kCacheWarps * 32, 3) cache_read_kernel(const _
                 if (token - B.r >= B.count) continue;
                 const float s = __half2float(__ushort_as_half(__ldcg((const unsigned short *)(block + (side ? value_scale_at(DIM, token, group) : key_scale_at(DIM, token, group))))));
                 const float m = __half2float(__ushort_as_half(__ldcg((const unsigned short *)(block + (side ? value_offset_at(DIM, token, group) : key_offset_at(DIM, token, group))))));
+                // (the code in the low four bits: behind 2^23, as conversions go through a slower pipe)
+                auto number = [](uint32_t u) { return __uint_as_float((u & 15u) | 0x4B000000u) - 8388608.0f; };
                 float v[8];
                 if (side) {
                     const uint32_t pair = token * (DIM / 8) + chunk / 2 * 2, shift = chunk % 2 * 4;
                     const uint32_t c0 = s_codes[warp][pair] >> shift, c1 = s_codes[warp][pair + 1] >> shift;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = fmaf(s, (float)(c0 >> 8 * j & 15u), m), v[4 + j] = fmaf(s, (float)(c1 >> 8 * j & 15u), m);
+                    for (int j = 0; j < 4; ++j) v[j] = fmaf(s, number(c0 >> 8 * j), m), v[4 + j] = fmaf(s, number(c1 >> 8 * j), m);
                 } else {
                     const uint32_t word = __ldcg((const uint32_t *)(block + key_word_at(DIM, token, group, t4)));
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = fmaf(s, (float)(word >> ((j & 1) * 16 + (j >> 1) * 4) & 15u), m);
+                    for (int j = 0; j < 8; ++j) v[j] = fmaf(s, number(word >> ((j & 1) * 16 + (j >> 1) * 4)), m);
                 }
                 const uint64_t to = (uint64_t)(B.row + token - B.r) * stride + head * DIM + chunk * 8;
                 if (R.f32) {
@@ -261,7 +266,7 @@ __global__ void __launch_bounds__(kCacheWarps * 32, 3) cache_read_kernel(const _
                 } else {
                     uint32_t w[4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) w[j] = round16<F16>(v[2 * j]) | (uint32_t)round16<F16>(v[2 * j + 1]) << 16;
+                    for (int j = 0; j < 4; ++j) w[j] = round16x2<F16>(v[2 * j], v[2 * j + 1]);
                     if (wide) {
                         *(uint4 *)(base + to) = make_uint4(w[0], w[1], w[2], w[3]);
                     } else {

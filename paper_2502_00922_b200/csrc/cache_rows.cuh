@@ -1,5 +1,8 @@
 // Which token a row of a call is, and where the cache has it.
 #pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
 #include "cache_layout.h"
 #include "decode_step.h"
 

@@ -77,6 +77,17 @@ template <bool F16>
 __device__ __forceinline__ uint16_t round16(float v) {
     return F16 ? __half_as_ushort(__float2half_rn(v)) : __bfloat16_as_ushort(__float2bfloat16_rn(v));
 }
+// Two values in one word, the first in its lower half
+template <bool F16>
+__device__ __forceinline__ uint32_t round16x2(float lo, float hi) {
+    if constexpr (F16) {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *(const uint32_t *)&h;
+    } else {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+        return *(const uint32_t *)&b;
+    }
+}
 // A value of the residual, past L1: the kernel in front may have written it, and may have read its place before.
 template <bool F16>
 __device__ __forceinline__ float load_value(const void *p, uint64_t at, bool is16) {

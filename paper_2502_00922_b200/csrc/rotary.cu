@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(kRotaryThreads) rotary_wide_kernel(const __gri
             uint32_t c[4], d[4];
             auto lo = [](uint32_t w) { return widen16<F16>((uint16_t)w); };
             auto hi = [](uint32_t w) { return widen16<F16>((uint16_t)(w >> 16)); };
-            auto both = [](float l, float h) { return round16<F16>(l) | (uint32_t)round16<F16>(h) << 16; };
+            auto both = [](float l, float h) { return round16x2<F16>(l, h); };
 #pragma unroll
             for (uint32_t j = 0; j < 4; ++j) {
                 if constexpr (NEIGHBOURS) {
