@@ -72,6 +72,9 @@ struct Walk {
     Steps steps;
     __device__ __forceinline__ void load(const AttentionArgs &A, uint32_t cols) {
         S = sequence_of(A.c, A.starts, A.rows, b);
+        know(A, cols);
+    }
+    __device__ __forceinline__ void know(const AttentionArgs &A, uint32_t cols) {
         steps = steps_of(S, A.window, A.sinks);
         tiles = (S.rows * A.group + cols - 1) / cols;
         units = tiles * A.c.kv_heads;
@@ -183,6 +186,7 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
     __shared__ __align__(8) uint64_t s_bar[2][W * STAGES];      // a stage's copies have arrived; a stage has been read
     __shared__ uint64_t s_start[W];                              // where in the line the first sequence of a warp begins
     __shared__ uint32_t s_start_b[W];                            // ... and which one it is
+    __shared__ Sequence s_start_s[W];
     __shared__ uint32_t s_here[W * STAGES][2];                   // blocks of a stage that are there
     __shared__ Piece s_piece[W][2];
     __shared__ uint2 s_join[2];                                  // units that this CTA is the last to arrive at: first CTA and number of pieces
@@ -198,13 +202,16 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
     pdl_wait_prior_grid();
 
     // The line: how long it is, and where in it this CTA starts (every warp finds out by itself).
+    Sequence seen;                                               // the last one that was weighed
     auto weight_of = [&](uint32_t b) -> uint64_t {
         if (b >= C.sequences) return 0;
-        const Sequence S = sequence_of(C, A.starts, A.rows, b);
+        const Sequence &S = seen;
+        seen = sequence_of(C, A.starts, A.rows, b);
         if (S.bad && tid < 32 && blockIdx.x == 0 && A.err) *A.err = (int32_t)b + 1;
         return (uint64_t)((S.rows * A.group + COLS - 1) / COLS) * C.kv_heads * steps_of(S, A.window, A.sinks).count;
     };
     const uint64_t first = weight_of(lane);
+    const Sequence first_seen = seen;
     uint64_t total = first;
     for (uint32_t b0 = 32; b0 < C.sequences; b0 += 32) total += weight_of(b0 + lane);
     for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(kFull, total, o);
@@ -235,7 +242,8 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
             if (behind) {                                        // (there is one: the line goes on behind its start)
                 const int k = __ffs(behind) - 1;
                 before += __shfl_sync(kFull, sum - w, k);
-                if (lane == 0) s_start[warp] = before, s_start_b[warp] = b0 + k;
+                if (lane == k) s_start_b[warp] = b0 + k, s_start_s[warp] = b0 ? seen : first_seen;
+                if (lane == 0) s_start[warp] = before;
                 break;
             }
             before += __shfl_sync(kFull, sum, 31);
@@ -247,7 +255,8 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
     Walk at;
     if (line_from < line_to) {
         at.b = s_start_b[reader];
-        at.load(A, COLS);
+        at.S = s_start_s[reader];
+        at.know(A, COLS);
         const uint64_t in = line_from - s_start[reader];
         at.unit = (uint32_t)quotient(in, at.steps.count);
         at.x = (uint32_t)(in - (uint64_t)at.unit * at.steps.count);
@@ -655,53 +664,47 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
     }
     __syncthreads();
 
-    // ---- units of which more than one warp has a piece: a run of pieces in the order of the line; a warp joins a column of a run
-    // Joins `count` pieces (N channels, every 32nd, of one column): value gets the sums, the result is their reference and weight.
-    auto join = [&](uint32_t count, auto tails, auto src, auto in, auto &value) -> float2 {
-        constexpr int N = (int)(sizeof(value) / sizeof(float));
-        float ref = -INFINITY, weight = 0.0f;
+    // ---- units of which more than one warp has a piece: a run of pieces in the order of the line
+    // Joins four channels of one column of `count` pieces: `load(i, value, tail)` brings a piece's sums, and their reference and weight.  Eight pieces are on
+    // their way together.
+    auto join = [&](uint32_t count, auto load, float4 &value, float2 &tail) {
+        value = make_float4(0, 0, 0, 0);
+        tail = make_float2(-INFINITY, 0.0f);
+        for (uint32_t base = 0; base < count; base += 8) {
+            float4 v[8];
+            float2 t[8];
 #pragma unroll
-        for (int j = 0; j < N; ++j) value[j] = 0.0f;
-        for (uint32_t base = 0; base < count; base += 32) {      // a lane has the reference and weight of one of 32 pieces
-            const uint32_t have = min(32u, count - base);
-            const float2 t = lane < have ? in(tails(base + lane) + DIM) : make_float2(-INFINITY, 0.0f);
-            float top = fmaxf(ref, t.x);
-            for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
-            const float scale = t.x == -INFINITY ? (t.y == 0.0f ? 0.0f : NAN) : ex2(t.x - top);
-            float sum = scale * t.y;
-            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
-            if (base) {
-                const float keep = ref == -INFINITY ? 1.0f : ex2(ref - top);
-                weight *= keep;
-#pragma unroll
-                for (int j = 0; j < N; ++j) value[j] *= keep;
+            for (uint32_t i = 0; i < 8; ++i) {
+                v[i] = make_float4(0, 0, 0, 0), t[i] = make_float2(-INFINITY, 0.0f);
+                if (base + i < count) load(base + i, v[i], t[i]);
             }
-            weight += sum;
-            ref = top;
-#pragma unroll 8
-            for (uint32_t i = 0; i < have; ++i) {
-                const float *const from = src(base + i) + lane;
-                const float by = __shfl_sync(kFull, scale, i);
+            float top = tail.x;
 #pragma unroll
-                for (int j = 0; j < N; ++j) value[j] = fmaf(by, in.one(from + 32 * j), value[j]);
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, t[i].x);
+            auto scale_of = [&](float2 from) { return from.x == -INFINITY ? (from.y == 0.0f ? 0.0f : NAN) : ex2(from.x - top); };
+            const float keep = scale_of(tail);
+            value.x *= keep, value.y *= keep, value.z *= keep, value.w *= keep;
+            tail = make_float2(top, tail.y * keep);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float scale = scale_of(t[i]);
+                value.x = fmaf(scale, v[i].x, value.x), value.y = fmaf(scale, v[i].y, value.y);
+                value.z = fmaf(scale, v[i].z, value.z), value.w = fmaf(scale, v[i].w, value.w);
+                tail.y = fmaf(scale, t[i].y, tail.y);
             }
         }
-        return make_float2(ref, weight);
     };
-    struct FromShared {
-        __device__ __forceinline__ float2 operator()(const float *p) const { return *(const float2 *)p; }
-        __device__ __forceinline__ float one(const float *p) const { return *p; }
-    };
-    struct FromGlobal {
-        __device__ __forceinline__ float2 operator()(const float *p) const { return __ldcg((const float2 *)p); }
-        __device__ __forceinline__ float one(const float *p) const { return __ldcg(p); }
-    };
-    auto put = [&](const Piece &P, uint32_t col, uint32_t d, float v) {
+    auto put = [&](const Piece &P, uint32_t col, uint32_t d, float4 v, float weight) {
         const uint32_t r = P.row0 + col;
         if (r >= P.rows) return;
+        const float by = weight == 0.0f ? 0.0f : 1.0f / weight;
         uint16_t *const to = A.out + (uint64_t)(P.first_row + r / A.group) * A.out_stride + (uint64_t)(P.head * A.group + r % A.group) * DIM + d;
-        *to = C.fp16 ? round16<true>(v) : round16<false>(v);
+        const uint32_t lo = C.fp16 ? round16x2<true>(v.x * by, v.y * by) : round16x2<false>(v.x * by, v.y * by);
+        const uint32_t hi = C.fp16 ? round16x2<true>(v.z * by, v.w * by) : round16x2<false>(v.z * by, v.w * by);
+        if (((uintptr_t)to & 7) == 0) *(uint2 *)to = make_uint2(lo, hi);
+        else to[0] = (uint16_t)lo, to[1] = (uint16_t)(lo >> 16), to[2] = (uint16_t)hi, to[3] = (uint16_t)(hi >> 16);
     };
+    constexpr uint32_t ITEMS = COLS * DIM / 4;
     const Piece *const all_pieces = &s_piece[0][0];
     const bool there = lane < 2 * W && all_pieces[lane].count != 0;
     const uint64_t begin = there ? all_pieces[lane].begin : 0;
@@ -711,25 +714,26 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
     // the unit that began in front of this CTA, and the one that goes on behind it and began here
     const bool open_lane = (runs >> lane & 1) && (begin < cta_from || begin + all_pieces[lane].count > cta_to);
     const uint32_t open_before = __ballot_sync(kFull, open_lane && begin < cta_from), open_behind = __ballot_sync(kFull, open_lane && begin >= cta_from);
-    for (uint32_t item = warp; item < __popc(runs) * COLS; item += W + 1) {
+    for (uint32_t item = tid; item < __popc(runs) * ITEMS; item += THREADS) {
         uint32_t left = runs;
-        for (uint32_t i = item / COLS; i; --i) left &= left - 1;
-        const uint32_t run = __ffs(left) - 1, col = item % COLS;
+        for (uint32_t i = item / ITEMS; i; --i) left &= left - 1;
+        const uint32_t run = __ffs(left) - 1, col = item % ITEMS / (DIM / 4), d = item % (DIM / 4) * 4;
         const uint32_t later = runs & ~((2u << run) - 1), members = places & ~((1u << run) - 1) & (later ? (1u << (__ffs(later) - 1)) - 1 : kFull);
-        const Piece P = all_pieces[run];
-        const uint32_t w0 = run / 2, odd = run % 2;              // (a run is every warp's first piece, but for its beginning, which may be a last one)
-        auto src = [&](uint32_t k) -> const float * { return (k == 0 && odd ? piece_at(w0, 1) : first_pieces + (w0 + k) * Shape::kPiece) + col * ROW; };
-        float value[G];
-        const float2 tail = join(__popc(members), src, src, FromShared{}, value);
-        const bool open = (open_before | open_behind) >> run & 1;
-        float *const piece = A.partials + (2 * (uint64_t)blockIdx.x + (open_before >> run & 1 ? 0 : 1)) * Shape::kPiece + col * ROW;
-        const float by = tail.y == 0.0f ? 0.0f : 1.0f / tail.y;
-#pragma unroll
-        for (int j = 0; j < G; ++j) {
-            if (open) __stcg(piece + 32 * j + lane, value[j]);
-            else put(P, col, 32 * j + lane, value[j] * by);
+        // (a run is every warp's first piece, but for its beginning, which may be a last one)
+        const float *const begin_at = (run % 2 ? piece_at(run / 2, 1) : first_pieces + run / 2 * Shape::kPiece) + col * ROW, *const rest_at = first_pieces + run / 2 * Shape::kPiece + col * ROW;
+        float4 value;
+        float2 tail;
+        join(__popc(members), [&](uint32_t i, float4 &v, float2 &t) {
+            const float *const from = i ? rest_at + i * Shape::kPiece : begin_at;
+            v = *(const float4 *)(from + d), t = *(const float2 *)(from + DIM);
+        }, value, tail);
+        if ((open_before | open_behind) >> run & 1) {
+            float *const piece = A.partials + (2 * (uint64_t)blockIdx.x + (open_before >> run & 1 ? 0 : 1)) * Shape::kPiece + col * ROW;
+            __stcg((float4 *)(piece + d), value);
+            if (d == 0) __stcg((float2 *)(piece + DIM), tail);
+        } else {
+            put(all_pieces[run], col, d, value, tail.y);
         }
-        if (open && lane == 0) __stcg((float2 *)(piece + DIM), tail);
     }
     if (!(open_before | open_behind)) return;
 
@@ -751,23 +755,19 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
         }
     }
     __syncthreads();
-    for (uint32_t k = 0; k < 2; ++k) {
+    for (uint32_t item = tid; item < 2 * ITEMS; item += THREADS) {
+        const uint32_t k = item / ITEMS, col = item % ITEMS / (DIM / 4), d = item % (DIM / 4) * 4;
         const uint2 J = s_join[k];
         if (J.y == 0) continue;
-        const Piece P = all_pieces[__ffs(k ? open_behind : open_before) - 1];
         // (the unit's first CTA has its piece in the second place, see above)
-        const float *const pieces = A.partials + 2 * (uint64_t)J.x * Shape::kPiece;
-        constexpr uint32_t PARTS = G % 2 ? 1 : 2;                // of a column's channels
-        for (uint32_t item = warp; item < COLS * PARTS; item += W + 1) {
-            const uint32_t col = item / PARTS, d = item % PARTS * (DIM / PARTS);
-            auto src = [&](uint32_t i) { return pieces + (i ? 2 * i : 1) * Shape::kPiece + col * ROW; };
-            float value[G / PARTS];
-            auto shifted = [&](uint32_t i) { return src(i) + d; };
-            const float2 tail = join(J.y, src, shifted, FromGlobal{}, value);
-            const float by = tail.y == 0.0f ? 0.0f : 1.0f / tail.y;
-#pragma unroll
-            for (int j = 0; j < G / PARTS; ++j) put(P, col, d + 32 * j + lane, value[j] * by);
-        }
+        const float *const pieces = A.partials + 2 * (uint64_t)J.x * Shape::kPiece + col * ROW;
+        float4 value;
+        float2 tail;
+        join(J.y, [&](uint32_t i, float4 &v, float2 &t) {
+            const float *const from = pieces + (i ? 2 * i : 1) * Shape::kPiece;
+            v = __ldcg((const float4 *)(from + d)), t = __ldcg((const float2 *)(from + DIM));
+        }, value, tail);
+        put(all_pieces[__ffs(k ? open_behind : open_before) - 1], col, d, value, tail.y);
     }
 }
 
