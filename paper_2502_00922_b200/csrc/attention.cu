@@ -20,6 +20,7 @@
 namespace huffllm {
 
 constexpr uint32_t kStepTokens = 2 * kCacheBlock;
+constexpr uint32_t kLead = 1;                     // steps that a unit's beginning takes as long as (its queries, its sums): they count in the line
 // A wait gives up after about a second: so many tries of one that sleeps for some microseconds, and of one that does not.
 constexpr uint32_t kWaitTries = 1u << 17, kPollTries = 1u << 25;
 constexpr int kSlack = 4;                        // a weight's exponent is set this far below its cap, so that few later ones are above it
@@ -39,11 +40,11 @@ struct AttentionShape {
 
 // Steps that some row of a sequence sees: the first tokens', then from the window's on.
 struct Steps {
-    uint32_t sink_end, from, count;                              // step x: x < sink_end ? x : from + x - sink_end
-    __device__ __forceinline__ uint32_t step(uint32_t x) const { return x < sink_end ? x : from + x - sink_end; }
+    uint32_t sink_end, from, count;                              // the first kLead of the `count` are none
+    __device__ __forceinline__ uint32_t step(uint32_t x) const { return x - kLead < sink_end ? x - kLead : from + x - kLead - sink_end; }
 };
 __device__ __forceinline__ Steps steps_of(const Sequence &S, uint32_t window, uint32_t sinks) {
-    Steps s{0, 0, 1};                                            // (rows that see nothing are a step of their own)
+    Steps s{0, 0, kLead + 1};                                    // (rows that see nothing are a step of their own)
     if (S.tokens == 0) return s;
     const uint32_t end = (uint32_t)(S.tokens - 1) / kStepTokens + 1;
     if (window) {
@@ -52,7 +53,7 @@ __device__ __forceinline__ Steps steps_of(const Sequence &S, uint32_t window, ui
         const uint32_t seen = min(sinks, (uint32_t)S.tokens);
         s.sink_end = min((seen + kStepTokens - 1) / kStepTokens, s.from);
     }
-    s.count = s.sink_end + end - s.from;
+    s.count = kLead + s.sink_end + end - s.from;
     return s;
 }
 
@@ -267,13 +268,13 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
         // The copies: a lane looks up its warp's next pages, and asks for them as soon as their stage has been read.
         const uint32_t page_blocks = C.page_tokens / kCacheBlock;
         bool more = lane < W && line_from < line_to;
-        uint32_t x = more ? at.x : 0, stage = 0, phase = 1, in_page[2] = {0, 0};   // (a fresh barrier's phase in front of its first is over)
+        uint32_t x = more ? max(at.x, kLead) : 0, stage = 0, phase = 1, in_page[2] = {0, 0};   // (a fresh barrier's phase in front of its first is over)
         int32_t page[2] = {-1, -1};
         bool wanted[2] = {false, false};
         auto look_up = [&]() {
-            if (x >= at.end) {
+            while (x >= at.end) {
                 more = at.next(A, COLS);
-                x = at.x;
+                x = kLead;
                 if (!more) return;
             }
             const uint32_t block = at.steps.step(x) * 2;
@@ -410,7 +411,7 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
             cap[n][0] = cap[n][1] = -INFINITY;
         }
 
-        for (uint32_t x = at.x; x < at.end; ++x) {
+        for (uint32_t x = max(at.x, kLead); x < at.end; ++x) {
             {
                 uint32_t tries = 0;
                 while (!mbar_try_wait(bars + 8 * stage, phase) && ++tries < kWaitTries) {}
@@ -665,28 +666,29 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
     __syncthreads();
 
     // ---- units of which more than one warp has a piece: a run of pieces in the order of the line
-    // Joins four channels of one column of `count` pieces: `load(i, value, tail)` brings a piece's sums, and their reference and weight.  Eight pieces are on
-    // their way together.
-    auto join = [&](uint32_t count, auto load, float4 &value, float2 &tail) {
+    // Joins four channels of one column of `count` pieces: `load(i, value, tail)` brings a piece's sums, and their reference and weight.  `batch`
+    // pieces are on their way together.
+    auto join = [&](auto batch, uint32_t count, auto load, float4 &value, float2 &tail) {
+        constexpr uint32_t N = decltype(batch)::value;
         value = make_float4(0, 0, 0, 0);
         tail = make_float2(-INFINITY, 0.0f);
-        for (uint32_t base = 0; base < count; base += 8) {
-            float4 v[8];
-            float2 t[8];
+        for (uint32_t base = 0; base < count; base += N) {
+            float4 v[N];
+            float2 t[N];
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) {
+            for (uint32_t i = 0; i < N; ++i) {
                 v[i] = make_float4(0, 0, 0, 0), t[i] = make_float2(-INFINITY, 0.0f);
                 if (base + i < count) load(base + i, v[i], t[i]);
             }
             float top = tail.x;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, t[i].x);
+            for (uint32_t i = 0; i < N; ++i) top = fmaxf(top, t[i].x);
             auto scale_of = [&](float2 from) { return from.x == -INFINITY ? (from.y == 0.0f ? 0.0f : NAN) : ex2(from.x - top); };
             const float keep = scale_of(tail);
             value.x *= keep, value.y *= keep, value.z *= keep, value.w *= keep;
             tail = make_float2(top, tail.y * keep);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (uint32_t i = 0; i < N; ++i) {
                 const float scale = scale_of(t[i]);
                 value.x = fmaf(scale, v[i].x, value.x), value.y = fmaf(scale, v[i].y, value.y);
                 value.z = fmaf(scale, v[i].z, value.z), value.w = fmaf(scale, v[i].w, value.w);
@@ -723,7 +725,7 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
         const float *const begin_at = (run % 2 ? piece_at(run / 2, 1) : first_pieces + run / 2 * Shape::kPiece) + col * ROW, *const rest_at = first_pieces + run / 2 * Shape::kPiece + col * ROW;
         float4 value;
         float2 tail;
-        join(__popc(members), [&](uint32_t i, float4 &v, float2 &t) {
+        join(std::integral_constant<uint32_t, 4>(), __popc(members), [&](uint32_t i, float4 &v, float2 &t) {
             const float *const from = i ? rest_at + i * Shape::kPiece : begin_at;
             v = *(const float4 *)(from + d), t = *(const float2 *)(from + DIM);
         }, value, tail);
@@ -763,7 +765,7 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
         const float *const pieces = A.partials + 2 * (uint64_t)J.x * Shape::kPiece + col * ROW;
         float4 value;
         float2 tail;
-        join(J.y, [&](uint32_t i, float4 &v, float2 &t) {
+        join(std::integral_constant<uint32_t, 8>(), J.y, [&](uint32_t i, float4 &v, float2 &t) {
             const float *const from = pieces + (i ? 2 * i : 1) * Shape::kPiece;
             v = __ldcg((const float4 *)(from + d)), t = __ldcg((const float2 *)(from + DIM));
         }, value, tail);
