@@ -231,7 +231,8 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
     const float scale = fmaxf(64.0f / temperature, fminf((float)(kBins - 1) / (top - least), 1e30f));
     const float width = 1.0f / (scale * temperature), to_log2 = -1.4426950408889634f / temperature;
     auto place = [&](float x) { return (top - x) * scale; };
-    auto weight = [&](float x) { return x == top ? 1.0f : exp2_approx((top - x) * to_log2); };
+    // (of the largest, were it infinite, this is no number: what equals the cut takes the cut's)
+    auto weight = [&](float x) { return exp2_approx((top - x) * to_log2); };
     // The bin of a place below kBins (2^23 and more has no fraction, and its low bits are the whole number; conversions go through a slower
     // pipe), and a weight's distance from that of the bin's upper edge, in 2^-22 of it: 1 - exp(-r) for r up to 1/64.
     auto bin_of = [](float place) { return __float_as_uint(__fadd_rd(place, 8388608.0f)) & (2 * kBins - 1); };
@@ -392,8 +393,8 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
                 }
                 return;
             }
-            // (most pieces have none within a bin and a half of its middle)
-            const float middle = top - ((float)bin + 0.5f) / scale, reach = 1.0f / scale + fabsf(middle) * 1e-6f;
+            // (most pieces have none within half a bin of its middle, give or take what rounding moves its edges)
+            const float middle = top - ((float)bin + 0.5f) / scale, reach = 0.505f / scale + (fabsf(middle) + fabsf(top)) * 1e-6f;
             R.each(tid, R.pieces, kSampleThreads, [&](uint4 v, uint32_t) {
                 const Piece16<TYPE> x(v);
                 float nearest = INFINITY;
@@ -643,10 +644,8 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
             const Piece16<TYPE> x(v);
 #pragma unroll
             for (int e = 0; e < R.N; ++e) {
-                if (x.x[e] > cut) {
-                    const float w = weight(x.x[e]);
-                    sum += w < least_weight ? 0.0f : w;
-                }
+                const float w = weight(x.x[e]);        // (a select costs less than a branch)
+                sum += x.x[e] > cut && !(w < least_weight) ? w : 0.0f;
                 equal += x.x[e] == cut;
             }
         });
@@ -679,7 +678,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
         S.table_equal[i] = other.warp_equal[i % kSampleWarps];
     }
     cluster.sync();                                    // (the last look at another CTA's shared memory)
-    const float cut_weight_given = cut == -INFINITY ? 0.0f : weight(cut), cut_weight = cut_weight_given < least_weight ? 0.0f : cut_weight_given;
+    const float cut_weight_given = cut == -INFINITY ? 0.0f : cut == top ? 1.0f : weight(cut), cut_weight = cut_weight_given < least_weight ? 0.0f : cut_weight_given;
     // the first warp: the stretch in which the mass exceeds what is drawn; a lane has some that follow each other
     constexpr uint32_t STRETCHES = kMostCluster * kSampleWarps / 32;    // of a lane
     if (warp == 0) {
