@@ -502,7 +502,8 @@ huffllm_status huffllm_decode_ffn(const huffllm_ffn *ffn, const void *h_dev, uin
                                   uint64_t out_stride, uint32_t h_type, void *workspace_dev, size_t workspace_bytes,
                                   int32_t *err_flag_dev, huffllm_stream stream);
 
-/* ------------------------------------------------ device: between and behind the products of a decode step */
+/* ------------------------------------------------ device: between and behind the products of a decode step
+ * All pointers of a call belong to the current device.  Nothing is read before the kernel in front on the stream has finished. */
 
 /*
  * Rotary positions with one or several axes (time, height and width of image and video tokens), for q and k in one launch.
@@ -541,11 +542,12 @@ huffllm_status huffllm_apply_rotary(const huffllm_rotary *args, huffllm_stream s
  * s * code + m: 5 bits a channel.  A group whose s or m would not be finite (NaN, infinities, values beyond fp16) stands for NaN.
  *
  * The pool is [pages][kv_heads][page_tokens / 16] blocks of 16 tokens; a block's bytes are the attention's business (cache_layout.h).
- * table[sequence][i] is the page of tokens i * page_tokens ..; entries that no token of the sequence lies on are never looked at.
+ * table[sequence][i] is the page of tokens i * page_tokens ..; entries with no token that a call
+ * writes or a row of it sees are not looked at (pages behind a window may be given away).
  * lengths[sequence] counts all of its tokens, those of the call included.  Table and lengths are read on the device, so a captured call
  * follows them as they grow.  Several sequences may share pages that are only read.
- * The calls set *err_flag (device, may be null) to sequence + 1 where a length is negative or beyond the table's row, a page is not one of the
- * pool's, or starts do not ascend within the rows of the call; what lies on such a page is neither written nor seen, nothing is read or
+ * The calls set *err_flag (device, may be null) to sequence + 1 where a length is negative or beyond the table's row (or 2^31 - 64), a page that
+ * is needed is not one of the pool's, or starts do not ascend within the rows of the call (-1: a copy never arrived within the wait limit); what lies on such a page is neither written nor seen, nothing is read or
  * written out of place, and other sequences are served.
  * A pool needs no initialisation.  huffllm_cache_bytes: its size for the given pages, heads and channels (pool, table and lengths may
  * be null there).

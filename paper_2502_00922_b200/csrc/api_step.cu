@@ -170,7 +170,9 @@ static huffllm_status check_attention(const huffllm_cache *cache, const huffllm_
     if (cache->sequences == 0 || cache->sequences > (1u << 20)) return fail(HUFFLLM_ERR_INVALID_ARG, "1 to 2^20 sequences");
     if (a->heads == 0 || a->heads % cache->kv_heads) return fail(HUFFLLM_ERR_INVALID_ARG, "heads must be a multiple of the cache's kv_heads");
     if (a->heads > 4096) return fail(HUFFLLM_ERR_UNSUPPORTED, "at most 4096 heads");
-    return check_rows(*cache, a->rows, a->starts, nullptr);
+    if ((st = check_rows(*cache, a->rows, a->starts, nullptr)) != HUFFLLM_OK) return st;
+    if (a->rows * a->heads > kMost) return fail(HUFFLLM_ERR_UNSUPPORTED, "rows times heads must stay below 2^31");
+    return HUFFLLM_OK;
 }
 
 huffllm_status huffllm_attention_control_bytes(const huffllm_cache *cache, const huffllm_attention *args, size_t *bytes) {

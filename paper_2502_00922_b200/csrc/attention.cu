@@ -152,6 +152,12 @@ __device__ __forceinline__ uint4 lds128(uint32_t at) {
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
     return v;
 }
+// What the product (a + rest) * s leaves beyond `product`, the rounded a * s.
+__device__ __forceinline__ uint32_t rest_half2(uint32_t a, uint32_t rest, uint32_t s, uint32_t product) {
+    const __half2 scale = *(const __half2 *)&s, left = __hfma2(*(const __half2 *)&a, scale, __hneg2(*(const __half2 *)&product));
+    const __half2 h = __hfma2(*(const __half2 *)&rest, scale, left);
+    return *(const uint32_t *)&h;
+}
 // N consecutive words of shared memory (N * 4-byte aligned for 1, 2, 4)
 template <int N>
 __device__ __forceinline__ void lds_words(uint32_t at, uint32_t *w) {
@@ -177,7 +183,9 @@ __device__ __forceinline__ void mma_f16_16816_new(float (&d)[4], uint32_t a0, ui
 }
 __device__ __forceinline__ void sts32(uint32_t at, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
 
-template <int DIM, int NT>
+// FINE: for results in FP16, which show what rounding p_t and p_t s_t,g to 11 bits costs (twice the error of the results' own rounding): both keep
+// what they leave, as a second number of 11 bits, exactly, and the products with values are taken twice.  (A seventh more instructions.)
+template <int DIM, int NT, bool FINE>
 __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) attention_kernel(const __grid_constant__ AttentionArgs A) {
     using Shape = AttentionShape<DIM, NT>;
     constexpr int G = Shape::kGroups, COLS = Shape::kCols, W = Shape::kWarps, STAGES = Shape::kStages, THREADS = W * 32 + 32;
@@ -577,17 +585,24 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const uint32_t blk = slot + k * BLOCK;
-                    uint32_t p[NT][2];
+                    uint32_t p[NT][2], rest[NT][2];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        p[n][0] = transposed(pack_half2(ex2(score[k][n][0]), ex2(score[k][n][1])));
-                        p[n][1] = transposed(pack_half2(ex2(score[k][n][2]), ex2(score[k][n][3])));
-                    }
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float e0 = ex2(score[k][n][2 * h]), e1 = ex2(score[k][n][2 * h + 1]);
+                            const uint32_t both = pack_half2(e0, e1);
+                            p[n][h] = transposed(both);
+                            if (FINE) rest[n][h] = transposed(pack_half2(e0 - low_half(both), e1 - high_half(both)));
+                        }
                     uint2 m = make_uint2(0, 0);
                     if (g < G) m = lds64(blk + value_offset_at(DIM, 0, 0) + (t4 * G + g) * 8);
                     const uint32_t ones = g == 0 ? 0x3C003C00u : 0u;
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) mma_f16_16816(off[n], m.x, ones, m.y, ones, p[n][0], p[n][1]);
+                    for (int n = 0; n < NT; ++n) {
+                        mma_f16_16816(off[n], m.x, ones, m.y, ones, p[n][0], p[n][1]);
+                        if (FINE) mma_f16_16816(off[n], m.x, ones, m.y, ones, rest[n][0], rest[n][1]);
+                    }
                     uint32_t w[2 * G];
 #pragma unroll
                     for (int j = 0; j < 2 * G; j += 4) {
@@ -601,10 +616,12 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
                             const uint32_t p0 = mul_half2(p[n][0], s.x), p1 = mul_half2(p[n][1], s.y);
+                            const uint32_t r0 = FINE ? rest_half2(p[n][0], rest[n][0], s.x, p0) : 0u, r1 = FINE ? rest_half2(p[n][1], rest[n][1], s.y, p1) : 0u;
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
                                 const uint32_t v = w[2 * i + h], v8 = v >> 8;
                                 mma_f16_16816(acc[n][2 * i + h], v & 0x000F000Fu, v & 0x00F000F0u, v8 & 0x000F000Fu, v8 & 0x00F000F0u, p0, p1);
+                                if (FINE) mma_f16_16816(acc[n][2 * i + h], v & 0x000F000Fu, v & 0x00F000F0u, v8 & 0x000F000Fu, v8 & 0x00F000F0u, r0, r1);
                             }
                         }
                     }
@@ -773,7 +790,7 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
     }
 }
 
-template <int DIM, int NT>
+template <int DIM, int NT, bool FINE>
 static cudaError_t launch_shape(const AttentionArgs &a, uint32_t sms, cudaStream_t stream) {
     using Shape = AttentionShape<DIM, NT>;
     static_assert(Shape::kSmem + 1536 <= 232448, "shared memory of a CTA");
@@ -782,23 +799,27 @@ static cudaError_t launch_shape(const AttentionArgs &a, uint32_t sms, cudaStream
     int dev = 0;
     cudaGetDevice(&dev);
     if (dev < 0 || dev >= 64 || !attr_set[dev].load(std::memory_order_acquire)) {
-        const cudaError_t e = cudaFuncSetAttribute(attention_kernel<DIM, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::kSmem);
+        const cudaError_t e = cudaFuncSetAttribute(attention_kernel<DIM, NT, FINE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::kSmem);
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) attr_set[dev].store(true, std::memory_order_release);
     }
-    return launch_behind(attention_kernel<DIM, NT>, dim3(sms < kAttentionCtas ? sms : kAttentionCtas), Shape::kWarps * 32 + 32, Shape::kSmem, stream, a);
+    return launch_behind(attention_kernel<DIM, NT, FINE>, dim3(sms < kAttentionCtas ? sms : kAttentionCtas), Shape::kWarps * 32 + 32, Shape::kSmem, stream, a);
 }
 
 // One tile of eight rows where a key head has no more than eight, two where it has (and registers hold them).
-cudaError_t launch_attention(const AttentionArgs &a, uint32_t sms, cudaStream_t stream) {
+template <bool FINE>
+static cudaError_t launch_dim(const AttentionArgs &a, uint32_t sms, cudaStream_t stream) {
     const bool two = (uint64_t)a.group * ((a.rows + a.c.sequences - 1) / a.c.sequences) > 8;
     switch (a.c.dim) {
-        case 64: return two ? launch_shape<64, 2>(a, sms, stream) : launch_shape<64, 1>(a, sms, stream);
-        case 96: return two ? launch_shape<96, 2>(a, sms, stream) : launch_shape<96, 1>(a, sms, stream);
-        case 128: return two ? launch_shape<128, 2>(a, sms, stream) : launch_shape<128, 1>(a, sms, stream);
-        case 192: return launch_shape<192, 1>(a, sms, stream);
-        default: return launch_shape<256, 1>(a, sms, stream);
+        case 64: return two ? launch_shape<64, 2, FINE>(a, sms, stream) : launch_shape<64, 1, FINE>(a, sms, stream);
+        case 96: return two ? launch_shape<96, 2, FINE>(a, sms, stream) : launch_shape<96, 1, FINE>(a, sms, stream);
+        case 128: return two ? launch_shape<128, 2, FINE>(a, sms, stream) : launch_shape<128, 1, FINE>(a, sms, stream);
+        case 192: return launch_shape<192, 1, FINE>(a, sms, stream);
+        default: return launch_shape<256, 1, FINE>(a, sms, stream);
     }
+}
+cudaError_t launch_attention(const AttentionArgs &a, uint32_t sms, cudaStream_t stream) {
+    return a.c.fp16 ? launch_dim<true>(a, sms, stream) : launch_dim<false>(a, sms, stream);
 }
 
 }  // namespace huffllm

@@ -19,7 +19,8 @@ __device__ __forceinline__ Sequence sequence_of(const CacheArgs &c, const int32_
     const int32_t n = __ldcg(c.lengths + b);
     const int32_t from = starts ? __ldcg(starts + b) : (int32_t)b, to = starts ? __ldcg(starts + b + 1) : (int32_t)b + 1;
     const bool rows_ok = from >= 0 && to >= from && (uint32_t)to <= rows;
-    const bool length_ok = n >= 0 && (uint64_t)n <= (uint64_t)c.table_stride * c.page_tokens;
+    // (the last 64 numbers are left to sums of positions)
+    const bool length_ok = n >= 0 && n <= 0x7FFFFFFF - 64 && (uint64_t)n <= (uint64_t)c.table_stride * c.page_tokens;
     s.first_row = rows_ok ? (uint32_t)from : 0u;
     s.rows = rows_ok ? (uint32_t)(to - from) : 0u;
     s.tokens = length_ok ? n : 0;

@@ -251,6 +251,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
         ties = 1;
     } else if (by_count || by_mass) {
         // ---- the bins
+        const bool two_sums = by_count || A.part >= 65536;
         const float units = __uint_as_float((127u + min(22u, (uint32_t)__clz(A.part))) << 23);
         // Where top_k is small, most of the row need not be looked at closely: of the largest logits of the threads' parts, which are that many
         // tokens, the top_k-th largest is not above the cut.  (Halving a range ten times is near enough.)
@@ -282,8 +283,8 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
                              "r"(below_edge(at))
                              : "memory");
         };
-        // Mass alone, in one addition: a weight in `units` of its bin's upper edge, as many as the CTA's logits leave of 32 bits (18 bits and more, 2^-19
-        // of a weight, where a CTA has up to 16384 logits).  units exp(-r) is a polynomial in how far the place is in its bin.
+        // Mass alone, in one addition: a weight in `units` of its bin's upper edge, as many as the CTA's logits leave of 32 bits (18 bits, 2^-19 of a
+        // weight, where a CTA has up to 16384 logits, and 16 at the least).  units exp(-r) is a polynomial in how far the place is in its bin.
         const float c1 = -units * width, c2 = 0.5f * units * width * width, c3 = -units * width * width * width / 6.0f;
         auto weigh_one = [&](float x) {
             const float at = place(x), whole = __fadd_rd(at, 8388608.0f), f = at - (whole - 8388608.0f);
@@ -311,7 +312,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
                 const Piece16<TYPE> x(v);
 #pragma unroll
                 for (int e = 0; e < R.N; ++e) {
-                    if (by_count) count_one(x.x[e]);
+                    if (two_sums) count_one(x.x[e]);
                     else weigh_one(x.x[e]);
                 }
             });
@@ -328,7 +329,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
                 below += other.below[bin];
             }
             S0.all_count[bin] = count;
-            S0.all_mass[bin] = expf(-(float)bin * width) * (float)(by_count ? (double)count - (double)below * 0x1p-22 : (double)below / units);
+            S0.all_mass[bin] = expf(-(float)bin * width) * (float)(two_sums ? (double)count - (double)below * 0x1p-22 : (double)below / units);
         }
         cluster.sync();
 

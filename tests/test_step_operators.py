@@ -8,8 +8,9 @@ Cache: nothing; codes, scales and offsets are exactly the format's, and s c + m 
 Attention: a score is a sum of fp32 products (exact factors) over `dim` channels, two products a channel (code and offset): off by
 (2 dim + 64) 2^-23 of the sum of their magnitudes, and by 2^-19 of the offsets' part, whose factor is a number of two fp16 halves.
 A weight is then off by twice that (its own and the largest's), by 2^-21 for the exponential, and by half a step of fp16 twice: as a factor of
-the sum, and times its scale.  What is too small for a full fp16 number (below 2^-14, where the largest is at most 2^15, or 2^14 over
-the largest scale of the values) is off by half of 2^-24: n such at most.  The sums over n tokens are off by (n + 64) 2^-23 of the sum of
+the sum, and times its scale.  What is too small for a full fp16 number (below 2^-14) is off by half of 2^-24: n such at most, where the
+largest weight is 2^11 or more, or 2^9 over the largest scale of the values (weights are held at most 2^15, their products with scales at
+most 2^14, and a larger weight than any before starts out sixteen times smaller than that).  The sums over n tokens are off by (n + 64) 2^-23 of the sum of
 magnitudes."""
 import math
 
@@ -315,7 +316,7 @@ def attention64(q, k, v, cached, scale, window, sinks):
                 w = np.exp(x - x.max())
                 p = w / w.sum()
                 most = np.nanmax(np.concatenate([[0.0], vs[seen, h // group].ravel()]))
-                small = 2.0 ** -25 / min(2.0 ** 15, 2.0 ** 13 / max(most, 2.0 ** -20))
+                small = 2.0 ** -25 / min(2.0 ** 11, 2.0 ** 9 / max(most, 2.0 ** -20))
                 rel = np.exp(off + np.nanmax(np.concatenate([[0.0], off]))) * (1 + 2.0 ** -21) * (1 + 2.0 ** -11) ** 2 - 1 + (n + 64) * 2.0 ** -23
                 out[i, h] = p @ vv
                 # the weights' errors move the sum, and (over the sum of weights) the mean
@@ -608,7 +609,7 @@ def test_sample_ties_go_to_the_lowest_index(hl, torch):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("vocab,rows", [(30011, 3), (150001, 2), (9001, 160)])
+@pytest.mark.parametrize("vocab,rows", [(30011, 3), (150001, 2), (9001, 160), (140001, 24)])
 def test_sample_crowded_logits(hl, torch, vocab, rows):
     """Thousands of tokens next to each other in their logits, a few distinct values of them or many; very high and very low temperatures."""
     rng = np.random.default_rng(vocab)
