@@ -148,9 +148,7 @@ static huffllm_status cache_move(bool append, const huffllm_cache *cache, void *
     r.f32 = type == HUFFLLM_ELEM_F32;
     r.err = err;
     const CacheArgs c = cache_args(*cache);
-    DeviceInfo dev;
-    if ((st = device_info(&dev)) != HUFFLLM_OK) return st;
-    return launched(append ? launch_cache_append(c, r, dev.sms, (cudaStream_t)stream) : launch_cache_read(c, r, dev.sms, (cudaStream_t)stream),
+    return launched(append ? launch_cache_append(c, r, (cudaStream_t)stream) : launch_cache_read(c, r, (cudaStream_t)stream),
                     append ? "cache append" : "cache read");
 }
 

@@ -12,7 +12,7 @@
 
 namespace huffllm {
 
-constexpr uint32_t kCacheWarps = 8;
+constexpr uint32_t kCacheWarps = 8;                   // of a CTA at most
 
 // The rows of a call that lie in one block.
 struct BlockRows {
@@ -29,12 +29,12 @@ __device__ __forceinline__ void for_blocks(const CacheArgs &C, const CacheRows &
     const uint32_t lane = threadIdx.x % 32, row = blockIdx.x * rows + lane;
     if (blockIdx.x == 0 && blockIdx.y == 0) report_faults(C, R.starts, R.rows, R.err);
     BlockRows B{row, 0, 0, -1, C.page_tokens / kCacheBlock};
+    const uint32_t b = sequences_of_rows(R.starts, C.sequences, blockIdx.x * rows, rows);
     if (lane < rows && row < R.rows) {
-        const uint32_t b = sequence_of_row(R.starts, C.sequences, row);
-        const Sequence S = sequence_of(C, R.starts, R.rows, b < C.sequences ? b : 0);
+        const Sequence S = sequence_of(C, R.starts, R.rows, b);
         const uint32_t i = row - S.first_row;
         const int32_t at = S.tokens - (int32_t)S.rows + (int32_t)i;
-        if (b < C.sequences && !S.bad && row >= S.first_row && i < S.rows && at >= 0 && (at % kCacheBlock == 0 || i == 0 || at == 0)) {
+        if (!S.bad && row >= S.first_row && i < S.rows && at >= 0 && (at % kCacheBlock == 0 || i == 0 || at == 0)) {
             B.r = at % kCacheBlock;
             B.count = min(kCacheBlock - B.r, S.rows - i);
             const int32_t page = __ldcg(C.table + (uint64_t)b * C.table_stride + at / C.page_tokens);
@@ -75,16 +75,16 @@ struct ValueItem {
 };
 
 template <uint32_t DIM, bool F16>
-__global__ void __launch_bounds__(kCacheWarps * 32, 4) cache_append_kernel(const __grid_constant__ CacheArgs C, const __grid_constant__ CacheRows R,
+__global__ void __launch_bounds__(kCacheWarps * 32, DIM <= 128 ? 4 : 3) cache_append_kernel(const __grid_constant__ CacheArgs C, const __grid_constant__ CacheRows R,
                                                                         const uint32_t rows) {
     constexpr uint32_t CHUNKS = DIM / 8, AT_ONCE = 2, G = cache_groups(DIM), kFull = 0xFFFFFFFFu;
     __shared__ uint32_t s_codes[kCacheWarps][kCacheBlock * DIM / 8];       // [token][16 channels][2]: a byte is two channels, eight apart
     pdl_launch_dependents();
     pdl_wait_prior_grid();
-    const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32;
     const bool wide = !(((uintptr_t)R.k | (uintptr_t)R.v) & 15) && R.k_stride % 8 == 0 && R.v_stride % 8 == 0;
     for_blocks(C, R, rows, [&](const BlockRows &B) {
-        for (uint32_t task = blockIdx.y * kCacheWarps + warp; task < 2 * C.kv_heads; task += gridDim.y * kCacheWarps) {
+        for (uint32_t task = blockIdx.y * warps + warp; task < 2 * C.kv_heads; task += gridDim.y * warps) {
             const uint32_t head = task / 2, side = task % 2;
             const uint16_t *const x = (side ? R.v : R.k) + head * DIM;
             const uint64_t stride = side ? R.v_stride : R.k_stride;
@@ -205,16 +205,16 @@ __global__ void __launch_bounds__(kCacheWarps * 32, 4) cache_append_kernel(const
 }
 
 template <uint32_t DIM, bool F16>
-__global__ void __launch_bounds__(kCacheWarps * 32, 5) cache_read_kernel(const __grid_constant__ CacheArgs C, const __grid_constant__ CacheRows R,
+__global__ void __launch_bounds__(kCacheWarps * 32, DIM <= 128 ? 5 : 3) cache_read_kernel(const __grid_constant__ CacheArgs C, const __grid_constant__ CacheRows R,
                                                                       const uint32_t rows) {
     constexpr uint32_t CHUNKS = DIM / 8, EACH = kCacheBlock * CHUNKS / 32;
     __shared__ uint32_t s_codes[kCacheWarps][kCacheBlock * DIM / 8];
     pdl_launch_dependents();
     pdl_wait_prior_grid();
-    const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32;
     const bool wide = !(((uintptr_t)R.k | (uintptr_t)R.v) & 15) && R.k_stride % 8 == 0 && R.v_stride % 8 == 0;
     for_blocks(C, R, rows, [&](const BlockRows &B) {
-        for (uint32_t task = blockIdx.y * kCacheWarps + warp; task < 2 * C.kv_heads; task += gridDim.y * kCacheWarps) {
+        for (uint32_t task = blockIdx.y * warps + warp; task < 2 * C.kv_heads; task += gridDim.y * warps) {
             const uint32_t head = task / 2, side = task % 2;
             uint16_t *const base = side ? R.v : R.k;
             if (!base) continue;
@@ -281,24 +281,25 @@ __global__ void __launch_bounds__(kCacheWarps * 32, 5) cache_read_kernel(const _
 }
 
 template <uint32_t DIM>
-static cudaError_t launch_move(bool append, const CacheArgs &c, const CacheRows &r, uint32_t sms, cudaStream_t stream) {
-    // Sixteen rows a CTA, as many as a block has, where that leaves every SM some CTAs (rows find their blocks lane by lane); else one.
-    const uint32_t tasks = (2 * c.kv_heads + kCacheWarps - 1) / kCacheWarps;
-    const uint32_t rows = (uint64_t)(r.rows / kCacheBlock) * tasks >= 2 * (uint64_t)sms ? kCacheBlock : 1;
-    const dim3 grid((r.rows + rows - 1) / rows, tasks);
+static cudaError_t launch_move(bool append, const CacheArgs &c, const CacheRows &r, cudaStream_t stream) {
+    // A warp for every head and side, up to eight a CTA.  Sixteen rows a CTA, as many as a block has, where sequences bring some eight rows or more
+    // (48 sequences with 34 rows each, eight heads: 106 us with a CTA a row); else one.
+    const uint32_t tasks = 2 * c.kv_heads, warps = tasks < kCacheWarps ? tasks : kCacheWarps;
+    const uint32_t rows = r.rows / 8 >= c.sequences ? kCacheBlock : 1;
+    const dim3 grid((r.rows + rows - 1) / rows, (tasks + warps - 1) / warps);
     auto kernel = append ? (c.fp16 ? cache_append_kernel<DIM, true> : cache_append_kernel<DIM, false>) : (c.fp16 ? cache_read_kernel<DIM, true> : cache_read_kernel<DIM, false>);
-    return launch_behind(kernel, grid, kCacheWarps * 32, 0, stream, c, r, rows);
+    return launch_behind(kernel, grid, warps * 32, 0, stream, c, r, rows);
 }
-static cudaError_t launch_dim(bool append, const CacheArgs &c, const CacheRows &r, uint32_t sms, cudaStream_t stream) {
+static cudaError_t launch_dim(bool append, const CacheArgs &c, const CacheRows &r, cudaStream_t stream) {
     switch (c.dim) {
-        case 64: return launch_move<64>(append, c, r, sms, stream);
-        case 96: return launch_move<96>(append, c, r, sms, stream);
-        case 128: return launch_move<128>(append, c, r, sms, stream);
-        case 192: return launch_move<192>(append, c, r, sms, stream);
-        default: return launch_move<256>(append, c, r, sms, stream);
+        case 64: return launch_move<64>(append, c, r, stream);
+        case 96: return launch_move<96>(append, c, r, stream);
+        case 128: return launch_move<128>(append, c, r, stream);
+        case 192: return launch_move<192>(append, c, r, stream);
+        default: return launch_move<256>(append, c, r, stream);
     }
 }
-cudaError_t launch_cache_append(const CacheArgs &c, const CacheRows &r, uint32_t sms, cudaStream_t stream) { return launch_dim(true, c, r, sms, stream); }
-cudaError_t launch_cache_read(const CacheArgs &c, const CacheRows &r, uint32_t sms, cudaStream_t stream) { return launch_dim(false, c, r, sms, stream); }
+cudaError_t launch_cache_append(const CacheArgs &c, const CacheRows &r, cudaStream_t stream) { return launch_dim(true, c, r, stream); }
+cudaError_t launch_cache_read(const CacheArgs &c, const CacheRows &r, cudaStream_t stream) { return launch_dim(false, c, r, stream); }
 
 }  // namespace huffllm

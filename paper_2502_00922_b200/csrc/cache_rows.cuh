@@ -33,23 +33,33 @@ __device__ __forceinline__ void report_faults(const CacheArgs &c, const int32_t 
     for (uint32_t b = threadIdx.x; b < c.sequences; b += blockDim.x)
         if (sequence_of(c, starts, rows, b).bad) *err = (int32_t)b + 1;
 }
-// The sequence that has row r, if one has: the last one that starts at or in front of it.
-__device__ __forceinline__ uint32_t sequence_of_row(const int32_t *starts, uint32_t sequences, uint32_t r) {
-    if (!starts) return r;
-    uint32_t lo = 0, hi = sequences;                       // starts[lo] <= r or lo == 0; starts[hi] > r or hi == sequences
+// The sequences that have the rows first + lane (lanes below `rows`, at most 32): the last ones that start at or in front of them.  All lanes of a
+// warp; where starts do not ascend, the first sequence that fits.
+__device__ __forceinline__ uint32_t sequences_of_rows(const int32_t *starts, uint32_t sequences, uint32_t first, uint32_t rows) {
+    constexpr uint32_t kFull = 0xFFFFFFFFu;
+    const uint32_t lane = threadIdx.x % 32;
+    if (!starts) return min(first + lane, sequences - 1);
+    auto run_of = [](uint32_t bits) -> uint32_t { return bits == kFull ? 32 : __ffs(~bits) - 1; };   // (what lies behind a start that is not passed does not count)
+    uint32_t lo = 0, hi = sequences;                       // starts[lo] <= first or lo == 0; starts[hi] > first or hi == sequences
     while (hi - lo > 1) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (__ldcg(starts + mid) <= (int32_t)r) lo = mid;
-        else hi = mid;
+        const uint32_t step = (hi - lo + 31) / 32, at = lo + lane * step;
+        const uint32_t there = __ballot_sync(kFull, lane == 0 || (at < hi && __ldcg(starts + at) <= (int32_t)first));
+        const uint32_t k = run_of(there) - 1;
+        hi = min(hi, lo + (k + 1) * step);
+        lo += k * step;
     }
-    return lo;
-}
-// The block that has token `at` of sequence b (key head h), or null where its page is none of the pool's.
-__device__ __forceinline__ uint8_t *block_of(const CacheArgs &c, uint32_t b, uint32_t at, uint32_t h) {
-    const int32_t page = __ldcg(c.table + (uint64_t)b * c.table_stride + at / c.page_tokens);
-    if (page < 0 || (uint32_t)page >= c.pages) return nullptr;
-    const uint64_t block = ((uint64_t)page * c.kv_heads + h) * (c.page_tokens / kCacheBlock) + at % c.page_tokens / kCacheBlock;
-    return c.pool + block * cache_block_bytes(c.dim);
+    if (rows == 1) return lo;
+    // the starts behind that one, a lane each: how many are at or in front of a row
+    const uint32_t next = lo + 1 + lane;
+    const int32_t start = next < sequences ? __ldcg(starts + next) : 0x7FFFFFFF;
+    uint32_t mine = lo;
+    for (uint32_t r = 1; r < rows; ++r) {
+        const uint32_t passed = run_of(__ballot_sync(kFull, start <= (int32_t)(first + r)));
+        if (lane == r) mine = lo + passed;
+        if (lane == r && passed == 32)                     // (so many sequences without a row)
+            while (mine + 1 < sequences && __ldcg(starts + mine + 1) <= (int32_t)(first + r)) ++mine;
+    }
+    return mine;
 }
 
 }  // namespace huffllm

@@ -33,8 +33,8 @@ struct CacheRows {
     uint32_t f32;                  // read: k and v are fp32
     int32_t *err;                  // may be null
 };
-cudaError_t launch_cache_append(const CacheArgs &c, const CacheRows &r, uint32_t sms, cudaStream_t stream);
-cudaError_t launch_cache_read(const CacheArgs &c, const CacheRows &r, uint32_t sms, cudaStream_t stream);
+cudaError_t launch_cache_append(const CacheArgs &c, const CacheRows &r, cudaStream_t stream);
+cudaError_t launch_cache_read(const CacheArgs &c, const CacheRows &r, cudaStream_t stream);
 
 constexpr uint32_t kAttentionCtas = 512;                  // most CTAs of a launch
 constexpr uint32_t kAttentionPartial = 16 * 132;          // most floats of a piece (a column's channels and four more: 16 columns of 128, eight of 256)
