@@ -108,11 +108,17 @@ huffllm_status huffllm_apply_rotary(const huffllm_rotary *args, huffllm_stream s
     r.tokens = (uint32_t)a.tokens;
     r.dim = a.head_dim;
     r.rot = a.rotary_dim;
-    r.axes = a.axes;
-    r.in_turn = a.in_turn != 0;
     r.neighbours = a.pairing == HUFFLLM_PAIR_NEIGHBOURS;
     r.fp16 = a.dtype == HUFFLLM_FP16;
-    for (uint32_t i = 0; i < a.axes; ++i) r.sections[i] = a.sections[i];
+    // the axis of every pair: one axis behind the other, or dealt in turn to those that have pairs left
+    uint32_t left[HUFFLLM_MAX_AXES] = {}, axis = 0;
+    for (uint32_t i = 0; i < a.axes; ++i) left[i] = a.sections[i];
+    for (uint32_t i = 0; i < a.rotary_dim / 2; ++i) {
+        while (left[axis] == 0) axis = (axis + 1) % a.axes;
+        r.axis_bits[i / 16] |= axis << i % 16 * 2;
+        --left[axis];
+        if (a.in_turn) axis = (axis + 1) % a.axes;
+    }
     return launched(launch_rotary(r, (cudaStream_t)stream), "rotary");
 }
 

@@ -2,8 +2,9 @@
 //
 // A warp has the tokens that a call brings of one block (up to 16), of one head, of its keys or of its values.  A lane has eight channels of a
 // token, which come and go as 16 bytes, four lanes have a group.  Eight codes are a word of the keys as it lies; of the values, a word has four
-// tokens of two channels, so these change places in shared memory, four by four bytes.  Bound by memory where rows are many (the
-// instructions are about ten a value), by latency where they are few: rows are then a CTA each, and heads spread over more of them.
+// tokens of two channels, so these change places in shared memory, four by four bytes.  Where rows are many, bound by instructions (18.6 million warp
+// instructions for 17 million values, half of them around the values: groups, addresses, places), where they are few by four
+// loads that follow each other: starts, length, page, row.  8294 rows of eight heads of 128 written 31 us, read back 24; 64 rows of one token 5 us each.
 #include <cuda_runtime.h>
 
 #include "cache_rows.cuh"

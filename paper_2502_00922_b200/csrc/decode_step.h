@@ -15,8 +15,8 @@ struct RotaryArgs {
     uint16_t *out[2];
     uint64_t in_stride[2], out_stride[2];
     uint32_t heads[2];
-    uint32_t tokens, dim, rot, axes, in_turn, neighbours, fp16;
-    uint32_t sections[4];
+    uint32_t tokens, dim, rot, neighbours, fp16;
+    uint32_t axis_bits[32];        // the axis of every pair, two bits each
 };
 cudaError_t launch_rotary(const RotaryArgs &a, cudaStream_t stream);
 

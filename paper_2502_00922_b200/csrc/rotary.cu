@@ -7,33 +7,7 @@
 
 namespace huffllm {
 
-// The axis of pair i where the axes' pairs are dealt in turn: rounds of those axes that have pairs left.
-__device__ __forceinline__ uint32_t axis_in_turn(const RotaryArgs &A, uint32_t i) {
-    uint32_t done = 0;                                   // pairs that an axis still in the game has had
-    for (;;) {
-        uint32_t live = 0, least = 0xFFFFFFFFu;
-        for (uint32_t a = 0; a < A.axes; ++a)
-            if (A.sections[a] > done) {
-                ++live;
-                least = min(least, A.sections[a]);
-            }
-        if (live == 0) return 0;
-        const uint32_t dealt = (least - done) * live;    // until the next axis has had all of its pairs
-        if (i < dealt) {
-            uint32_t k = i % live;
-            for (uint32_t a = 0; a < A.axes; ++a)
-                if (A.sections[a] > done && k-- == 0) return a;
-        }
-        i -= dealt;
-        done = least;
-    }
-}
-__device__ __forceinline__ uint32_t axis_of(const RotaryArgs &A, uint32_t i) {
-    if (A.in_turn) return axis_in_turn(A, i);
-    uint32_t a = 0;
-    while (a + 1 < A.axes && i >= A.sections[a]) i -= A.sections[a++];
-    return a;
-}
+__device__ __forceinline__ uint32_t axis_of(const RotaryArgs &A, uint32_t i) { return A.axis_bits[i / 16] >> i % 16 * 2 & 3u; }
 
 // Sine and cosine of position * frequency.  The product is taken in turns and in 64 bits: 2^31 turns are off by 2^-23 of one at most,
 // those of a position of a million by 2^-33, and what is left behind the whole turns is exact in either.
@@ -72,11 +46,12 @@ __global__ void __launch_bounds__(128) rotary_kernel(const __grid_constant__ Rot
 
 // Heads whose channels lie on 16-byte boundaries: a thread turns eight channels with the eight half a rotary_dim away (or four pairs of
 // neighbours), in as many heads as threads leave it.  A CTA has a token; its sines and cosines meet in shared memory while the
-// heads are on their way.  Bound by memory for many tokens, by the way there and back for few.
+// heads are on their way.  5003 tokens of 32 heads of 128: 21 us, 3.8 TB/s, 0.58 of the measured copy rate (value by value 44); what is left is the way
+// of a CTA from positions by sines to its heads.  One token 6.9 us, most of them the call.
 constexpr uint32_t kRotaryThreads = 256, kRotaryEach = 2;
 template <bool F16, bool NEIGHBOURS>
 __global__ void __launch_bounds__(kRotaryThreads) rotary_wide_kernel(const __grid_constant__ RotaryArgs A) {
-    __shared__ float2 s_turn[512];
+    __shared__ float4 s_turn[256];                       // cosines and sines of two pairs; of an item's pairs `turned` apart, so that neighbours read neighbours
     pdl_launch_dependents();
     pdl_wait_prior_grid();
     const uint32_t token = blockIdx.x, pairs = A.rot / 2, tid = threadIdx.x;
@@ -105,8 +80,10 @@ __global__ void __launch_bounds__(kRotaryThreads) rotary_wide_kernel(const __gri
             if (!NEIGHBOURS && part[k] < turned) y[k] = __ldcg((const uint4 *)(from[k] + pairs));
         }
         if (!known) {
+            constexpr uint32_t PER = NEIGHBOURS ? 4 : 8;              // pairs of an item
             for (uint32_t i = tid; i < pairs; i += blockDim.x)
-                s_turn[i] = turn_of(__ldcg(A.positions + (uint64_t)axis_of(A, i) * A.tokens + token), __ldcg(A.frequencies + i));
+                ((float2 *)s_turn)[(i % PER / 2 * turned + i / PER) * 2 + i % 2] =
+                    turn_of(__ldcg(A.positions + (uint64_t)axis_of(A, i) * A.tokens + token), __ldcg(A.frequencies + i));
             __syncthreads();
             known = true;
         }
@@ -125,12 +102,13 @@ __global__ void __launch_bounds__(kRotaryThreads) rotary_wide_kernel(const __gri
 #pragma unroll
             for (uint32_t j = 0; j < 4; ++j) {
                 if constexpr (NEIGHBOURS) {
-                    const float2 t = s_turn[part[k] * 4 + j];
-                    c[j] = both(lo(a[j]) * t.x - hi(a[j]) * t.y, hi(a[j]) * t.x + lo(a[j]) * t.y);
+                    const float4 t = s_turn[j / 2 * turned + part[k]];
+                    const float cosine = j % 2 ? t.z : t.x, sine = j % 2 ? t.w : t.y;
+                    c[j] = both(lo(a[j]) * cosine - hi(a[j]) * sine, hi(a[j]) * cosine + lo(a[j]) * sine);
                 } else {
-                    const float2 t = s_turn[part[k] * 8 + 2 * j], u = s_turn[part[k] * 8 + 2 * j + 1];
-                    c[j] = both(lo(a[j]) * t.x - lo(b[j]) * t.y, hi(a[j]) * u.x - hi(b[j]) * u.y);
-                    d[j] = both(lo(b[j]) * t.x + lo(a[j]) * t.y, hi(b[j]) * u.x + hi(a[j]) * u.y);
+                    const float4 t = s_turn[j * turned + part[k]];
+                    c[j] = both(lo(a[j]) * t.x - lo(b[j]) * t.y, hi(a[j]) * t.z - hi(b[j]) * t.w);
+                    d[j] = both(lo(b[j]) * t.x + lo(a[j]) * t.y, hi(b[j]) * t.z + hi(a[j]) * t.w);
                 }
             }
             *(uint4 *)to[k] = make_uint4(c[0], c[1], c[2], c[3]);
