@@ -95,85 +95,85 @@ __global__ void __launch_bounds__(kCacheWarps * 32, DIM <= 128 ? 4 : 3) cache_ap
                 // four pieces of 16 bytes (a lane's, of two tokens or more) on their way together; tokens that the call does not bring are passed over
 #pragma unroll 1
                 for (uint32_t k0 = B.r * CHUNKS / 32; k0 * 32 < (B.r + B.count) * CHUNKS; k0 += AT_ONCE) {
-                uint4 raw[AT_ONCE];
+                    uint4 raw[AT_ONCE];
 #pragma unroll
-                for (uint32_t k = 0; k < AT_ONCE; ++k) {
-                    const uint32_t i = (k0 + k) * 32 + lane, token = i / CHUNKS, chunk = i % CHUNKS;
-                    raw[k] = make_uint4(0, 0, 0, 0);
-                    if (token - B.r >= B.count) continue;      // (wraps in front of the first)
-                    const uint16_t *const from = x + (uint64_t)(B.row + token - B.r) * stride + chunk * 8;
-                    if (wide) {
-                        raw[k] = __ldcg((const uint4 *)from);
-                    } else {
-                        uint32_t e[8];
+                    for (uint32_t k = 0; k < AT_ONCE; ++k) {
+                        const uint32_t i = (k0 + k) * 32 + lane, token = i / CHUNKS, chunk = i % CHUNKS;
+                        raw[k] = make_uint4(0, 0, 0, 0);
+                        if (token - B.r >= B.count) continue;      // (wraps in front of the first)
+                        const uint16_t *const from = x + (uint64_t)(B.row + token - B.r) * stride + chunk * 8;
+                        if (wide) {
+                            raw[k] = __ldcg((const uint4 *)from);
+                        } else {
+                            uint32_t e[8];
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) e[j] = __ldcg((const unsigned short *)from + j);
-                        raw[k] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+                            for (int j = 0; j < 8; ++j) e[j] = __ldcg((const unsigned short *)from + j);
+                            raw[k] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+                        }
                     }
-                }
 #pragma unroll
-                for (uint32_t k = 0; k < AT_ONCE; ++k) {
-                    if ((k0 + k) * 32 >= (B.r + B.count) * CHUNKS) break;
-                    const uint32_t i = (k0 + k) * 32 + lane, token = i / CHUNKS, chunk = i % CHUNKS, group = chunk / 4, t4 = chunk % 4;
-                    const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
-                    // smallest and largest of the group, two at a time; a NaN stays one
-                    using Two = std::conditional_t<F16, __half2, __nv_bfloat162>;
-                    auto two = [](const uint32_t &u) { return *(const Two *)&u; };
-                    auto word = [](const Two &t) { return *(const uint32_t *)&t; };
-                    uint32_t low2 = word(__hmin2_nan(__hmin2_nan(two(w[0]), two(w[1])), __hmin2_nan(two(w[2]), two(w[3]))));
-                    uint32_t high2 = word(__hmax2_nan(__hmax2_nan(two(w[0]), two(w[1])), __hmax2_nan(two(w[2]), two(w[3]))));
+                    for (uint32_t k = 0; k < AT_ONCE; ++k) {
+                        if ((k0 + k) * 32 >= (B.r + B.count) * CHUNKS) break;
+                        const uint32_t i = (k0 + k) * 32 + lane, token = i / CHUNKS, chunk = i % CHUNKS, group = chunk / 4, t4 = chunk % 4;
+                        const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+                        // smallest and largest of the group, two at a time; a NaN stays one
+                        using Two = std::conditional_t<F16, __half2, __nv_bfloat162>;
+                        auto two = [](const uint32_t &u) { return *(const Two *)&u; };
+                        auto word = [](const Two &t) { return *(const uint32_t *)&t; };
+                        uint32_t low2 = word(__hmin2_nan(__hmin2_nan(two(w[0]), two(w[1])), __hmin2_nan(two(w[2]), two(w[3]))));
+                        uint32_t high2 = word(__hmax2_nan(__hmax2_nan(two(w[0]), two(w[1])), __hmax2_nan(two(w[2]), two(w[3]))));
 #pragma unroll
-                    for (int o = 1; o < 4; o <<= 1) {
-                        const uint32_t l = __shfl_xor_sync(kFull, low2, o), h = __shfl_xor_sync(kFull, high2, o);
-                        low2 = word(__hmin2_nan(two(low2), two(l)));
-                        high2 = word(__hmax2_nan(two(high2), two(h)));
-                    }
-                    const uint32_t low_turned = prmt(low2, 0, 0x1032), high_turned = prmt(high2, 0, 0x1032);
-                    const float low = widen16<F16>((uint16_t)word(__hmin2_nan(two(low2), two(low_turned))));
-                    const float high = widen16<F16>((uint16_t)word(__hmax2_nan(two(high2), two(high_turned))));
-                    // (high - low) / 15 as fp32 has it: the quotient by the reciprocal, and once more what that leaves over (Markstein's division)
-                    const float span = high - low, first = span * (1.0f / 15.0f), span15 = fmaf(fmaf(-15.0f, first, span), 1.0f / 15.0f, first);
-                    __half s = __float2half_rn(span15), m = __float2half_rn(low);
-                    const bool sound = __half2float(s) < INFINITY && fabsf(__half2float(m)) < INFINITY;
-                    if (!sound) s = __ushort_as_half(0x7FFFu), m = __ushort_as_half(0);
-                    const float fs = __half2float(s), fm = __half2float(m), by = sound && fs != 0.0f ? __fdividef(1.0f, 15.0f * fs) : 0.0f;
-                    // The code is (x - m) / s rounded.  In fp32 the quotient is off by less than 15 * 2^-22: 64 bits decide next to a border alone.  (Taken as
-                    // a part of 15, which cuts it off at both ends for nothing; 1.5 * 2^23 more is whole.)
-                    float code[8], edge = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float v = widen16<F16>((uint16_t)(w[j >> 1] >> (j & 1) * 16)), q = __saturatef((v - fm) * by);
-                        code[j] = fmaf(q, 15.0f, 12582912.0f) - 12582912.0f;
-                        edge = fmaxf(edge, fabsf(fmaf(q, 15.0f, -code[j])));
-                    }
-                    if (edge > 0.499995f && by != 0.0f) {
+                        for (int o = 1; o < 4; o <<= 1) {
+                            const uint32_t l = __shfl_xor_sync(kFull, low2, o), h = __shfl_xor_sync(kFull, high2, o);
+                            low2 = word(__hmin2_nan(two(low2), two(l)));
+                            high2 = word(__hmax2_nan(two(high2), two(h)));
+                        }
+                        const uint32_t low_turned = prmt(low2, 0, 0x1032), high_turned = prmt(high2, 0, 0x1032);
+                        const float low = widen16<F16>((uint16_t)word(__hmin2_nan(two(low2), two(low_turned))));
+                        const float high = widen16<F16>((uint16_t)word(__hmax2_nan(two(high2), two(high_turned))));
+                        // (high - low) / 15 as fp32 has it: the quotient by the reciprocal, and once more what that leaves over (Markstein's division)
+                        const float span = high - low, first = span * (1.0f / 15.0f), span15 = fmaf(fmaf(-15.0f, first, span), 1.0f / 15.0f, first);
+                        __half s = __float2half_rn(span15), m = __float2half_rn(low);
+                        const bool sound = __half2float(s) < INFINITY && fabsf(__half2float(m)) < INFINITY;
+                        if (!sound) s = __ushort_as_half(0x7FFFu), m = __ushort_as_half(0);
+                        const float fs = __half2float(s), fm = __half2float(m), by = sound && fs != 0.0f ? __fdividef(1.0f, 15.0f * fs) : 0.0f;
+                        // The code is (x - m) / s rounded.  In fp32 the quotient is off by less than 15 * 2^-22: 64 bits decide next to a border alone.  (Taken as
+                        // a part of 15, which cuts it off at both ends for nothing; 1.5 * 2^23 more is whole.)
+                        float code[8], edge = 0.0f;
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             const float v = widen16<F16>((uint16_t)(w[j >> 1] >> (j & 1) * 16)), q = __saturatef((v - fm) * by);
-                            if (fabsf(fmaf(q, 15.0f, -code[j])) > 0.499995f) code[j] = exact_code(v, fm, fs);
+                            code[j] = fmaf(q, 15.0f, 12582912.0f) - 12582912.0f;
+                            edge = fmaxf(edge, fabsf(fmaf(q, 15.0f, -code[j])));
+                        }
+                        if (edge > 0.499995f && by != 0.0f) {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const float v = widen16<F16>((uint16_t)(w[j >> 1] >> (j & 1) * 16)), q = __saturatef((v - fm) * by);
+                                if (fabsf(fmaf(q, 15.0f, -code[j])) > 0.499995f) code[j] = exact_code(v, fm, fs);
+                            }
+                        }
+                        // (whole numbers in fp32: 2^23 more has them in its low bits)
+                        auto join2 = [](float a, float b, float by) { return __float_as_uint(fmaf(b, by, a + 8388608.0f)); };
+                        const bool here = token - B.r < B.count;
+                        if (side == 0) {
+                            const uint32_t even = __float_as_uint(fmaf(fmaf(fmaf(code[6], 16.0f, code[4]), 16.0f, code[2]), 16.0f, code[0] + 8388608.0f));
+                            const uint32_t odd = __float_as_uint(fmaf(fmaf(fmaf(code[7], 16.0f, code[5]), 16.0f, code[3]), 16.0f, code[1] + 8388608.0f));
+                            if (here) *(uint32_t *)(block + key_word_at(DIM, token, group, t4)) = prmt(even, odd, 0x5410);
+                        } else {
+                            // eight channels of 16 come from this lane, the others from its neighbour; each gets half of their bytes
+                            const uint32_t front = prmt(join2(code[0], code[1], 256.0f), join2(code[2], code[3], 256.0f), 0x5410);
+                            const uint32_t back = prmt(join2(code[4], code[5], 256.0f), join2(code[6], code[7], 256.0f), 0x5410);
+                            const uint32_t other = __shfl_xor_sync(kFull, lane & 1 ? front : back, 1);
+                            if (here) s_codes[warp][token * (DIM / 8) + chunk] = lane & 1 ? other | back << 4 : front | other << 4;
+                        }
+                        if (here && t4 == 0) {
+                            *(__half *)(block + (side ? value_scale_at(DIM, token, group) : key_scale_at(DIM, token, group))) = s;
+                            *(__half *)(block + (side ? value_offset_at(DIM, token, group) : key_offset_at(DIM, token, group))) = m;
+                            // (keys' offsets are read in pairs, and what is read is multiplied by 0: it must be a number)
+                            if (G % 2 && side == 0 && group + 1 == G) *(__half *)(block + key_offset_at(DIM, token, group + 1)) = __ushort_as_half(0);
                         }
                     }
-                    // (whole numbers in fp32: 2^23 more has them in its low bits)
-                    auto join2 = [](float a, float b, float by) { return __float_as_uint(fmaf(b, by, a + 8388608.0f)); };
-                    const bool here = token - B.r < B.count;
-                    if (side == 0) {
-                        const uint32_t even = __float_as_uint(fmaf(fmaf(fmaf(code[6], 16.0f, code[4]), 16.0f, code[2]), 16.0f, code[0] + 8388608.0f));
-                        const uint32_t odd = __float_as_uint(fmaf(fmaf(fmaf(code[7], 16.0f, code[5]), 16.0f, code[3]), 16.0f, code[1] + 8388608.0f));
-                        if (here) *(uint32_t *)(block + key_word_at(DIM, token, group, t4)) = prmt(even, odd, 0x5410);
-                    } else {
-                        // eight channels of 16 come from this lane, the others from its neighbour; each gets half of their bytes
-                        const uint32_t front = prmt(join2(code[0], code[1], 256.0f), join2(code[2], code[3], 256.0f), 0x5410);
-                        const uint32_t back = prmt(join2(code[4], code[5], 256.0f), join2(code[6], code[7], 256.0f), 0x5410);
-                        const uint32_t other = __shfl_xor_sync(kFull, lane & 1 ? front : back, 1);
-                        if (here) s_codes[warp][token * (DIM / 8) + chunk] = lane & 1 ? other | back << 4 : front | other << 4;
-                    }
-                    if (here && t4 == 0) {
-                        *(__half *)(block + (side ? value_scale_at(DIM, token, group) : key_scale_at(DIM, token, group))) = s;
-                        *(__half *)(block + (side ? value_offset_at(DIM, token, group) : key_offset_at(DIM, token, group))) = m;
-                        // (keys' offsets are read in pairs, and what is read is multiplied by 0: it must be a number)
-                        if (G % 2 && side == 0 && group + 1 == G) *(__half *)(block + key_offset_at(DIM, token, group + 1)) = __ushort_as_half(0);
-                    }
-                }
                 }
                 if (side == 0) return;
                 __syncwarp();
