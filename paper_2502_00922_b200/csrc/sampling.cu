@@ -254,6 +254,8 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
     } else if (by_count || by_mass) {
         // ---- the bins
         const bool two_sums = by_count || A.part >= 65536;
+        // (distances below 2^16: as many of them as a CTA has logits have to add up within 32 bits)
+        const uint32_t below_shift = A.part <= 65536 ? 0 : 16 - __clz(A.part - 1), below_half = below_shift ? 1u << (below_shift - 1) : 0u;
         const float units = __uint_as_float((127u + min(22u, (uint32_t)__clz(A.part))) << 23);
         // Where top_k is small, most of the row need not be looked at closely: of the largest logits of the threads' parts, which are that many
         // tokens, the top_k-th largest is not above the cut.  (Halving a range ten times is near enough.  200 x 150001 in BF16, top_k 400: 134 -> 55 us.)
@@ -282,7 +284,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
                          : "memory");
             if (by_mass)
                 asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.f32 p, %0, %1;\n\t@p red.shared.add.u32 [%2], %3;\n\t}" ::"f"(at), "f"((float)kBins), "r"(below_at + bin),
-                             "r"(below_edge(at))
+                             "r"((below_edge(at) + below_half) >> below_shift)
                              : "memory");
         };
         // Mass alone, in one addition: a weight in `units` of its bin's upper edge, as many as the CTA's logits leave of 32 bits (18 bits, 2^-19 of a
@@ -331,7 +333,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
                 below += other.below[bin];
             }
             S0.all_count[bin] = count;
-            S0.all_mass[bin] = expf(-(float)bin * width) * (float)(two_sums ? (double)count - (double)below * 0x1p-22 : (double)below / units);
+            S0.all_mass[bin] = expf(-(float)bin * width) * (float)(two_sums ? (double)count - (double)(below << below_shift) * 0x1p-22 : (double)below / units);
         }
         cluster.sync();
 

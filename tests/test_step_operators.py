@@ -386,6 +386,13 @@ def test_attention_several_tokens(hl, torch, dim, group, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("extra", [1, 2, 3, 5, 7])
+def test_attention_strides_off_every_boundary(hl, torch, extra):
+    attention_case(hl, torch, 96, 6, 2, 16, "fp16", [40, 3, 700], [3, 1, 2], extra=extra)
+    attention_case(hl, torch, 128, 4, 4, 32, "bf16", [2000, 3], None, extra=extra)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("window,sinks", [(1, 0), (16, 4), (33, 0), (33, 40), (64, 16), (100, 1), (1000, 4), (2 ** 32 - 1, 2 ** 32 - 1)])
 @pytest.mark.parametrize("counts", [None, [1, 7, 50, 128]])
 def test_attention_window_and_first_tokens(hl, torch, window, sinks, counts):
@@ -628,6 +635,22 @@ def test_sample_crowded_logits(hl, torch, vocab, rows):
                 # weights of up to 150000 like tokens lie 7e-6 of the mass apart: a draw lands within a few tokens of the exact one
                 place, got = np.searchsorted(kept, want), np.searchsorted(kept, tokens[i])
                 assert 0 <= got < len(kept) + 1 and abs(int(got) - int(place)) <= 2 + 1e-5 * len(kept) * 2, (kind, t, i, tokens[i], want)
+
+
+@pytest.mark.gpu
+def test_sample_one_crowded_bin_of_a_large_part(hl, torch):
+    """All of a large vocabulary at the far end of one bin (1/64 in the exponent wide, as one token is masked)."""
+    rng = np.random.default_rng(16)
+    rows, vocab = 190, 150001
+    x = np.full((rows, vocab), 5.46875, np.float32)
+    x[:, 77], x[:, 5] = 5.5, -np.inf
+    settings = {"temperature": [1.01] * rows, "top_p": [0.61234] * rows}
+    u = rng.random(rows)
+    tokens, seen = run_sample(hl, torch, x, "bf16", settings, u)
+    for i in range(0, rows, 40):
+        want, near, kept = sample64(seen[i], np.float64(np.float32(1.01)), 0, float(np.float32(0.61234)), 0.0, float(np.float32(u[i])))
+        place, got = np.searchsorted(kept, want), np.searchsorted(kept, tokens[i])
+        assert abs(int(got) - int(place)) <= 2 + 1e-5 * len(kept) * 2, (i, tokens[i], want)
 
 
 @pytest.mark.gpu
