@@ -24,6 +24,7 @@ namespace huffllm {
 constexpr uint32_t kSampleThreads = 256, kSampleEach = 4,   // CTAs an SM has room for
                     kSampleWarps = kSampleThreads / 32;
 constexpr uint32_t kBins = 2048;
+constexpr uint32_t kBeyond = kBins + 1;                // (in the place of a bin's number) what lies beyond all of them
 constexpr uint32_t kMostList = 2 * kBins;              // a bin with fewer logits is searched in shared memory, in a list that lies where the bins were
 constexpr uint32_t kShortList = 256, kMostNear = 2048;
 constexpr uint32_t kMostCluster = 8;
@@ -189,6 +190,9 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
     const float t_given = A.temperature ? __ldcg(A.temperature + row) : 1.0f, p = A.top_p ? __ldcg(A.top_p + row) : 1.0f, u = __ldcg(A.uniform + row);
     const float min_given = A.min_p ? __ldcg(A.min_p + row) : 0.0f, least_weight = min_given > 1.0f ? 1.0f : min_given;
     const int32_t k_given = A.top_k ? __ldcg(A.top_k + row) : 0;
+    // A weight beyond the bins is below exp(-32) < 2^-46.  Those of a whole row are less than any draw but one next to 0 or to 1 leaves on either side.
+    const float beyond = (float)A.vocab * 0x1p-46f;
+    const bool at_ends = !(u > beyond && u < 1.0f - beyond);
     const bool first_only = !(t_given > 1e-30f) || p <= 0.0f || k_given == 1;
     const float temperature = t_given > 1e-30f ? t_given : 1.0f;
 
@@ -383,14 +387,15 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
             __syncthreads();
         };
         float *const list = (float *)S.count;
+        auto lies_in = [&](float x, uint32_t bin) {
+            const float at = place(x);
+            return bin == kBeyond ? at >= (float)kBins : at < (float)kBins && bin_of(at) == bin;
+        };
         // All of a bin's logits into the first CTA's list.
         auto gather = [&](uint32_t bin, uint32_t which) {
             float *const list0 = (float *)S0.count;
-            auto in_bin = [&](float x) {
-                const float at = place(x);
-                return at < (float)kBins && bin_of(at) == bin;
-            };
-            if (by_near) {
+            auto in_bin = [&](float x) { return lies_in(x, bin); };
+            if (by_near) {                             // (beyond the bins: of no CTA, as its near logits alone are top_k)
                 for (uint32_t i = tid; i < nears; i += kSampleThreads) {
                     if (!in_bin(S.near[i])) continue;
                     const uint32_t to = atomicAdd(&S0.listed[which], 1u);
@@ -405,7 +410,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
                 float nearest = INFINITY;
 #pragma unroll
                 for (int e = 0; e < R.N; ++e) nearest = fminf(nearest, fabsf(x.x[e] - middle));
-                if (nearest > reach) return;
+                if (nearest > reach && bin != kBeyond) return;
                 uint32_t hits = 0;
 #pragma unroll
                 for (int e = 0; e < R.N; ++e) hits |= in_bin(x.x[e]) ? 1u << e : 0u;
@@ -523,8 +528,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
                 const Piece16<TYPE> x(piece);
 #pragma unroll
                 for (int e = 0; e < R.N; ++e) {
-                    const float at = place(x.x[e]);
-                    if (!(at < (float)kBins) || bin_of(at) != bin) continue;
+                    if (!lies_in(x.x[e], bin)) continue;
                     const uint32_t key = key_of(x.x[e]);
                     if (what == kCountEqual ? key == edge : key > edge) v += what == kMassAbove ? mass20(x.x[e]) : 1u;
                 }
@@ -581,6 +585,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
 
         double mass = 0.0;                             // of what top_k leaves
         uint32_t limit = kBins, lowest = 0;
+        bool unfilled = false;
         if (rank == 0)
             for (uint32_t w = 0; w < kSampleWarps; ++w) mass += S.scan_mass[w];
         if (by_count) {
@@ -590,12 +595,21 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
                 find(true, (uint32_t)k_given, 0.0, kBins);
                 bin = S.found_bin, before = S.found_count, mass_before = S.found_mass;
                 __syncthreads();
+                // Fewer than top_k in the bins.  Which of the others stay shows in a draw at one of the ends alone (and not where top_p cuts, which is within
+                // the bins): else the cut is the bins' far end, found without a look at the row.
+                if (bin == kBins && at_ends && !by_mass) {
+                    bin = kBeyond, before = 0;
+                    for (uint32_t w = 0; w < kSampleWarps; ++w) before += S.scan_count[w];
+                }
+                unfilled = bin == kBins;
             }
             const Edge e = search(bin, true, (double)((uint32_t)k_given - before), 0);
             const double row_mass = e.by_row && by_mass ? row_total(S.named[0].bin, e.key, kMassAbove) : 0.0;
-            if (rank == 0 && bin < kBins) {
+            if (rank == 0 && bin != kBins) {
                 cut = value_of(e.key);
                 ties = (uint32_t)k_given - before - (uint32_t)e.above;
+            }
+            if (rank == 0 && bin < kBins) {
                 limit = bin + 1;
                 lowest = e.key;
                 if (by_mass) {
@@ -628,6 +642,15 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
                 cut = edge;
                 ties = (uint32_t)fmin(fmax(need, 1.0), (double)have);
             }
+        }
+        if (unfilled && cut == -INFINITY) {
+            uint32_t low = key_of(-INFINITY), high = key_of(top);          // the largest value whose place is beyond the bins
+            while (high - low > 1) {
+                const uint32_t mid = low + (high - low) / 2;
+                if (place(value_of(mid)) < (float)kBins) high = mid;
+                else low = mid;
+            }
+            cut = value_of(low);
         }
         __syncthreads();
         if (rank == 0 && tid < ctas) {

@@ -1,0 +1,74 @@
+"""The choice of the next token at its borders: cuts far below the largest logit, logits next to a cut by min_p, masses of very many tokens,
+temperatures at the ends of fp32.  Against 64 bits; helpers are those of the operators' other tests."""
+import numpy as np
+import pytest
+
+from test_step_operators import hl, run_sample, torch  # noqa: F401
+
+
+def kept64(x, t, k):
+    """The tokens that top_k leaves, in the order of indexes, and their weights in 64 bits."""
+    order = np.argsort(-x, kind="stable")[:k]
+    kept = np.sort(order)
+    return kept, np.exp((x[kept] - x.max()) / t)
+
+
+@pytest.mark.gpu
+def test_top_k_of_three_logits_at_a_low_temperature(hl, torch):  # noqa: F811
+    """Places 48 and 70 in the exponent below the largest: the first token is not among the two that stay."""
+    x = np.array([[3.0, 10.0, 5.0]] * 4)
+    settings = {"temperature": [0.1] * 4, "top_k": [2, 2, 1, 3]}
+    assert run_sample(hl, torch, x, "f32", settings, [0.0, 1e-30, 0.0, 0.0])[0].tolist() == [1, 1, 1, 0]
+    x = np.array([[-1.0, 0.0, 0.0, 50.0]] * 3)                             # equals at the cut: the first of them stays
+    assert run_sample(hl, torch, x, "f32", {"top_k": [2] * 3}, [0.0, 0.5, 1.0])[0].tolist() == [1, 3, 3]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "fp16"])
+@pytest.mark.parametrize("vocab", [7, 300, 5003, 40009, 140001])
+def test_top_k_far_below_the_largest_logit(hl, torch, vocab, dtype):  # noqa: F811
+    """The last logits that stay lie 32 to 80 in the exponent below the largest; those that do not lie in front of and behind them.  A draw of 0
+    or of next to it takes the first token that stays, one of 1 or more the last.  Weights are above 2^-126, and off by 2e-6 of themselves: a
+    draw is held to its token unless the masses up to some token come as near as 1e-5 of the draw."""
+    rng = np.random.default_rng(vocab)
+    u = np.array([0.0, 1e-30, 1e-20, 1e-13, 1e-10, 1e-9, 1e-5, 0.5, 1.0 - 2.0 ** -24, 1.0, 2.0, 0.0] * 2, np.float32)
+    rows = len(u)
+    t = rng.choice([0.1, 0.05, 0.3], rows).astype(np.float32)
+    k = np.minimum(rng.choice([2, 5, 40, 100, 500], rows), vocab - 1)
+    x = np.empty((rows, vocab))
+    for i in range(rows):
+        x[i] = 10.0 - t[i] * rng.uniform(33, 80, vocab)
+        near = rng.choice(vocab, max(1, int(k[i]) // 3), replace=False)
+        x[i, near] = 10.0 - t[i] * rng.uniform(0, 31, len(near)) * (np.arange(len(near)) > 0)
+        if i % 3 == 0:                                                     # many equals at the cut
+            x[i] = np.round(x[i] * 4) / 4
+    tokens, seen = run_sample(hl, torch, x, dtype, {"temperature": t.tolist(), "top_k": k.tolist()}, u)
+    held = 0
+    for i in range(rows):
+        kept, w = kept64(seen[i], float(t[i]), int(k[i]))
+        assert tokens[i] in kept, (i, u[i], tokens[i])
+        run = np.cumsum(w)
+        aim = float(u[i]) * run[-1]
+        if u[i] >= 1:
+            want = kept[-1]
+        else:
+            at = int(np.searchsorted(run, aim, "right"))
+            if u[i] > 0 and np.min(np.abs(run - aim)) < 1e-5 * aim:
+                continue
+            want = kept[at]
+        assert tokens[i] == want, (i, u[i], tokens[i], want)
+        held += 1
+    assert held >= rows - 6
+
+
+@pytest.mark.gpu
+def test_top_k_that_the_row_cannot_fill(hl, torch):  # noqa: F811
+    """top_k of as many as are above minus infinity, of more, and next to the vocabulary: all of them stay, however small."""
+    x = np.full((6, 3000), -np.inf)
+    x[:, 100:140] = np.linspace(-60, -40, 40)
+    x[:, 2000] = 0.0
+    k = [41, 42, 500, 2999, 40, 30]
+    for u, want in ((0.0, [100] * 4 + [101, 111]), (1.0, [2000] * 6)):
+        assert run_sample(hl, torch, x, "f32", {"top_k": k}, [u] * 6)[0].tolist() == want
+    x[:, 2500:2510] = np.linspace(-70, -61, 10)                            # behind the largest
+    assert run_sample(hl, torch, x, "f32", {"top_k": [51, 60, 50, 2999, 41, 49]}, [1.0] * 6)[0].tolist() == [2509, 2509, 2509, 2509, 2000, 2509]
