@@ -18,6 +18,7 @@
 // warps that end at different times.  40 sequences of up to 8192 tokens, 64 heads over 8: 59 us, 4.35 TB/s; one of 4096, 32 over 8: 12.4 us.
 // Tiles of sixteen rows (pieces of prompts) are bound by the issue of what surrounds the matrix instructions (500 instructions a step, of which 72 are those).
 #include <cuda_runtime.h>
+#include <cfloat>
 
 #include "cache_rows.cuh"
 #include "decode_common.cuh"
@@ -366,7 +367,7 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
             }
             // a row's largest value goes to 2^14 .. 2^15 (by a power of two: exact), so that fp16 holds whatever bf16 does
             auto wide_lo = [&](uint32_t w) { return C.fp16 ? widen16<true>((uint16_t)w) : widen16<false>((uint16_t)w); };
-            float most = 0.0f, nan = 0.0f;
+            float most = 0.0f, nan = 0.0f * A.scale;
 #pragma unroll
             for (int i = 0; i < G; ++i)
 #pragma unroll
@@ -379,7 +380,7 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
             most = fmaxf(most, __shfl_xor_sync(kFull, most, 2));
             nan += __shfl_xor_sync(kFull, nan, 1);
             nan += __shfl_xor_sync(kFull, nan, 2);
-            const int shift = max(-90, min(100, 14 - ((int)(__float_as_uint(most) >> 23) - 127)));
+            const int shift = max(14 - 127, min(100, 14 - ((int)(__float_as_uint(most) >> 23) - 127)));
             const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
             float sums[G];
 #pragma unroll
@@ -403,7 +404,8 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
                 if (t4 * 2 == i) s0 = sums[i], s1 = i + 1 < G ? sums[i + 1] : 0.0f;
             q_sum[n][0] = pack_half2(s0, s1);
             q_sum[n][1] = pack_half2(s0 - low_half(q_sum[n][0]), s1 - high_half(q_sum[n][0]));
-            const float f = A.scale * 1.4426950408889634f * __uint_as_float((uint32_t)(127 - shift) << 23) * 16777216.0f + nan;
+            // (beyond fp32, which takes queries of 2^120 or so, the largest number does as well: scores that differ at all are then 2^50 apart, or more)
+            const float f = fminf(fmaxf(A.scale * 1.4426950408889634f * __uint_as_float((uint32_t)(127 - shift) << 23) * 16777216.0f, -FLT_MAX), FLT_MAX) + nan;
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 factor[n][c] = __shfl_sync(kFull, f, (t4 * 2 + c) * 4);
