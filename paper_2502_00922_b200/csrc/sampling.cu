@@ -106,7 +106,7 @@ struct alignas(16) SampleShared {
     double table_mass[kMostCluster * kSampleWarps];
     uint32_t table_equal[kMostCluster * kSampleWarps];
     uint32_t found_bin, found_count, listed[2], nears;
-    double found_mass;
+    double found_mass, min_reach;
     struct {
         uint32_t bin, lowest;
         double want;
@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
     R.kept = min(R.pieces, A.kept_pieces);
 
     const float t_given = A.temperature ? __ldcg(A.temperature + row) : 1.0f, p = A.top_p ? __ldcg(A.top_p + row) : 1.0f, u = __ldcg(A.uniform + row);
-    const float min_given = A.min_p ? __ldcg(A.min_p + row) : 0.0f, least_weight = min_given > 1.0f ? 1.0f : min_given;
+    const float min_p = A.min_p ? __ldcg(A.min_p + row) : 0.0f;
     const int32_t k_given = A.top_k ? __ldcg(A.top_k + row) : 0;
     // A weight beyond the bins is below exp(-32) < 2^-46.  Those of a whole row are less than any draw but one next to 0 or to 1 leaves on either side.
     const float beyond = (float)A.vocab * 0x1p-46f;
@@ -220,6 +220,8 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
     if (warp == 0) {
         top = warp_max(lane < kSampleWarps ? S.warp_top[lane] : -INFINITY);
         least = warp_min(lane < kSampleWarps ? S.warp_least[lane] : INFINITY);
+        // min_p as a distance between logits, in 64 bits (a weight in 32 is 1 for what lies next to the largest)
+        if (lane == 0 && min_p > 0.0f) S.min_reach = min_p < 1.0f ? (double)temperature * log((double)min_p) : 0.0;
         if (lane == 0) S.cta_top = top, S.cta_least = least, S.listed[0] = S.listed[1] = S.nears = 0;
     }
     cluster.sync();
@@ -662,6 +664,11 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
         ties = S.ties;
     }
 
+    if (min_p > 0.0f) {
+        const float least = __double2float_ru((double)top + S.min_reach);
+        if (least > cut) cut = nextafterf(least, -INFINITY), ties = 0;
+    }
+
     // ---- the draw, in the order of indexes: warps have stretches of the row, lanes pieces of 16 bytes that follow each other
     // a warp's mass above the cut of a stretch, and how many equal it, into the warp's place
     auto sum_stretch = [&](uint32_t from, uint32_t to) {
@@ -673,7 +680,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
 #pragma unroll
             for (int e = 0; e < R.N; ++e) {
                 const float w = weight(x.x[e]);        // (a select costs less than a branch)
-                sum += x.x[e] > cut && !(w < least_weight) ? w : 0.0f;
+                sum += x.x[e] > cut ? w : 0.0f;
                 equal += x.x[e] == cut;
             }
         });
@@ -689,8 +696,8 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
         uint32_t equal = 0;
         for (uint32_t i = lane; i < S.nears; i += 32) {
             if (S.near_piece[i] / stretch != warp) continue;
-            const float x = S.near[i], w = x > cut ? weight(x) : 0.0f;
-            if (!(w < least_weight)) sum += (uint64_t)((double)w * 0x1p40);
+            const float x = S.near[i];
+            if (x > cut) sum += (uint64_t)((double)weight(x) * 0x1p40);
             equal += x == cut;
         }
         for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
@@ -706,7 +713,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
         S.table_equal[i] = other.warp_equal[i % kSampleWarps];
     }
     cluster.sync();                                    // (the last look at another CTA's shared memory)
-    const float cut_weight_given = cut == -INFINITY ? 0.0f : cut == top ? 1.0f : weight(cut), cut_weight = cut_weight_given < least_weight ? 0.0f : cut_weight_given;
+    const float cut_weight = cut == -INFINITY ? 0.0f : cut == top ? 1.0f : weight(cut);
     // the first warp: the stretch in which the mass exceeds what is drawn; a lane has some that follow each other
     constexpr uint32_t STRETCHES = kMostCluster * kSampleWarps / 32;    // of a lane
     if (warp == 0) {
@@ -809,7 +816,6 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
             w[e] = 0.0f;
             if (x.x[e] > cut) w[e] = weight(x.x[e]);
             if (x.x[e] == cut && seen++ < ties) w[e] = cut_weight;
-            if (w[e] < least_weight) w[e] = 0.0f;
             m += w[e];
         }
         double m_to = m;

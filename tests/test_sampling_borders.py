@@ -72,3 +72,31 @@ def test_top_k_that_the_row_cannot_fill(hl, torch):  # noqa: F811
         assert run_sample(hl, torch, x, "f32", {"top_k": k}, [u] * 6)[0].tolist() == want
     x[:, 2500:2510] = np.linspace(-70, -61, 10)                            # behind the largest
     assert run_sample(hl, torch, x, "f32", {"top_k": [51, 60, 50, 2999, 41, 49]}, [1.0] * 6)[0].tolist() == [2509, 2509, 2509, 2509, 2000, 2509]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("vocab", [5, 3001, 60001])
+def test_min_p_next_to_a_logit(hl, torch, vocab):  # noqa: F811
+    """min_p of 1 leaves the largest and its equals, however near the others come; below 1, logits one step of fp32 to either side of the cut."""
+    rng = np.random.default_rng(vocab)
+    x = np.float32(1.0) - rng.integers(1, 4, (8, vocab)) * np.float32(2.0 ** -24)
+    x[:, vocab // 3] = x[:, vocab // 2] = 1.0
+    for t in (1.0, 50.0, 1e4):
+        for least in (1.0, 2.0):
+            got = run_sample(hl, torch, x, "f32", {"temperature": [t] * 8, "min_p": [least] * 8}, [0.0, 0.2, 0.4, 0.49, 0.51, 0.7, 0.99, 1.0])[0]
+            assert got.tolist() == [vocab // 3] * 4 + [vocab // 2] * 4, (t, least)
+    cases = []
+    for least in (0.9, 0.5, 0.1, 0.013):
+        for t in (0.7, 1.0, 3.0):
+            least32, t32 = float(np.float32(least)), float(np.float32(t))
+            cut = np.float32(t32 * np.log(least32))                        # largest logit 0: what is at or above it stays
+            if float(cut) < t32 * np.log(least32):
+                cut = np.nextafter(cut, np.float32(np.inf))
+            cases.append((t32, least32, cut, np.nextafter(cut, np.float32(-np.inf))))
+    x = np.full((len(cases), vocab), -np.inf, np.float32)
+    for i, (_, _, stays, goes) in enumerate(cases):
+        x[i, vocab // 2], x[i, 1], x[i, 0] = 0.0, stays, goes
+        x[i, vocab - 1] = goes
+    settings = {"temperature": [c[0] for c in cases], "min_p": [c[1] for c in cases]}
+    assert run_sample(hl, torch, x, "f32", settings, [0.0] * len(cases))[0].tolist() == [1] * len(cases)
+    assert run_sample(hl, torch, x, "f32", settings, [1.0] * len(cases))[0].tolist() == [vocab // 2] * len(cases)
