@@ -97,15 +97,20 @@ struct alignas(16) SampleShared {
     uint32_t below[kBins];
     uint32_t all_count[kBins];                         // the first CTA: all CTAs' bins
     float all_mass[kBins];
-    float near[kMostNear];                             // a CTA's logits that may be above the cut, where top_k is small,
-    uint32_t near_piece[kMostNear];                    // and the pieces that have them
+    union {
+        struct {
+            float near[kMostNear];                     // a CTA's logits that may be above the cut, where top_k is small,
+            uint32_t near_piece[kMostNear];            // and the pieces that have them
+        };
+        uint64_t below_wide[kBins];                    // or `below` of a CTA with so many logits that 32 bits would not hold it
+    };
     double warp_mass[kSampleWarps], scan_mass[kSampleWarps];
     uint32_t warp_equal[kSampleWarps], scan_count[kSampleWarps], sums[2][kSampleWarps];
     float warp_top[kSampleWarps], warp_least[kSampleWarps];
     float cta_top, cta_least;
     double table_mass[kMostCluster * kSampleWarps];
     uint32_t table_equal[kMostCluster * kSampleWarps];
-    uint32_t found_bin, found_count, listed[2], nears;
+    uint32_t found_bin, found_count, listed[2], nears, wide;
     double found_mass, min_reach;
     struct {
         uint32_t bin, lowest;
@@ -138,16 +143,22 @@ struct RowPart {
         return r;
     }
     __device__ __forceinline__ uint4 raw(uint32_t i) const { return i < kept ? data[i] : from_memory(i); }
-    // f(piece, its number) for the pieces first, first + step .. below end; four are on their way together (they may come from L2).
-    template <typename F>
-    __device__ __forceinline__ void each(uint32_t first, uint32_t end, uint32_t step, F f) const {
+    // f(piece, its number) for the pieces first, first + step .. below end; four are on their way together (they may come from L2), and behind
+    // every four g().
+    template <typename F, typename G>
+    __device__ __forceinline__ void each(uint32_t first, uint32_t end, uint32_t step, F f, G g) const {
         for (uint32_t i0 = first; i0 < end; i0 += 4 * step) {
             uint4 v[4];
 #pragma unroll
             for (uint32_t j = 0; j < 4; ++j) v[j] = i0 + j * step < end ? raw(i0 + j * step) : make_uint4(kFull, kFull, kFull, kFull);
 #pragma unroll
             for (uint32_t j = 0; j < 4; ++j) f(v[j], i0 + j * step);
+            g();
         }
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(uint32_t first, uint32_t end, uint32_t step, F f) const {
+        each(first, end, step, f, [] {});
     }
 };
 
@@ -222,7 +233,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
         least = warp_min(lane < kSampleWarps ? S.warp_least[lane] : INFINITY);
         // min_p as a distance between logits, in 64 bits (a weight in 32 is 1 for what lies next to the largest)
         if (lane == 0 && min_p > 0.0f) S.min_reach = min_p < 1.0f ? (double)temperature * log((double)min_p) : 0.0;
-        if (lane == 0) S.cta_top = top, S.cta_least = least, S.listed[0] = S.listed[1] = S.nears = 0;
+        if (lane == 0) S.cta_top = top, S.cta_least = least, S.listed[0] = S.listed[1] = S.nears = S.wide = 0;
     }
     cluster.sync();
     {
@@ -259,9 +270,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
         ties = 1;
     } else if (by_count || by_mass) {
         // ---- the bins
-        const bool two_sums = by_count || A.part >= 65536;
-        // (distances below 2^16: as many of them as a CTA has logits have to add up within 32 bits)
-        const uint32_t below_shift = A.part <= 65536 ? 0 : 16 - __clz(A.part - 1), below_half = below_shift ? 1u << (below_shift - 1) : 0u;
+        const bool two_sums = by_count || A.part >= 16384, may_be_wide = by_mass && A.part > 65536;
         const float units = __uint_as_float((127u + min(22u, (uint32_t)__clz(A.part))) << 23);
         // Where top_k is small, most of the row need not be looked at closely: of the largest logits of the threads' parts, which are that many
         // tokens, the top_k-th largest is not above the cut.  (Halving a range ten times is near enough.  200 x 150001 in BF16, top_k 400: 134 -> 55 us.)
@@ -290,11 +299,11 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
                          : "memory");
             if (by_mass)
                 asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.f32 p, %0, %1;\n\t@p red.shared.add.u32 [%2], %3;\n\t}" ::"f"(at), "f"((float)kBins), "r"(below_at + bin),
-                             "r"((below_edge(at) + below_half) >> below_shift)
+                             "r"(below_edge(at))
                              : "memory");
         };
-        // Mass alone, in one addition: a weight in `units` of its bin's upper edge, as many as the CTA's logits leave of 32 bits (18 bits, 2^-19 of a
-        // weight, where a CTA has up to 16384 logits, and 16 at the least).  units exp(-r) is a polynomial in how far the place is in its bin.
+        // Mass alone, in one addition: a weight in `units` of its bin's upper edge, as many as the CTA's logits leave of 32 bits (2^18 or more where a CTA
+        // has less than 16384 logits: a weight is off by 2^-19 of itself at most).  units exp(-r) is a polynomial in how far the place is in its bin.
         const float c1 = -units * width, c2 = 0.5f * units * width * width, c3 = -units * width * width * width / 6.0f;
         auto weigh_one = [&](float x) {
             const float at = place(x), whole = __fadd_rd(at, 8388608.0f), f = at - (whole - 8388608.0f);
@@ -318,14 +327,24 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
         if (by_near) {
             for (uint32_t i = tid; i < nears; i += kSampleThreads) count_one(S.near[i]);
         } else {
-            R.each(tid, R.pieces, kSampleThreads, [&](uint4 v, uint32_t) {
-                const Piece16<TYPE> x(v);
+            // (distances are below 2^16: 2^16 logits add up within 32 bits; behind so many, the sums go to 64)
+            const bool wide = may_be_wide && R.count > 65536;
+            const uint32_t chunk = wide ? 65536 / R.N : R.pieces;
+            for (uint32_t from = 0; from < R.pieces; from += chunk) {
+                R.each(from + tid, min(R.pieces, from + chunk), kSampleThreads, [&](uint4 v, uint32_t) {
+                    const Piece16<TYPE> x(v);
 #pragma unroll
-                for (int e = 0; e < R.N; ++e) {
-                    if (two_sums) count_one(x.x[e]);
-                    else weigh_one(x.x[e]);
-                }
-            });
+                    for (int e = 0; e < R.N; ++e) {
+                        if (two_sums) count_one(x.x[e]);
+                        else weigh_one(x.x[e]);
+                    }
+                });
+                if (!wide) break;
+                __syncthreads();
+                for (uint32_t i = tid; i < kBins; i += kSampleThreads) S.below_wide[i] = (from ? S.below_wide[i] : 0) + S.below[i], S.below[i] = 0;
+                __syncthreads();
+            }
+            if (wide && tid == 0) S.wide = 1;
         }
         cluster.sync();
         const uint32_t share = kBins / ctas;
@@ -336,10 +355,10 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
             for (uint32_t r = 0; r < ctas; ++r) {
                 const SampleShared &other = *cluster.map_shared_rank(&S, r);
                 count += other.count[bin];
-                below += other.below[bin];
+                below += may_be_wide && other.wide ? other.below_wide[bin] : other.below[bin];
             }
             S0.all_count[bin] = count;
-            S0.all_mass[bin] = expf(-(float)bin * width) * (float)(two_sums ? (double)count - (double)(below << below_shift) * 0x1p-22 : (double)below / units);
+            S0.all_mass[bin] = expf(-(float)bin * width) * (float)(two_sums ? (double)count - (double)below * 0x1p-22 : (double)below / units);
         }
         cluster.sync();
 
@@ -672,7 +691,8 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
     // ---- the draw, in the order of indexes: warps have stretches of the row, lanes pieces of 16 bytes that follow each other
     // a warp's mass above the cut of a stretch, and how many equal it, into the warp's place
     auto sum_stretch = [&](uint32_t from, uint32_t to) {
-        float sum = 0.0f;
+        float sum = 0.0f;                              // of four pieces; a lane may have so many that 32 bits do not do
+        double m = 0.0;
         uint32_t equal = 0;
         R.each(from + lane, to, 32, [&](uint4 v, uint32_t) {
             if (!(piece_max<TYPE>(v) >= cut)) return;
@@ -683,8 +703,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
                 sum += x.x[e] > cut ? w : 0.0f;
                 equal += x.x[e] == cut;
             }
-        });
-        double m = sum;
+        }, [&] { m += sum, sum = 0.0f; });
         for (int o = 16; o; o >>= 1) m += __shfl_xor_sync(kFull, m, o);
         equal = __reduce_add_sync(kFull, equal);
         if (lane == 0) S.warp_mass[warp] = m, S.warp_equal[warp] = equal;

@@ -100,3 +100,45 @@ def test_min_p_next_to_a_logit(hl, torch, vocab):  # noqa: F811
     settings = {"temperature": [c[0] for c in cases], "min_p": [c[1] for c in cases]}
     assert run_sample(hl, torch, x, "f32", settings, [0.0] * len(cases))[0].tolist() == [1] * len(cases)
     assert run_sample(hl, torch, x, "f32", settings, [1.0] * len(cases))[0].tolist() == [vocab // 2] * len(cases)
+
+
+def last_that_stays(n_top, below, n_below, p):
+    """n_top tokens of weight 1 and n_below of exp(-below), which lie behind them: how many of those stay, in 64 bits and before rounding up."""
+    w = np.exp(-np.float64(below))
+    return (p * (n_top + n_below * w) - n_top) / w
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,vocab", [(70, 480000), (300, 60000), (3, 8000000), (1, 1 << 25)])
+def test_cuts_by_mass_among_very_many_tokens(hl, torch, rows, vocab):  # noqa: F811
+    """Nearly all tokens alike, at the place of a bin of 1/64 in the exponent where weights held in few bits round worst: the number that top_p
+    leaves shows what their masses came to.  Weights and their sums are good to 1e-6."""
+    n_top = vocab // 10
+    scan = np.arange(1, 1024, dtype=np.float32) / np.float32(65536.0)
+    held = 65536.0 * np.exp(-scan.astype(np.float64))
+    below = scan[np.argmin(np.abs(held - np.floor(held) - 0.4999))] + np.float32(7 / 64)
+    x = torch.full((rows, vocab), float(-below), device="cuda")
+    x[:, :n_top] = 0.0
+    x[:, vocab - 1] = -float("inf")                                        # (bins of 1/64)
+    p = float(np.float32(0.61234))
+    tokens = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    hl.sample(hl.Sampling(x, hl.ELEM_F32, rows, vocab, torch.ones(rows, device="cuda"), tokens, top_p=torch.full((rows,), p, device="cuda")))
+    want = n_top + last_that_stays(n_top, float(below), vocab - 1 - n_top, p) - 1
+    got = tokens.cpu().numpy()
+    assert np.all(np.abs(got - want) <= 1 + 1e-6 * vocab), (got[0], want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("by", [0.3, 0.7, 1.1])
+def test_draws_among_very_many_tokens(hl, torch, by):  # noqa: F811
+    """Half of a row has weight 1, the other half exp(-by): where a draw falls shows what either half came to.  Good to 2e-6 of the row."""
+    vocab = 1 << 25
+    x = torch.zeros((1, vocab), device="cuda")
+    x[:, vocab // 2:] = -by
+    w = np.exp(-float(np.float32(by)))
+    for u in (0.25, 0.5, 0.9):
+        tokens = torch.zeros(1, dtype=torch.int32, device="cuda")
+        hl.sample(hl.Sampling(x, hl.ELEM_F32, 1, vocab, torch.tensor([u], device="cuda"), tokens))
+        aim = float(np.float32(u)) * (1 + w) * (vocab // 2)
+        want = aim if aim < vocab // 2 else vocab // 2 + (aim - vocab // 2) / w
+        assert abs(int(tokens) - want) <= 2 + 2e-6 * vocab, (u, int(tokens), want)
