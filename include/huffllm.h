@@ -610,7 +610,7 @@ huffllm_status huffllm_cache_attention(const huffllm_cache *cache, const huffllm
  *     top_p   of these the shortest row with at least top_p of their mass  (at least the first; 1 or more: all)
  *     min_p   of these the ones with w_i >= min_p                          (0 or less: all; 1 or more: the largest)
  * The token is the first one (in the order of indexes) of those that stay up to which their mass is more than uniform * all of it.
- * temperature 0 or less: the first of the largest.  A NaN logit is as good as minus infinity; where there is plus infinity, only such
+ * temperature 0 or less (or NaN): the first of the largest; one below 1e-30 or above 1e30 counts as that.  A NaN logit is as good as minus infinity; where there is plus infinity, only such
  * tokens have a mass, the same each.  A row with nothing above minus infinity gives -1.
  * The four settings are device arrays of a value per row, or null (temperature 1, the others off); uniform is in [0, 1) (outside: the first or
  * the last that stays).  Masses are added up in 32 bits or more, the same way in every call.  No workspace.

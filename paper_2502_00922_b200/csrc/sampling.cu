@@ -204,8 +204,8 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleEach) sample_kernel(con
     // A weight beyond the bins is below exp(-32) < 2^-46.  Those of a whole row are less than any draw but one next to 0 or to 1 leaves on either side.
     const float beyond = (float)A.vocab * 0x1p-46f;
     const bool at_ends = !(u > beyond && u < 1.0f - beyond);
-    const bool first_only = !(t_given > 1e-30f) || p <= 0.0f || k_given == 1;
-    const float temperature = t_given > 1e-30f ? t_given : 1.0f;
+    const bool first_only = !(t_given > 0.0f) || p <= 0.0f || k_given == 1;
+    const float temperature = first_only ? 1.0f : fminf(fmaxf(t_given, 1e-30f), 1e30f);       // (beyond, its products leave fp32)
 
     // ---- the row into shared memory; its largest and smallest logit
     float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, least = INFINITY;   // of four parts of the thread's logits

@@ -142,3 +142,14 @@ def test_draws_among_very_many_tokens(hl, torch, by):  # noqa: F811
         aim = float(np.float32(u)) * (1 + w) * (vocab // 2)
         want = aim if aim < vocab // 2 else vocab // 2 + (aim - vocab // 2) / w
         assert abs(int(tokens) - want) <= 2 + 2e-6 * vocab, (u, int(tokens), want)
+
+
+@pytest.mark.gpu
+def test_temperatures_at_the_ends_of_fp32(hl, torch):  # noqa: F811
+    """Next to 0 equals at the top share the mass still, and nothing else has any; without bound every token above minus infinity has the same."""
+    x = np.array([[1.0, 5.0, 5.0, -2.0, 5.0, -np.inf]] * 3)
+    for t in (1e-25, 1e-33, 1e-40):
+        assert run_sample(hl, torch, x, "f32", {"temperature": [t] * 3}, [0.1, 0.5, 0.9])[0].tolist() == [1, 2, 4], t
+    for t in (1e25, 3e38, float("inf")):
+        for extra in ({}, {"top_k": [6] * 3}, {"min_p": [0.5] * 3}, {"top_p": [0.9999] * 3}):
+            assert run_sample(hl, torch, x, "f32", {"temperature": [t] * 3, **extra}, [0.1, 0.5, 0.99])[0].tolist() == [0, 2, 4], (t, extra)
