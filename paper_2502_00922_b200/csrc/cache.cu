@@ -137,8 +137,8 @@ __global__ void __launch_bounds__(kCacheWarps * 32, DIM <= 128 ? 4 : 3) cache_ap
                         const bool sound = __half2float(s) < INFINITY && fabsf(__half2float(m)) < INFINITY;
                         if (!sound) s = __ushort_as_half(0x7FFFu), m = __ushort_as_half(0);
                         const float fs = __half2float(s), fm = __half2float(m), by = sound && fs != 0.0f ? __fdividef(1.0f, 15.0f * fs) : 0.0f;
-                        // The code is (x - m) / s rounded.  In fp32 the quotient is off by less than 15 * 2^-22: 64 bits decide next to a border alone.  (Taken as
-                        // a part of 15, which cuts it off at both ends for nothing; 1.5 * 2^23 more is whole.)
+                        // The code is (x - m) / s rounded.  In fp32 the quotient is off by less than 15 * 1.5 * 2^-22 = 5.4e-6 (difference and product 2^-24, division two
+                        // last places): 64 bits decide within 1e-5 of a border alone.  (Taken as a part of 15, which cuts it off at both ends for nothing; 1.5 * 2^23 more is whole.)
                         float code[8], edge = 0.0f;
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
@@ -146,11 +146,11 @@ __global__ void __launch_bounds__(kCacheWarps * 32, DIM <= 128 ? 4 : 3) cache_ap
                             code[j] = fmaf(q, 15.0f, 12582912.0f) - 12582912.0f;
                             edge = fmaxf(edge, fabsf(fmaf(q, 15.0f, -code[j])));
                         }
-                        if (edge > 0.499995f && by != 0.0f) {
+                        if (edge > 0.49999f && by != 0.0f) {
 #pragma unroll
                             for (int j = 0; j < 8; ++j) {
                                 const float v = widen16<F16>((uint16_t)(w[j >> 1] >> (j & 1) * 16)), q = __saturatef((v - fm) * by);
-                                if (fabsf(fmaf(q, 15.0f, -code[j])) > 0.499995f) code[j] = exact_code(v, fm, fs);
+                                if (fabsf(fmaf(q, 15.0f, -code[j])) > 0.49999f) code[j] = exact_code(v, fm, fs);
                             }
                         }
                         // (whole numbers in fp32: 2^23 more has them in its low bits)
