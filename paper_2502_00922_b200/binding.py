@@ -90,6 +90,8 @@ class Rotary(C.Structure):
     def __init__(self, dtype: int, tokens: int, head_dim: int, positions, frequencies, q, q_heads: int, q_out, k=None, k_heads: int = 0, k_out=None,
                  rotary_dim: int = 0, sections=None, in_turn: bool = False, pairing: int = PAIR_HALVES, q_stride: int = 0, k_stride: int = 0,
                  q_out_stride: int = 0, k_out_stride: int = 0):
+        _array("int32", positions)
+        _array("float32", frequencies)
         rotary_dim = rotary_dim or head_dim
         sections = list(sections) if sections is not None else [rotary_dim // 2]
         if not 1 <= len(sections) <= MAX_AXES:
@@ -107,9 +109,12 @@ class Cache(C.Structure):
 
     def __init__(self, dtype: int, kv_heads: int, head_dim: int, page_tokens: int, pages: int, pool=None, table=None, lengths=None,
                  sequences: int = 0, table_stride: int = 0):
-        """table: [sequences][table_stride] int32 tensor, lengths: [sequences]; the two numbers are taken from a table that has a shape."""
-        if table is not None and not isinstance(table, int):
-            sequences, table_stride = sequences or table.shape[0], table_stride or table.shape[1]
+        """table: [sequences][entries] int32 tensor (it may be part of a larger one), lengths: [sequences] int32; the two numbers are the table's
+        shape and stride where they are not given."""
+        _array("int32", lengths)
+        if table is not None and not isinstance(table, int) and not (sequences and table_stride):
+            rows, step = _table(table)
+            sequences, table_stride = sequences or rows, table_stride or step
         super().__init__(dtype, kv_heads, head_dim, page_tokens, pages, _ptr(pool), sequences, table_stride, _ptr(table), _ptr(lengths))
         self._keep = _one_device(pool, table, lengths)
 
@@ -121,6 +126,7 @@ class Attention(C.Structure):
 
     def __init__(self, q, heads: int, out, rows: int, scale: float, starts=None, window: int = 0, sinks: int = 0, q_stride: int = 0,
                  out_stride: int = 0):
+        _array("int32", starts)
         super().__init__(heads, scale, window, sinks, rows, q_stride, out_stride, _ptr(q), _ptr(out), _ptr(starts))
         self._keep = _one_device(q, out, starts)
 
@@ -133,6 +139,8 @@ class Sampling(C.Structure):
 
     def __init__(self, logits, logits_type: int, rows: int, vocab: int, uniform, tokens, dtype: int = BF16, temperature=None, top_k=None,
                  top_p=None, min_p=None, stride: int = 0):
+        _array("int32", top_k, tokens)
+        _array("float32", temperature, top_p, min_p, uniform)
         super().__init__(logits_type, dtype, rows, vocab, stride, _ptr(logits), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
                          _ptr(uniform), _ptr(tokens))
         self._keep = _one_device(logits, temperature, top_k, top_p, min_p, uniform, tokens)
@@ -254,6 +262,25 @@ def _one_device(*tensors):
     if len(devices) > 1:
         raise ValueError("tensors of one call on different devices: " + ", ".join(sorted(map(str, devices))))
     return tensors
+
+
+def _array(kind, *tensors):
+    """Refuses a tensor that a call would take for something else: the device arrays of a call are int32 or float32, one value behind the other."""
+    for t in tensors:
+        if t is None or isinstance(t, int):
+            continue
+        packed = t.flags.c_contiguous if isinstance(t, np.ndarray) else t.is_contiguous()
+        if not str(t.dtype).endswith(kind) or not packed:
+            raise ValueError(f"a packed {kind} array is wanted, not {t.dtype}{'' if packed else ' with strides'}")
+
+
+def _table(t):
+    """Sequences of a page table, and values from one to the next: it may be part of a larger tensor."""
+    rows, columns = t.shape
+    step, each = [n // 4 for n in t.strides] if isinstance(t, np.ndarray) else t.stride()
+    if not str(t.dtype).endswith("int32") or (each != 1 and columns > 1) or step < 0:
+        raise ValueError("a page table is int32, the entries of a sequence one behind the other")
+    return rows, step
 
 
 def _stream(stream):
@@ -705,6 +732,7 @@ class PreparedAppend(_Prepared):
     """A huffllm_cache_append call, marshalled once."""
 
     def __init__(self, cache: Cache, k_dev, v_dev, rows: int, starts=None, k_stride: int = 0, v_stride: int = 0, err_flag_dev=None):
+        _array("int32", starts, err_flag_dev)
         self._keep = cache, _one_device(cache._keep[0], k_dev, v_dev, starts, err_flag_dev)
         ptr = lambda t: C.c_void_p(_ptr(t))
         self._fn = _unconverted("huffllm_cache_append")
@@ -721,6 +749,7 @@ class PreparedRead(_Prepared):
     """A huffllm_cache_read call, marshalled once."""
 
     def __init__(self, cache: Cache, k_dev, v_dev, elem_type: int, rows: int, starts=None, k_stride: int = 0, v_stride: int = 0, err_flag_dev=None):
+        _array("int32", starts, err_flag_dev)
         self._keep = cache, _one_device(cache._keep[0], k_dev, v_dev, starts, err_flag_dev)
         ptr = lambda t: C.c_void_p(_ptr(t))
         self._fn = _unconverted("huffllm_cache_read")
@@ -751,6 +780,7 @@ class PreparedAttention(_Prepared):
     """A huffllm_cache_attention call, marshalled once."""
 
     def __init__(self, cache: Cache, attention: Attention, workspace_dev, workspace_bytes_: int, err_flag_dev=None):
+        _array("int32", err_flag_dev)
         self._keep = cache, attention, _one_device(cache._keep[0], attention._keep[0], workspace_dev, err_flag_dev)
         ptr = lambda t: C.c_void_p(_ptr(t))
         self._fn = _unconverted("huffllm_cache_attention")

@@ -1,0 +1,61 @@
+"""Calls of the cache as programs make them: page tables that are part of a larger tensor, arrays of other types."""
+import numpy as np
+import pytest
+
+from test_step_operators import FAKE, Pages, a_cache, attention64, check, hl, run_attention, to_bits, to_f64, torch, up, values  # noqa: F401
+
+
+def test_tables_that_are_part_of_a_larger_tensor(hl, torch):  # noqa: F811
+    """The stride is the tensor's; what the call cannot read as it lies, or would read as something else, is refused."""
+    whole = torch.zeros((6, 20), dtype=torch.int32)
+    lengths = torch.zeros(6, dtype=torch.int32)
+    make = lambda table, n=lengths: hl.Cache(hl.BF16, 2, 64, 32, 9, FAKE, table, n)
+    for table, sequences, stride in ((whole, 6, 20), (whole[:, :5], 6, 20), (whole[1:4, 3:9], 3, 20), (whole[::2], 3, 40), (whole[:1], 1, 20)):
+        c = make(table, lengths[:sequences])
+        assert (c.sequences, c.table_stride, c.table) == (sequences, stride, table.data_ptr())
+    assert make(np.zeros((3, 8), np.int32)[:, :4], None).table_stride == 8
+    for table in (whole.T, whole[:, ::2], whole.long(), whole.float(), np.zeros((3, 8), np.int64)):
+        with pytest.raises(ValueError):
+            make(table, None)
+    for n in (lengths.long(), torch.zeros(12, dtype=torch.int32)[::2]):
+        with pytest.raises(ValueError):
+            make(whole, n)
+
+
+def test_arrays_of_other_types_or_with_strides(hl, torch):  # noqa: F811
+    i32, f32 = torch.zeros(8, dtype=torch.int32), torch.zeros(8)
+    rotary = lambda positions, frequencies: hl.Rotary(hl.BF16, 8, 16, positions, frequencies, FAKE, 1, FAKE)
+    attention = lambda starts: hl.Attention(FAKE, 4, FAKE, 7, 0.1, starts=starts)
+    sampling = lambda **kw: hl.Sampling(**{**dict(logits=FAKE, logits_type=hl.ELEM_F32, rows=8, vocab=9, uniform=f32, tokens=i32), **kw})
+    append = lambda starts, err=None: hl.PreparedAppend(a_cache(hl), FAKE, FAKE, 7, starts=starts, err_flag_dev=err)
+    read = lambda starts, err=None: hl.PreparedRead(a_cache(hl), FAKE, FAKE, hl.ELEM_16, 7, starts=starts, err_flag_dev=err)
+    rotary(i32[None], f32), attention(i32), sampling(top_k=i32, top_p=f32), append(i32, i32[:1]), read(i32)
+    whole = torch.zeros((3, 16), dtype=torch.int32)
+    for call in (lambda: rotary(i32.long(), f32), lambda: rotary(whole[:, :8], f32), lambda: rotary(i32, f32.double()), lambda: rotary(i32, f32.half()),
+                 lambda: rotary(i32, torch.zeros(16)[::2]), lambda: attention(i32.long()), lambda: attention(np.zeros(8, np.int64)), lambda: append(i32.long()),
+                 lambda: append(i32, i32.long()), lambda: read(whole[:, 0]), lambda: sampling(top_k=i32.long()), lambda: sampling(top_k=f32), lambda: sampling(top_p=f32.double()),
+                 lambda: sampling(temperature=f32.half()), lambda: sampling(min_p=torch.zeros(16)[::2]), lambda: sampling(uniform=f32.double()), lambda: sampling(tokens=i32.long())):
+        with pytest.raises(ValueError):
+            call()
+
+
+@pytest.mark.gpu
+def test_a_table_that_is_part_of_a_larger_tensor(hl, torch):  # noqa: F811
+    rng = np.random.default_rng(61)
+    lengths, kv, dim, heads = [40, 3, 70], 2, 64, 4
+    p = Pages(hl, torch, "bf16", kv, dim, 16, lengths, rng)
+    whole = torch.full((3, 40), 2 ** 30, dtype=torch.int32, device="cuda")
+    whole[:, 4:4 + p.table.shape[1]] = p.table
+    p.table = whole[:, 4:4 + p.table.shape[1]]
+    p.cache = p._cache(p.pool)
+    k, v = (to_bits(rng.standard_normal((113, kv, dim)), "bf16") for _ in range(2))
+    hl.cache_append(p.cache, up(torch, k, "bf16"), up(torch, v, "bf16"), 113, starts=p.starts(lengths), err_flag_dev=p.err)
+    q = to_bits(rng.standard_normal((3, heads * dim)), "bf16")
+    got = values(run_attention(p, up(torch, q, "bf16"), heads, 3, 0.125, None, 0, 0)).reshape(3, 1, heads, dim)
+    assert p.error() == 0
+    at = 0
+    for b, n in enumerate(lengths):
+        kb, vb = (to_f64(t[at: at + n].reshape(-1), "bf16").reshape(n, kv, dim) for t in (k, v))
+        want, tol = attention64(to_f64(q[b], "bf16").reshape(1, heads, dim), kb, vb, n - 1, 0.125, 0, 0)
+        check(got[b], want, tol, "bf16")
+        at += n
