@@ -20,6 +20,14 @@ bool stride_of(uint64_t given, uint64_t packed, uint64_t *out) {
     return *out >= packed && *out <= (1ull << 40);
 }
 
+// Do rows of `values` 16-bit values each overlap?  Known where the strides are alike, and of the first rows; with other strides rows may lie between rows.
+bool rows_overlap(const uint16_t *a, const uint16_t *b, uint64_t values, uint64_t a_stride, uint64_t b_stride, uint64_t rows) {
+    const uint64_t apart = (uint64_t)((uintptr_t)a < (uintptr_t)b ? (uintptr_t)b - (uintptr_t)a : (uintptr_t)a - (uintptr_t)b), width = 2 * values;
+    if (rows == 1 || a_stride != b_stride) return apart < width;
+    const uint64_t step = 2 * a_stride, k = apart / step, left = apart % step;       // the later one's first row lies behind the other's row k, or in front of its row k + 1
+    return (k < rows && left < width) || (k + 1 < rows && step - left < width);
+}
+
 huffllm_status check_cache(const huffllm_cache *c, bool pool) {
     if (!c) return fail(HUFFLLM_ERR_INVALID_ARG, "null pointer");
     if (c->dtype > HUFFLLM_FP16) return fail(HUFFLLM_ERR_INVALID_ARG, "unknown type");
@@ -200,7 +208,6 @@ huffllm_status huffllm_cache_attention(const huffllm_cache *cache, const huffllm
     if (st != HUFFLLM_OK) return st;
     const huffllm_attention &a = *args;
     if (!a.q || !a.out || !workspace) return fail(HUFFLLM_ERR_INVALID_ARG, "null pointer");
-    if (a.q == a.out) return fail(HUFFLLM_ERR_INVALID_ARG, "out must not overlap q");
     if (!aligned(a.q, 2) || !aligned(a.out, 2) || !aligned(workspace, 256) || !aligned(err_flag, 4))
         return fail(HUFFLLM_ERR_INVALID_ARG, "q and out must be 2-byte, workspace 256-byte, err_flag 4-byte aligned");
     size_t need = 0;
@@ -211,6 +218,7 @@ huffllm_status huffllm_cache_attention(const huffllm_cache *cache, const huffllm
     k.c = cache_args(*cache);
     if (!stride_of(a.q_stride, (uint64_t)a.heads * cache->head_dim, &k.q_stride) || !stride_of(a.out_stride, (uint64_t)a.heads * cache->head_dim, &k.out_stride))
         return fail(HUFFLLM_ERR_INVALID_ARG, "stride below the values of a row (or above 2^40)");
+    if (rows_overlap(a.q, a.out, (uint64_t)a.heads * cache->head_dim, k.q_stride, k.out_stride, a.rows)) return fail(HUFFLLM_ERR_INVALID_ARG, "out must not overlap q");
     k.q = a.q;
     k.out = a.out;
     k.starts = a.starts;

@@ -1,8 +1,9 @@
-"""Calls of the cache as programs make them: page tables that are part of a larger tensor, arrays of other types."""
+"""Calls of the cache as programs make them: page tables that are part of a larger tensor, arrays of other types,
+outputs over queries."""
 import numpy as np
 import pytest
 
-from test_step_operators import FAKE, Pages, a_cache, attention64, check, hl, run_attention, to_bits, to_f64, torch, up, values  # noqa: F401
+from test_step_operators import FAKE, Pages, a_cache, attention64, check, hl, refused, run_attention, to_bits, to_f64, torch, up, values  # noqa: F401
 
 
 def test_tables_that_are_part_of_a_larger_tensor(hl, torch):  # noqa: F811
@@ -59,3 +60,29 @@ def test_a_table_that_is_part_of_a_larger_tensor(hl, torch):  # noqa: F811
         want, tol = attention64(to_f64(q[b], "bf16").reshape(1, heads, dim), kb, vb, n - 1, 0.125, 0, 0)
         check(got[b], want, tol, "bf16")
         at += n
+
+
+def test_outputs_over_queries_are_refused(hl):  # noqa: F811
+    """Where the strides are alike every overlap shows: rows of 512 values (1024 bytes), 7 of them."""
+    run = lambda **kw: hl.cache_attention(a_cache(hl), hl.Attention(**{**dict(heads=8, rows=7, scale=0.1, starts=FAKE), **kw}), FAKE, 1 << 40, stream=0)
+    q = 1 << 24
+    for out, stride in ((q + 2, 0), (q - 2, 0), (q + 1022, 0), (q + 7 * 1024 - 2, 0), (q - 7 * 1024 + 2, 0), (q + 1022, 2048), (q - 1022, 2048), (q + 4096 + 2, 2048),
+                        (q + 4096 - 1022, 2048), (q, 2048), (q + 6 * 4096 + 1022, 2048)):
+        refused(hl, "INVALID_ARG", lambda: run(q=q, out=out, q_stride=stride, out_stride=stride))
+
+
+@pytest.mark.gpu
+def test_outputs_between_queries(hl, torch):  # noqa: F811
+    """Rows of a tensor that have queries and outputs side by side."""
+    rng = np.random.default_rng(62)
+    lengths, kv, dim, heads = [40, 3, 70], 2, 64, 4
+    p = Pages(hl, torch, "bf16", kv, dim, 16, lengths, rng)
+    k, v = (to_bits(rng.standard_normal((113, kv, dim)), "bf16") for _ in range(2))
+    hl.cache_append(p.cache, up(torch, k, "bf16"), up(torch, v, "bf16"), 113, starts=p.starts(lengths), err_flag_dev=p.err)
+    q = to_bits(rng.standard_normal((3, 2 * heads * dim)), "bf16")
+    both = up(torch, q, "bf16")
+    apart = values(run_attention(p, up(torch, q, "bf16"), heads, 3, 0.125, None, 0, 0, q_stride=512)).reshape(3, -1)
+    for first in (0, 256):
+        both.copy_(up(torch, q if first == 0 else np.roll(q, 256, 1), "bf16"))
+        run_attention(p, both[:, first:], heads, 3, 0.125, None, 0, 0, 512, 512, out=both[:, 256 - first:])
+        assert p.error() == 0 and np.array_equal(values(both)[:, 256 - first: 512 - first], apart)
