@@ -547,8 +547,9 @@ huffllm_status huffllm_apply_rotary(const huffllm_rotary *args, huffllm_stream s
  * lengths[sequence] counts all of its tokens, those of the call included.  Table and lengths are read on the device, so a captured call
  * follows them as they grow.  Several sequences may share pages that are only read.
  * The calls set *err_flag (device, may be null) to sequence + 1 where a length is negative or beyond the table's row (or 2^31 - 64), a page that
- * is needed is not one of the pool's, or starts do not ascend within the rows of the call (-1: a copy never arrived within the wait limit); what lies on such a page is neither written nor seen, nothing is read or
- * written out of place, and other sequences are served.
+ * is needed is not one of the pool's, or starts do not ascend within the rows of the call (-1: a copy never arrived within the wait limit).  What lies
+ * on such a page is neither written nor seen, nothing is read or written out of place, and other sequences are served; but where starts do not ascend,
+ * append and read, which look a row's sequence up among them, may pass over any sequence's rows.
  * A pool needs no initialisation.  huffllm_cache_bytes: its size for the given pages, heads and channels (pool, table and lengths may
  * be null there).
  */

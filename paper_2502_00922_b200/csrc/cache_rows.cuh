@@ -27,7 +27,8 @@ __device__ __forceinline__ Sequence sequence_of(const CacheArgs &c, const int32_
     s.bad = !rows_ok || !length_ok;
     return s;
 }
-// One CTA's look at every sequence: a row finds its own by starts that ascend, and cannot tell where they do not.
+// One CTA's look at every sequence: a row finds its own by starts that ascend, and cannot tell where they do not.  (Rows are passed over then; a
+// look at all starts by every CTA would cost as many reads as there are sequences and CTAs.)
 __device__ __forceinline__ void report_faults(const CacheArgs &c, const int32_t *starts, uint32_t rows, int32_t *err) {
     if (!err) return;
     for (uint32_t b = threadIdx.x; b < c.sequences; b += blockDim.x)

@@ -1,9 +1,9 @@
 """Calls of the cache as programs make them: page tables that are part of a larger tensor, arrays of other types,
-outputs over queries."""
+outputs over queries, starts that do not ascend."""
 import numpy as np
 import pytest
 
-from test_step_operators import FAKE, Pages, a_cache, attention64, check, hl, refused, run_attention, to_bits, to_f64, torch, up, values  # noqa: F401
+from test_step_operators import FAKE, Pages, a_cache, attention64, check, hl, ints, refused, run_attention, stands_for, to_bits, to_f64, torch, up, values  # noqa: F401
 
 
 def test_tables_that_are_part_of_a_larger_tensor(hl, torch):  # noqa: F811
@@ -86,3 +86,44 @@ def test_outputs_between_queries(hl, torch):  # noqa: F811
         both.copy_(up(torch, q if first == 0 else np.roll(q, 256, 1), "bf16"))
         run_attention(p, both[:, first:], heads, 3, 0.125, None, 0, 0, 512, 512, out=both[:, 256 - first:])
         assert p.error() == 0 and np.array_equal(values(both)[:, 256 - first: 512 - first], apart)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bad", [[0, 40, 30, 50], [0, 40, 20, 10], [50, 40, 30, 50], [0, 110, 90, 110], [100, 0, 90, 110], [-5, 40, 90, 110], [0, 40, 90, 111]])
+def test_starts_that_do_not_ascend(hl, torch, bad):  # noqa: F811
+    """A sequence whose starts are no rows is named.  Every token is what it was, or what its own row says; what is read goes to rows of its own."""
+    rng = np.random.default_rng(63)
+    lengths, kv, dim = [40, 50, 20], 2, 64
+    p = Pages(hl, torch, "bf16", kv, dim, 16, lengths, rng)
+    old, new = ([to_bits(rng.standard_normal((110, kv, dim)), "bf16") for _ in range(2)] for _ in range(2))
+    stands = lambda bits: stands_for(to_f64(bits.reshape(-1), "bf16").reshape(110, kv, dim))
+
+    def cache_read(starts):
+        out = [torch.full((110, kv * dim), 7.0, device="cuda") for _ in range(2)]
+        p.err.zero_()
+        hl.cache_read(p.cache, out[0], out[1], hl.ELEM_F32, 110, starts=ints(torch, starts), err_flag_dev=p.err)
+        return [values(t).reshape(110, kv, dim) for t in out], p.error()
+    good = [0, 40, 90, 110]
+    at_fault = [b + 1 for b in range(3) if not 0 <= bad[b] <= bad[b + 1] <= 110]
+    hl.cache_append(p.cache, up(torch, old[0], "bf16"), up(torch, old[1], "bf16"), 110, starts=ints(torch, good), err_flag_dev=p.err)
+    assert p.error() == 0
+    got, err = cache_read(bad)
+    assert err in at_fault
+    for side in range(2):
+        want = stands(old[side])
+        for r in range(110):                               # the tokens that row r may be
+            may = [want[good[b] + lengths[b] - bad[b + 1] + r] for b in range(3)
+                   if b + 1 not in at_fault and bad[b] <= r < bad[b + 1] and lengths[b] - bad[b + 1] + r >= 0]
+            assert np.all(got[side][r] == 7.0) or any(np.array_equal(got[side][r], m) for m in may), r
+    p.err.zero_()
+    hl.cache_append(p.cache, up(torch, new[0], "bf16"), up(torch, new[1], "bf16"), 110, starts=ints(torch, bad), err_flag_dev=p.err)
+    assert p.error() in at_fault
+    got, err = cache_read(good)
+    assert err == 0
+    for side in range(2):
+        was, now = stands(old[side]), stands(new[side])
+        for b in range(3):
+            for i in range(lengths[b]):
+                row = bad[b + 1] - lengths[b] + i
+                may = [was[good[b] + i]] + ([now[row]] if b + 1 not in at_fault and bad[b] <= row < bad[b + 1] else [])
+                assert any(np.array_equal(got[side][good[b] + i], m) for m in may), (b, i)
