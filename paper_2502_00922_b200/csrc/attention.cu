@@ -803,7 +803,10 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
 template <int DIM, int NT, bool FINE>
 static cudaError_t launch_shape(const AttentionArgs &a, uint32_t sms, cudaStream_t stream) {
     using Shape = AttentionShape<DIM, NT>;
-    static_assert(Shape::kSmem + 1536 <= 232448, "shared memory of a CTA");
+    // (the kernel's arrays: barriers and blocks by stage, starts, pieces, units to join, up to the 128 bytes that the ring is aligned to)
+    constexpr uint32_t kArrays = Shape::kWarps * (Shape::kStages * (2 * sizeof(uint64_t) + 2 * sizeof(uint32_t)) + sizeof(uint64_t) + sizeof(uint32_t) +
+                                                  sizeof(Sequence) + 2 * sizeof(Piece)) + 2 * sizeof(uint2);
+    static_assert(Shape::kSmem + (kArrays + 127) / 128 * 128 <= 232448, "shared memory of a CTA");
     static_assert(Shape::kPiece <= kAttentionPartial, "a piece's place in the workspace");
     static std::atomic<bool> attr_set[64];   // set twice by racing threads at worst: the call is idempotent
     int dev = 0;
