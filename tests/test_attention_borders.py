@@ -102,3 +102,12 @@ def test_the_bound_of_fp16_results_tells_one_number_from_two():
             got = ((ws[..., None] * c).reshape(n, dim).sum(0) + (w[:, None] * m).repeat(32, 1).sum(0)) / w.sum()
             outside.append(np.max(np.abs(got - want) / (tol + rounding(np.abs(want) + tol, "fp16"))) > 1.5)
         assert sum(outside) >= 2, (dim, n, outside)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim,heads,kv,dtype,lengths,counts,window,sinks", [
+    (64, 4, 2, "bf16", [600, 257], [600, 257], 0, 0), (128, 8, 2, "fp16", [700], [650], 0, 0), (96, 9, 1, "bf16", [300, 5, 400], [300, 5, 129], 100, 4),
+    (128, 5, 1, "bf16", [40, 513], [40, 513], 33, 0), (256, 2, 2, "fp16", [350], [350], 0, 0), (192, 3, 1, "bf16", [0, 270], [7, 270], 64, 20)])
+def test_whole_prompts(hl, torch, dim, heads, kv, dtype, lengths, counts, window, sinks):  # noqa: F811
+    """Hundreds of new tokens in a call, their own keys among those that they see."""
+    attention_case(hl, torch, dim, heads, kv, 64, dtype, lengths, counts, window=window, sinks=sinks)
