@@ -584,8 +584,10 @@ huffllm_status huffllm_cache_read(const huffllm_cache *cache, void *k_dev, void 
  *     out = sum_j p_j v_j,   p = softmax(scale * q k_j) over the tokens j that the row's token i sees:
  *     j <= i, and, where window is not 0, j > i - window or j < sinks (the first tokens stay visible)
  * Query heads h * heads / kv_heads .. share key head h.  q and out: [rows][heads][head_dim] words of the cache's dtype; out must not overlap q.
- * A row that sees nothing is 0.  Tokens that are not seen have no influence, whatever the cache holds for them.  Sums and softmax are fp32;
- * probabilities and queries are multiplied in 11 bits or more; codes, scales and offsets exactly.  Results are the same from run to run.
+ * A row that sees nothing is 0.  Tokens that are not seen have no influence, whatever the cache holds for them.  Sums and softmax are fp32; codes,
+ * scales, offsets and queries are multiplied exactly (queries below 2^-24 of their row's largest in fewer bits).  A token's weight, and that times a
+ * scale of its values, are rounded to 11 bits each where results are BF16, to 22 where they are FP16; both end at 2^-33 of the row's largest weight
+ * times the largest scale that it sees (2^-35, where that scale is below 1/4).  Results are the same from run to run.
  * The workspace (256-byte aligned, huffllm_attention_workspace_bytes or more) is zero-filled once after allocation; its first
  * huffllm_attention_control_bytes bytes are counters that every call leaves zero; the rest is overwritten freely.  One workspace serves every
  * call that it is large enough for, one call at a time.
@@ -611,10 +613,12 @@ huffllm_status huffllm_cache_attention(const huffllm_cache *cache, const huffllm
  *     top_p   of these the shortest row with at least top_p of their mass  (at least the first; 1 or more: all)
  *     min_p   of these the ones with w_i >= min_p                          (0 or less: all; 1 or more: the largest)
  * The token is the first one (in the order of indexes) of those that stay up to which their mass is more than uniform * all of it.
- * temperature 0 or less (or NaN): the first of the largest; one below 1e-30 or above 1e30 counts as that.  A NaN logit is as good as minus infinity; where there is plus infinity, only such
- * tokens have a mass, the same each.  A row with nothing above minus infinity gives -1.
+ * temperature 0 or less (or NaN): the first of the largest; one below 1e-30 or above 1e30 counts as that.  A NaN logit is as good as minus infinity;
+ * where there is plus infinity, only such tokens have a mass, the same each.  A row with nothing above minus infinity gives -1.
  * The four settings are device arrays of a value per row, or null (temperature 1, the others off); uniform is in [0, 1) (outside: the first or
- * the last that stays).  Masses are added up in 32 bits or more, the same way in every call.  No workspace.
+ * the last that stays).  top_k and min_p are exact.  Weights are good to 2^-19 of themselves, and 2^-22 for every unit that their exponent is below 0; below
+ * 2^-126 they are 0.  They are added up in 32 bits or more, the same way in every call: a draw, or a cut by mass, that is nearer to a border may fall to
+ * either side of it.  No workspace.
  */
 typedef struct huffllm_sampling {
     uint32_t logits_type, dtype;           /* huffllm_elem; dtype: of 16-bit logits                */

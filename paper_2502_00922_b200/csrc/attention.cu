@@ -15,7 +15,7 @@
 //
 // Long lines are bound by memory: 65536 steps of 32 tokens x 128 channels more (335 MB) take 55 us more, 6.1 TB/s, 0.93 of the measured copy rate.  Some
 // 17 us are a launch's own: 5 to 6 before the first sums (lengths, page, block and queries come one behind the other), 5 to 8 for joining, the rest
-// warps that end at different times.  40 sequences of up to 8192 tokens, 64 heads over 8: 59 us, 4.35 TB/s; one of 4096, 32 over 8: 12.4 us.
+// warps that end at different times.  40 sequences of up to 8192 tokens, 64 heads over 8: 60 us, 4.3 TB/s; one of 4096, 32 over 8: 12.4 us.
 // Tiles of sixteen rows (pieces of prompts) are bound by the issue of what surrounds the matrix instructions (500 instructions a step, of which 72 are those).
 #include <cuda_runtime.h>
 #include <cfloat>
@@ -33,7 +33,8 @@ constexpr uint32_t kWaitTries = 1u << 17, kPollTries = 1u << 25;
 constexpr int kSlack = 4;                        // a weight's exponent is set this far below its cap, so that few later ones are above it
 
 // As many warps as registers and shared memory hold: 128 registers a thread where a lane's sums are 32 (sixteen warps), 255 where they are 64 (eight; with
-// 186 registers and eleven warps the sums spill: pieces of 48 tokens over 2000 in an 8B-shaped layer 64 us instead of 54).
+// 186 registers and eleven warps the sums spill: pieces of 48 tokens over 2000 in an 8B-shaped layer 64 us instead of 54).  Measured at 128 channels; 64
+// channels with sixteen rows spill 230 bytes at 128 registers.
 template <int DIM, int NT>
 struct AttentionShape {
     static constexpr int kGroups = DIM / 32, kCols = 8 * NT;
@@ -193,7 +194,9 @@ __device__ __forceinline__ void mma_f16_16816_new(float (&d)[4], uint32_t a0, ui
 __device__ __forceinline__ void sts32(uint32_t at, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
 
 // FINE: for results in FP16, which show what rounding p_t and p_t s_t,g to 11 bits costs (twice the error of the results' own rounding): both keep
-// what they leave, as a second number of 11 bits, exactly, and the products with values are taken twice.  (A seventh more instructions.)
+// what they leave, as a second number of 11 bits, exactly, and the products with values are taken twice.  (A seventh more instructions.)  Results in BF16
+// have one of 11 bits: with both, 40 sequences of up to 8192 tokens take 66 us instead of 60, pieces of prompts 63 instead of 54, and the error against
+// 64 bits, 1.7e-3 of the values, is that of rounding the results either way.
 template <int DIM, int NT, bool FINE>
 __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) attention_kernel(const __grid_constant__ AttentionArgs A) {
     using Shape = AttentionShape<DIM, NT>;

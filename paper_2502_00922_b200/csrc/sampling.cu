@@ -5,10 +5,11 @@
 // in shared memory as far as that goes and else in L2.  2048 bins of equal width in the logit (at most 1/64 in the weight's exponent) count the
 // tokens above every edge, and the weights' mass, in whole numbers and so in any order.  The bin in which top_k or top_p end goes to a
 // list of the first CTA, which finds the cut by halving the range of its values.  Where top_k is small, the largest logits of parts of the row bound the
-// cut from below, and only what is above that bound, a list too, is looked at again.
+// cut from below, and only what is above that bound, a list too, is looked at again.  min_p is a logit, and raises the cut.
 //
-// Few rows are bound by the way from phase to phase (ten barriers of the cluster): 32000 logits 16.7 us.  Many are bound by instructions, 20 a
-// logit where top_k bounds the cut, else 80: 200 rows of 150001 in BF16 53 us, 64 of 128000 in fp32, top_p alone, 48 us (read once: 9 and 5 us).
+// Few rows are bound by the way from phase to phase (ten barriers of the cluster): 32000 logits 17.8 us.  Many are bound by instructions, 20 a
+// logit where top_k bounds the cut, else 80: 200 rows of 150001 in BF16 54 us, 64 of 128000 in fp32, top_p alone, 48 us (read once: 9 and 5 us).
+// Weights are fp32: of 25600 rows of 128000 tokens five fell to the other side of a border than 64 bits (two with weights in 64, 65 us for 64 of them).
 // Four CTAs an SM of 256 threads, as the phases of one wait for each other: 64 x 128000 with two of 512 threads and the row in shared memory 67 us.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
