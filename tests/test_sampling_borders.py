@@ -109,10 +109,11 @@ def last_that_stays(n_top, below, n_below, p):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("counted", [False, True])
 @pytest.mark.parametrize("rows,vocab", [(70, 480000), (300, 60000), (3, 8000000), (1, 1 << 25)])
-def test_cuts_by_mass_among_very_many_tokens(hl, torch, rows, vocab):  # noqa: F811
+def test_cuts_by_mass_among_very_many_tokens(hl, torch, rows, vocab, counted):  # noqa: F811
     """Nearly all tokens alike, at the place of a bin of 1/64 in the exponent where weights held in few bits round worst: the number that top_p
-    leaves shows what their masses came to.  Weights and their sums are good to 1e-6."""
+    leaves shows what their masses came to.  Weights and their sums are good to 1e-6.  With top_k in front, which leaves out some thousandth of them, too."""
     n_top = vocab // 10
     scan = np.arange(1, 1024, dtype=np.float32) / np.float32(65536.0)
     held = 65536.0 * np.exp(-scan.astype(np.float64))
@@ -122,8 +123,10 @@ def test_cuts_by_mass_among_very_many_tokens(hl, torch, rows, vocab):  # noqa: F
     x[:, vocab - 1] = -float("inf")                                        # (bins of 1/64)
     p = float(np.float32(0.61234))
     tokens = torch.zeros(rows, dtype=torch.int32, device="cuda")
-    hl.sample(hl.Sampling(x, hl.ELEM_F32, rows, vocab, torch.ones(rows, device="cuda"), tokens, top_p=torch.full((rows,), p, device="cuda")))
-    want = n_top + last_that_stays(n_top, float(below), vocab - 1 - n_top, p) - 1
+    top_k = vocab - vocab // 1000
+    hl.sample(hl.Sampling(x, hl.ELEM_F32, rows, vocab, torch.ones(rows, device="cuda"), tokens, top_p=torch.full((rows,), p, device="cuda"),
+                          top_k=torch.full((rows,), top_k, dtype=torch.int32, device="cuda") if counted else None))
+    want = n_top + last_that_stays(n_top, float(below), (top_k if counted else vocab - 1) - n_top, p) - 1
     got = tokens.cpu().numpy()
     assert np.all(np.abs(got - want) <= 1 + 1e-6 * vocab), (got[0], want)
 
