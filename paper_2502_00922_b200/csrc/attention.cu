@@ -210,6 +210,7 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
     __shared__ Sequence s_start_s[W];
     __shared__ uint32_t s_here[W * STAGES][2];                   // blocks of a stage that are there
     __shared__ Piece s_piece[W][2];
+    __shared__ uint32_t s_late[W];                               // a wait of the warp that gave up: 1 + 2 * stage + phase
     __shared__ uint2 s_join[2];                                  // units that this CTA is the last to arrive at: first CTA and number of pieces
     float *const first_pieces = (float *)(smem + Shape::kRingBytes);
     auto piece_at = [&](uint32_t w, uint32_t which) { return which ? (float *)(smem + w * STAGES * 2 * BLOCK) : first_pieces + w * Shape::kPiece; };
@@ -217,7 +218,7 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
     const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32, g = lane / 4, t4 = lane % 4;
 
     if (warp < W && lane < STAGES) mbar_init(smem_u32(&s_bar[0][warp * STAGES + lane]), 1), mbar_init(smem_u32(&s_bar[1][warp * STAGES + lane]), 1);
-    if (warp < W && lane < 2) s_piece[warp][lane].count = 0;
+    if (warp < W && lane < 2) s_piece[warp][lane].count = 0, s_late[warp] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     pdl_launch_dependents();
     pdl_wait_prior_grid();
@@ -436,7 +437,10 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
             {
                 uint32_t tries = 0;
                 while (!mbar_try_wait(bars + 8 * stage, phase) && ++tries < kWaitTries) {}
-                if (tries == kWaitTries && A.err) *A.err = -1;
+                if (tries == kWaitTries) {
+                    s_late[warp] = 1 + 2 * stage + phase;
+                    if (A.err) *A.err = -1;
+                }
             }
             const uint32_t base = at.steps.step(x) * kStepTokens, slot = ring + stage * 2 * BLOCK;
             const bool here0 = s_here[warp * STAGES + stage][0], here1 = s_here[warp * STAGES + stage][1];
@@ -692,6 +696,9 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
             if (lane == 0) s_piece[warp][which] = Piece{at_first, at.steps.count, at.S.first_row, rows_all, head, row0};
         }
     }
+    // (what is late may still land: the CTA's memory stays its own for another wait)
+    if (const uint32_t late = s_late[warp])
+        for (uint32_t tries = 0; !mbar_try_wait(bars + 8 * ((late - 1) / 2), (late - 1) % 2) && tries < kWaitTries; ++tries) {}
     }
     __syncthreads();
 
@@ -806,9 +813,9 @@ __global__ void __launch_bounds__(AttentionShape<DIM, NT>::kWarps * 32 + 32, 1) 
 template <int DIM, int NT, bool FINE>
 static cudaError_t launch_shape(const AttentionArgs &a, uint32_t sms, cudaStream_t stream) {
     using Shape = AttentionShape<DIM, NT>;
-    // (the kernel's arrays: barriers and blocks by stage, starts, pieces, units to join, up to the 128 bytes that the ring is aligned to)
+    // (the kernel's arrays: barriers and blocks by stage, starts, pieces, late waits, units to join, up to the 128 bytes that the ring is aligned to)
     constexpr uint32_t kArrays = Shape::kWarps * (Shape::kStages * (2 * sizeof(uint64_t) + 2 * sizeof(uint32_t)) + sizeof(uint64_t) + sizeof(uint32_t) +
-                                                  sizeof(Sequence) + 2 * sizeof(Piece)) + 2 * sizeof(uint2);
+                                                  sizeof(Sequence) + 2 * sizeof(Piece) + sizeof(uint32_t)) + 2 * sizeof(uint2);
     static_assert(Shape::kSmem + (kArrays + 127) / 128 * 128 <= 232448, "shared memory of a CTA");
     static_assert(Shape::kPiece <= kAttentionPartial, "a piece's place in the workspace");
     static std::atomic<bool> attr_set[64];   // set twice by racing threads at worst: the call is idempotent
